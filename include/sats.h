@@ -372,6 +372,157 @@ enum { SATS_PATH_SINGLE_TOKEN = 1, SATS_PATH_BATCH_MFMA = 2, SATS_PATH_BATCH_SPL
 int sats_query_path(int64_t n_tokens, int64_t d, int64_t d_ff, int elem_bytes, int aligned16, int n_cus,
                     int *path);
 
+/*
+ * Serving: what a token passes between two MLPs, and from the last one to the
+ * next id.  bf16 or float32 throughout (elem_bytes 2 or 4), sums and softmax
+ * statistics in float32 or wider, each result rounded once.
+ *
+ * Keys and values are kept in pages of page_size tokens.  A cache holds them
+ * for every layer, in device arrays of the caller, each head's part of a page
+ * contiguous:
+ *   k, v   [n_layers][n_pages][n_kv_heads][page_size][head_dim]
+ * page_size is a power of two up to 4096, head_dim a multiple of 8 up to 256,
+ * both arrays 16-byte aligned.
+ *
+ * A batch names the new tokens of n_seqs sequences, whose rows follow each
+ * other: sequence s has rows q_start[s] .. q_start[s + 1] - 1 of n_tokens, and
+ * with them kv_len[s] tokens in all, so that new token i is at place
+ * kv_len[s] - (q_start[s + 1] - q_start[s]) + i.  table[s] is its page table
+ * row: token j is in page table[s][j / page_size] at j % page_size, -1 where
+ * there is no page.  max_q_len and max_kv_len are upper bounds, on the host,
+ * of the new tokens and the length of any sequence; they decide the launches
+ * (a batch replayed from a graph may change within them).
+ *
+ * The state of the pages is the table [n_seqs][max_pages], the lengths
+ * len[n_seqs] and refs[n_pages], the number of table entries that name each
+ * page.  A page of 0 refs is free.
+ *
+ * Device contents are not trusted as far as memory goes: a length, sequence or
+ * page number out of its range is cut off or passed over (the key of a page
+ * that is not there is not seen, the token of one is not stored), and reads or
+ * writes nothing outside the arrays.
+ */
+typedef struct {
+  void *k, *v;
+  int64_t n_layers, n_pages, n_kv_heads, page_size, head_dim;
+  int32_t elem_bytes;
+} sats_kv_cache;
+
+typedef struct {
+  const int32_t *table, *q_start, *kv_len; /* device */
+  int64_t n_seqs, max_pages, n_tokens, max_q_len, max_kv_len;
+} sats_kv_batch;
+
+typedef struct {
+  int32_t *table, *len, *refs; /* device */
+  int64_t n_seqs, max_pages;
+} sats_kv_pages;
+
+/*
+ * Norm of each head of q and k, and the position rotation, in one pass:
+ *   x <- x / sqrt(mean(x^2) + eps) * weight       (q_norm, k_norm [head_dim]; NULL: no norm)
+ *   (a, b) <- (a cos - b sin, b cos + a sin)      for the rot_dim / 2 pairs
+ * A pair is (i, i + rot_dim / 2), with interleaved (2 i, 2 i + 1); dims from
+ * rot_dim on are not rotated.  rope [n_pos][rot_dim] (float32, device) holds the
+ * rot_dim / 2 cosines of a position, then the sines.  Rows of heads are dense;
+ * the strides are elements from one token to the next, so q, k and v may be
+ * parts of one projection's output.  An output may be its own input (same
+ * pointer and stride); other overlap is rejected.  Arrays and strides on 16
+ * bytes, with head_dim and rot_dim multiples of 32 bytes' worth of elements,
+ * move in 16-byte pieces, others element by element.
+ *
+ * sats_qk_norm_rope: positions [n_tokens] (device; cut off to 0 .. n_pos - 1).
+ * sats_qkv_append: the batch's tokens; keys and values (these as they are) go
+ * to their places in `layer` of the cache.  positions NULL: the tokens' places.
+ */
+int sats_qk_norm_rope(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *q_norm,
+                      const void *k_norm, float eps, const float *rope, int64_t n_pos, const int32_t *positions,
+                      void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride, int64_t n_tokens,
+                      int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim, int64_t rot_dim, int interleaved,
+                      int elem_bytes, hipStream_t stream);
+int sats_qkv_append(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                    const void *q_norm, const void *k_norm, float eps, const float *rope, int64_t n_pos,
+                    const int32_t *positions, void *q_out, int64_t q_out_stride, const sats_kv_cache *cache,
+                    int64_t layer, const sats_kv_batch *batch, int64_t n_q_heads, int64_t rot_dim, int interleaved,
+                    hipStream_t stream);
+
+/*
+ * Attention of the batch's new tokens over one layer of the cache:
+ *   out = sum_j p_j v_j,   p = softmax over the visible j of scale (q . k_j)
+ * A token at place i sees the keys j <= i; with window > 0 only those with
+ * i - j < window or j < n_sinks.  Query head h reads cache head
+ * h / (n_q_heads / n_kv_heads).  q [n_tokens][n_q_heads][head_dim] at q_stride
+ * elements a token; out the same, dense; lse [n_tokens][n_q_heads] (float32, or
+ * NULL) the logarithm of the sum of exp(scale q . k_j).  A token that sees
+ * nothing gives zeros and -inf.  What a key that is not seen holds (NaN,
+ * infinities) does not matter.  q, out and rows of q on 16 bytes.
+ */
+int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *cache, int64_t layer,
+                         const sats_kv_batch *batch, int64_t n_q_heads, float scale, int64_t window, int64_t n_sinks,
+                         void *out, float *lse, hipStream_t stream);
+
+/*
+ * Bookkeeping of the pages, on the device.  A call takes n items (up to 65535;
+ * seqs NULL: sequences 0 .. n - 1); a sequence may be in it once.
+ *
+ * sats_cache_extend: item i's sequence grows by add[i] tokens: its table gets
+ * the pages that these need.  A last page that is not full and that other
+ * sequences share is replaced by a copy of its own.
+ * sats_cache_fork: sequence dst[i], which has to be empty, becomes a copy of
+ * src[i] (no dst is a src): full pages are shared, a last page that is not full
+ * is copied (its tokens, in every layer).
+ * New pages are the free pages of lowest number, in ascending order over the
+ * items (a copy first).  Without enough free pages nothing changes.  status
+ * (device int32 [2], or NULL): pages that were missing, and items that were left
+ * out (no such sequence, no room in the table, dst in use, add < 0).
+ *
+ * sats_cache_free: gives back the pages that lie wholly in the tokens
+ * begin[i] .. end[i] - 1 of item i's sequence (NULL: from 0, to its length); their
+ * table entries become -1.  An end at or past the length cuts the sequence to
+ * begin[i] tokens.
+ * sats_cache_compact: moves pages (contents, table entries, refs) so that those in
+ * use are 0 .. n_used - 1: the ones beyond go to the free ones below, both in
+ * ascending order.  n_used: device int32, or NULL.
+ * sats_cache_copy: contents of pages src_pages[i] to dst_pages[i], every layer
+ * (no page twice in dst_pages, none in both; no bookkeeping).
+ */
+int sats_cache_extend(const sats_kv_cache *cache, const sats_kv_pages *pages, const int32_t *seqs, const int32_t *add,
+                      int64_t n, int32_t *status, hipStream_t stream);
+int sats_cache_fork(const sats_kv_cache *cache, const sats_kv_pages *pages, const int32_t *src, const int32_t *dst,
+                    int64_t n, int32_t *status, hipStream_t stream);
+int sats_cache_free(const sats_kv_cache *cache, const sats_kv_pages *pages, const int32_t *seqs, const int32_t *begin,
+                    const int32_t *end, int64_t n, hipStream_t stream);
+int sats_cache_compact(const sats_kv_cache *cache, const sats_kv_pages *pages, int32_t *n_used, hipStream_t stream);
+int sats_cache_copy(const sats_kv_cache *cache, const int32_t *src_pages, const int32_t *dst_pages, int64_t n,
+                    hipStream_t stream);
+
+/*
+ * The next id of n rows of logits [vocab], `stride` elements apart, from one
+ * number u[i] of [0, 1) a row.  Per row (device arrays, or NULL for the value in
+ * brackets): temperature [1; not above 0: the largest logit], top_k [0: all],
+ * top_p [1], min_p [0].  Id i weighs w_i = round(2^40 exp((l_i - max) / T)), a whole
+ * number (the exponential in float32; NaN logits count as -inf).  In the order of
+ * falling logit, the lower id first where two are equal, an id is kept while its
+ * rank is below top_k, the weights before it are below top_p times those of the
+ * top k, and exp(..) >= min_p; the first id always, one of weight 0 never.
+ * tokens[i] is the first id, in the order of ids, at which the running sum of kept
+ * weights exceeds u[i] times their total, so that it does not depend on any order
+ * of summation; -1 for a row without a logit above -inf.  prob [n] (or NULL): its
+ * share of the kept weights; n_kept [n] (or NULL): how many ids were kept.
+ * vocab <= 2^22.
+ */
+int sats_sample(const void *logits, int elem_bytes, int64_t stride, int64_t n, int64_t vocab, const float *temperature,
+                const int32_t *top_k, const float *top_p, const float *min_p, const float *u, int32_t *tokens,
+                float *prob, int32_t *n_kept, hipStream_t stream);
+
+/*
+ * Allocate the scratch memory of (current device, stream) for serving calls of up to
+ * max_items items over n_pages pages, and max_rows rows of vocab logits (zeros: none).
+ * Without it a call allocates what it needs, once; a call under stream capture that
+ * would have to allocate returns SATS_ERR_WORKSPACE.
+ */
+int sats_reserve_serving(int64_t max_items, int64_t n_pages, int64_t max_rows, int64_t vocab, hipStream_t stream);
+
 /* Free every workspace of the calling process, and the kept buffers of the
  * routing-table construction and of the calibration (synchronises each
  * device). */

@@ -19,10 +19,11 @@ Modules
   sats      -- SATS calibration (Eq. 6-10)
   lora      -- LoRA-aware routed sparse MLP (Section 5, fine-tuned models)
   route     -- routing-table construction (Eq. 11-14)
+  serving   -- head norms and rotation, attention over a paged cache, its pages, sampling
 
 Parity status of each function is stated in its docstring.  The inter-layer
 glue of a stack (``mlp.glue``) is a convention of this library, not something
 the paper defines: parity unpinned by the paper (pinned only by its own
 invariants).
 """
-from . import numerics, mlp, calibrate, sats, lora, route  # noqa: F401
+from . import numerics, mlp, calibrate, sats, lora, route, serving  # noqa: F401

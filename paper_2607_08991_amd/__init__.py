@@ -1,4 +1,5 @@
-"""Routed, threshold-sparsified gated MLP for AMD Instinct MI355X (gfx950).
+"""Routed, threshold-sparsified gated MLP for AMD Instinct MI355X (gfx950), and the
+serving operators around it.
 
 The computation lives in libsats.so (hand-written HIP kernels behind the C ABI
 of include/sats.h).  This package is its ctypes binding, the build script and
@@ -14,4 +15,6 @@ from ._lib import (  # noqa: F401
     SATS_BATCH_COMPACT, SATS_SINGLE_AUTO, SATS_SINGLE_OFF, SATS_PATH_SINGLE_TOKEN, SATS_PATH_BATCH_MFMA,
     SATS_PATH_BATCH_SPLIT, SATS_PATH_BATCH_COMPACT, sats_mlp_forward_noalloc,
     SATS_K_DEC_REDUCE, SATS_K_DENSE_DOWN, SATS_K_DEC_REDUCE_LORA, SATS_K_ROUTE_MERGE,
+    KVCache, KVBatch, KVPages, sats_qk_norm_rope, sats_qkv_append, sats_paged_attention, sats_cache_extend,
+    sats_cache_fork, sats_cache_free, sats_cache_compact, sats_cache_copy, sats_sample, sats_reserve_serving,
 )

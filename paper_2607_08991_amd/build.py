@@ -13,7 +13,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libsats.so")
-SOURCES = [os.path.join(CSRC, "sats.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("sats.hip", "serve.hip")]
 DEPS = SOURCES + [os.path.join(CSRC, "kernels.hpp"), os.path.join(ROOT, "include", "sats.h")]
 ARCH = "gfx950"
 

@@ -1,0 +1,30 @@
+// What the host sides of the library's translation units share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <stddef.h>
+
+#include "../../include/sats.h"
+
+namespace sats_host {
+
+// Records the text of the calling thread's last error and returns `code`.
+int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+void clear_error();
+
+// Compute units of the current device (0 on an error).
+int device_cus();
+
+// The serving operators' scratch memory of (current device, stream): at least `bytes`,
+// grown where it is smaller (SATS_ERR_WORKSPACE under stream capture or for want of
+// memory; what is there then stays).
+int serve_workspace(hipStream_t stream, size_t bytes, char **mem);
+
+}  // namespace sats_host
+
+#define SATS_HIP_TRY(expr)                                                                                  \
+  do {                                                                                                      \
+    hipError_t e_ = (expr);                                                                                 \
+    if (e_ != hipSuccess) return sats_host::fail(SATS_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_));     \
+  } while (0)

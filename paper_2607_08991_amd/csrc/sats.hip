@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "../../include/sats.h"
+#include "host.hpp"
 #include "kernels.hpp"
 #include "decode.hpp"
 #include "dense.hpp"
@@ -498,6 +499,10 @@ struct Workspace {
     size_t refused = SIZE_MAX;  // a size that could not be allocated: not tried again until sats_reserve
     bool captured = false;
   } tiled[2];
+  // The serving operators' scratch memory (serve.hip).
+  char *serve = nullptr;
+  size_t serve_bytes = 0;
+  bool serve_captured = false;
 };
 constexpr size_t kPfCounterBytes = (kPfCounters * sizeof(unsigned) + 255) / 256 * 256;
 
@@ -2082,6 +2087,47 @@ int route_build(const float *lb, const float *ls, const int32_t *ids, int64_t n,
 
 // =============================================================== C ABI
 
+// What the serving operators' translation unit uses.
+namespace sats_host {
+
+int fail(int code, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_err = buf;
+  return code;
+}
+void clear_error() { g_err.clear(); }
+int device_cus() { return ::device_cus(); }
+
+int serve_workspace(hipStream_t stream, size_t bytes, char **mem) try {
+  int dev = 0, rc = 0;
+  HIP_TRY(hipGetDevice(&dev));
+  std::lock_guard<std::mutex> lk(g_ws_mu);
+  Workspace &w = g_ws[{dev, stream}];
+  const bool capturing = stream_captures(stream);
+  if (w.serve_bytes < bytes) {
+    if (capturing)
+      return ::fail(SATS_ERR_WORKSPACE, "%zu bytes of scratch memory are not there under stream capture: call "
+                    "sats_reserve_serving first", bytes);
+    size_t got = 0;
+    char *m = alloc_or(std::max(bytes, 2 * w.serve_bytes), bytes, &got);
+    if (!m) return ::fail(SATS_ERR_WORKSPACE, "workspace allocation of %zu bytes failed", bytes);
+    if (w.serve) HIP_TRY(hipStreamSynchronize(stream));  // the old buffer may still be in use
+    if ((rc = drop_or_keep(w, w.serve, w.serve_captured))) return rc;
+    w.serve = m, w.serve_bytes = got, w.serve_captured = false;
+  }
+  if (capturing) w.serve_captured = true;
+  *mem = w.serve;
+  return SATS_OK;
+} catch (const std::exception &) {  // (host memory: nothing is thrown through the C entry points)
+  return SATS_ERR_WORKSPACE;
+}
+
+}  // namespace sats_host
+
 extern "C" {
 
 int sats_mlp_forward(const sats_bf16 *x, const int32_t *token_ids, const sats_bf16 *W_gate,
@@ -2233,6 +2279,7 @@ int sats_release(void) {
     if (kv.second.counters) HIP_TRY(hipFree(kv.second.counters));
     for (const Workspace::Tiled &t : kv.second.tiled)
       if (t.mem) HIP_TRY(hipFree(t.mem));
+    if (kv.second.serve) HIP_TRY(hipFree(kv.second.serve));
     for (void *t : kv.second.kept) HIP_TRY(hipFree(t));
   }
   g_ws.clear();

@@ -1,0 +1,441 @@
+// Host side of the serving operators declared in include/sats.h: argument checks,
+// scratch memory and launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "host.hpp"
+
+#include "attend.hpp"
+#include "pages.hpp"
+#include "rope.hpp"
+#include "sample.hpp"
+
+namespace {
+
+using sats_host::clear_error;
+using sats_host::fail;
+
+bool on16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+size_t align_up(size_t v) { return (v + 255) & ~size_t(255); }
+
+struct Carve {
+  char *base;
+  size_t off = 0;
+  template <typename T> T *take(size_t count) {
+    T *p = reinterpret_cast<T *>(base ? base + off : nullptr);
+    off += align_up(std::max<size_t>(count, 1) * sizeof(T));
+    return p;
+  }
+};
+
+constexpr int64_t kMaxCount = (int64_t)1 << 30;
+
+int launched(const char *what) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? SATS_OK : fail(SATS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+// Bytes of an array of keys (or values) of every layer.
+double pool_bytes(const sats_kv_cache *c) {
+  return (double)c->n_layers * (double)c->n_pages * (double)c->n_kv_heads * (double)c->page_size * (double)c->head_dim *
+         c->elem_bytes;
+}
+
+int check_cache(const sats_kv_cache *c, bool data) {
+  if (!c) return fail(SATS_ERR_NULL, "cache must be non-null");
+  if (data && (!c->k || !c->v)) return fail(SATS_ERR_NULL, "the cache's k and v must be non-null");
+  if (c->elem_bytes != 2 && c->elem_bytes != 4) return fail(SATS_ERR_ARG, "elem_bytes must be 2 or 4");
+  if (c->n_layers < 1 || c->n_pages < 1 || c->n_kv_heads < 1 || c->n_layers > 4096 || c->n_pages > kMaxCount ||
+      c->n_kv_heads > 1024)
+    return fail(SATS_ERR_SHAPE, "a cache has 1 to 4096 layers, 1 to 2^30 pages and 1 to 1024 heads");
+  if (c->page_size < 1 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)))
+    return fail(SATS_ERR_SHAPE, "page_size must be a power of two up to 4096");
+  if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8)
+    return fail(SATS_ERR_SHAPE, "head_dim must be a multiple of 8 from 8 to 256");
+  if (pool_bytes(c) > 1e18) return fail(SATS_ERR_SHAPE, "the cache is too large");
+  if (data && (!on16(c->k) || !on16(c->v))) return fail(SATS_ERR_ARG, "the cache's k and v must be 16-byte aligned");
+  return SATS_OK;
+}
+
+int log2_of(int64_t v) {
+  int s = 0;
+  while (((int64_t)1 << s) < v) ++s;
+  return s;
+}
+
+sats::PoolView pool_view(const sats_kv_cache *c) {
+  return {c->n_pages, (int)c->n_kv_heads, (int)c->page_size, log2_of(c->page_size)};
+}
+
+int check_batch(const sats_kv_batch *b) {
+  if (!b) return fail(SATS_ERR_NULL, "batch must be non-null");
+  if (b->n_seqs < 0 || b->n_tokens < 0 || b->max_pages < 0 || b->max_q_len < 0 || b->max_kv_len < 0 ||
+      b->n_seqs > kMaxCount || b->n_tokens > kMaxCount || b->max_pages > kMaxCount || b->max_q_len > kMaxCount ||
+      b->max_kv_len >= (int64_t)1 << 31)
+    return fail(SATS_ERR_SHAPE, "a batch's sizes must be >= 0, at most 2^30 (lengths below 2^31)");
+  if (b->n_tokens > 0 && b->n_seqs < 1) return fail(SATS_ERR_SHAPE, "tokens without a sequence");
+  if (b->n_tokens > 0 && (!b->table || !b->q_start || !b->kv_len))
+    return fail(SATS_ERR_NULL, "the batch's table, q_start and kv_len must be non-null");
+  return SATS_OK;
+}
+
+sats::BatchView batch_view(const sats_kv_batch *b) {
+  return {b->table, b->q_start, b->kv_len, (int)b->n_seqs, b->max_pages, b->n_tokens, b->max_q_len, b->max_kv_len};
+}
+
+char *layer_of(void *pool, const sats_kv_cache *c, int64_t layer) {
+  return static_cast<char *>(pool) + layer * c->n_pages * c->n_kv_heads * c->page_size * c->head_dim * c->elem_bytes;
+}
+
+// Bytes from a row's start to the last row's end, for n rows of `row` elements at a stride.
+int64_t span(int64_t n, int64_t stride, int64_t row, int esz) { return n > 0 ? ((n - 1) * stride + row) * esz : 0; }
+
+bool overlap(const void *a, int64_t na, const void *b, int64_t nb) {
+  const char *x = static_cast<const char *>(a), *y = static_cast<const char *>(b);
+  return na > 0 && nb > 0 && x < y + nb && y < x + na;
+}
+
+// ------------------------------------------------------------- norm and rotation
+
+int run_rope(sats::RopeArgs a, int esz, bool append, hipStream_t stream) {
+  const int64_t n = a.n_tokens;
+  if (n < 0 || n > kMaxCount || a.n_q < 0 || a.n_kv < 0 || a.n_q > 4096 || a.n_kv > 1024)
+    return fail(SATS_ERR_SHAPE, "n_tokens, n_q_heads or n_kv_heads out of range");
+  if (a.dim < 2 || a.dim > 256 || a.dim % 2) return fail(SATS_ERR_SHAPE, "head_dim must be even, at most 256");
+  if (a.rot < 0 || a.rot > a.dim || a.rot % 2) return fail(SATS_ERR_SHAPE, "rot_dim must be even, 0 to head_dim");
+  if (a.rot > 0 && (a.n_pos < 1 || a.n_pos >= (int64_t)1 << 31)) return fail(SATS_ERR_SHAPE, "rope needs 1 to 2^31 positions");
+  if (a.pairs < 0 || a.pairs > 1) return fail(SATS_ERR_ARG, "interleaved must be 0 or 1");
+  if (!(a.eps >= 0.0f) || std::isinf(a.eps)) return fail(SATS_ERR_ARG, "eps must be finite and >= 0");
+  a.rows = a.n_q + a.n_kv * (append ? 2 : 1);
+  if (n == 0 || a.rows == 0) return SATS_OK;
+  if ((a.n_q && (!a.q || !a.q_out)) || (a.n_kv && (!a.k || (append ? !a.v : !a.k_out))))
+    return fail(SATS_ERR_NULL, "q, k, v and the outputs must be non-null");
+  if (a.rot > 0 && (!a.rope || (!append && !a.positions))) return fail(SATS_ERR_NULL, "rope and positions must be non-null");
+  const int64_t qrow = (int64_t)a.n_q * a.dim, krow = (int64_t)a.n_kv * a.dim;
+  if (a.q_stride < qrow || a.q_out_stride < qrow || a.k_stride < krow || (append ? a.v_stride : a.k_out_stride) < krow)
+    return fail(SATS_ERR_SHAPE, "a token stride is below the token's row");
+  // outputs over inputs: the same rows, or apart
+  const int64_t sq = span(n, a.q_stride, qrow, esz), sk = span(n, a.k_stride, krow, esz);
+  const int64_t sqo = span(n, a.q_out_stride, qrow, esz), sko = append ? 0 : span(n, a.k_out_stride, krow, esz);
+  const bool q_same = a.q_out == a.q && a.q_out_stride == a.q_stride;
+  const bool k_same = !append && a.k_out == a.k && a.k_out_stride == a.k_stride;
+  const int64_t sv = append ? span(n, a.v_stride, krow, esz) : 0;
+  if (!q_same && (overlap(a.q_out, sqo, a.q, sq) || overlap(a.q_out, sqo, a.k, sk) || overlap(a.q_out, sqo, a.v, sv)))
+    return fail(SATS_ERR_ARG, "q_out overlaps the inputs without being q itself");
+  if (!append && !k_same && (overlap(a.k_out, sko, a.k, sk) || overlap(a.k_out, sko, a.q, sq)))
+    return fail(SATS_ERR_ARG, "k_out overlaps the inputs without being k itself");
+  if (!append && !(q_same && k_same) && overlap(a.q_out, sqo, a.k_out, sko))
+    return fail(SATS_ERR_ARG, "q_out and k_out overlap");
+  const int vec = 16 / esz;
+  const bool wide = a.dim % (2 * vec) == 0 && a.rot % (2 * vec) == 0 && on16(a.q) && on16(a.k) && on16(a.v) &&
+                    on16(a.q_norm) && on16(a.k_norm) && on16(a.rope) && on16(a.q_out) && on16(a.k_out) &&
+                    a.q_stride % vec == 0 && a.k_stride % vec == 0 && a.v_stride % vec == 0 &&
+                    a.q_out_stride % vec == 0 && a.k_out_stride % vec == 0;
+  const int units = a.dim / (2 * (wide ? vec : 1));
+  a.lanes = 1;
+  while (a.lanes < units && a.lanes < 64) a.lanes *= 2;
+  a.per = 1;
+  const int64_t groups = (a.rows + a.per - 1) / a.per, threads = n * groups * a.lanes;
+  if (threads > (int64_t)sats::kThreads * 0x7fffffff) return fail(SATS_ERR_SHAPE, "too many rows for one call");
+  const dim3 grid((unsigned)((threads + sats::kThreads - 1) / sats::kThreads));
+  auto go = [&](auto fn) { fn<<<grid, sats::kThreads, 0, stream>>>(a); };
+  if (esz == 2) wide ? go(sats::rope_kernel<uint16_t, 8, 1>) : go(sats::rope_kernel<uint16_t, 1, 2>);
+  else wide ? go(sats::rope_kernel<float, 4, 1>) : go(sats::rope_kernel<float, 1, 2>);
+  return launched("rope_kernel");
+}
+
+// ------------------------------------------------------------- pages
+
+struct PagesScratch {
+  int32_t *off, *ids, *to, *src, *dst, *valid, *ctl;
+};
+size_t pages_layout(char *base, int64_t n, int64_t n_pages, PagesScratch *out) {
+  Carve c{base};
+  PagesScratch s;
+  const int64_t moves = std::max(n, n_pages);
+  s.ctl = c.take<int32_t>(16);
+  s.off = c.take<int32_t>(n + 1);
+  s.ids = c.take<int32_t>(n_pages);
+  s.to = c.take<int32_t>(n_pages);
+  s.src = c.take<int32_t>(moves);
+  s.dst = c.take<int32_t>(moves);
+  s.valid = c.take<int32_t>(n);
+  if (out) *out = s;
+  return c.off;
+}
+
+int check_pages(const sats_kv_cache *c, const sats_kv_pages *p, int64_t n, bool data) {
+  int rc = check_cache(c, data);
+  if (rc) return rc;
+  if (!p) return fail(SATS_ERR_NULL, "pages must be non-null");
+  if (p->n_seqs < 0 || p->max_pages < 0 || p->n_seqs > kMaxCount || p->max_pages > kMaxCount || n < 0 || n > 65535 ||
+      p->max_pages * c->page_size >= (int64_t)1 << 31)
+    return fail(SATS_ERR_SHAPE, "n_seqs or max_pages out of range, or more than 65535 items");
+  if (p->n_seqs * std::max<int64_t>(p->max_pages, 1) >= (int64_t)1 << 38) return fail(SATS_ERR_SHAPE, "the page table is too large");
+  if (!p->table || !p->len || !p->refs) return fail(SATS_ERR_NULL, "table, len and refs must be non-null");
+  return SATS_OK;
+}
+
+sats::PagesArgs pages_args(const sats_kv_cache *c, const sats_kv_pages *p, const int32_t *seqs, const int32_t *other,
+                           int64_t n, const PagesScratch *s) {
+  sats::PagesArgs a{};
+  a.table = p->table, a.len = p->len, a.refs = p->refs;
+  a.n_seqs = p->n_seqs, a.max_pages = p->max_pages, a.n_pages = c->n_pages;
+  a.page = (int)c->page_size, a.shift = log2_of(c->page_size);
+  a.seqs = seqs, a.other = other, a.n = (int)n;
+  if (s) a.off = s->off, a.ids = s->ids, a.to = s->to, a.src = s->src, a.dst = s->dst, a.valid = s->valid, a.ctl = s->ctl;
+  return a;
+}
+
+int copy_pages(const sats_kv_cache *c, const int32_t *src, const int32_t *dst, const int32_t *valid, const int32_t *ctl,
+               int64_t n, hipStream_t stream) {
+  sats::CopyArgs a{static_cast<char *>(c->k), static_cast<char *>(c->v), c->n_pages, c->n_layers, (int)c->n_kv_heads,
+                   (int)c->page_size, (int)(c->head_dim * c->elem_bytes), src, dst, valid, ctl, (int)n};
+  const int64_t waves = n * c->n_layers * 2 * c->n_kv_heads, per = sats::kThreads / 64;
+  const int64_t grid = std::clamp<int64_t>((waves + per - 1) / per, 1, 2048);
+  sats::pages_copy_kernel<<<(unsigned)grid, sats::kThreads, 0, stream>>>(a);
+  return launched("pages_copy_kernel");
+}
+
+// ------------------------------------------------------------- sampling
+
+struct SampleScratch {
+  float *cmax;
+  int32_t *cid;
+  uint32_t *ccnt, *n_list, *hcnt;
+  sats::u64 *csum, *hsum, *list;
+};
+size_t sample_layout(char *base, int64_t n, int64_t vocab, SampleScratch *out) {
+  Carve c{base};
+  SampleScratch s;
+  const int64_t chunks = (vocab + sats::kSampChunk - 1) / sats::kSampChunk;
+  s.cmax = c.take<float>(n * chunks);
+  s.cid = c.take<int32_t>(n * chunks);
+  s.ccnt = c.take<uint32_t>(n * chunks);
+  s.csum = c.take<sats::u64>(n * chunks);
+  s.n_list = c.take<uint32_t>(n);
+  s.hcnt = c.take<uint32_t>(n * sats::kSampBins);
+  s.hsum = c.take<sats::u64>(n * sats::kSampBins);
+  s.list = c.take<sats::u64>(n * vocab);
+  if (out) *out = s;
+  return c.off;
+}
+
+constexpr int64_t kMaxVocab = (int64_t)sats::kSampChunk * sats::kPickThreads;
+
+template <typename T> void launch_sample(const sats::SampleArgs &a, bool wide, hipStream_t stream) {
+  const dim3 grid((unsigned)a.chunks, (unsigned)a.n);
+  constexpr int V = 16 / sizeof(T);
+  if (wide) {
+    sats::sample_max_kernel<T, V><<<grid, sats::kThreads, 0, stream>>>(a);
+    sats::sample_hist_kernel<T, V><<<grid, sats::kThreads, 0, stream>>>(a);
+    sats::sample_cut_kernel<T, V><<<grid, sats::kThreads, 0, stream>>>(a);
+  } else {
+    sats::sample_max_kernel<T, 1><<<grid, sats::kThreads, 0, stream>>>(a);
+    sats::sample_hist_kernel<T, 1><<<grid, sats::kThreads, 0, stream>>>(a);
+    sats::sample_cut_kernel<T, 1><<<grid, sats::kThreads, 0, stream>>>(a);
+  }
+  sats::sample_pick_kernel<T><<<(unsigned)a.n, sats::kPickThreads, 0, stream>>>(a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int sats_qk_norm_rope(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *q_norm,
+                      const void *k_norm, float eps, const float *rope, int64_t n_pos, const int32_t *positions,
+                      void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride, int64_t n_tokens,
+                      int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim, int64_t rot_dim, int interleaved,
+                      int elem_bytes, hipStream_t stream) {
+  clear_error();
+  if (elem_bytes != 2 && elem_bytes != 4) return fail(SATS_ERR_ARG, "elem_bytes must be 2 or 4");
+  if (n_q_heads < 0 || n_q_heads > 4096 || n_kv_heads < 0 || n_kv_heads > 1024 || head_dim < 2 || head_dim > 256 ||
+      rot_dim < 0 || rot_dim > head_dim)
+    return fail(SATS_ERR_SHAPE, "heads, head_dim or rot_dim out of range");
+  sats::RopeArgs a{};
+  a.q = q, a.k = k, a.q_stride = q_stride, a.k_stride = k_stride;
+  a.q_norm = q_norm, a.k_norm = k_norm, a.eps = eps;
+  a.rope = rope, a.n_pos = n_pos, a.positions = positions;
+  a.q_out = q_out, a.k_out = k_out, a.q_out_stride = q_out_stride, a.k_out_stride = k_out_stride;
+  a.n_q = (int)n_q_heads, a.n_kv = (int)n_kv_heads, a.dim = (int)head_dim, a.rot = (int)rot_dim, a.pairs = interleaved;
+  a.n_tokens = n_tokens;
+  return run_rope(a, elem_bytes, false, stream);
+}
+
+int sats_qkv_append(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                    const void *q_norm, const void *k_norm, float eps, const float *rope, int64_t n_pos,
+                    const int32_t *positions, void *q_out, int64_t q_out_stride, const sats_kv_cache *cache,
+                    int64_t layer, const sats_kv_batch *batch, int64_t n_q_heads, int64_t rot_dim, int interleaved,
+                    hipStream_t stream) {
+  clear_error();
+  int rc = check_cache(cache, true);
+  if (rc || (rc = check_batch(batch))) return rc;
+  if (layer < 0 || layer >= cache->n_layers) return fail(SATS_ERR_SHAPE, "layer outside the cache");
+  if (n_q_heads < 0 || n_q_heads > 4096 || rot_dim < 0 || rot_dim > cache->head_dim)
+    return fail(SATS_ERR_SHAPE, "heads or rot_dim out of range");
+  sats::RopeArgs a{};
+  a.q = q, a.k = k, a.v = v, a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+  a.q_norm = q_norm, a.k_norm = k_norm, a.eps = eps;
+  a.rope = rope, a.n_pos = n_pos, a.positions = positions;
+  a.q_out = q_out, a.q_out_stride = q_out_stride;
+  a.n_q = (int)n_q_heads, a.n_kv = (int)cache->n_kv_heads, a.dim = (int)cache->head_dim, a.rot = (int)rot_dim;
+  a.pairs = interleaved;
+  a.n_tokens = batch->n_tokens;
+  a.k_pool = layer_of(cache->k, cache, layer), a.v_pool = layer_of(cache->v, cache, layer);
+  a.batch = batch_view(batch), a.pool = pool_view(cache);
+  return run_rope(a, cache->elem_bytes, true, stream);
+}
+
+int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *cache, int64_t layer,
+                         const sats_kv_batch *batch, int64_t n_q_heads, float scale, int64_t window, int64_t n_sinks,
+                         void *out, float *lse, hipStream_t stream) {
+  clear_error();
+  int rc = check_cache(cache, true);
+  if (rc || (rc = check_batch(batch))) return rc;
+  if (layer < 0 || layer >= cache->n_layers) return fail(SATS_ERR_SHAPE, "layer outside the cache");
+  if (n_q_heads < 1 || n_q_heads > 4096 || n_q_heads % cache->n_kv_heads)
+    return fail(SATS_ERR_SHAPE, "n_q_heads must be a multiple of the cache's heads, at most 4096");
+  if (window < 0 || n_sinks < 0 || (n_sinks && !window)) return fail(SATS_ERR_ARG, "window and n_sinks must be >= 0, sinks need a window");
+  if (!std::isfinite(scale)) return fail(SATS_ERR_ARG, "scale must be finite");
+  if (batch->n_tokens == 0) return SATS_OK;
+  if (!q || !out) return fail(SATS_ERR_NULL, "q and out must be non-null");
+  const int esz = cache->elem_bytes;
+  const int64_t row = n_q_heads * cache->head_dim, n = batch->n_tokens;
+  if (q_stride < row) return fail(SATS_ERR_SHAPE, "q_stride is below the token's row");
+  if (!on16(q) || !on16(out) || q_stride * esz % 16) return fail(SATS_ERR_ARG, "q, out and the rows of q must be 16-byte aligned");
+  if (overlap(out, n * row * esz, q, span(n, q_stride, row, esz))) return fail(SATS_ERR_ARG, "out overlaps q");
+  sats::AttendArgs a{};
+  a.q = q, a.q_stride = q_stride, a.out = out, a.lse = lse;
+  a.k = layer_of(cache->k, cache, layer), a.v = layer_of(cache->v, cache, layer);
+  a.batch = batch_view(batch), a.pool = pool_view(cache);
+  a.n_q = (int)n_q_heads, a.dim = (int)cache->head_dim, a.scale = scale, a.window = window, a.sinks = n_sinks;
+  const dim3 grid((unsigned)n, (unsigned)n_q_heads);
+  if (esz == 2) sats::attend_simple_kernel<uint16_t><<<grid, 64, 0, stream>>>(a);
+  else sats::attend_simple_kernel<float><<<grid, 64, 0, stream>>>(a);
+  return launched("attend_simple_kernel");
+}
+
+int sats_cache_free(const sats_kv_cache *cache, const sats_kv_pages *pages, const int32_t *seqs, const int32_t *begin,
+                    const int32_t *end, int64_t n, hipStream_t stream) {
+  clear_error();
+  int rc = check_pages(cache, pages, n, false);
+  if (rc || n == 0) return rc;
+  sats::PagesArgs a = pages_args(cache, pages, seqs, nullptr, n, nullptr);
+  a.begin = begin, a.end = end;
+  sats::pages_free_kernel<<<(unsigned)n, sats::kThreads, 0, stream>>>(a);
+  return launched("pages_free_kernel");
+}
+
+int sats_cache_extend(const sats_kv_cache *cache, const sats_kv_pages *pages, const int32_t *seqs, const int32_t *add,
+                      int64_t n, int32_t *status, hipStream_t stream) {
+  clear_error();
+  int rc = check_pages(cache, pages, n, true);
+  if (rc || n == 0) return rc;
+  if (!add) return fail(SATS_ERR_NULL, "add must be non-null");
+  char *mem = nullptr;
+  PagesScratch s;
+  if ((rc = sats_host::serve_workspace(stream, pages_layout(nullptr, n, cache->n_pages, nullptr), &mem))) return rc;
+  pages_layout(mem, n, cache->n_pages, &s);
+  sats::PagesArgs a = pages_args(cache, pages, seqs, add, n, &s);
+  a.status = status;
+  sats::pages_plan_kernel<false><<<1, sats::kPlanThreads, 0, stream>>>(a);
+  if ((rc = launched("pages_plan_kernel"))) return rc;
+  return copy_pages(cache, s.src, s.dst, s.valid, s.ctl, n, stream);
+}
+
+int sats_cache_fork(const sats_kv_cache *cache, const sats_kv_pages *pages, const int32_t *src, const int32_t *dst,
+                    int64_t n, int32_t *status, hipStream_t stream) {
+  clear_error();
+  int rc = check_pages(cache, pages, n, true);
+  if (rc || n == 0) return rc;
+  if (!src || !dst) return fail(SATS_ERR_NULL, "src and dst must be non-null");
+  char *mem = nullptr;
+  PagesScratch s;
+  if ((rc = sats_host::serve_workspace(stream, pages_layout(nullptr, n, cache->n_pages, nullptr), &mem))) return rc;
+  pages_layout(mem, n, cache->n_pages, &s);
+  sats::PagesArgs a = pages_args(cache, pages, src, dst, n, &s);
+  a.status = status;
+  sats::pages_plan_kernel<true><<<1, sats::kPlanThreads, 0, stream>>>(a);
+  if ((rc = launched("pages_plan_kernel"))) return rc;
+  if (pages->max_pages) {
+    const dim3 grid((unsigned)((pages->max_pages + sats::kThreads - 1) / sats::kThreads), (unsigned)n);
+    sats::pages_fork_rows_kernel<<<grid, sats::kThreads, 0, stream>>>(a);
+    if ((rc = launched("pages_fork_rows_kernel"))) return rc;
+  }
+  return copy_pages(cache, s.src, s.dst, s.valid, s.ctl, n, stream);
+}
+
+int sats_cache_compact(const sats_kv_cache *cache, const sats_kv_pages *pages, int32_t *n_used, hipStream_t stream) {
+  clear_error();
+  int rc = check_pages(cache, pages, 0, true);
+  if (rc) return rc;
+  char *mem = nullptr;
+  PagesScratch s;
+  if ((rc = sats_host::serve_workspace(stream, pages_layout(nullptr, 0, cache->n_pages, nullptr), &mem))) return rc;
+  pages_layout(mem, 0, cache->n_pages, &s);
+  sats::PagesArgs a = pages_args(cache, pages, nullptr, nullptr, 0, &s);
+  a.n_used = n_used;
+  sats::pages_compact_plan_kernel<<<1, sats::kPlanThreads, 0, stream>>>(a);
+  if ((rc = launched("pages_compact_plan_kernel"))) return rc;
+  const int64_t entries = pages->n_seqs * pages->max_pages;
+  if (entries) {
+    sats::pages_remap_kernel<<<(unsigned)((entries + sats::kThreads - 1) / sats::kThreads), sats::kThreads, 0, stream>>>(a);
+    if ((rc = launched("pages_remap_kernel"))) return rc;
+  }
+  return copy_pages(cache, s.src, s.dst, nullptr, s.ctl, std::max<int64_t>(cache->n_pages / 2, 1), stream);
+}
+
+int sats_cache_copy(const sats_kv_cache *cache, const int32_t *src_pages, const int32_t *dst_pages, int64_t n,
+                    hipStream_t stream) {
+  clear_error();
+  const int rc = check_cache(cache, true);
+  if (rc) return rc;
+  if (n < 0 || n > kMaxCount) return fail(SATS_ERR_SHAPE, "n must be >= 0, at most 2^30");
+  if (n == 0) return SATS_OK;
+  if (!src_pages || !dst_pages) return fail(SATS_ERR_NULL, "src_pages and dst_pages must be non-null");
+  return copy_pages(cache, src_pages, dst_pages, nullptr, nullptr, n, stream);
+}
+
+int sats_sample(const void *logits, int elem_bytes, int64_t stride, int64_t n, int64_t vocab, const float *temperature,
+                const int32_t *top_k, const float *top_p, const float *min_p, const float *u, int32_t *tokens,
+                float *prob, int32_t *n_kept, hipStream_t stream) {
+  clear_error();
+  if (elem_bytes != 2 && elem_bytes != 4) return fail(SATS_ERR_ARG, "elem_bytes must be 2 or 4");
+  if (n < 0 || n > 65535 || vocab < 1 || vocab > kMaxVocab) return fail(SATS_ERR_SHAPE, "need 0 <= n < 65536 and 1 <= vocab <= 2^22");
+  if (n == 0) return SATS_OK;
+  if (!logits || !u || !tokens) return fail(SATS_ERR_NULL, "logits, u and tokens must be non-null");
+  if (stride < vocab) return fail(SATS_ERR_SHAPE, "stride is below vocab");
+  char *mem = nullptr;
+  SampleScratch s;
+  int rc = sats_host::serve_workspace(stream, sample_layout(nullptr, n, vocab, nullptr), &mem);
+  if (rc) return rc;
+  sample_layout(mem, n, vocab, &s);
+  sats::SampleArgs a{};
+  a.logits = logits, a.stride = stride, a.vocab = vocab, a.n = (int)n;
+  a.chunks = (int)((vocab + sats::kSampChunk - 1) / sats::kSampChunk);
+  a.temperature = temperature, a.top_k = top_k, a.top_p = top_p, a.min_p = min_p, a.u = u;
+  a.tokens = tokens, a.prob = prob, a.n_kept = n_kept;
+  a.cmax = s.cmax, a.cid = s.cid, a.hsum = s.hsum, a.hcnt = s.hcnt, a.csum = s.csum, a.ccnt = s.ccnt;
+  a.list = s.list, a.n_list = s.n_list;
+  const bool wide = on16(logits) && stride * elem_bytes % 16 == 0;
+  if (elem_bytes == 2) launch_sample<uint16_t>(a, wide, stream);
+  else launch_sample<float>(a, wide, stream);
+  return launched("sample kernels");
+}
+
+int sats_reserve_serving(int64_t max_items, int64_t n_pages, int64_t max_rows, int64_t vocab, hipStream_t stream) {
+  clear_error();
+  if (max_items < 0 || max_items > 65535 || n_pages < 0 || n_pages > kMaxCount || max_rows < 0 || max_rows > 65535 ||
+      vocab < 0 || vocab > kMaxVocab)
+    return fail(SATS_ERR_SHAPE, "bad sizes for sats_reserve_serving");
+  size_t bytes = 0;
+  if (n_pages) bytes = std::max(bytes, pages_layout(nullptr, max_items, n_pages, nullptr));
+  if (max_rows && vocab) bytes = std::max(bytes, sample_layout(nullptr, max_rows, vocab, nullptr));
+  char *mem = nullptr;
+  return sats_host::serve_workspace(stream, bytes, &mem);
+}
+
+}  // extern "C"
