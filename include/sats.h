@@ -516,12 +516,14 @@ int sats_sample(const void *logits, int elem_bytes, int64_t stride, int64_t n, i
                 float *prob, int32_t *n_kept, hipStream_t stream);
 
 /*
- * Allocate the scratch memory of (current device, stream) for serving calls of up to
- * max_items items over n_pages pages, and max_rows rows of vocab logits (zeros: none).
+ * Allocate the scratch memory of (current device, stream) for serving calls: page calls
+ * of up to max_items items over n_pages pages, sampling of max_rows rows of vocab
+ * logits, attention of any batch with heads of head_dim (zeros: none).
  * Without it a call allocates what it needs, once; a call under stream capture that
  * would have to allocate returns SATS_ERR_WORKSPACE.
  */
-int sats_reserve_serving(int64_t max_items, int64_t n_pages, int64_t max_rows, int64_t vocab, hipStream_t stream);
+int sats_reserve_serving(int64_t max_items, int64_t n_pages, int64_t max_rows, int64_t vocab, int64_t head_dim,
+                         hipStream_t stream);
 
 /* Free every workspace of the calling process, and the kept buffers of the
  * routing-table construction and of the calibration (synchronises each

@@ -89,7 +89,7 @@ SIGNATURES = {
     "sats_cache_compact": ([_P] * 3 + [_S], _N),
     "sats_cache_copy": ([_P] * 3 + [_I, _S], _N),
     "sats_sample": ([_P, _N, _I, _I, _I] + [_P] * 8 + [_S], _N),
-    "sats_reserve_serving": ([_I] * 4 + [_S], _N),
+    "sats_reserve_serving": ([_I] * 5 + [_S], _N),
     "sats_calibrate_sats": ([_P, _I] + [_P] * 3 + [_I] * 3 + [ctypes.c_double] * 3 + [_N] + [_P] * 3 + [_S], _N),
 }
 
@@ -536,6 +536,6 @@ def sats_sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min
           _i32(n_kept, one, "n_kept"), _stream(stream))
 
 
-def sats_reserve_serving(max_items=0, n_pages=0, max_rows=0, vocab=0, stream=None):
+def sats_reserve_serving(max_items=0, n_pages=0, max_rows=0, vocab=0, head_dim=0, stream=None):
     """Scratch memory of the serving calls, ahead of stream capture."""
-    _call("sats_reserve_serving", max_items, n_pages, max_rows, vocab, _stream(stream))
+    _call("sats_reserve_serving", max_items, n_pages, max_rows, vocab, head_dim, _stream(stream))

@@ -33,6 +33,9 @@ struct Carve {
 
 constexpr int64_t kMaxCount = (int64_t)1 << 30;
 
+// Attention: workgroups that a launch aims at, and key blocks below which no tile is split.
+constexpr int kRowsTarget = 4096, kRowsLeast = 8, kTileTarget = 512, kTileLeast = 4;
+
 int launched(const char *what) {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? SATS_OK : fail(SATS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
@@ -145,6 +148,76 @@ int run_rope(sats::RopeArgs a, int esz, bool append, hipStream_t stream) {
   if (esz == 2) wide ? go(sats::rope_kernel<uint16_t, 8, 1>) : go(sats::rope_kernel<uint16_t, 1, 2>);
   else wide ? go(sats::rope_kernel<float, 4, 1>) : go(sats::rope_kernel<float, 1, 2>);
   return launched("rope_kernel");
+}
+
+// ------------------------------------------------------------- attention
+
+// The split of a launch: row tiles of R rows, their number at most, and over how many
+// workgroups a tile's blocks of `keys` keys go.
+struct AttendPlan {
+  int tiles, splits, per_split;
+};
+AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int target, int least, int64_t max_q) {
+  const sats::BatchView &b = a.batch;
+  const int64_t per_seq = (max_q * a.group + R - 1) / R;
+  AttendPlan p;
+  p.tiles = (int)std::min<int64_t>(b.n_seqs * per_seq, b.n_tokens * a.group / R + b.n_seqs);
+  int64_t range = std::min<int64_t>(b.max_kv, b.max_pages << a.pool.shift);  // keys that a tile can see
+  if (a.window) range = std::min(range, a.window + R / a.group + 1 + a.sinks + 2 * keys);
+  const int64_t blocks = std::max<int64_t>(1, (range + keys - 1) / keys + 1);
+  const int64_t want = std::max<int64_t>(1, target / std::max<int64_t>(1, (int64_t)p.tiles * a.pool.n_kv));
+  p.per_split = (int)std::max<int64_t>(least, (blocks + want - 1) / want);
+  p.splits = (int)((blocks + p.per_split - 1) / p.per_split);
+  return p;
+}
+
+size_t attend_bytes(const AttendPlan &p, int R, int n_kv, int dim) {
+  return p.splits > 1 ? (size_t)p.tiles * n_kv * p.splits * R * (dim + 2) * sizeof(float) : 0;
+}
+
+template <typename T, int R, typename Kernel>
+int launch_attention(sats::AttendArgs a, const AttendPlan &p, Kernel kernel, char *mem, hipStream_t stream) {
+  const int64_t grid_x = (int64_t)p.tiles * a.pool.n_kv;
+  if (grid_x > 0x7fffffff || p.splits > 65535) return fail(SATS_ERR_SHAPE, "too many rows for one call");
+  a.tiles = p.tiles, a.splits = p.splits, a.per_split = p.per_split;
+  a.part = reinterpret_cast<float *>(mem);
+  a.part_ml = a.part + grid_x * p.splits * R * a.dim;
+  kernel<<<dim3((unsigned)grid_x, (unsigned)p.splits), 256, 0, stream>>>(a);
+  int rc = launched("attention kernel");
+  if (rc || p.splits == 1) return rc;
+  sats::attend_join_kernel<T, R><<<dim3((unsigned)grid_x, (unsigned)((std::min<int64_t>(R, a.batch.max_q * a.group) + 3) / 4)), 256, 0, stream>>>(a);
+  return launched("attend_join_kernel");
+}
+
+// Sequences of at most 16 rows a cache head, and all of float32, go in tiles of 16 rows,
+// the others in tiles of 128.  A batch of one sequence needs no launch for the former.
+template <typename T> int run_attention(sats::AttendArgs a, hipStream_t stream) {
+  constexpr bool bf16 = sizeof(T) == 2;
+  AttendPlan small{}, large{};
+  const bool any_large = bf16 && a.batch.max_q * a.group > 16;
+  if (!any_large || a.batch.n_seqs > 1) {
+    small = attend_plan(a, 16, sats::RowsOf<T>::kKeys, kRowsTarget, kRowsLeast, any_large ? 16 / a.group : a.batch.max_q);
+  }
+  if (any_large) large = attend_plan(a, sats::kTileRows, sats::kTileKeys, kTileTarget, kTileLeast, a.batch.max_q);
+  const size_t bytes = std::max(attend_bytes(small, 16, a.pool.n_kv, a.dim),
+                                attend_bytes(large, sats::kTileRows, a.pool.n_kv, a.dim));
+  char *mem = nullptr;
+  int rc = bytes ? sats_host::serve_workspace(stream, bytes, &mem) : SATS_OK;
+  if (rc) return rc;
+  if (small.tiles) {
+    a.small = 1, a.large = !bf16;
+    auto kernel = a.dim <= 64 ? sats::attend_rows_kernel<T, 64> : a.dim <= 128 ? sats::attend_rows_kernel<T, 128>
+                                                                                : sats::attend_rows_kernel<T, 256>;
+    if ((rc = launch_attention<T, 16>(a, small, kernel, mem, stream))) return rc;
+  }
+  if constexpr (bf16)
+    if (large.tiles) {
+      a.small = small.tiles == 0, a.large = 1;
+      auto kernel = a.dim <= 64 ? sats::attend_tile_kernel<64> : a.dim <= 128 ? sats::attend_tile_kernel<128>
+                                                                              : sats::attend_tile_kernel<256>;
+      rc = launch_attention<T, sats::kTileRows>(a, large, kernel, mem, stream);
+    }
+  return rc;
 }
 
 // ------------------------------------------------------------- pages
@@ -311,11 +384,10 @@ int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *c
   a.q = q, a.q_stride = q_stride, a.out = out, a.lse = lse;
   a.k = layer_of(cache->k, cache, layer), a.v = layer_of(cache->v, cache, layer);
   a.batch = batch_view(batch), a.pool = pool_view(cache);
-  a.n_q = (int)n_q_heads, a.dim = (int)cache->head_dim, a.scale = scale, a.window = window, a.sinks = n_sinks;
-  const dim3 grid((unsigned)n, (unsigned)n_q_heads);
-  if (esz == 2) sats::attend_simple_kernel<uint16_t><<<grid, 64, 0, stream>>>(a);
-  else sats::attend_simple_kernel<float><<<grid, 64, 0, stream>>>(a);
-  return launched("attend_simple_kernel");
+  a.n_q = (int)n_q_heads, a.group = (int)(n_q_heads / cache->n_kv_heads), a.dim = (int)cache->head_dim;
+  a.scale = scale, a.window = window, a.sinks = n_sinks;
+  if (batch->max_q_len == 0) return SATS_OK;
+  return esz == 2 ? run_attention<uint16_t>(a, stream) : run_attention<float>(a, stream);
 }
 
 int sats_cache_free(const sats_kv_cache *cache, const sats_kv_pages *pages, const int32_t *seqs, const int32_t *begin,
@@ -426,12 +498,16 @@ int sats_sample(const void *logits, int elem_bytes, int64_t stride, int64_t n, i
   return launched("sample kernels");
 }
 
-int sats_reserve_serving(int64_t max_items, int64_t n_pages, int64_t max_rows, int64_t vocab, hipStream_t stream) {
+int sats_reserve_serving(int64_t max_items, int64_t n_pages, int64_t max_rows, int64_t vocab, int64_t head_dim,
+                         hipStream_t stream) {
   clear_error();
   if (max_items < 0 || max_items > 65535 || n_pages < 0 || n_pages > kMaxCount || max_rows < 0 || max_rows > 65535 ||
-      vocab < 0 || vocab > kMaxVocab)
+      vocab < 0 || vocab > kMaxVocab || head_dim < 0 || head_dim > 256)
     return fail(SATS_ERR_SHAPE, "bad sizes for sats_reserve_serving");
   size_t bytes = 0;
+  // attention: a launch that splits its tiles has at most the target's workgroups
+  if (head_dim)
+    bytes = (size_t)std::max(kRowsTarget * 16, kTileTarget * sats::kTileRows) * (head_dim + 2) * sizeof(float);
   if (n_pages) bytes = std::max(bytes, pages_layout(nullptr, max_items, n_pages, nullptr));
   if (max_rows && vocab) bytes = std::max(bytes, sample_layout(nullptr, max_rows, vocab, nullptr));
   char *mem = nullptr;

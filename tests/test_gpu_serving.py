@@ -693,7 +693,7 @@ def test_a_decode_step_in_a_graph(sats):
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(s):
-        sats.sats_reserve_serving(n, 80, n, vocab, stream=s)
+        sats.sats_reserve_serving(n, 80, n, vocab, dim, stream=s)
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph, stream=s):
             step(a)
