@@ -326,58 +326,86 @@ def sats_route_table(loss_base, loss_sparse, token_ids, heldout_ids, vocab, r_ta
 
 # ------------------------------------------------------------------ serving
 
+# These calls are short enough for the binding to show, so it looks at each tensor once.
+
+_torch = None
+_raw_stream = None
+
+
+def _setup():
+    global _torch, _raw_stream
+    import torch
+    of_device = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    current = getattr(torch._C, "_cuda_getDevice", None)
+    _raw_stream = ((lambda: of_device(current())) if of_device and current
+                   else lambda: torch.cuda.current_stream().cuda_stream)
+    _torch = torch
+    return torch
+
+
+def _cur_stream(stream):
+    if stream is None:
+        return _raw_stream()
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
 def _elem_bytes(t) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
+    torch = _torch or _setup()
+    dt = t.dtype
+    if dt is torch.bfloat16:
         return 2
-    if t.dtype == torch.float32:
+    if dt is torch.float32:
         return 4
-    raise ValueError(f"bfloat16 or float32 is required, got {t.dtype}")
+    raise ValueError(f"bfloat16 or float32 is required, got {dt}")
 
 
-def _i32(t, shape=None, name="index array"):
-    """Pointer of a contiguous device int32 tensor (of this shape)."""
+def _array(t, dtype, n, name):
+    """Pointer of a contiguous device tensor of this type (and of n elements in one dimension)."""
     if t is None:
         return None
-    import torch
-    if t.dtype != torch.int32:
-        raise ValueError(f"{name}: int32 is required, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError(f"{name}: shape {shape} is required, got {tuple(t.shape)}")
-    return _ptr(t)
-
-
-def _f32(t, shape=None, name="array"):
-    if t is None:
-        return None
-    import torch
-    if t.dtype != torch.float32:
-        raise ValueError(f"{name}: float32 is required, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError(f"{name}: shape {shape} is required, got {tuple(t.shape)}")
-    return _ptr(t)
-
-
-def _heads(t, dtype, name, shape=None):
-    """(pointer, token stride) of [tokens][heads][head_dim] rows whose heads are dense."""
+    if t.dtype is not dtype:
+        raise ValueError(f"{name}: {dtype} is required, got {t.dtype}")
+    if n is not None and t.shape != (n,):
+        raise ValueError(f"{name}: shape ({n},) is required, got {tuple(t.shape)}")
     if not t.is_cuda:
         raise ValueError(f"{name}: device tensors are required")
-    if t.dtype != dtype or t.dim() != 3 or (shape is not None and tuple(t.shape) != shape):
-        raise ValueError(f"{name}: {dtype} [tokens][heads][head_dim]{'' if shape is None else f' = {shape}'} is required")
-    st, sz = t.stride(), t.shape
-    if (sz[2] > 1 and st[2] != 1) or (sz[1] > 1 and st[1] != sz[2]):
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous tensors are required")
+    return t.data_ptr()
+
+
+def _i32(t, n, name):
+    return _array(t, (_torch or _setup()).int32, n, name)
+
+
+def _f32(t, n, name):
+    return _array(t, (_torch or _setup()).float32, n, name)
+
+
+def _heads(t, dtype, name, shape):
+    """(pointer, token stride) of [tokens][heads][head_dim] rows whose heads are dense."""
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name}: {dtype} {shape} is required, got {t.dtype} {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: device tensors are required")
+    n, h, d = shape
+    s0, s1, s2 = t.stride()
+    if (s2 != 1 and d > 1) or (s1 != d and h > 1):
         raise ValueError(f"{name}: the heads of a token must be dense")
-    return t.data_ptr(), (st[0] if sz[0] > 1 else sz[1] * sz[2])
+    return t.data_ptr(), (s0 if n > 1 else h * d)
 
 
 class KVCache:
     """Keys and values of every layer in pages: k, v [n_layers][n_pages][n_kv_heads][page_size][head_dim]."""
 
+    __slots__ = ("k", "v", "dtype", "c", "ref")
+
     def __init__(self, k, v):
-        if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype:
+        shape, esz = k.shape, _elem_bytes(k)
+        if len(shape) != 5 or shape != v.shape or k.dtype is not v.dtype:
             raise ValueError("k and v must be alike: [n_layers][n_pages][n_kv_heads][page_size][head_dim]")
-        self.k, self.v = k, v
-        self.c = SatsKvCache(_ptr(k), _ptr(v), *k.shape, _elem_bytes(k))
+        self.k, self.v, self.dtype = k, v, k.dtype
+        self.c = SatsKvCache(_ptr(k), _ptr(v), *shape, esz)
         self.ref = ctypes.byref(self.c)
 
 
@@ -385,57 +413,52 @@ class KVBatch:
     """The new tokens of a batch of sequences (sats_kv_batch).
 
     table [n_seqs][max_pages], q_start [n_seqs + 1] and kv_len [n_seqs] are device
-    int32; max_q_len and max_kv_len are upper bounds (default: n_tokens, and what the
-    table can hold).
+    int32; max_q_len (default: n_tokens) and max_kv_len are upper bounds.
     """
 
-    def __init__(self, table, q_start, kv_len, n_tokens, max_q_len=None, max_kv_len=None, page_size=None):
-        if table.dim() != 2:
-            raise ValueError("table must be [n_seqs][max_pages]")
-        n, width = table.shape
+    __slots__ = ("keep", "n_tokens", "c", "ref")
+
+    def __init__(self, table, q_start, kv_len, n_tokens, max_q_len=None, max_kv_len=None):
+        n, width = _table(table)
         if max_kv_len is None:
-            if page_size is None:
-                raise ValueError("max_kv_len (or page_size, for the most that the table can hold) is required")
-            max_kv_len = width * page_size
+            raise ValueError("max_kv_len is required: an upper bound of kv_len")
         self.keep = (table, q_start, kv_len)
         self.n_tokens = n_tokens
-        self.c = SatsKvBatch(_i32(table, None, "table"), _i32(q_start, (n + 1,), "q_start"),
-                             _i32(kv_len, (n,), "kv_len"), n, width, n_tokens,
-                             n_tokens if max_q_len is None else max_q_len, max_kv_len)
+        self.c = SatsKvBatch(_i32(table, None, "table"), _i32(q_start, n + 1, "q_start"), _i32(kv_len, n, "kv_len"),
+                             n, width, n_tokens, n_tokens if max_q_len is None else max_q_len, max_kv_len)
         self.ref = ctypes.byref(self.c)
 
 
 class KVPages:
     """The pages' state: table [n_seqs][max_pages], len [n_seqs], refs [n_pages], device int32."""
 
+    __slots__ = ("table", "len", "refs", "n_pages", "c", "ref")
+
     def __init__(self, table, len, refs):
-        if table.dim() != 2:
-            raise ValueError("table must be [n_seqs][max_pages]")
-        n, width = table.shape
+        n, width = _table(table)
         self.table, self.len, self.refs = table, len, refs
-        self.c = SatsKvPages(_i32(table, None, "table"), _i32(len, (n,), "len"), _i32(refs, None, "refs"), n, width)
+        self.n_pages = refs.numel()
+        self.c = SatsKvPages(_i32(table, None, "table"), _i32(len, n, "len"), _i32(refs, self.n_pages, "refs"), n, width)
         self.ref = ctypes.byref(self.c)
 
 
+def _table(table):
+    shape = table.shape
+    if len(shape) != 2:
+        raise ValueError("table must be [n_seqs][max_pages]")
+    return shape
+
+
 def _of_pool(cache, pages):
-    if pages.refs.numel() != cache.c.n_pages:
+    if pages.n_pages != cache.c.n_pages:
         raise ValueError("refs must have an entry for every page of the cache")
-
-
-def _norm(t, q, dim, name):
-    if t is None:
-        return None
-    if t.dtype != q.dtype or tuple(t.shape) != (dim,):
-        raise ValueError(f"{name}: {q.dtype} [{dim}] is required")
-    return _ptr(t)
 
 
 def _rope(rope):
     if rope is None:
         return None, 0, 0
-    if rope.dim() != 2:
-        raise ValueError("rope must be [n_pos][rot_dim]")
-    return _f32(rope, None, "rope"), rope.shape[0], rope.shape[1]
+    n_pos, rot = rope.shape
+    return _f32(rope, None, "rope"), n_pos, rot
 
 
 def sats_qk_norm_rope(q, k, rope, positions, q_out, k_out, q_norm=None, k_norm=None, eps=1e-6, interleaved=False,
@@ -444,96 +467,101 @@ def sats_qk_norm_rope(q, k, rope, positions, q_out, k_out, q_norm=None, k_norm=N
 
     rope [n_pos][rot_dim] float32: cosines, then sines, of a position's angles (None: no rotation).
     """
-    n, hq, d = q.shape
+    shape, dt, esz = q.shape, q.dtype, _elem_bytes(q)
+    n, hq, d = shape
     hk = k.shape[1]
-    qp, qs = _heads(q, q.dtype, "q")
-    kp, ks = _heads(k, q.dtype, "k", (n, hk, d))
-    op, os_ = _heads(q_out, q.dtype, "q_out", (n, hq, d))
-    tp, ts = _heads(k_out, q.dtype, "k_out", (n, hk, d))
+    qp, qs = _heads(q, dt, "q", shape)
+    kp, ks = _heads(k, dt, "k", (n, hk, d))
+    op, os_ = _heads(q_out, dt, "q_out", shape)
+    tp, ts = _heads(k_out, dt, "k_out", (n, hk, d))
     rp, n_pos, rot = _rope(rope)
-    _call("sats_qk_norm_rope", qp, qs, kp, ks, _norm(q_norm, q, d, "q_norm"), _norm(k_norm, q, d, "k_norm"), eps, rp,
-          n_pos, _i32(positions, (n,), "positions"), op, os_, tp, ts, n, hq, hk, d, rot, int(interleaved),
-          _elem_bytes(q), _stream(stream))
+    _call("sats_qk_norm_rope", qp, qs, kp, ks, _array(q_norm, dt, d, "q_norm"), _array(k_norm, dt, d, "k_norm"), eps,
+          rp, n_pos, _i32(positions, n, "positions"), op, os_, tp, ts, n, hq, hk, d, rot, int(interleaved), esz,
+          _cur_stream(stream))
 
 
 def sats_qkv_append(q, k, v, rope, q_out, cache, layer, batch, q_norm=None, k_norm=None, eps=1e-6, positions=None,
                     interleaved=False, stream=None):
     """sats_qk_norm_rope of a batch's tokens, with k and v appended to a layer of the cache."""
-    n, hq, d = q.shape
-    dt, c = cache.k.dtype, cache.c
-    rows = (n, c.n_kv_heads, c.head_dim)
+    shape, dt, c = q.shape, cache.dtype, cache.c
+    n, hq, d = shape
     if n != batch.n_tokens or d != c.head_dim:
         raise ValueError("q must have the batch's tokens and the cache's head_dim")
-    qp, qs = _heads(q, dt, "q")
+    rows = (n, c.n_kv_heads, d)
+    qp, qs = _heads(q, dt, "q", shape)
     kp, ks = _heads(k, dt, "k", rows)
     vp, vs = _heads(v, dt, "v", rows)
-    op, os_ = _heads(q_out, dt, "q_out", (n, hq, d))
+    op, os_ = _heads(q_out, dt, "q_out", shape)
     rp, n_pos, rot = _rope(rope)
-    _call("sats_qkv_append", qp, qs, kp, ks, vp, vs, _norm(q_norm, q, d, "q_norm"), _norm(k_norm, q, d, "k_norm"), eps,
-          rp, n_pos, _i32(positions, (n,), "positions"), op, os_, cache.ref, layer, batch.ref, hq, rot,
-          int(interleaved), _stream(stream))
+    _call("sats_qkv_append", qp, qs, kp, ks, vp, vs, _array(q_norm, dt, d, "q_norm"), _array(k_norm, dt, d, "k_norm"),
+          eps, rp, n_pos, _i32(positions, n, "positions"), op, os_, cache.ref, layer, batch.ref, hq, rot,
+          int(interleaved), _cur_stream(stream))
 
 
 def sats_paged_attention(q, cache, layer, batch, out, scale, window=0, n_sinks=0, lse=None, stream=None):
     """Attention of a batch's new tokens over a layer of the cache (window 0: every earlier key)."""
-    n, hq, d = q.shape
+    shape, dt = q.shape, cache.dtype
+    n, hq, d = shape
     if n != batch.n_tokens or d != cache.c.head_dim:
         raise ValueError("q must have the batch's tokens and the cache's head_dim")
-    if out.shape != q.shape or out.dtype != q.dtype:
+    if out.shape != shape or out.dtype is not dt:
         raise ValueError("out must be like q")
-    qp, qs = _heads(q, cache.k.dtype, "q")
+    qp, qs = _heads(q, dt, "q", shape)
+    if lse is not None and lse.shape != (n, hq):
+        raise ValueError("lse must be [n_tokens][n_q_heads]")
     _call("sats_paged_attention", qp, qs, cache.ref, layer, batch.ref, hq, scale, window, n_sinks, _ptr(out),
-          _f32(lse, (n, hq), "lse"), _stream(stream))
+          _f32(lse, None, "lse"), _cur_stream(stream))
 
 
 def sats_cache_extend(cache, pages, seqs, add, status=None, stream=None):
     """Room for add[i] more tokens in sequence seqs[i] (None: i); status int32 [2]: pages missing, items left out."""
     _of_pool(cache, pages)
     n = add.numel()
-    _call("sats_cache_extend", cache.ref, pages.ref, _i32(seqs, (n,), "seqs"), _i32(add, (n,), "add"), n,
-          _i32(status, (2,), "status"), _stream(stream))
+    _call("sats_cache_extend", cache.ref, pages.ref, _i32(seqs, n, "seqs"), _i32(add, n, "add"), n,
+          _i32(status, 2, "status"), _cur_stream(stream))
 
 
 def sats_cache_fork(cache, pages, src, dst, status=None, stream=None):
     """Sequence dst[i] (empty) becomes a copy of src[i]; status as in sats_cache_extend."""
     _of_pool(cache, pages)
     n = src.numel()
-    _call("sats_cache_fork", cache.ref, pages.ref, _i32(src, (n,), "src"), _i32(dst, (n,), "dst"), n,
-          _i32(status, (2,), "status"), _stream(stream))
+    _call("sats_cache_fork", cache.ref, pages.ref, _i32(src, n, "src"), _i32(dst, n, "dst"), n,
+          _i32(status, 2, "status"), _cur_stream(stream))
 
 
 def sats_cache_free(cache, pages, seqs, begin=None, end=None, stream=None):
     """Gives back the pages wholly in tokens begin[i] .. end[i] - 1 (None: from 0, to the length) of seqs[i]."""
     _of_pool(cache, pages)
     n = seqs.numel()
-    _call("sats_cache_free", cache.ref, pages.ref, _i32(seqs, (n,), "seqs"), _i32(begin, (n,), "begin"),
-          _i32(end, (n,), "end"), n, _stream(stream))
+    _call("sats_cache_free", cache.ref, pages.ref, _i32(seqs, n, "seqs"), _i32(begin, n, "begin"),
+          _i32(end, n, "end"), n, _cur_stream(stream))
 
 
 def sats_cache_compact(cache, pages, n_used=None, stream=None):
     """Moves the pages in use to the front of the pool; n_used (device int32 [1]): how many they are."""
     _of_pool(cache, pages)
-    _call("sats_cache_compact", cache.ref, pages.ref, _i32(n_used, (1,), "n_used"), _stream(stream))
+    _call("sats_cache_compact", cache.ref, pages.ref, _i32(n_used, 1, "n_used"), _cur_stream(stream))
 
 
 def sats_cache_copy(cache, src_pages, dst_pages, stream=None):
     """Contents of pages src_pages[i] to dst_pages[i], in every layer."""
     n = src_pages.numel()
-    _call("sats_cache_copy", cache.ref, _i32(src_pages, (n,), "src_pages"), _i32(dst_pages, (n,), "dst_pages"), n,
-          _stream(stream))
+    _call("sats_cache_copy", cache.ref, _i32(src_pages, n, "src_pages"), _i32(dst_pages, n, "dst_pages"), n,
+          _cur_stream(stream))
 
 
 def sats_sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, n_kept=None,
                 stream=None):
     """The next id of each row of logits [n][vocab] (rows may be strided) from u [n]."""
-    if not logits.is_cuda or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
-        raise ValueError("logits must be a device tensor [n][vocab] with dense rows")
     n, vocab = logits.shape
-    one = (n,)
-    _call("sats_sample", logits.data_ptr(), _elem_bytes(logits), logits.stride(0) if n > 1 else vocab, n, vocab,
-          _f32(temperature, one, "temperature"), _i32(top_k, one, "top_k"), _f32(top_p, one, "top_p"),
-          _f32(min_p, one, "min_p"), _f32(u, one, "u"), _i32(tokens, one, "tokens"), _f32(prob, one, "prob"),
-          _i32(n_kept, one, "n_kept"), _stream(stream))
+    esz = _elem_bytes(logits)
+    s0, s1 = logits.stride()
+    if not logits.is_cuda or (vocab > 1 and s1 != 1):
+        raise ValueError("logits must be a device tensor [n][vocab] with dense rows")
+    _call("sats_sample", logits.data_ptr(), esz, s0 if n > 1 else vocab, n, vocab,
+          _f32(temperature, n, "temperature"), _i32(top_k, n, "top_k"), _f32(top_p, n, "top_p"),
+          _f32(min_p, n, "min_p"), _f32(u, n, "u"), _i32(tokens, n, "tokens"), _f32(prob, n, "prob"),
+          _i32(n_kept, n, "n_kept"), _cur_stream(stream))
 
 
 def sats_reserve_serving(max_items=0, n_pages=0, max_rows=0, vocab=0, head_dim=0, stream=None):

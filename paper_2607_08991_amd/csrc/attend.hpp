@@ -674,13 +674,17 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
 
 // ------------------------------------------------------------------ join
 
-// Joins the parts of a tile's rows where it was split: a wave per row.
-template <typename T, int R>
+// Joins the parts of a tile's rows where it was split: W waves per row, each part of a row
+// held by `lanes` lanes, so that a wave adds 64 / lanes parts at a time and the W waves'
+// loads are all in flight.  The order of a row's sum depends on the batch's bounds alone.
+template <typename T, int R, int W>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   constexpr int kKeys = R == 16 ? RowsOf<T>::kKeys : kTileKeys;
+  __shared__ float ls[W > 1 ? W : 1];
+  __shared__ f32x4 os[W > 1 ? W : 1][64];
   const RowTile t = find_tile<R>(a, blockIdx.x / a.pool.n_kv);
-  const int r = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (t.seq < 0 || r >= t.count) return;
+  const int wave = threadIdx.x >> 6, r = blockIdx.y * (4 / W) + wave / W, w = wave % W, lane = threadIdx.x & 63;
+  if (t.seq < 0 || (W > 1 ? (int)blockIdx.y : r) >= t.count) return;  // (W > 1: a row a workgroup)
   const KeyBlocks kb = key_blocks<kKeys>(a, t);
   const int parts = kb.n > a.per_split ? (kb.n + a.per_split - 1) / a.per_split : 1;
   if (parts == 1) return;
@@ -690,21 +694,33 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 #pragma unroll
   for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
   const float at0 = top == -INFINITY ? 0.0f : top;
+  const int lanes = a.dim <= 64 ? 16 : a.dim <= 128 ? 32 : 64, sub = lane / lanes, per = 64 / lanes;
+  const int d = lane % lanes * 4, dd = d < a.dim ? d : 0;
   float l = 0.0f;
   f32x4 o = f32x4{0, 0, 0, 0};
-  const int d = lane * 4 < a.dim ? lane * 4 : 0;
-  for (int z0 = 0; z0 < parts; z0 += 64) {
-    float f = 0.0f, lz = 0.0f;
-    if (z0 + lane < parts) {
-      const float *p = a.part_ml + (at + (int64_t)(z0 + lane) * R) * 2;
-      f = exp2_fast(p[0] - at0), lz = p[1] * f;
-    }
-    l += wave_sum(lz);
-    const int n = parts - z0 < 64 ? parts - z0 : 64;
-#pragma unroll 8
-    for (int z = 0; z < n; ++z) o += *reinterpret_cast<const f32x4 *>(a.part + (at + (int64_t)(z0 + z) * R) * a.dim + d) * __shfl(f, z);
+#pragma unroll 4
+  for (int z0 = w * per; z0 < parts; z0 += W * per) {
+    const int z = z0 + sub < parts ? z0 + sub : parts - 1;
+    const float *ml = a.part_ml + (at + (int64_t)z * R) * 2;
+    const float f = z0 + sub < parts ? exp2_fast(ml[0] - at0) : 0.0f;
+    const f32x4 x = *reinterpret_cast<const f32x4 *>(a.part + (at + (int64_t)z * R) * a.dim + dd);
+    if (f != 0.0f) l += ml[1] * f, o += x * f;  // (f is NaN where the row's maximum is an infinity)
   }
-  if (lane * 4 < a.dim) put_row<T>(a, t, r, blockIdx.x % a.pool.n_kv, lane * 4, o, top, l);
+  for (int m = lanes; m < 64; m <<= 1) {
+    l += __shfl_xor(l, m);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], m);
+  }
+  if constexpr (W > 1) {
+    os[w][lane] = o;
+    if (lane == 0) ls[w] = l;
+    __syncthreads();
+    if (w) return;
+    o = f32x4{0, 0, 0, 0}, l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) o += os[i][lane], l += ls[i];
+  }
+  if (lane < lanes && d < a.dim) put_row<T>(a, t, r, blockIdx.x % a.pool.n_kv, d, o, top, l);
 }
 
 }  // namespace sats

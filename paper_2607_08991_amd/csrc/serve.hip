@@ -33,6 +33,8 @@ struct Carve {
 
 constexpr int64_t kMaxCount = (int64_t)1 << 30;
 
+// Parts up to which one wave joins a row.
+constexpr int kJoinWave = 16;
 // Attention: workgroups that a launch aims at, and key blocks below which no tile is split.
 constexpr int kRowsTarget = 4096, kRowsLeast = 8, kTileTarget = 512, kTileLeast = 4;
 
@@ -185,7 +187,9 @@ int launch_attention(sats::AttendArgs a, const AttendPlan &p, Kernel kernel, cha
   kernel<<<dim3((unsigned)grid_x, (unsigned)p.splits), 256, 0, stream>>>(a);
   int rc = launched("attention kernel");
   if (rc || p.splits == 1) return rc;
-  sats::attend_join_kernel<T, R><<<dim3((unsigned)grid_x, (unsigned)((std::min<int64_t>(R, a.batch.max_q * a.group) + 3) / 4)), 256, 0, stream>>>(a);
+  const int64_t rows = std::min<int64_t>(R, a.batch.max_q * a.group);
+  if (p.splits > kJoinWave) sats::attend_join_kernel<T, R, 4><<<dim3((unsigned)grid_x, (unsigned)rows), 256, 0, stream>>>(a);
+  else sats::attend_join_kernel<T, R, 1><<<dim3((unsigned)grid_x, (unsigned)((rows + 3) / 4)), 256, 0, stream>>>(a);
   return launched("attend_join_kernel");
 }
 
