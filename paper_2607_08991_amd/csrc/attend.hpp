@@ -144,8 +144,17 @@ __device__ __forceinline__ int64_t block_key(const KeyBlocks &k, int b, int keys
   return (b < k.n_sink ? b : k.first + (b - k.n_sink)) * keys;
 }
 
-__device__ __forceinline__ bool sees(const AttendArgs &a, int64_t place, int64_t j) {
-  return j <= place && (!a.window || place - j < a.window || j < a.sinks);
+// Which keys of the block from j0 on the token at `place` sees: key j0 + i where
+// i <= last and (i >= from or i < sink).  (Differences cut off to 32 bits: a block is short.)
+struct Sight {
+  int last, from, sink;
+  __device__ __forceinline__ bool sees(int i) const { return (i <= last) & ((i >= from) | (i < sink)); }
+};
+__device__ __forceinline__ int cut_off(int64_t v) {
+  return (int)(v < -(1 << 30) ? -(1 << 30) : v > 1 << 30 ? 1 << 30 : v);
+}
+__device__ __forceinline__ Sight sight_of(const AttendArgs &a, int64_t place, int64_t j0) {
+  return {cut_off(place - j0), a.window ? cut_off(place - j0 - a.window + 1) : 0, cut_off(a.sinks - j0)};
 }
 // Whether any row of a tile at places low .. high sees key j.
 __device__ __forceinline__ bool any_sees(const AttendArgs &a, const KeyBlocks &k, int64_t len, int64_t j) {
@@ -338,18 +347,22 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_rows_kernel(Atte
       load(b + 4, page);
       page_next = page_of(b + 8);
     }
+#pragma unroll
+    for (int kt = 0; kt < kTiles; ++kt) s[kt] *= scale2;
+    if (!whole) {
+      const Sight sight = sight_of(a, place, j0);
+      const uint32_t here = (uint32_t)there >> (4 * g);
+#pragma unroll
+      for (int kt = 0; kt < kTiles; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          s[kt][i] = ((here >> (16 * kt + i) & 1) != 0) & sight.sees(16 * kt + 4 * g + i) ? s[kt][i] : -INFINITY;
+    }
     float top = -INFINITY;
 #pragma unroll
     for (int kt = 0; kt < kTiles; ++kt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[kt][i] *= scale2;
-        if (!whole) {
-          const int k = 16 * kt + 4 * g + i;
-          if (!(there >> k & 1) || !sees(a, place, j0 + k)) s[kt][i] = -INFINITY;
-        }
-        top = fmaxf(top, s[kt][i]);
-      }
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, s[kt][i]);
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
     const float mn = fmaxf(m, top), at0 = mn == -INFINITY ? 0.0f : mn, f = exp2_fast(m - at0);
@@ -476,12 +489,123 @@ __device__ __forceinline__ void stage_barrier() {
   asm volatile("" ::: "memory");
 }
 
+// The state of a wave's 32 rows: O^T, and of this lane's row the running maximum (of the
+// scores before the scale) and the sum.
+template <int DT> struct TileSums {
+  f32x16_t acc[DT / 32];
+  float m, l;
+};
+
+// One block for one wave: scores, softmax step, product.  `there`: the block's keys that
+// some row of the tile sees.  Returns whether values of keys on which the rows disagree
+// hold infinities or NaN (ODD false: the product then has to be made again with ODD).
+template <int DT, bool ODD>
+__device__ __forceinline__ bool tile_step(const AttendArgs &a, TileSums<DT> &t, const bf16x8_t (&qv)[DT / 16], float scale2,
+                                          const uint8_t *kt, const uint8_t *vt, uint64_t there, int64_t j0, int64_t place,
+                                          int64_t low, int64_t high) {
+  constexpr int kRow = DT * 2, kChunks = kRow / 16, kOut = DT / 32, kSteps = DT / 16;
+  constexpr int kLine = kRow < 256 ? 256 / kRow : 1, kMask = (kRow / 32 < 8 ? kRow / 32 : 8) - 1;
+  const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5;
+  f32x16_t s[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[x][i] = 0.0f;
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st) {
+      const int r = 32 * x + col;
+      const u32x4 kv = *reinterpret_cast<const u32x4 *>(kt + r * kRow + ((2 * st + hf) ^ ((r / kLine) & (2 * kMask + 1))) * 16);
+      s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kv), qv[st], s[x], 0, 0, 0);
+    }
+  }
+  bool odd = false;
+  const bool whole = there == ~0ull && j0 + kTileKeys - 1 <= low &&
+                     (!a.window || high - j0 < a.window || j0 + kTileKeys <= a.sinks);
+  if (!whole) {
+    const Sight sight = sight_of(a, place, j0);
+    const uint64_t here = there >> (4 * hf);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int k = 32 * x + 8 * (i >> 2) + (i & 3);  // (and 4 hf)
+        s[x][i] = ((here >> k & 1) != 0) & sight.sees(k + 4 * hf) ? s[x][i] : -INFINITY;
+      }
+    for (int c = lane; c < kTileKeys * kChunks; c += 64) odd |= odd_value<uint16_t>(*reinterpret_cast<const u32x4 *>(vt + c * 16));
+    odd = __any(odd);
+    if (odd && !ODD) return true;
+  }
+  float top = s[0][0];
+#pragma unroll
+  for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+  top = fmaxf(top, __shfl_xor(top, 32));
+  // the maximum moves, and the sums are scaled to it, only where a weight would pass 2^8
+  if (__any(!((top - t.m) * scale2 <= 8.0f))) {
+    const float mn = fmaxf(t.m, top), f = mn == t.m ? 1.0f : exp2_fast((t.m - mn) * scale2);
+    t.m = mn;
+    t.l *= f;
+#pragma unroll
+    for (int o = 0; o < kOut; ++o)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t.acc[o][i] *= f;
+  }
+  const float base = t.m == -INFINITY ? 0.0f : -t.m * scale2;
+  float sum = 0.0f;
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[x][i] = exp2_fast(fmaf(s[x][i], scale2, base));
+      sum += s[x][i];
+    }
+  t.l += sum;
+#pragma unroll
+  for (int st = 0; st < 4; ++st) {
+    bf16x8_t p;  // contraction slot (hf, e): key 16 st + 8 (e / 4) + 4 hf + e % 4
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[st >> 1][8 * (st & 1) + e];
+#pragma unroll
+    for (int o = 0; o < kOut; ++o) {
+      i16x4_t v2[2];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int r = 16 * st + 8 * y + 4 * hf + ((lane & 15) >> 2);
+        const int c = (4 * o + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (2 * ((r / kLine) & kMask));
+        v2[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(vt + r * kRow + c * 16 + (lane & 1) * 8));
+        if (ODD && odd) v2[y] = sane(v2[y]);
+      }
+      bf16x8_t v8;
+      __builtin_memcpy(&v8, v2, 16);
+      t.acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, p, t.acc[o], 0, 0, 0);
+    }
+  }
+  if (ODD && odd) {
+#pragma unroll 1
+    for (int k = 0; k < kTileKeys; ++k) {
+      float p = 0.0f;
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if ((k >> 5) == x && ((k >> 3) & 3) == i >> 2 && (k & 3) == (i & 3)) p = s[x][i];
+      p = __shfl(p, col + 32 * ((k >> 2) & 1));
+#pragma unroll
+      for (int o = 0; o < kOut; ++o)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int d = 32 * o + 8 * (e >> 2) + 4 * hf + (e & 3);
+          const uint16_t *v = reinterpret_cast<const uint16_t *>(vt + k * kRow + ((d >> 3) ^ (2 * ((k / kLine) & kMask))) * 16);
+          if (p != 0.0f && odd_bits(v[d & 7])) t.acc[o][e] += p * bf16_to_f32(v[d & 7]);
+        }
+    }
+  }
+  return false;
+}
+
 template <int DT>
 __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a) {
   constexpr int kRow = DT * 2, kChunks = kRow / 16, kLoads = kTileKeys * kChunks / 256, kOut = DT / 32, kSteps = DT / 16;
   constexpr int kLine = kRow < 256 ? 256 / kRow : 1, kMask = (kRow / 32 < 8 ? kRow / 32 : 8) - 1;
-  auto k_place = [](int r, int c) { return c ^ ((r / kLine) & (2 * kMask + 1)); };
-  auto v_place = [](int r, int c) { return c ^ (2 * ((r / kLine) & kMask)); };
   // (arrays of their own, so that reads of one do not wait for loads into another)
   __shared__ __align__(16) uint8_t k0[kTileKeys * kRow], k1[kTileKeys * kRow], v0[kTileKeys * kRow], v1[kTileKeys * kRow];
 
@@ -492,13 +616,14 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
   const int parts = kb.n > a.per_split ? (kb.n + a.per_split - 1) / a.per_split : 1;
   if (z >= parts) return;
   const int b0 = z * a.per_split, b_end = kb.n < b0 + a.per_split ? kb.n : b0 + a.per_split;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, col = lane & 31, hf = lane >> 5;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, hf = lane >> 5;
   const int row = 32 * w + col, r_in = row < t.count ? row : t.count - 1;  // (rows past the last repeat it)
   const int64_t place = t.place0 + (t.first + r_in) / a.group;
   // places of this wave's first and last row
   const int w_lo = 32 * w < t.count ? 32 * w : t.count - 1, w_hi = 32 * w + 31 < t.count ? 32 * w + 31 : t.count - 1;
   const int64_t low = t.place0 + (t.first + w_lo) / a.group, high = t.place0 + (t.first + w_hi) / a.group;
 
+  // q with the scale's sign (zeros for a scale of 0), so that the largest product is the largest score
   bf16x8_t qv[kSteps];
   {
     const int r = t.first + r_in;
@@ -507,11 +632,12 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
       const int c = 2 * s + hf;
-      const u32x4 x = c * 8 < a.dim ? *reinterpret_cast<const u32x4 *>(q + c * 8) : u32x4{0, 0, 0, 0};
+      u32x4 x = c * 8 < a.dim && a.scale != 0.0f ? *reinterpret_cast<const u32x4 *>(q + c * 8) : u32x4{0, 0, 0, 0};
+      if (a.scale < 0.0f) x ^= 0x80008000u;
       qv[s] = __builtin_bit_cast(bf16x8_t, x);
     }
   }
-  const float scale2 = a.scale * kLog2e;
+  const float scale2 = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;
   const char *zeros = reinterpret_cast<const char *>(attend_zeros);
   const int64_t head_bytes = ((int64_t)kvh << a.pool.shift) * a.dim * 2;
   const int64_t page_bytes = ((int64_t)a.pool.n_kv << a.pool.shift) * a.dim * 2;
@@ -519,153 +645,74 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
   const int row_bytes = a.dim * 2;
 
   auto page_of = [&](int b) { return b < b_end ? key_page(a, t, kb, block_key(kb, b, kTileKeys) + lane) : -1; };
-  // wave w loads rows 16 w .. of the block (K and V)
-  auto issue = [&](int b, int page, uint8_t *kd, uint8_t *vd) {
+  // wave w loads rows 16 w .. 16 w + 15 of the block (K and V); where all of them are there, in
+  // one page and whole, from one address and fixed offsets
+  auto issue = [&](int b, int page, uint64_t there, uint8_t *kd, uint8_t *vd) {
     const int j0 = (int)(block_key(kb, b, kTileKeys) & (a.pool.page - 1));
+    uint8_t *kw = kd + w * kLoads * 1024, *vw = vd + w * kLoads * 1024;
+    if (a.pool.shift >= 4 && (there >> (16 * w) & 0xffffu) == 0xffffu && a.dim == DT) {
+      const int64_t p = __builtin_amdgcn_readlane(page, 16 * w);
+      const int64_t off = p * page_bytes + ((j0 + 16 * w) & (a.pool.page - 1)) * kRow;
+      const char *ks = kp + off, *vs = vp + off;
 #pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = (i * 64 + lane) / kChunks, x = lane % kChunks;
+        load_to_lds(ks + (uint32_t)(r * kRow + (x ^ ((r / kLine) & (2 * kMask + 1))) * 16), kw + i * 1024);
+        load_to_lds(vs + (uint32_t)(r * kRow + (x ^ (2 * ((r / kLine) & kMask))) * 16), vw + i * 1024);
+      }
+      return;
+    }
+#pragma unroll 1
     for (int i = 0; i < kLoads; ++i) {
-      const int at = (w * kLoads + i) * 64 + lane, r = at / kChunks, x = at % kChunks;
-      const int p = __shfl(page, r), slot = (j0 + r) & (a.pool.page - 1);
-      const int64_t off = p * page_bytes + slot * row_bytes;
-      const int kc = k_place(r, x), vc = v_place(r, x);  // (the exchange is its own inverse)
-      load_to_lds(p >= 0 && kc * 8 < a.dim ? kp + off + kc * 16 : zeros, kd + (w * kLoads + i) * 1024);
-      load_to_lds(p >= 0 && vc * 8 < a.dim ? vp + off + vc * 16 : zeros, vd + (w * kLoads + i) * 1024);
+      const int r = (i * 64 + lane) / kChunks, x = lane % kChunks, p = __shfl(page, 16 * w + r);
+      const int64_t off = p * page_bytes + ((j0 + 16 * w + r) & (a.pool.page - 1)) * row_bytes;
+      const int kc = x ^ ((r / kLine) & (2 * kMask + 1)), vc = x ^ (2 * ((r / kLine) & kMask));
+      load_to_lds(p >= 0 && kc * 8 < a.dim ? kp + off + kc * 16 : zeros, kw + i * 1024);
+      load_to_lds(p >= 0 && vc * 8 < a.dim ? vp + off + vc * 16 : zeros, vw + i * 1024);
     }
   };
 
-  f32x16_t acc[kOut];
-#pragma unroll
-  for (int o = 0; o < kOut; ++o)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[o][i] = 0.0f;
-  float m = -INFINITY, l = 0.0f;
-
-  auto work = [&](int b, int page, const uint8_t *kt, const uint8_t *vt) {
-    const int64_t j0 = block_key(kb, b, kTileKeys);
-    const uint64_t there = __ballot(page >= 0);
-    const bool whole = there == ~0ull && j0 + kTileKeys - 1 <= low &&
-                       (!a.window || high - j0 < a.window || j0 + kTileKeys <= a.sinks);
-    f32x16_t s[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[x][i] = 0.0f;
-#pragma unroll
-      for (int st = 0; st < kSteps; ++st) {
-        const int r = 32 * x + col;
-        const u32x4 kv = *reinterpret_cast<const u32x4 *>(kt + r * kRow + k_place(r, 2 * st + hf) * 16);
-        s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kv), qv[st], s[x], 0, 0, 0);
-      }
-    }
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[x][i] *= scale2;
-    bool odd = false;
-    if (!whole) {
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int k = 32 * x + 8 * (i >> 2) + 4 * hf + (i & 3);
-          if (!(there >> k & 1) || !sees(a, place, j0 + k)) s[x][i] = -INFINITY;
-        }
-      for (int c = lane; c < kTileKeys * kChunks; c += 64) odd |= odd_value<uint16_t>(*reinterpret_cast<const u32x4 *>(vt + c * 16));
-      odd = __any(odd);
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[x][i]);
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float mn = fmaxf(m, top), at0 = mn == -INFINITY ? 0.0f : mn, f = exp2_fast(m - at0);
-    m = mn;
-    float sum = 0.0f;
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[x][i] = exp2_fast(s[x][i] - at0);
-        sum += s[x][i];
-      }
-    l = l * f + sum;
+  TileSums<DT> sums;
+  // The tile's blocks; block b lives in buffer (b - b0) % 2: it has landed when every load is
+  // done, and the other buffer is free when every wave is past the barrier.  Returns
+  // whether a product has to be made again.
+  auto run = [&](auto kind) {
+    constexpr bool kOdd = decltype(kind)::kOdd;
 #pragma unroll
     for (int o = 0; o < kOut; ++o)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[o][i] *= f;
-    auto product = [&](auto kind) {
-      constexpr bool kOdd = decltype(kind)::kOdd;
-#pragma unroll
-      for (int st = 0; st < 4; ++st) {
-        bf16x8_t p;  // contraction slot (hf, e): key 16 st + 8 (e / 4) + 4 hf + e % 4
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[st >> 1][8 * (st & 1) + e];
-#pragma unroll
-        for (int o = 0; o < kOut; ++o) {
-          i16x4_t v2[2];
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const int r = 16 * st + 8 * y + 4 * hf + ((lane & 15) >> 2);
-            const int c = 4 * o + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-            v2[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(vt + r * kRow + v_place(r, c) * 16 + (lane & 1) * 8));
-            if (kOdd) v2[y] = sane(v2[y]);
-          }
-          bf16x8_t v8;
-          __builtin_memcpy(&v8, v2, 16);
-          acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, p, acc[o], 0, 0, 0);
-        }
-      }
+      for (int i = 0; i < 16; ++i) sums.acc[o][i] = 0.0f;
+    sums.m = -INFINITY, sums.l = 0.0f;
+    bool again = false;
+    int next = page_of(b0), after = page_of(b0 + 1);
+    uint64_t there = 0, there_next = __ballot(next >= 0);
+    if (b0 < b_end) issue(b0, next, there_next, k0, v0);
+    auto step = [&](int b, uint8_t *kt, uint8_t *vt, uint8_t *kn, uint8_t *vn) {
+      stage_barrier();
+      there = there_next, next = after;
+      there_next = __ballot(next >= 0);
+      if (b + 1 < b_end) issue(b + 1, next, there_next, kn, vn);
+      after = page_of(b + 2);
+      if (!again)
+        again = tile_step<DT, kOdd>(a, sums, qv, scale2, kt, vt, there, block_key(kb, b, kTileKeys), place, low, high);
     };
-    if (!odd) {
-      product(Plain{});
-    } else {
-      product(Odd{});
-#pragma unroll 1
-      for (int k = 0; k < kTileKeys; ++k) {
-        float p = 0.0f;
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if ((k >> 5) == x && ((k >> 3) & 3) == i >> 2 && (k & 3) == (i & 3)) p = s[x][i];
-        p = __shfl(p, col + 32 * ((k >> 2) & 1));
-#pragma unroll
-        for (int o = 0; o < kOut; ++o)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int d = 32 * o + 8 * (e >> 2) + 4 * hf + (e & 3);
-            const float v = Elem<uint16_t>::get(reinterpret_cast<const uint16_t *>(vt + k * kRow + v_place(k, d >> 3) * 16) + (d & 7));
-            if (p != 0.0f && odd_of(v)) acc[o][e] += p * v;
-          }
-      }
+    for (int b = b0; b < b_end; b += 2) {
+      step(b, k0, v0, k1, v1);
+      if (b + 1 < b_end) step(b + 1, k1, v1, k0, v0);
     }
+    return again;
   };
+  if (__syncthreads_or(run(Plain{}))) run(Odd{});
 
-  // block b lives in buffer (b - b0) % 2: it has landed when every load is done, and the
-  // other buffer is free when every wave is past the barrier
-  int page = page_of(b0), next = page_of(b0 + 1);
-  if (b0 < b_end) issue(b0, page, k0, v0);
-  for (int b = b0; b < b_end; b += 2) {
-    stage_barrier();
-    int after = page_of(b + 2);
-    if (b + 1 < b_end) issue(b + 1, next, k1, v1);
-    work(b, page, k0, v0);
-    if (b + 1 >= b_end) break;
-    page = next, next = after;
-    stage_barrier();
-    after = page_of(b + 3);
-    if (b + 2 < b_end) issue(b + 2, next, k0, v0);
-    work(b + 1, page, k1, v1);
-    page = next, next = after;
-  }
+  float l = sums.l;
   l += __shfl_xor(l, 32);
   if (row >= t.count) return;
+  const float m = sums.m * scale2;
 #pragma unroll
   for (int o = 0; o < kOut; ++o)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const f32x4 v = {acc[o][4 * e], acc[o][4 * e + 1], acc[o][4 * e + 2], acc[o][4 * e + 3]};
+      const f32x4 v = {sums.acc[o][4 * e], sums.acc[o][4 * e + 1], sums.acc[o][4 * e + 2], sums.acc[o][4 * e + 3]};
       const int d = 32 * o + 8 * e + 4 * hf;
       if (parts > 1) put_part(a, ((int64_t)blockIdx.x * a.splits + z) * kTileRows + row, d, v, m, l);
       else put_row<uint16_t>(a, t, row, kvh, d, v, m, l);

@@ -36,7 +36,7 @@ constexpr int64_t kMaxCount = (int64_t)1 << 30;
 // Parts up to which one wave joins a row.
 constexpr int kJoinWave = 16;
 // Attention: workgroups that a launch aims at, and key blocks below which no tile is split.
-constexpr int kRowsTarget = 4096, kRowsLeast = 8, kTileTarget = 512, kTileLeast = 4;
+constexpr int kRowsTarget = 2048, kRowsLeast = 16, kTileTarget = 512, kTileLeast = 4;
 
 int launched(const char *what) {
   const hipError_t e = hipGetLastError();
