@@ -475,10 +475,17 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_rows_kernel(Atte
 // same piece of 8 rows; V: two pieces of 4 rows) read different banks.
 constexpr int kTileRows = 128, kTileKeys = 64;
 
-// 16 bytes of each lane into LDS at dst + 16 * lane (dst the same for the whole wave).
-__device__ __forceinline__ void load_to_lds(const void *src, uint8_t *dst) {
+// 16 bytes of each lane into LDS at dst + OFF + 16 * lane, from src + OFF (dst the same for
+// the whole wave).
+template <int OFF> __device__ __forceinline__ void load_to_lds(const char *src, uint8_t *dst) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
-                                   (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
+                                   (__attribute__((address_space(3))) void *)dst, 16, OFF, 0);
+}
+// The same from base + off, base the same for the whole wave.
+template <int OFF> __device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint8_t *dst) {
+  const __amdgpu_buffer_rsrc_t r =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), (short)0, 0x7fffffff, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)dst, 16, (int)off, 0, OFF, 0);
 }
 
 // Every load of this wave has landed, and every wave is here.
@@ -489,97 +496,179 @@ __device__ __forceinline__ void stage_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// The state of a wave's 32 rows: O^T, and of this lane's row the running maximum (of the
-// scores before the scale) and the sum.
-template <int DT> struct TileSums {
-  f32x16_t acc[DT / 32];
-  float m, l;
+// Pages of a tile's keys: lane i holds the table's entry held + i, -1 where there is no such page.
+struct HeldPages {
+  int64_t first = -1;
+  int page = -1;
 };
 
-// One block for one wave: scores, softmax step, product.  `there`: the block's keys that
-// some row of the tile sees.  Returns whether values of keys on which the rows disagree
-// hold infinities or NaN (ODD false: the product then has to be made again with ODD).
-template <int DT, bool ODD>
-__device__ __forceinline__ bool tile_step(const AttendArgs &a, TileSums<DT> &t, const bf16x8_t (&qv)[DT / 16], float scale2,
-                                          const uint8_t *kt, const uint8_t *vt, uint64_t there, int64_t j0, int64_t place,
-                                          int64_t low, int64_t high) {
-  constexpr int kRow = DT * 2, kChunks = kRow / 16, kOut = DT / 32, kSteps = DT / 16;
-  constexpr int kLine = kRow < 256 ? 256 / kRow : 1, kMask = (kRow / 32 < 8 ? kRow / 32 : 8) - 1;
-  const int lane = threadIdx.x & 63, col = lane & 31, hf = lane >> 5;
-  f32x16_t s[2];
-#pragma unroll
-  for (int x = 0; x < 2; ++x) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[x][i] = 0.0f;
-#pragma unroll
-    for (int st = 0; st < kSteps; ++st) {
-      const int r = 32 * x + col;
-      const u32x4 kv = *reinterpret_cast<const u32x4 *>(kt + r * kRow + ((2 * st + hf) ^ ((r / kLine) & (2 * kMask + 1))) * 16);
-      s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kv), qv[st], s[x], 0, 0, 0);
-    }
+// A wave's 32 rows.  The matrix products of block b + 1's scores are issued among the
+// exponentials of block b, and the maximum of b + 1 among the products of P and V of b:
+// neither the matrix cores nor the vector unit waits for the other.
+template <int DT> struct TileWave {
+  static constexpr int kRow = DT * 2, kChunks = kRow / 16, kOut = DT / 32, kSteps = DT / 16;
+  static constexpr int kLine = kRow < 256 ? 256 / kRow : 1, kMask = (kRow / 32 < 8 ? kRow / 32 : 8) - 1;
+  // where piece c of row r lies
+  __device__ __forceinline__ static int k_place(int r, int c) { return c ^ ((r / kLine) & (2 * kMask + 1)); }
+  __device__ __forceinline__ static int v_place(int r, int c) { return c ^ (2 * ((r / kLine) & kMask)); }
+
+  bf16x8_t q[kSteps];
+  f32x16_t acc[kOut];
+  float m, l;  // of this lane's row: maximum (of the scores before the scale), sum
+  float scale2;
+  int64_t place, low, high;  // of this lane's row, of the wave's first and last row
+
+  // Offsets of this lane's first pieces; the others' differ in fixed bits.  (Formed anew for
+  // each block: kept, they would take the registers of a whole operand.)
+  __device__ __forceinline__ static int k_base() {
+    const int lane = threadIdx.x & 63, r = lane & 31;
+    int at = r * kRow + k_place(r, lane >> 5) * 16;
+    asm volatile("" : "+v"(at));
+    return at;
   }
-  bool odd = false;
-  const bool whole = there == ~0ull && j0 + kTileKeys - 1 <= low &&
-                     (!a.window || high - j0 < a.window || j0 + kTileKeys <= a.sinks);
-  if (!whole) {
-    const Sight sight = sight_of(a, place, j0);
+  __device__ __forceinline__ static int v_base() {
+    const int lane = threadIdx.x & 63, r = 4 * (lane >> 5) + ((lane & 15) >> 2);
+    int at = r * kRow + v_place(r, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + (lane & 1) * 8;
+    asm volatile("" : "+v"(at));
+    return at;
+  }
+  // K's piece for product st of keys 32 x .. (piece 2 st + hf of row 32 x + lane % 32)
+  __device__ __forceinline__ static bf16x8_t k_piece(const uint8_t *kt, int base, int x, int st) {
+    return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4 *>(kt + (base ^ (32 * st)) + 32 * x * kRow));
+  }
+  // V^T's piece for keys 16 st .., dims 32 o ..: slot (hf, e) is key 16 st + 8 (e / 4) + 4 hf + e % 4
+  template <bool SANE> __device__ __forceinline__ static bf16x8_t v_piece(const uint8_t *vt, int base, int st, int o) {
+    i16x4_t v2[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const int r = 16 * st + 8 * y;  // (and the row of v_base; 8 rows on, the pieces' exchange differs where a row is short)
+      const int at = (base ^ (v_place(r, 4 * o) * 16)) + r * kRow;
+      v2[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(vt + at));
+      if (SANE) v2[y] = sane(v2[y]);
+    }
+    bf16x8_t v8;
+    __builtin_memcpy(&v8, v2, 16);
+    return v8;
+  }
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int o = 0; o < kOut; ++o)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[o][i] = 0.0f;
+    m = -INFINITY, l = 0.0f;
+  }
+
+  // Scores of the block in kt.
+  __device__ __forceinline__ void scores(const uint8_t *kt, f32x16_t (&s)[2]) const {
+    const int kx = k_base();
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[x][i] = 0.0f;
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_piece(kt, kx, x, st), q[st], s[x], 0, 0, 0);
+  }
+
+  // -inf for the keys that a row does not see (`there`: the keys that some row of the tile sees).
+  __device__ __forceinline__ bool whole(const AttendArgs &a, uint64_t there, int64_t j0) const {
+    return there == ~0ull && j0 + kTileKeys - 1 <= low && (!a.window || high - j0 < a.window || j0 + kTileKeys <= a.sinks);
+  }
+  __device__ __forceinline__ void mask(const AttendArgs &a, uint64_t there, int64_t j0, f32x16_t (&s)[2]) const {
+    const int hf = (threadIdx.x & 63) >> 5;
+    const Sight sight = sight_of(a, place, j0 + 4 * hf);
     const uint64_t here = there >> (4 * hf);
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int k = 32 * x + 8 * (i >> 2) + (i & 3);  // (and 4 hf)
-        s[x][i] = ((here >> k & 1) != 0) & sight.sees(k + 4 * hf) ? s[x][i] : -INFINITY;
+        const int k = 32 * x + 8 * (i >> 2) + (i & 3);
+        s[x][i] = ((here >> k & 1) != 0) & sight.sees(k) ? s[x][i] : -INFINITY;
       }
-    for (int c = lane; c < kTileKeys * kChunks; c += 64) odd |= odd_value<uint16_t>(*reinterpret_cast<const u32x4 *>(vt + c * 16));
-    odd = __any(odd);
-    if (odd && !ODD) return true;
   }
-  float top = s[0][0];
-#pragma unroll
-  for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i >> 4][i & 15]);
-  top = fmaxf(top, __shfl_xor(top, 32));
-  // the maximum moves, and the sums are scaled to it, only where a weight would pass 2^8
-  if (__any(!((top - t.m) * scale2 <= 8.0f))) {
-    const float mn = fmaxf(t.m, top), f = mn == t.m ? 1.0f : exp2_fast((t.m - mn) * scale2);
-    t.m = mn;
-    t.l *= f;
-#pragma unroll
-    for (int o = 0; o < kOut; ++o)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) t.acc[o][i] *= f;
+  // Whether a block's values hold infinities or NaN.
+  __device__ __forceinline__ static bool odd_block(const uint8_t *vt) {
+    bool odd = false;
+    for (int c = threadIdx.x & 63; c < kTileKeys * kChunks; c += 64)
+      odd |= odd_value<uint16_t>(*reinterpret_cast<const u32x4 *>(vt + c * 16));
+    return __any(odd);
   }
-  const float base = t.m == -INFINITY ? 0.0f : -t.m * scale2;
-  float sum = 0.0f;
+
+  // The row's maximum moves to `top` (a lane's own), and the sums are scaled to it, only where a
+  // weight would pass 2^8.
+  __device__ __forceinline__ void rescale(float top) {
+    top = fmaxf(top, __shfl_xor(top, 32));
+    if (__any(!((top - m) * scale2 <= 8.0f))) {
+      const float mn = fmaxf(m, top), f = mn == m ? 1.0f : exp2_fast((m - mn) * scale2);
+      m = mn;
+      l *= f;
 #pragma unroll
-  for (int x = 0; x < 2; ++x)
+      for (int o = 0; o < kOut; ++o)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[x][i] = exp2_fast(fmaf(s[x][i], scale2, base));
-      sum += s[x][i];
-    }
-  t.l += sum;
-#pragma unroll
-  for (int st = 0; st < 4; ++st) {
-    bf16x8_t p;  // contraction slot (hf, e): key 16 st + 8 (e / 4) + 4 hf + e % 4
-#pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[st >> 1][8 * (st & 1) + e];
-#pragma unroll
-    for (int o = 0; o < kOut; ++o) {
-      i16x4_t v2[2];
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const int r = 16 * st + 8 * y + 4 * hf + ((lane & 15) >> 2);
-        const int c = (4 * o + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (2 * ((r / kLine) & kMask));
-        v2[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(vt + r * kRow + c * 16 + (lane & 1) * 8));
-        if (ODD && odd) v2[y] = sane(v2[y]);
-      }
-      bf16x8_t v8;
-      __builtin_memcpy(&v8, v2, 16);
-      t.acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, p, t.acc[o], 0, 0, 0);
+        for (int i = 0; i < 16; ++i) acc[o][i] *= f;
     }
   }
-  if (ODD && odd) {
+
+  // Weights of block b (scores s, in place) and, where NEXT, the scores of the next block.
+  template <bool NEXT> __device__ __forceinline__ void weights(f32x16_t (&s)[2], const uint8_t *kt, f32x16_t (&sn)[2]) {
+    const float base = m == -INFINITY ? 0.0f : -m * scale2;
+    float sum[2] = {0.0f, 0.0f};
+    constexpr int kSlots = 2 * kSteps, kPer = 32 / (kSlots < 32 ? kSlots : 32), kAhead = 4;
+    bf16x8_t ring[kAhead];
+    const int kx = k_base();
+    if (NEXT) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) ring[i] = k_piece(kt, kx, i & 1, i >> 1);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sn[x][i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+      if (NEXT) {
+        sn[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % kAhead], q[i >> 1], sn[i & 1], 0, 0, 0);
+        if (i + kAhead < kSlots) ring[i % kAhead] = k_piece(kt, kx, (i + kAhead) & 1, (i + kAhead) >> 1);
+      }
+#pragma unroll
+      for (int e = i * kPer; e < (i + 1) * kPer && e < 32; ++e) {
+        s[e >> 4][e & 15] = exp2_fast(fmaf(s[e >> 4][e & 15], scale2, base));
+        sum[e & 1] += s[e >> 4][e & 15];
+      }
+      if (NEXT) __builtin_amdgcn_sched_barrier(0);
+    }
+    l += sum[0] + sum[1];
+  }
+
+  // O^T += V^T P^T, and (NEXT) the largest of the next scores sn in *top (a lane's own).
+  template <bool SANE, bool NEXT>
+  __device__ __forceinline__ void product(const f32x16_t (&s)[2], const uint8_t *vt, const f32x16_t (&sn)[2], float *top) {
+    constexpr int kSlots = 4 * kOut, kAhead = 4;
+    bf16x8_t ring[kAhead], p;
+    float t = sn[0][0];
+    const int vx = v_base();
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ring[i] = v_piece<SANE>(vt, vx, i / kOut, i % kOut);
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+      const int st = i / kOut, o = i % kOut;
+      if (o == 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[st >> 1][8 * (st & 1) + e];
+      }
+      acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % kAhead], p, acc[o], 0, 0, 0);
+      if (i + kAhead < kSlots) ring[i % kAhead] = v_piece<SANE>(vt, vx, (i + kAhead) / kOut, (i + kAhead) % kOut);
+#pragma unroll
+      for (int e = i * 32 / kSlots; NEXT && e < (i + 1) * 32 / kSlots; ++e) t = fmaxf(t, sn[e >> 4][e & 15]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (NEXT) *top = t;
+  }
+  // ... and the infinities and NaN that it left out, where a row sees them.
+  __device__ __forceinline__ void add_odd(const f32x16_t (&s)[2], const uint8_t *vt) {
+    const int lane = threadIdx.x & 63, hf = lane >> 5;
 #pragma unroll 1
     for (int k = 0; k < kTileKeys; ++k) {
       float p = 0.0f;
@@ -588,24 +677,23 @@ __device__ __forceinline__ bool tile_step(const AttendArgs &a, TileSums<DT> &t, 
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if ((k >> 5) == x && ((k >> 3) & 3) == i >> 2 && (k & 3) == (i & 3)) p = s[x][i];
-      p = __shfl(p, col + 32 * ((k >> 2) & 1));
+      p = __shfl(p, (lane & 31) + 32 * ((k >> 2) & 1));
 #pragma unroll
       for (int o = 0; o < kOut; ++o)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int d = 32 * o + 8 * (e >> 2) + 4 * hf + (e & 3);
-          const uint16_t *v = reinterpret_cast<const uint16_t *>(vt + k * kRow + ((d >> 3) ^ (2 * ((k / kLine) & kMask))) * 16);
-          if (p != 0.0f && odd_bits(v[d & 7])) t.acc[o][e] += p * bf16_to_f32(v[d & 7]);
+          const uint16_t v = reinterpret_cast<const uint16_t *>(vt + k * kRow + v_place(k, d >> 3) * 16)[d & 7];
+          if (p != 0.0f && odd_bits(v)) acc[o][e] += p * bf16_to_f32(v);
         }
     }
   }
-  return false;
-}
+};
 
 template <int DT>
 __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a) {
-  constexpr int kRow = DT * 2, kChunks = kRow / 16, kLoads = kTileKeys * kChunks / 256, kOut = DT / 32, kSteps = DT / 16;
-  constexpr int kLine = kRow < 256 ? 256 / kRow : 1, kMask = (kRow / 32 < 8 ? kRow / 32 : 8) - 1;
+  using Wave = TileWave<DT>;
+  constexpr int kRow = Wave::kRow, kChunks = Wave::kChunks, kLoads = kTileKeys * kChunks / 256;
   // (arrays of their own, so that reads of one do not wait for loads into another)
   __shared__ __align__(16) uint8_t k0[kTileKeys * kRow], k1[kTileKeys * kRow], v0[kTileKeys * kRow], v1[kTileKeys * kRow];
 
@@ -618,101 +706,164 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
   const int b0 = z * a.per_split, b_end = kb.n < b0 + a.per_split ? kb.n : b0 + a.per_split;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, hf = lane >> 5;
   const int row = 32 * w + col, r_in = row < t.count ? row : t.count - 1;  // (rows past the last repeat it)
-  const int64_t place = t.place0 + (t.first + r_in) / a.group;
-  // places of this wave's first and last row
-  const int w_lo = 32 * w < t.count ? 32 * w : t.count - 1, w_hi = 32 * w + 31 < t.count ? 32 * w + 31 : t.count - 1;
-  const int64_t low = t.place0 + (t.first + w_lo) / a.group, high = t.place0 + (t.first + w_hi) / a.group;
 
-  // q with the scale's sign (zeros for a scale of 0), so that the largest product is the largest score
-  bf16x8_t qv[kSteps];
-  {
+  Wave wave;
+  wave.place = t.place0 + (t.first + r_in) / a.group;
+  wave.low = t.place0 + (t.first + (32 * w < t.count ? 32 * w : t.count - 1)) / a.group;
+  wave.high = t.place0 + (t.first + (32 * w + 31 < t.count ? 32 * w + 31 : t.count - 1)) / a.group;
+  wave.scale2 = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;
+  {  // q with the scale's sign (zeros for a scale of 0), so that the largest product is the largest score
     const int r = t.first + r_in;
     const uint16_t *q = (const uint16_t *)a.q + (t.start + r / a.group) * a.q_stride +
                         (int64_t)(kvh * a.group + r % a.group) * a.dim;
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
+    for (int s = 0; s < Wave::kSteps; ++s) {
       const int c = 2 * s + hf;
       u32x4 x = c * 8 < a.dim && a.scale != 0.0f ? *reinterpret_cast<const u32x4 *>(q + c * 8) : u32x4{0, 0, 0, 0};
       if (a.scale < 0.0f) x ^= 0x80008000u;
-      qv[s] = __builtin_bit_cast(bf16x8_t, x);
+      wave.q[s] = __builtin_bit_cast(bf16x8_t, x);
     }
   }
-  const float scale2 = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;
   const char *zeros = reinterpret_cast<const char *>(attend_zeros);
   const int64_t head_bytes = ((int64_t)kvh << a.pool.shift) * a.dim * 2;
   const int64_t page_bytes = ((int64_t)a.pool.n_kv << a.pool.shift) * a.dim * 2;
   const char *kp = (const char *)a.k + head_bytes, *vp = (const char *)a.v + head_bytes;
   const int row_bytes = a.dim * 2;
+  const int32_t *table = a.batch.table + t.seq * a.batch.max_pages;
 
-  auto page_of = [&](int b) { return b < b_end ? key_page(a, t, kb, block_key(kb, b, kTileKeys) + lane) : -1; };
-  // wave w loads rows 16 w .. 16 w + 15 of the block (K and V); where all of them are there, in
+  HeldPages held;
+  // page of key `lane` of a block where some row of the tile sees it, else -1
+  auto page_of = [&](int b) {
+    if (b >= b_end) return -1;
+    const int64_t j0 = block_key(kb, b, kTileKeys), p0 = j0 >> a.pool.shift, p1 = (j0 + kTileKeys - 1) >> a.pool.shift;
+    if (held.first < 0 || p0 < held.first || p1 >= held.first + 64) {
+      held.first = p0;
+      const int p = p0 + lane < a.batch.max_pages ? table[p0 + lane] : -1;
+      held.page = p >= 0 && p < a.pool.n_pages ? p : -1;
+    }
+    const int p = __shfl(held.page, (int)(((j0 + lane) >> a.pool.shift) - held.first));
+    const bool inside = j0 + kTileKeys <= t.len && j0 + kTileKeys - 1 <= kb.high &&
+                        (!a.window || kb.low - j0 < a.window || j0 + kTileKeys <= a.sinks);
+    return inside || any_sees(a, kb, t.len, j0 + lane) ? p : -1;
+  };
+  // wave w loads rows 16 w .. 16 w + 15 of a block of K or V; where all of them are there, in
   // one page and whole, from one address and fixed offsets
-  auto issue = [&](int b, int page, uint64_t there, uint8_t *kd, uint8_t *vd) {
+  auto issue = [&](int b, int page, uint64_t there, const char *pool, uint8_t *to, auto place) {
     const int j0 = (int)(block_key(kb, b, kTileKeys) & (a.pool.page - 1));
-    uint8_t *kw = kd + w * kLoads * 1024, *vw = vd + w * kLoads * 1024;
+    to += w * kLoads * 1024;
+    constexpr int kStep = 64 / kChunks;  // rows of a load
+    const int r0 = lane / kChunks, x = lane % kChunks;
     if (a.pool.shift >= 4 && (there >> (16 * w) & 0xffffu) == 0xffffu && a.dim == DT) {
       const int64_t p = __builtin_amdgcn_readlane(page, 16 * w);
-      const int64_t off = p * page_bytes + ((j0 + 16 * w) & (a.pool.page - 1)) * kRow;
-      const char *ks = kp + off, *vs = vp + off;
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int r = (i * 64 + lane) / kChunks, x = lane % kChunks;
-        load_to_lds(ks + (uint32_t)(r * kRow + (x ^ ((r / kLine) & (2 * kMask + 1))) * 16), kw + i * 1024);
-        load_to_lds(vs + (uint32_t)(r * kRow + (x ^ (2 * ((r / kLine) & kMask))) * 16), vw + i * 1024);
+      const char *from = pool + p * page_bytes + ((j0 + 16 * w) & (a.pool.page - 1)) * kRow;
+      uint32_t off = r0 * kRow + place(r0, x) * 16;  // (a load's rows begin at multiples of kStep: their exchange is in other bits)
+      asm volatile("" : "+v"(off));
+      load_to_lds<0>(from, off, to);
+      load_to_lds<1024>(from, off ^ (place(kStep, 0) * 16), to);
+      if constexpr (kLoads > 2) {
+        load_to_lds<2048>(from, off ^ (place(2 * kStep, 0) * 16), to);
+        load_to_lds<3072>(from, off ^ (place(3 * kStep, 0) * 16), to);
+      }
+      if constexpr (kLoads > 4) {
+        from += 4096;
+        load_to_lds<0>(from, off ^ (place(4 * kStep, 0) * 16), to + 4096);
+        load_to_lds<1024>(from, off ^ (place(5 * kStep, 0) * 16), to + 4096);
+        load_to_lds<2048>(from, off ^ (place(6 * kStep, 0) * 16), to + 4096);
+        load_to_lds<3072>(from, off ^ (place(7 * kStep, 0) * 16), to + 4096);
       }
       return;
     }
 #pragma unroll 1
     for (int i = 0; i < kLoads; ++i) {
-      const int r = (i * 64 + lane) / kChunks, x = lane % kChunks, p = __shfl(page, 16 * w + r);
+      const int r = i * kStep + r0, c = place(r, x), p = __shfl(page, 16 * w + r);
       const int64_t off = p * page_bytes + ((j0 + 16 * w + r) & (a.pool.page - 1)) * row_bytes;
-      const int kc = x ^ ((r / kLine) & (2 * kMask + 1)), vc = x ^ (2 * ((r / kLine) & kMask));
-      load_to_lds(p >= 0 && kc * 8 < a.dim ? kp + off + kc * 16 : zeros, kw + i * 1024);
-      load_to_lds(p >= 0 && vc * 8 < a.dim ? vp + off + vc * 16 : zeros, vw + i * 1024);
+      load_to_lds<0>(p >= 0 && c * 8 < a.dim ? pool + off + c * 16 : zeros, to + i * 1024);
     }
   };
+  auto issue_k = [&](int b, int page, uint64_t there, uint8_t *to) { issue(b, page, there, kp, to, Wave::k_place); };
+  auto issue_v = [&](int b, int page, uint64_t there, uint8_t *to) { issue(b, page, there, vp, to, Wave::v_place); };
 
-  TileSums<DT> sums;
-  // The tile's blocks; block b lives in buffer (b - b0) % 2: it has landed when every load is
-  // done, and the other buffer is free when every wave is past the barrier.  Returns
-  // whether a product has to be made again.
+  // The tile's blocks.  K of block b is in buffer (b - b0) % 2, V likewise.  At the barrier of
+  // step b every wave's loads (K of b + 1, V of b) have landed, and K of b and V of
+  // b - 1 have been read by all.  Returns whether the blocks have to be taken again.
   auto run = [&](auto kind) {
     constexpr bool kOdd = decltype(kind)::kOdd;
-#pragma unroll
-    for (int o = 0; o < kOut; ++o)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sums.acc[o][i] = 0.0f;
-    sums.m = -INFINITY, sums.l = 0.0f;
+    wave.clear();
     bool again = false;
-    int next = page_of(b0), after = page_of(b0 + 1);
-    uint64_t there = 0, there_next = __ballot(next >= 0);
-    if (b0 < b_end) issue(b0, next, there_next, k0, v0);
-    auto step = [&](int b, uint8_t *kt, uint8_t *vt, uint8_t *kn, uint8_t *vn) {
+    if (b0 >= b_end) return again;
+    f32x16_t sa[2], sb[2];
+    held.first = -1;
+    int page = page_of(b0), next = page_of(b0 + 1);
+    uint64_t there = __ballot(page >= 0), there_next = __ballot(next >= 0);
+    issue_k(b0, page, there, k0);
+    issue_v(b0, page, there, v0);
+    if (b0 + 1 < b_end) issue_k(b0 + 1, next, there_next, k1);
+    stage_barrier();
+    wave.scores(k0, sa);
+    bool some = !wave.whole(a, there, block_key(kb, b0, kTileKeys));  // rows disagree on a key of the block at hand
+    if (some) wave.mask(a, there, block_key(kb, b0, kTileKeys), sa);
+    float top = sa[0][0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) top = fmaxf(top, sa[i >> 4][i & 15]);
+    wave.rescale(top);
+    // block b, of scores s, whose K was in kt, and the scores sn of block b + 1
+    auto step = [&](int b, f32x16_t (&s)[2], f32x16_t (&sn)[2], uint8_t *kt, uint8_t *kn, uint8_t *vt, uint8_t *vn) {
       stage_barrier();
-      there = there_next, next = after;
-      there_next = __ballot(next >= 0);
-      if (b + 1 < b_end) issue(b + 1, next, there_next, kn, vn);
-      after = page_of(b + 2);
-      if (!again)
-        again = tile_step<DT, kOdd>(a, sums, qv, scale2, kt, vt, there, block_key(kb, b, kTileKeys), place, low, high);
+      page = page_of(b + 2);
+      there = __ballot(page >= 0);
+      if (b + 2 < b_end) issue_k(b + 2, page, there, kt);
+      issue_v(b + 1, next, there_next, vn);
+      const bool odd = some && Wave::odd_block(vt);
+      wave.template weights<true>(s, kn, sn);
+      const int64_t j1 = block_key(kb, b + 1, kTileKeys);
+      some = !wave.whole(a, there_next, j1);
+      if (some) wave.mask(a, there_next, j1, sn);
+      if (kOdd && odd) {
+        wave.template product<true, true>(s, vt, sn, &top);
+        wave.add_odd(s, vt);
+      } else {
+        wave.template product<false, true>(s, vt, sn, &top);
+        again |= odd;
+      }
+      wave.rescale(top);
+      next = page, there_next = there;
     };
-    for (int b = b0; b < b_end; b += 2) {
-      step(b, k0, v0, k1, v1);
-      if (b + 1 < b_end) step(b + 1, k1, v1, k0, v0);
+    auto last = [&](f32x16_t (&s)[2], uint8_t *vt) {
+      stage_barrier();
+      const bool odd = some && Wave::odd_block(vt);
+      wave.template weights<false>(s, vt, s);
+      if (kOdd && odd) {
+        wave.template product<true, false>(s, vt, s, &top);
+        wave.add_odd(s, vt);
+      } else {
+        wave.template product<false, false>(s, vt, s, &top);
+        again |= odd;
+      }
+    };
+    int b = b0;
+    for (; b + 2 < b_end; b += 2) {
+      step(b, sa, sb, k0, k1, v0, v1);
+      step(b + 1, sb, sa, k1, k0, v1, v0);
+    }
+    if (b + 1 < b_end) {
+      step(b, sa, sb, k0, k1, v0, v1);
+      last(sb, v1);
+    } else {
+      last(sa, v0);
     }
     return again;
   };
   if (__syncthreads_or(run(Plain{}))) run(Odd{});
 
-  float l = sums.l;
+  float l = wave.l;
   l += __shfl_xor(l, 32);
   if (row >= t.count) return;
-  const float m = sums.m * scale2;
+  const float m = wave.m * wave.scale2;
 #pragma unroll
-  for (int o = 0; o < kOut; ++o)
+  for (int o = 0; o < Wave::kOut; ++o)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const f32x4 v = {sums.acc[o][4 * e], sums.acc[o][4 * e + 1], sums.acc[o][4 * e + 2], sums.acc[o][4 * e + 3]};
+      const f32x4 v = {wave.acc[o][4 * e], wave.acc[o][4 * e + 1], wave.acc[o][4 * e + 2], wave.acc[o][4 * e + 3]};
       const int d = 32 * o + 8 * e + 4 * hf;
       if (parts > 1) put_part(a, ((int64_t)blockIdx.x * a.splits + z) * kTileRows + row, d, v, m, l);
       else put_row<uint16_t>(a, t, row, kvh, d, v, m, l);
