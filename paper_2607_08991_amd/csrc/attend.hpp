@@ -662,7 +662,6 @@ template <int DT> struct TileWave {
       if (i + kAhead < kSlots) ring[i % kAhead] = v_piece<SANE>(vt, vx, (i + kAhead) / kOut, (i + kAhead) % kOut);
 #pragma unroll
       for (int e = i * 32 / kSlots; NEXT && e < (i + 1) * 32 / kSlots; ++e) t = fmaxf(t, sn[e >> 4][e & 15]);
-      __builtin_amdgcn_sched_barrier(0);
     }
     if (NEXT) *top = t;
   }

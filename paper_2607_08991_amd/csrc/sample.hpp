@@ -14,9 +14,10 @@
 //
 // Nothing is sorted.  Four launches, each over chunks of the rows but the last:
 //   max     the row's largest logit;
-//   hist    weights and counts by bins of (max - l) / T, where k or p ask for it;
-//   cut     the bins in which k and p can end: their ids go to a list, the weights of
-//           the bins before them to a sum per chunk;
+//   hist    weights (for p) and counts (for k) by bins of (max - l) / T; the row's last
+//           workgroup finds the bins in which k and p can end;
+//   cut     the ids of those bins go to a list, the weights of the bins before them to a
+//           sum per chunk;
 //   pick    a workgroup per row: k and p end at an element of the list, found by its
 //           (logit, id) key 8 bits at a time; then the chunk, then the id, of the draw.
 #pragma once
@@ -26,16 +27,28 @@
 
 namespace sats {
 
+typedef unsigned long long u64;
+
 constexpr int kSampChunk = 4096;  // ids of a chunk
+constexpr int kSampThreads = 1024;
+constexpr int kSampSpan = 16;     // chunks that a workgroup takes, at most (a power of two)
 constexpr int kSampBins = 2048;
 constexpr float kSampScale = 70.0f;   // bins per unit of (max - l) / T: weights past bin 2047 round to 0
 constexpr int kPickThreads = 1024;
-typedef unsigned long long u64;
+
+// Where k and p can end in a row, from its bins.
+struct RowCut {
+  int k_bin;          // bin that holds the last of the top k (kSampBins: all are in)
+  int p_lo, p_hi;     // bins in which p can end
+  int64_t k_left;     // ids of k_bin that are among the top k
+  u64 k_before;       // weights of the bins before k_bin
+  u64 p_before;       // weights of the bins before p_lo
+};
 
 struct SampleArgs {
   const void *logits;
   int64_t stride, vocab;
-  int n, chunks;
+  int n, chunks, span;  // span: chunks of a workgroup (of the launches over chunks)
   const float *temperature, *top_p, *min_p, *u;
   const int32_t *top_k;
   int32_t *tokens, *n_kept;
@@ -49,12 +62,14 @@ struct SampleArgs {
   uint32_t *ccnt;     // [n][chunks] ... and how many
   u64 *list;          // [n][vocab] keys of the ids to look at
   uint32_t *n_list;   // [n]
+  unsigned *arrived;  // [n] workgroups of the row that have added their bins
+  RowCut *cuts;       // [n]
 };
 
 // What a row asks for.
 struct RowRule {
   bool first;     // the largest logit alone
-  bool cut;       // k or p may end the kept ids
+  bool by_k, by_p;  // k, p may end the kept ids
   float inv_t, min_p;
   int64_t k;
   double p;
@@ -69,19 +84,26 @@ __device__ __forceinline__ RowRule row_rule(const SampleArgs &a, int r) {
   q.inv_t = 1.0f / t;
   q.k = k > 0 && k < a.vocab ? k : a.vocab;
   q.p = p < 1.0f ? (double)p : 1.0;
-  q.cut = !q.first && (q.k < a.vocab || q.p < 1.0);
+  q.by_k = !q.first && q.k < a.vocab;
+  q.by_p = !q.first && q.p < 1.0;
   return q;
 }
 
 __device__ __forceinline__ float logit_of(const SampleArgs &a, float v) { return v == v ? v : -INFINITY; }
 
-// exp((x - max) / T), 0 for what can have no weight.
+// (x - max) / T, and its exponential: 0 for what can have no weight.
+__device__ __forceinline__ float below(float x, float top, float inv_t) { return x == top ? 0.0f : (x - top) * inv_t; }
+__device__ __forceinline__ float share_of(float z) { return z > -30.0f ? expf(z) : 0.0f; }
 __device__ __forceinline__ float share_of(float x, float top, float inv_t, float *z) {
-  const float d = x == top ? 0.0f : (x - top) * inv_t;
-  *z = d;
-  return d > -30.0f ? expf(d) : 0.0f;
+  *z = below(x, top, inv_t);
+  return share_of(*z);
 }
-__device__ __forceinline__ u64 weight_of(float share) { return (u64)rintf(share * 1099511627776.0f); }
+__device__ __forceinline__ u64 weight_of(float share) {  // round(2^40 share), in two parts of 32 bits
+  const float f = share * 1099511627776.0f, high = truncf(f * 0x1p-20f);
+  return (u64)(uint32_t)high * (1u << 20) + (uint32_t)rintf(fmaf(high, -0x1p20f, f));
+}
+// Whether an id at z has a weight (2^40 exp(-28) rounds to 1).
+__device__ __forceinline__ bool weighs(float z) { return z > -28.0f || weight_of(share_of(z)) != 0; }
 __device__ __forceinline__ int bin_of(float z) {
   const int b = (int)(-z * kSampScale);
   return b < kSampBins - 1 ? b : kSampBins - 1;
@@ -117,14 +139,16 @@ __device__ __forceinline__ float row_max(const SampleArgs &a, int r, int32_t *id
   return m;
 }
 
-// Calls f(logit, id) for this thread's ids of a chunk, 256 threads, V consecutive ids at a time.
+// Calls f(logit, id) for this thread's ids of a workgroup's span: a wave takes span * 256
+// consecutive ids, which are of one chunk, V consecutive ones a lane and step.
 template <typename T, int V, typename F>
-__device__ __forceinline__ void for_chunk(const SampleArgs &a, int r, int chunk, F f) {
+__device__ __forceinline__ void for_span(const SampleArgs &a, int r, F f) {
   const T *row = (const T *)a.logits + (int64_t)r * a.stride;
-  const int64_t lo = (int64_t)chunk * kSampChunk, hi = lo + kSampChunk < a.vocab ? lo + kSampChunk : a.vocab;
-#pragma unroll
-  for (int step = 0; step < kSampChunk / (kThreads * V); ++step) {
-    const int64_t i = lo + (step * kThreads + (int)threadIdx.x) * V;
+  const int per = a.span * 256;
+  const int64_t lo = ((int64_t)blockIdx.x * (kSampThreads / 64) + (threadIdx.x >> 6)) * per;
+  const int64_t hi = lo + per < a.vocab ? lo + per : a.vocab;
+#pragma unroll 4
+  for (int64_t i = lo + (threadIdx.x & 63) * V; i < hi; i += 64 * V) {
     if (i + V <= hi) {
       float x[V];
       load_vec_cached<T, V>(row + i, x);
@@ -136,18 +160,18 @@ __device__ __forceinline__ void for_chunk(const SampleArgs &a, int r, int chunk,
     }
   }
 }
-
 template <typename T, int V>
-__global__ __launch_bounds__(kThreads) void sample_max_kernel(SampleArgs a) {
-  __shared__ float sm[4];
-  __shared__ int32_t si[4];
-  const int chunk = blockIdx.x, r = blockIdx.y;
-  for (int b = chunk * kThreads + threadIdx.x; b < kSampBins; b += a.chunks * kThreads)
+__global__ __launch_bounds__(kSampThreads) void sample_max_kernel(SampleArgs a) {
+  constexpr int kWaves = kSampThreads / 64;
+  __shared__ float sm[kWaves];
+  __shared__ uint32_t si[kWaves];
+  const int r = blockIdx.y, w = threadIdx.x >> 6;
+  for (int b = blockIdx.x * kSampThreads + threadIdx.x; b < kSampBins; b += gridDim.x * kSampThreads)
     a.hsum[(int64_t)r * kSampBins + b] = 0, a.hcnt[(int64_t)r * kSampBins + b] = 0;
-  if (chunk == 0 && threadIdx.x == 0) a.n_list[r] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.n_list[r] = 0, a.arrived[r] = 0;
   float m = -INFINITY;
   uint32_t at = 0x7fffffff;
-  for_chunk<T, V>(a, r, chunk, [&](float x, uint32_t i) {
+  for_span<T, V>(a, r, [&](float x, uint32_t i) {
     if (x > m) m = x, at = i;  // (a thread's ids rise)
   });
 #pragma unroll
@@ -156,65 +180,36 @@ __global__ __launch_bounds__(kThreads) void sample_max_kernel(SampleArgs a) {
     const uint32_t y = __shfl_xor(at, d);
     if (x > m || (x == m && y < at)) m = x, at = y;
   }
-  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m, si[threadIdx.x >> 6] = (int32_t)at;
+  if ((threadIdx.x & 63) == 0) sm[w] = m, si[w] = at;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < 4; ++w)
-      if (sm[w] > m || (sm[w] == m && (uint32_t)si[w] < at)) m = sm[w], at = (uint32_t)si[w];
-    a.cmax[(int64_t)r * a.chunks + chunk] = m;
-    a.cid[(int64_t)r * a.chunks + chunk] = (int32_t)at;
+  const int per = kWaves / a.span, c = blockIdx.x * a.span + threadIdx.x;  // waves of a chunk
+  if ((int)threadIdx.x < a.span && c < a.chunks) {
+    m = -INFINITY, at = 0x7fffffff;
+    for (int i = threadIdx.x * per; i < (int)(threadIdx.x + 1) * per; ++i)
+      if (sm[i] > m || (sm[i] == m && si[i] < at)) m = sm[i], at = si[i];
+    a.cmax[(int64_t)r * a.chunks + c] = m;
+    a.cid[(int64_t)r * a.chunks + c] = (int32_t)at;
   }
 }
 
-template <typename T, int V>
-__global__ __launch_bounds__(kThreads) void sample_hist_kernel(SampleArgs a) {
-  __shared__ u64 hs[kSampBins];
-  __shared__ uint32_t hc[kSampBins];
-  const int chunk = blockIdx.x, r = blockIdx.y;
-  const RowRule q = row_rule(a, r);
-  if (!q.cut) return;
-  int32_t id;
-  const float top = row_max(a, r, &id);
-  for (int b = threadIdx.x; b < kSampBins; b += kThreads) hs[b] = 0, hc[b] = 0;
-  __syncthreads();
-  for_chunk<T, V>(a, r, chunk, [&](float x, uint32_t) {
-    float z;
-    const u64 w = weight_of(share_of(x, top, q.inv_t, &z));
-    if (w) {
-      const int b = bin_of(z);
-      atomicAdd(&hs[b], w);
-      atomicAdd(&hc[b], 1u);
-    }
-  });
-  __syncthreads();
-  for (int b = threadIdx.x; b < kSampBins; b += kThreads)
-    if (hc[b]) {
-      atomicAdd(&a.hsum[(int64_t)r * kSampBins + b], hs[b]);
-      atomicAdd(&a.hcnt[(int64_t)r * kSampBins + b], hc[b]);
-    }
-}
-
-// Where k and p can end, from a row's bins.
-struct RowCut {
-  int k_bin;          // bin that holds the last of the top k (kSampBins: all are in)
-  u64 k_before;       // weights of the bins before it
-  int64_t k_left;     // ids of that bin that are among the top k
-  int p_lo, p_hi;     // bins in which p can end
-  u64 p_before;       // weights of the bins before p_lo
-};
-
-// Prefix sums of the bins by 256 threads (8 bins each); lds: 8 words.
-__device__ __forceinline__ RowCut row_cut(const SampleArgs &a, int r, const RowRule &q, u64 *lds_s, uint32_t *lds_c,
-                                          RowCut *out) {
+// Finds a row's cut from its bins, by the first 256 threads of a workgroup (8 bins each).
+__device__ __forceinline__ void row_cut(const SampleArgs &a, int r, const RowRule &q, u64 *lds_s, uint32_t *lds_c,
+                                        RowCut *out) {
   constexpr int kPer = kSampBins / kThreads;
-  const u64 *hs = a.hsum + (int64_t)r * kSampBins;
-  const uint32_t *hc = a.hcnt + (int64_t)r * kSampBins;
   u64 s[kPer], inc_s = 0;
   uint32_t c[kPer], inc_c = 0;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (tid < kThreads) {
+  const bool on = tid < kThreads;
+  if (on) {
+    const u64 *hs = a.hsum + (int64_t)r * kSampBins + tid * kPer;
+    const uint32_t *hc = a.hcnt + (int64_t)r * kSampBins + tid * kPer;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) s[i] = hs[tid * kPer + i], c[i] = hc[tid * kPer + i], inc_s += s[i], inc_c += c[i];
+    for (int i = 0; i < kPer; ++i) {  // (added by other workgroups of this launch)
+      s[i] = __hip_atomic_load(hs + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      c[i] = __hip_atomic_load(hc + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) inc_s += s[i], inc_c += c[i];
   }
   const u64 own_s = inc_s;
   const uint32_t own_c = inc_c;
@@ -224,21 +219,23 @@ __device__ __forceinline__ RowCut row_cut(const SampleArgs &a, int r, const RowR
     const uint32_t oc = __shfl_up(inc_c, d);
     if (lane >= d) inc_s += o, inc_c += oc;
   }
-  if (tid < kThreads && lane == 63) lds_s[wave] = inc_s, lds_c[wave] = inc_c;
-  if (tid == 0) out->k_bin = kSampBins, out->k_left = 0, out->p_lo = out->p_hi = kSampBins - 1;
+  if (on && lane == 63) lds_s[wave] = inc_s, lds_c[wave] = inc_c;
   __syncthreads();
-  u64 bs = 0, total = 0;
-  uint32_t bc = 0, count = 0;
+  u64 s0 = inc_s - own_s, total = 0;
+  int64_t c0 = inc_c - own_c, count = 0;
 #pragma unroll
   for (int w = 0; w < kThreads / 64; ++w) {
-    if (w < wave) bs += lds_s[w], bc += lds_c[w];
+    if (w < wave) s0 += lds_s[w], c0 += lds_c[w];
     total += lds_s[w], count += lds_c[w];
   }
-  const u64 s0 = bs + inc_s - own_s;
-  const uint32_t c0 = bc + inc_c - own_c;
-  if (tid == 0) out->k_before = total;
+  // The counts are there where k is asked for, the weights where p is: what is not there is 0
+  // and not looked at.
+  if (tid == 0) {
+    out->k_bin = kSampBins, out->k_left = 0, out->k_before = total;
+    out->p_lo = kSampBins, out->p_hi = -1, out->p_before = 0;
+  }
   __syncthreads();
-  if (tid < kThreads && q.k < (int64_t)count) {
+  if (on && q.by_k && q.k < count) {
     u64 x = s0;
     int64_t y = c0;
 #pragma unroll
@@ -248,81 +245,135 @@ __device__ __forceinline__ RowCut row_cut(const SampleArgs &a, int r, const RowR
     }
   }
   __syncthreads();
+  if (!q.by_p) return;
+  // The top k weigh at least `low`, and at most the weight of their last bin more.  p ends in
+  // the last bin with weights whose sum before it is below p times that.
   const int kb = out->k_bin;
-  const u64 low = out->k_before;  // the top k weigh at least this much, at most that of their last bin more
-  u64 high = low;
-  if (kb < kSampBins) high += hs[kb];
-  if (tid < kThreads) {
-    // p ends in the last bin with ids whose weights before are below p * (weight of the top k):
-    // the first candidates are in that bin for `low` (or later), the last in that for `high`
+  const u64 low = out->k_before;
+  if (on && kb / kPer == tid) lds_s[4] = s[kb % kPer];
+  if (kb == kSampBins && tid == 0) lds_s[4] = 0;
+  __syncthreads();
+  if (on) {
     u64 x = s0;
-    const double dl = q.p * (double)low, dh = q.p * (double)high;
+    const double dl = q.p * (double)low, dh = q.p * (double)(low + lds_s[4]);
+    if (tid == 0 && !(dl > 0.0)) out->p_lo = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      if (c[i]) {
-        const double before = (double)x, after = (double)(x + s[i]);
-        if (before < dl && !(after < dl)) out->p_lo = tid * kPer + i;
-        if (before < dh && !(after < dh)) out->p_hi = tid * kPer + i;
-      }
-      if (tid == 0 && i == 0 && !(dl > 0.0)) out->p_lo = 0;
+      const double before = (double)x, after = (double)(x + s[i]);
+      if (before < dl && !(after < dl)) out->p_lo = tid * kPer + i, out->p_before = x;
+      if (before < dh && !(after < dh)) out->p_hi = tid * kPer + i;
       x += s[i];
     }
   }
   __syncthreads();
-  {
-    u64 x = s0;
-    if (tid < kThreads) {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        if (tid * kPer + i == out->p_lo) out->p_before = x;
-        x += s[i];
-      }
-    }
-  }
-  __syncthreads();
-  return *out;
 }
 
 template <typename T, int V>
-__global__ __launch_bounds__(kThreads) void sample_cut_kernel(SampleArgs a) {
-  __shared__ u64 ls[4];
+__global__ __launch_bounds__(kSampThreads) void sample_hist_kernel(SampleArgs a) {
+  __shared__ u64 hs[kSampBins];
+  __shared__ uint32_t hc[kSampBins];
+  __shared__ u64 ls[8];
   __shared__ uint32_t lc[4];
-  __shared__ RowCut cut_lds;
-  const int chunk = blockIdx.x, r = blockIdx.y;
+  __shared__ RowCut cut;
+  __shared__ int last;
+  const int r = blockIdx.y;
+  const RowRule q = row_rule(a, r);
+  if (!q.by_k && !q.by_p) return;
+  int32_t id;
+  const float top = row_max(a, r, &id);
+  for (int b = threadIdx.x; b < kSampBins; b += kSampThreads) hs[b] = 0, hc[b] = 0;
+  __syncthreads();
+  if (q.by_p) {
+    for_span<T, V>(a, r, [&](float x, uint32_t) {
+      float z;
+      const u64 w = weight_of(share_of(x, top, q.inv_t, &z));
+      if (w) {
+        const int b = bin_of(z);
+        atomicAdd(&hs[b], w);
+        if (q.by_k) atomicAdd(&hc[b], 1u);
+      }
+    });
+  } else {
+    for_span<T, V>(a, r, [&](float x, uint32_t) {
+      const float z = below(x, top, q.inv_t);
+      if (weighs(z)) atomicAdd(&hc[bin_of(z)], 1u);
+    });
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < kSampBins; b += kSampThreads) {
+    if (hs[b]) atomicAdd(&a.hsum[(int64_t)r * kSampBins + b], hs[b]);
+    if (hc[b]) atomicAdd(&a.hcnt[(int64_t)r * kSampBins + b], hc[b]);
+  }
+  if (!arrive_last(a.arrived + r, gridDim.x, &last)) return;
+  row_cut(a, r, q, ls, lc, &cut);
+  if (threadIdx.x == 0) a.cuts[r] = cut;
+}
+
+constexpr uint32_t kCutList = 4096;
+
+template <typename T, int V>
+__global__ __launch_bounds__(kSampThreads) void sample_cut_kernel(SampleArgs a) {
+  __shared__ u64 ls[kSampThreads / 64];
+  __shared__ uint32_t lc[kSampThreads / 64];
+  const int r = blockIdx.y;
   const RowRule q = row_rule(a, r);
   if (q.first) return;
   int32_t id;
   const float top = row_max(a, r, &id);
-  RowCut cut;
-  cut.p_lo = kSampBins, cut.p_hi = -1, cut.k_bin = -1;
-  if (q.cut) cut = row_cut(a, r, q, ls, lc, &cut_lds);
+  // bins below `sure` are kept whole (but for k_bin), those up to `maybe`, and k_bin, go to the list
+  int sure = kSampBins, maybe = -1, k_bin = -1;
+  if (q.by_k || q.by_p) {
+    const RowCut cut = a.cuts[r];
+    k_bin = cut.k_bin;
+    if (q.by_p) sure = cut.p_lo, maybe = cut.p_hi;
+    else sure = k_bin;  // (p 1: the top k, to the last)
+  }
+  // the list is gathered in LDS, so that a workgroup counts in the row's list once (what does
+  // not fit is counted one by one)
+  __shared__ u64 keys[kCutList];
+  __shared__ uint32_t n_keys, first;
+  if (threadIdx.x == 0) n_keys = 0;
+  __syncthreads();
   u64 sum = 0;
   uint32_t cnt = 0;
   u64 *list = a.list + (int64_t)r * a.vocab;
-  for_chunk<T, V>(a, r, chunk, [&](float x, uint32_t i) {
-    float z;
-    const float share = share_of(x, top, q.inv_t, &z);
-    const u64 w = weight_of(share);
-    if (!w) return;
+  for_span<T, V>(a, r, [&](float x, uint32_t i) {
+    const float z = below(x, top, q.inv_t);
+    if (!(z > -30.0f)) return;
     const int b = bin_of(z);
-    if (b < cut.p_lo && b != cut.k_bin) {
-      if (share >= q.min_p) sum += w, ++cnt;
-    } else if (b <= cut.p_hi || b == cut.k_bin) {
-      list[atomicAdd(&a.n_list[r], 1u)] = key_of(x, i);
+    const bool listed = ((b >= sure) & (b <= maybe)) | (b == k_bin);
+    if (b < sure || listed) {
+      const float share = share_of(z);
+      const u64 w = weight_of(share);
+      if (listed) {
+        if (!w) return;
+        const uint32_t at = atomicAdd(&n_keys, 1u);
+        if (at < kCutList) keys[at] = key_of(x, i);
+        else list[atomicAdd(&a.n_list[r], 1u)] = key_of(x, i);
+      } else if (share >= q.min_p) {
+        sum += w, cnt += w != 0;
+      }
     }
   });
   sum = wave_sum(sum);
   const u64 c = wave_sum((u64)cnt);
-  __syncthreads();
   if ((threadIdx.x & 63) == 0) ls[threadIdx.x >> 6] = sum, lc[threadIdx.x >> 6] = (uint32_t)c;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    a.csum[(int64_t)r * a.chunks + chunk] = ls[0] + ls[1] + ls[2] + ls[3];
-    a.ccnt[(int64_t)r * a.chunks + chunk] = lc[0] + lc[1] + lc[2] + lc[3];
+  const int per = kSampThreads / 64 / a.span, chunk = blockIdx.x * a.span + threadIdx.x;
+  if ((int)threadIdx.x < a.span && chunk < a.chunks) {
+    sum = 0, cnt = 0;
+    for (int i = threadIdx.x * per; i < (int)(threadIdx.x + 1) * per; ++i) sum += ls[i], cnt += lc[i];
+    a.csum[(int64_t)r * a.chunks + chunk] = sum;
+    a.ccnt[(int64_t)r * a.chunks + chunk] = cnt;
   }
+  const uint32_t n = n_keys < kCutList ? n_keys : kCutList;
+  if (threadIdx.x == 0 && n) first = atomicAdd(&a.n_list[r], n);
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < n; i += kSampThreads) list[first + i] = keys[i];
 }
 
-constexpr int kPickList = 4096;  // keys of the list that are held in LDS
+constexpr int kPickList = 2048;  // keys of the list that are held in LDS
+constexpr int kPickWave = 2048;  // ... that one wave looks through
 
 struct PickLds {
   u64 sum[256];
@@ -330,11 +381,9 @@ struct PickLds {
   u64 key_and, key_or, base, weight, found;
   int64_t left;
   uint32_t one;
-  u64 scan_s[kPickThreads / 64];
-  uint32_t scan_c[kPickThreads / 64];
+  u64 scan[kPickThreads / 64];
   u64 chunk[kPickThreads];
-  RowCut cut;
-  u64 keys[kPickList];
+  u64 keys[kPickList], weights[kPickList];  // (weights: in the low 48 bits, the bin above)
 };
 
 // Exclusive prefix of one u64 per thread over the workgroup; *total its sum.
@@ -358,46 +407,69 @@ __device__ __forceinline__ u64 pick_scan(u64 v, u64 *lds, u64 *total) {
   return base + inc - v;
 }
 
-// The key, among those of the list in bins [lo, hi], at which the kept ids end: the
-// `left`-th smallest (BY_COUNT), or the last one whose weights before it, from `base` on,
-// are below `limit`.  Each step splits the keys that are left by the 8 highest bits in
-// which they differ and goes on with one part.  *upto: base and the weights up to it.
-template <bool BY_COUNT>
-__device__ u64 pick_end(const u64 *list, uint32_t n, int lo, int hi, float top, float inv_t, int64_t left, u64 base,
-                        double limit, PickLds &l, u64 *upto) {
+__device__ __forceinline__ float key_logit(u64 key) {
+  const uint32_t up = ~(uint32_t)(key >> 32);
+  return __uint_as_float(up & 0x80000000u ? up & 0x7fffffffu : ~up);
+}
+
+// The keys of a row's list in bins [lo, hi], with their weights.
+struct PickKeys {
+  const u64 *list;
+  const u64 *weights;  // with the bins, or null
+  uint32_t n;
+  float top, inv_t;
+  int lo, hi;
+  __device__ __forceinline__ u64 weigh(u64 key) const {
+    float z;
+    const u64 w = weight_of(share_of(key_logit(key), top, inv_t, &z));
+    return (u64)bin_of(z) << 48 | w;
+  }
+  template <int THREADS, typename F> __device__ __forceinline__ void each(int tid, u64 fixed, u64 value, F f) const {
+    for (uint32_t i = tid; i < n; i += THREADS) {
+      const u64 key = list[i];
+      if ((key & fixed) != value) continue;
+      const u64 w = weights ? weights[i] : weigh(key);
+      const int b = (int)(w >> 48);
+      if (b >= lo && b <= hi) f(key, w & ((1ull << 48) - 1));
+    }
+  }
+};
+
+// The key at which the kept ids end: the `left`-th smallest (BY_COUNT), or the last one
+// whose weights before it, from `base` on, are below `limit`.  Each step splits the keys
+// that are left by the 8 highest bits in which they differ and goes on with one part.
+// *upto: base and the weights up to it.  By the whole workgroup or by its first wave.
+template <bool BY_COUNT, int THREADS>
+__device__ u64 pick_end(const PickKeys &k, int64_t left, u64 base, double limit, PickLds &l, u64 *upto) {
   u64 fixed = 0, value = 0;  // bits that are decided, and what they are
   const int tid = threadIdx.x;
+  auto meet = [] {
+    if constexpr (THREADS > 64) {
+      __syncthreads();
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  };
   for (;;) {
-    __syncthreads();
-    if (tid < 256) l.sum[tid] = 0, l.cnt[tid] = 0;
+    meet();
+    for (int b = tid; b < 256; b += THREADS) l.sum[b] = 0, l.cnt[b] = 0;
     if (tid == 0) l.key_and = ~0ull, l.key_or = 0;
-    __syncthreads();
+    meet();
     u64 ka = ~0ull, ko = 0;
-    auto each = [&](auto f) {
-      for (uint32_t i = tid; i < n; i += kPickThreads) {
-        const u64 key = list[i];
-        if ((key & fixed) != value) continue;
-        const uint32_t up = ~(uint32_t)(key >> 32);
-        const float x = __uint_as_float(up & 0x80000000u ? up & 0x7fffffffu : ~up);
-        float z;
-        const u64 w = weight_of(share_of(x, top, inv_t, &z));
-        const int b = bin_of(z);
-        if (b >= lo && b <= hi) f(key, w);
-      }
-    };
-    each([&](u64 key, u64) { ka &= key, ko |= key; });
+    k.template each<THREADS>(tid, fixed, value, [&](u64 key, u64) { ka &= key, ko |= key; });
 #pragma unroll
     for (int d = 32; d; d >>= 1) ka &= __shfl_xor(ka, d), ko |= __shfl_xor(ko, d);
     if ((tid & 63) == 0 && ko) atomicAnd(&l.key_and, ka), atomicOr(&l.key_or, ko);
-    __syncthreads();
-    const u64 diff = l.key_and ^ l.key_or;
+    meet();
+    const u64 key_and = l.key_and, diff = key_and ^ l.key_or;
     const int high = diff ? 63 - __clzll((long long)diff) : 7, shift = high > 7 ? high - 7 : 0;
-    each([&](u64 key, u64 w) {
+    k.template each<THREADS>(tid, fixed, value, [&](u64 key, u64 w) {
       const int b = (int)(key >> shift) & 255;
       atomicAdd(&l.sum[b], w);
       atomicAdd(&l.cnt[b], 1u);
     });
-    __syncthreads();
+    meet();
     if (tid < 64) {  // four parts a lane
       u64 s[4], inc = 0;
       uint32_t c[4], incc = 0;
@@ -425,40 +497,48 @@ __device__ u64 pick_end(const u64 *list, uint32_t n, int lo, int hi, float top, 
       if (tid == winner) l.found = (u64)part, l.base = at, l.left = cat, l.one = size;
       if (winner < 0 && tid == 0) l.found = 0, l.base = base, l.left = 0, l.one = 0;
     }
-    __syncthreads();
-    const u64 mask = 255ull << shift;
+    meet();
     // (bits above `high` are common to the keys that are left)
     const u64 above = shift + 8 < 64 ? ~0ull << (shift + 8) : 0;
-    fixed = above | mask;
-    value = (l.key_and & above) | l.found << shift;
+    fixed = above | 255ull << shift;
+    value = (key_and & above) | l.found << shift;
     base = l.base;
     left -= l.left;
-    const uint32_t size = l.one;
-    if (size <= 1 || shift == 0) break;
+    if (l.one <= 1 || shift == 0) break;
   }
   // the one key that is left (all bits are decided where shift reached 0)
-  __syncthreads();
+  meet();
   if (tid == 0) l.found = 0, l.weight = 0;
-  __syncthreads();
-  for (uint32_t i = tid; i < n; i += kPickThreads) {
-    const u64 key = list[i];
-    if ((key & fixed) != value) continue;
-    const uint32_t up = ~(uint32_t)(key >> 32);
-    const float x = __uint_as_float(up & 0x80000000u ? up & 0x7fffffffu : ~up);
-    float z;
-    const u64 w = weight_of(share_of(x, top, inv_t, &z));
-    const int b = bin_of(z);
-    if (b >= lo && b <= hi) l.found = key, l.weight = w;
-  }
-  __syncthreads();
+  meet();
+  k.template each<THREADS>(tid, fixed, value, [&](u64 key, u64 w) { l.found = key, l.weight = w; });
+  meet();
   *upto = base + l.weight;
   return l.found;
+}
+
+// The key at which a row's kept ids end.
+template <int THREADS>
+__device__ __forceinline__ u64 pick_last(const RowRule &q, const RowCut &cut, PickKeys k, PickLds &l) {
+  u64 all = cut.k_before, end = ~0ull, unused;
+  if (cut.k_bin < kSampBins) {
+    k.lo = k.hi = cut.k_bin;
+    end = pick_end<true, THREADS>(k, cut.k_left, cut.k_before, 0.0, l, &all);
+  }
+  if (!q.by_p) return end;
+  k.lo = cut.p_lo, k.hi = cut.p_hi;
+  return pick_end<false, THREADS>(k, 0, cut.p_before, q.p * (double)all, l, &unused);
 }
 
 template <typename T>
 __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a) {
   __shared__ PickLds l;
+  __shared__ u64 end_lds;
   const int r = blockIdx.x, tid = threadIdx.x;
+  // everything that the row has so far, in one wait (what a row without a cut has not is not used)
+  const bool mine_there = tid < a.chunks;
+  const u64 csum = mine_there ? a.csum[(int64_t)r * a.chunks + tid] : 0;
+  const uint32_t ccnt = mine_there ? a.ccnt[(int64_t)r * a.chunks + tid] : 0, n = a.n_list[r];
+  const RowCut cut = a.cuts[r];
   const RowRule q = row_rule(a, r);
   int32_t id;
   const float top = row_max(a, r, &id);
@@ -471,42 +551,47 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
     }
     return;
   }
-  u64 last = ~0ull;
-  const u64 *list = a.list + (int64_t)r * a.vocab;
-  uint32_t n = 0;
-  if (q.cut) {
-    const RowCut cut = row_cut(a, r, q, l.scan_s, l.scan_c, &l.cut);
-    n = a.n_list[r];
-    if (n <= kPickList) {
-      for (uint32_t i = tid; i < n; i += kPickThreads) l.keys[i] = list[i];
-      list = l.keys;
-    }
-    u64 all = cut.k_before, unused;
-    if (cut.k_bin < kSampBins)
-      (void)pick_end<true>(list, n, cut.k_bin, cut.k_bin, top, q.inv_t, cut.k_left, cut.k_before, 0.0, l, &all);
-    last = pick_end<false>(list, n, cut.p_lo, cut.p_hi, top, q.inv_t, 0, cut.p_before, q.p * (double)all, l, &unused);
-  }
   // weights and counts of each chunk
-  __syncthreads();
-  u64 kept = 0;
-  if (tid < a.chunks) l.chunk[tid] = a.csum[(int64_t)r * a.chunks + tid], kept = a.ccnt[(int64_t)r * a.chunks + tid];
-  __syncthreads();
-  for (uint32_t i = tid; i < n; i += kPickThreads) {
-    const u64 key = list[i];
-    if (key > last) continue;
-    const uint32_t up = ~(uint32_t)(key >> 32);
-    const float x = __uint_as_float(up & 0x80000000u ? up & 0x7fffffffu : ~up);
-    float z;
-    const float share = share_of(x, top, q.inv_t, &z);
-    if (share >= q.min_p) atomicAdd(&l.chunk[(uint32_t)key / kSampChunk], weight_of(share)), ++kept;
+  u64 kept = ccnt;
+  if (mine_there) l.chunk[tid] = csum;
+  u64 last = ~0ull;
+  if (q.by_k || q.by_p) {
+    PickKeys k{a.list + (int64_t)r * a.vocab, nullptr, n, top, q.inv_t, 0, 0};
+    if (n <= kPickList) {
+      for (uint32_t i = tid; i < n; i += kPickThreads) {
+        const u64 key = k.list[i];
+        l.keys[i] = key;
+        l.weights[i] = k.weigh(key);
+      }
+      k.list = l.keys, k.weights = l.weights;
+    }
+    __syncthreads();
+    if (n <= kPickWave) {
+      if (tid < 64) {
+        const u64 end = pick_last<64>(q, cut, k, l);
+        if (tid == 0) end_lds = end;
+      }
+      __syncthreads();
+      last = end_lds;
+    } else {
+      last = pick_last<kPickThreads>(q, cut, k, l);
+    }
+    __syncthreads();
+    for (uint32_t i = tid; i < n; i += kPickThreads) {
+      const u64 key = k.list[i];
+      if (key > last) continue;
+      float z;
+      const float share = share_of(key_logit(key), top, q.inv_t, &z);
+      if (share >= q.min_p) atomicAdd(&l.chunk[(uint32_t)key / kSampChunk], weight_of(share)), ++kept;
+    }
   }
   __syncthreads();
   u64 total, count;
-  const u64 mine = tid < a.chunks ? l.chunk[tid] : 0, before = pick_scan(mine, l.scan_s, &total);
+  const u64 mine = tid < a.chunks ? l.chunk[tid] : 0, before = pick_scan(mine, l.scan, &total);
   if (tid == 0) l.found = 0, l.base = 0;
-  (void)pick_scan(kept, l.scan_s, &count);
+  (void)pick_scan(kept, l.scan, &count);
   const double u = (double)fmaxf(a.u[r], 0.0f);
-  u64 at = (u64)fmin(u * (double)total, 18014398509481984.0 * 512.0);
+  u64 at = (u64)fmin(u * (double)total, 0x1p63);
   at = at < total ? at : total - 1;
   if (at >= before && at < before + mine) l.found = (u64)tid, l.base = before;
   __syncthreads();
@@ -527,7 +612,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
     sum += w[i];
   }
   u64 chunk_total;
-  u64 x = base + pick_scan(sum, l.scan_s, &chunk_total);
+  u64 x = base + pick_scan(sum, l.scan, &chunk_total);
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     if (at >= x && at < x + w[i]) {

@@ -283,7 +283,9 @@ struct SampleScratch {
   float *cmax;
   int32_t *cid;
   uint32_t *ccnt, *n_list, *hcnt;
+  unsigned *arrived;
   sats::u64 *csum, *hsum, *list;
+  sats::RowCut *cuts;
 };
 size_t sample_layout(char *base, int64_t n, int64_t vocab, SampleScratch *out) {
   Carve c{base};
@@ -294,6 +296,8 @@ size_t sample_layout(char *base, int64_t n, int64_t vocab, SampleScratch *out) {
   s.ccnt = c.take<uint32_t>(n * chunks);
   s.csum = c.take<sats::u64>(n * chunks);
   s.n_list = c.take<uint32_t>(n);
+  s.arrived = c.take<unsigned>(n);
+  s.cuts = c.take<sats::RowCut>(n);
   s.hcnt = c.take<uint32_t>(n * sats::kSampBins);
   s.hsum = c.take<sats::u64>(n * sats::kSampBins);
   s.list = c.take<sats::u64>(n * vocab);
@@ -304,16 +308,16 @@ size_t sample_layout(char *base, int64_t n, int64_t vocab, SampleScratch *out) {
 constexpr int64_t kMaxVocab = (int64_t)sats::kSampChunk * sats::kPickThreads;
 
 template <typename T> void launch_sample(const sats::SampleArgs &a, bool wide, hipStream_t stream) {
-  const dim3 grid((unsigned)a.chunks, (unsigned)a.n);
+  const dim3 grid((unsigned)((a.chunks + a.span - 1) / a.span), (unsigned)a.n);
   constexpr int V = 16 / sizeof(T);
   if (wide) {
-    sats::sample_max_kernel<T, V><<<grid, sats::kThreads, 0, stream>>>(a);
-    sats::sample_hist_kernel<T, V><<<grid, sats::kThreads, 0, stream>>>(a);
-    sats::sample_cut_kernel<T, V><<<grid, sats::kThreads, 0, stream>>>(a);
+    sats::sample_max_kernel<T, V><<<grid, sats::kSampThreads, 0, stream>>>(a);
+    sats::sample_hist_kernel<T, V><<<grid, sats::kSampThreads, 0, stream>>>(a);
+    sats::sample_cut_kernel<T, V><<<grid, sats::kSampThreads, 0, stream>>>(a);
   } else {
-    sats::sample_max_kernel<T, 1><<<grid, sats::kThreads, 0, stream>>>(a);
-    sats::sample_hist_kernel<T, 1><<<grid, sats::kThreads, 0, stream>>>(a);
-    sats::sample_cut_kernel<T, 1><<<grid, sats::kThreads, 0, stream>>>(a);
+    sats::sample_max_kernel<T, 1><<<grid, sats::kSampThreads, 0, stream>>>(a);
+    sats::sample_hist_kernel<T, 1><<<grid, sats::kSampThreads, 0, stream>>>(a);
+    sats::sample_cut_kernel<T, 1><<<grid, sats::kSampThreads, 0, stream>>>(a);
   }
   sats::sample_pick_kernel<T><<<(unsigned)a.n, sats::kPickThreads, 0, stream>>>(a);
 }
@@ -495,7 +499,10 @@ int sats_sample(const void *logits, int elem_bytes, int64_t stride, int64_t n, i
   a.temperature = temperature, a.top_k = top_k, a.top_p = top_p, a.min_p = min_p, a.u = u;
   a.tokens = tokens, a.prob = prob, a.n_kept = n_kept;
   a.cmax = s.cmax, a.cid = s.cid, a.hsum = s.hsum, a.hcnt = s.hcnt, a.csum = s.csum, a.ccnt = s.ccnt;
-  a.list = s.list, a.n_list = s.n_list;
+  a.list = s.list, a.n_list = s.n_list, a.arrived = s.arrived, a.cuts = s.cuts;
+  // chunks of a workgroup: about a workgroup per compute unit
+  a.span = 1;
+  while (a.span < sats::kSampSpan && n * a.chunks > 256 * a.span) a.span *= 2;
   const bool wide = on16(logits) && stride * elem_bytes % 16 == 0;
   if (elem_bytes == 2) launch_sample<uint16_t>(a, wide, stream);
   else launch_sample<float>(a, wide, stream);
