@@ -215,6 +215,7 @@ __device__ __forceinline__ i16x4_t sane(i16x4_t v) {  // infinities and NaN as z
 }
 __device__ __forceinline__ bool odd_of(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
 
+template <int N> struct Const { static constexpr int value = N; };
 struct Plain { static constexpr bool kOdd = false; };
 struct Odd { static constexpr bool kOdd = true; };
 
@@ -229,20 +230,17 @@ template <typename T> struct RowsOf {
   static constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;  // keys of a block
 };
 
-template <typename T, int DT>
-__global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_rows_kernel(AttendArgs a) {
+// FULL: heads of DT dims; else products of dims that a head has not are passed over.
+template <typename T, int DT, bool FULL>
+__global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_rows_kernel(AttendArgs a) {
   constexpr int kKeys = RowsOf<T>::kKeys, kVec = Elem<T>::kVec, kRow = DT * (int)sizeof(T), kChunks = kRow / 16;
   constexpr int kTiles = kKeys / 16, kSteps = kChunks / 4, kLoads = kKeys * kChunks / 64, kOut = DT / 16;
-  // 16-byte pieces of V's rows are exchanged so that the rows of a transposing read
-  // (bf16: 8 rows of 32 bytes; float32: 4 rows, 4 apart, of 64) lie in different banks
-  constexpr int kLine = kRow < 256 ? 256 / kRow : 1, kMask = (kRow / 32 < 8 ? kRow / 32 : 8) - 1;
-  auto place_of = [](int r, int c) {
-    if constexpr (sizeof(T) == 2) return c ^ (2 * ((r / kLine) & kMask));
-    else return c ^ (4 * ((r >> 2) & 3));
-  };
-  __shared__ __align__(16) uint8_t lds[4][kKeys * kRow];
+  // V's rows lie a little apart, so that the rows that are read together (bf16: 32 bytes of 8
+  // rows; float32: 64 bytes of 4 rows, 4 apart) are in different banks
+  constexpr int kPitch = kRow + (sizeof(T) == 2 ? 32 : 16);
+  constexpr int kPart = kKeys * kPitch > 16 * DT * 4 ? kKeys * kPitch : 16 * DT * 4;  // (the waves' sums are joined there)
+  __shared__ __align__(16) uint8_t lds[4][kPart];
   __shared__ float ml[4][16][2];
-  static_assert(sizeof lds >= 4 * 16 * DT * 4, "the waves' sums are joined there");
 
   const int kvh = blockIdx.x % a.pool.n_kv, z = blockIdx.y;
   const RowTile t = find_tile<16>(a, blockIdx.x / a.pool.n_kv);
@@ -319,6 +317,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_rows_kernel(Atte
       s[kt] = f32x4{0, 0, 0, 0};
 #pragma unroll
       for (int st = 0; st < kSteps; ++st) {
+        if (!FULL && st * 4 * kVec >= a.dim) break;
         if constexpr (sizeof(T) == 2) {
           s[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kr[kt * kSteps + st]),
                                                           __builtin_bit_cast(bf16x8_t, qv[st]), s[kt], 0, 0, 0);
@@ -340,7 +339,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_rows_kernel(Atte
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int at = i * 64 + lane, r = at / kChunks;
-      *reinterpret_cast<u32x4 *>(mine + r * kRow + place_of(r, at % kChunks) * 16) = vr[i];
+      *reinterpret_cast<u32x4 *>(mine + r * kPitch + at % kChunks * 16) = vr[i];
     }
     page = page_next;
     if (b + 4 < b_end) {
@@ -387,12 +386,12 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_rows_kernel(Atte
         for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[e >> 2][e & 3];
 #pragma unroll
         for (int o = 0; o < kOut; ++o) {
+          if (!FULL && 16 * o >= a.dim) break;
           i16x4_t v2[2];
 #pragma unroll
           for (int kt = 0; kt < 2; ++kt) {
-            const int r = 16 * kt + 4 * g + (row >> 2), c = 2 * o + ((row & 3) >> 1);
-            v2[kt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_i16x4 *)(mine + r * kRow + place_of(r, c) * 16 + (row & 1) * 8));
+            const int r = 16 * kt + 4 * g + (row >> 2);
+            v2[kt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(mine + r * kPitch + 32 * o + (row & 3) * 8));
             if (kOdd) v2[kt] = sane(v2[kt]);
           }
           bf16x8_t v8;
@@ -401,14 +400,15 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_rows_kernel(Atte
         }
       } else {
 #pragma unroll
-        for (int o = 0; o < kOut; ++o)
+        for (int o = 0; o < kOut; ++o) {
+          if (!FULL && 16 * o >= a.dim) break;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int r = 4 * g + i, c = 4 * o + (row >> 2);
-            float v = *reinterpret_cast<const float *>(mine + r * kRow + place_of(r, c) * 16 + (row & 3) * 4);
+            float v = *reinterpret_cast<const float *>(mine + (4 * g + i) * kPitch + (16 * o + row) * 4);
             if (kOdd) v = odd_of(v) ? 0.0f : v;
             acc[o] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[0][i], acc[o], 0, 0, 0);
           }
+        }
       }
     };
     if (!odd) {
@@ -429,7 +429,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_rows_kernel(Atte
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int d = 16 * o + 4 * g + e;
-            const float v = Elem<T>::get(reinterpret_cast<const T *>(mine + k * kRow + place_of(k, d / kVec) * 16) + d % kVec);
+            const float v = Elem<T>::get(reinterpret_cast<const T *>(mine + k * kPitch) + d);
             if (p != 0.0f && odd_of(v)) acc[o][e] += p * v;
           }
       }
@@ -505,7 +505,7 @@ struct HeldPages {
 // A wave's 32 rows.  The matrix products of block b + 1's scores are issued among the
 // exponentials of block b, and the maximum of b + 1 among the products of P and V of b:
 // neither the matrix cores nor the vector unit waits for the other.
-template <int DT> struct TileWave {
+template <int DT, bool FULL> struct TileWave {
   static constexpr int kRow = DT * 2, kChunks = kRow / 16, kOut = DT / 32, kSteps = DT / 16;
   static constexpr int kLine = kRow < 256 ? 256 / kRow : 1, kMask = (kRow / 32 < 8 ? kRow / 32 : 8) - 1;
   // where piece c of row r lies
@@ -517,6 +517,7 @@ template <int DT> struct TileWave {
   float m, l;  // of this lane's row: maximum (of the scores before the scale), sum
   float scale2;
   int64_t place, low, high;  // of this lane's row, of the wave's first and last row
+  int dim;                   // (where not FULL, products of dims that a head has not are passed over)
 
   // Offsets of this lane's first pieces; the others' differ in fixed bits.  (Formed anew for
   // each block: kept, they would take the registers of a whole operand.)
@@ -567,9 +568,11 @@ template <int DT> struct TileWave {
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[x][i] = 0.0f;
 #pragma unroll
-    for (int st = 0; st < kSteps; ++st)
+    for (int st = 0; st < kSteps; ++st) {
+      if (!FULL && 16 * st >= dim) break;
 #pragma unroll
       for (int x = 0; x < 2; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_piece(kt, kx, x, st), q[st], s[x], 0, 0, 0);
+    }
   }
 
   // -inf for the keys that a row does not see (`there`: the keys that some row of the tile sees).
@@ -628,7 +631,7 @@ template <int DT> struct TileWave {
     }
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) {
-      if (NEXT) {
+      if (NEXT && (FULL || 16 * (i >> 1) < dim)) {
         sn[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % kAhead], q[i >> 1], sn[i & 1], 0, 0, 0);
         if (i + kAhead < kSlots) ring[i % kAhead] = k_piece(kt, kx, (i + kAhead) & 1, (i + kAhead) >> 1);
       }
@@ -658,7 +661,7 @@ template <int DT> struct TileWave {
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[st >> 1][8 * (st & 1) + e];
       }
-      acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % kAhead], p, acc[o], 0, 0, 0);
+      if (FULL || 32 * o < dim) acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % kAhead], p, acc[o], 0, 0, 0);
       if (i + kAhead < kSlots) ring[i % kAhead] = v_piece<SANE>(vt, vx, (i + kAhead) / kOut, (i + kAhead) % kOut);
 #pragma unroll
       for (int e = i * 32 / kSlots; NEXT && e < (i + 1) * 32 / kSlots; ++e) t = fmaxf(t, sn[e >> 4][e & 15]);
@@ -689,9 +692,9 @@ template <int DT> struct TileWave {
   }
 };
 
-template <int DT>
+template <int DT, bool FULL>
 __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a) {
-  using Wave = TileWave<DT>;
+  using Wave = TileWave<DT, FULL>;
   constexpr int kRow = Wave::kRow, kChunks = Wave::kChunks, kLoads = kTileKeys * kChunks / 256;
   // (arrays of their own, so that reads of one do not wait for loads into another)
   __shared__ __align__(16) uint8_t k0[kTileKeys * kRow], k1[kTileKeys * kRow], v0[kTileKeys * kRow], v1[kTileKeys * kRow];
@@ -707,6 +710,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
   const int row = 32 * w + col, r_in = row < t.count ? row : t.count - 1;  // (rows past the last repeat it)
 
   Wave wave;
+  wave.dim = a.dim;
   wave.place = t.place0 + (t.first + r_in) / a.group;
   wave.low = t.place0 + (t.first + (32 * w < t.count ? 32 * w : t.count - 1)) / a.group;
   wave.high = t.place0 + (t.first + (32 * w + 31 < t.count ? 32 * w + 31 : t.count - 1)) / a.group;
@@ -752,24 +756,24 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
     to += w * kLoads * 1024;
     constexpr int kStep = 64 / kChunks;  // rows of a load
     const int r0 = lane / kChunks, x = lane % kChunks;
-    if (a.pool.shift >= 4 && (there >> (16 * w) & 0xffffu) == 0xffffu && a.dim == DT) {
+    if (a.pool.shift >= 4 && (there >> (16 * w) & 0xffffu) == 0xffffu) {
       const int64_t p = __builtin_amdgcn_readlane(page, 16 * w);
-      const char *from = pool + p * page_bytes + ((j0 + 16 * w) & (a.pool.page - 1)) * kRow;
+      const char *from = pool + p * page_bytes + ((j0 + 16 * w) & (a.pool.page - 1)) * row_bytes;
       uint32_t off = r0 * kRow + place(r0, x) * 16;  // (a load's rows begin at multiples of kStep: their exchange is in other bits)
       asm volatile("" : "+v"(off));
-      load_to_lds<0>(from, off, to);
-      load_to_lds<1024>(from, off ^ (place(kStep, 0) * 16), to);
-      if constexpr (kLoads > 2) {
-        load_to_lds<2048>(from, off ^ (place(2 * kStep, 0) * 16), to);
-        load_to_lds<3072>(from, off ^ (place(3 * kStep, 0) * 16), to);
-      }
-      if constexpr (kLoads > 4) {
-        from += 4096;
-        load_to_lds<0>(from, off ^ (place(4 * kStep, 0) * 16), to + 4096);
-        load_to_lds<1024>(from, off ^ (place(5 * kStep, 0) * 16), to + 4096);
-        load_to_lds<2048>(from, off ^ (place(6 * kStep, 0) * 16), to + 4096);
-        load_to_lds<3072>(from, off ^ (place(7 * kStep, 0) * 16), to + 4096);
-      }
+      // load i; of a head of fewer dims the rows are closer, and pieces past its end read zeros
+      auto load = [&](auto i_) {
+        constexpr int i = decltype(i_)::value;
+        if constexpr (FULL) {
+          load_to_lds<i % 4 * 1024>(from + i / 4 * 4096, off ^ (place(i * kStep, 0) * 16), to + i / 4 * 4096);
+        } else {
+          const int c = place(i * kStep + r0, x);
+          load_to_lds<0>(from, c * 8 < a.dim ? (uint32_t)((i * kStep + r0) * row_bytes + c * 16) : 0x80000000u, to + i * 1024);
+        }
+      };
+      load(Const<0>{}), load(Const<1>{});
+      if constexpr (kLoads > 2) load(Const<2>{}), load(Const<3>{});
+      if constexpr (kLoads > 4) load(Const<4>{}), load(Const<5>{}), load(Const<6>{}), load(Const<7>{});
       return;
     }
 #pragma unroll 1

@@ -14,6 +14,7 @@ namespace sats {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanPer = 16;  // refs that a thread looks at in one step of the free list's scan
+constexpr int kPlanItems = 1024, kPlanIds = 4096;  // items and new pages whose lists are held in LDS
 
 struct PagesArgs {
   int32_t *table, *len, *refs;
@@ -25,7 +26,8 @@ struct PagesArgs {
   int32_t *status;              // [0] pages that were missing, [1] items left out; or null
   int32_t *n_used;
   // scratch
-  int32_t *off;                 // [n + 1] first new page of an item in `ids`
+  int32_t *off;                 // [n] first new page of an item in `ids`
+  int32_t *len_of;              // [n] its sequence's length
   int32_t *ids;                 // free pages that the call takes / pages that move away
   int32_t *to;                  // compaction: where a page goes, [n_pages]
   int32_t *src, *dst, *valid;   // moves: from, to, tokens (0: none)
@@ -41,19 +43,19 @@ struct CopyArgs {
   int n;
 };
 
-// Exclusive prefix over the workgroup of one int per thread; *total its sum.
-__device__ __forceinline__ int plan_scan(int v, int *lds, int *total) {
+// Exclusive prefix over the workgroup of one number per thread; *total its sum.
+template <typename N> __device__ __forceinline__ N plan_scan(N v, N *lds, N *total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int inc = v;
+  N inc = v;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(inc, d);
+    const N o = __shfl_up(inc, d);
     if (lane >= d) inc += o;
   }
   __syncthreads();  // (lds may still be read by the call before)
   if (lane == 63) lds[wave] = inc;
   __syncthreads();
-  int base = 0, sum = 0;
+  N base = 0, sum = 0;
 #pragma unroll
   for (int w = 0; w < kPlanThreads / 64; ++w) {
     if (w < wave) base += lds[w];
@@ -65,25 +67,40 @@ __device__ __forceinline__ int plan_scan(int v, int *lds, int *total) {
 
 __device__ __forceinline__ int item_seq(const PagesArgs &a, int i) { return a.seqs ? a.seqs[i] : i; }
 
-// Calls f(page, rank) for the first `want` pages whose refs satisfy `is`, in ascending order,
-// from page `from` up to `to`; the number found.
-template <typename Is, typename F>
-__device__ __forceinline__ int pages_where(const PagesArgs &a, int64_t from, int64_t to, int64_t want, int *lds, Is is, F f) {
+// refs p0 .. p0 + 15 of pages below `to` (0xffffffff past it).
+__device__ __forceinline__ void load_refs(const int32_t *refs, int64_t p0, int64_t to, int32_t (&r)[kPlanPer]) {
+  if (p0 + kPlanPer <= to && ((uintptr_t)(refs + p0) & 15) == 0) {
+#pragma unroll
+    for (int i = 0; i < kPlanPer; i += 4) {
+      const u32x4 v = *reinterpret_cast<const u32x4 *>(refs + p0 + i);
+      r[i] = (int32_t)v.x, r[i + 1] = (int32_t)v.y, r[i + 2] = (int32_t)v.z, r[i + 3] = (int32_t)v.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPlanPer; ++i) r[i] = p0 + i < to ? refs[p0 + i] : -1;
+  }
+}
+
+// Calls f(page, rank) for the first `want` pages from `from` up to `to` whose refs are 0 (FREE)
+// or not, in ascending order; the number found.
+template <bool FREE, typename F>
+__device__ __forceinline__ int64_t pages_where(const int32_t *refs, int64_t from, int64_t to, int64_t want, int *lds, F f) {
   int64_t found = 0;
   for (int64_t base = from; base < to && found < want; base += kPlanThreads * kPlanPer) {
     const int64_t p0 = base + (int64_t)threadIdx.x * kPlanPer;
+    int32_t v[kPlanPer];
+    load_refs(refs, p0, to, v);
     uint32_t hit = 0;
 #pragma unroll
     for (int i = 0; i < kPlanPer; ++i)
-      if (p0 + i < to && is(a.refs[p0 + i])) hit |= 1u << i;
+      if (p0 + i < to && (v[i] == 0) == FREE) hit |= 1u << i;
     int total;
-    int64_t r = found + plan_scan(__popc(hit), lds, &total);
-    for (; hit; hit &= hit - 1, ++r)
-      if (r < want) f(p0 + __ffs(hit) - 1, r);
+    int64_t r = found + plan_scan((int)__popc(hit), lds, &total);
+    for (; hit && r < want; hit &= hit - 1, ++r) f(p0 + __ffs(hit) - 1, r);
     found += total;
   }
   __syncthreads();
-  return (int)(found < want ? found : want);
+  return found < want ? found : want;
 }
 
 // The last page of a sequence of n tokens where n ends inside it and the page is there, else -1.
@@ -100,10 +117,16 @@ __device__ __forceinline__ int32_t part_page(const PagesArgs &a, int s, int n) {
 template <bool FORK>
 __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesArgs a) {
   __shared__ int lds[kPlanThreads / 64];
+  __shared__ long long lds_need[kPlanThreads / 64];
   __shared__ int left_out;
+  __shared__ int32_t lds_off[kPlanItems], lds_src[kPlanItems], lds_len[kPlanItems], lds_ids[kPlanIds];
+  // what the steps hand to each other: in LDS where it fits (a step is then a few hundred
+  // nanoseconds, in memory a microsecond)
+  int32_t *off = a.n <= kPlanItems ? lds_off : a.off, *src_of = a.n <= kPlanItems ? lds_src : a.src;
+  int32_t *len_of = a.n <= kPlanItems ? lds_len : a.len_of;
   if (threadIdx.x == 0) left_out = 0;
   __syncthreads();
-  int total = 0;
+  long long total = 0;  // (a sum of needs may pass 32 bits; where it can be met it does not)
   for (int base = 0; base < a.n; base += kPlanThreads) {
     const int i = base + threadIdx.x;
     int need = 0, src = -1;
@@ -124,60 +147,59 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesArgs a) {
         }
       }
       if (!ok) atomicAdd(&left_out, 1), need = -1;
-      a.src[i] = src;
+      src_of[i] = src;
+      len_of[i] = (int32_t)n;
     }
-    int sum;
-    const int at = total + plan_scan(need > 0 ? need : 0, lds, &sum);
-    if (i < a.n) a.off[i] = need < 0 ? -1 - at : at;  // (negative: left out)
+    long long sum;
+    const int at = (int)(total + plan_scan<long long>(need > 0 ? need : 0, lds_need, &sum));
+    if (i < a.n) {
+      off[i] = need < 0 ? -1 - at : at;  // (negative: left out)
+      if (FORK) a.off[i] = off[i];
+    }
     total += sum;
   }
-  if (threadIdx.x == 0) a.off[a.n] = total;
-  const int found = pages_where(a, 0, a.n_pages, total, lds, [](int r) { return r == 0; },
-                                [&](int64_t p, int64_t r) { a.ids[r] = (int32_t)p; });
+  int32_t *ids = total <= kPlanIds ? lds_ids : a.ids;
+  const int64_t found = pages_where<true>(a.refs, 0, a.n_pages, total, lds, [&](int64_t p, int64_t r) { ids[r] = (int32_t)p; });
   const bool go = found == total;
   if (threadIdx.x == 0) {
     a.ctl[0] = go;
     a.ctl[1] = a.n;
-    if (a.status) a.status[0] = total - found, a.status[1] = left_out;
+    if (a.status) a.status[0] = (int32_t)(total - found < 0x7fffffff ? total - found : 0x7fffffff), a.status[1] = left_out;
   }
   if (!go) return;
-  // what the items get (the scratch arrays written above are this workgroup's own)
+  // what the items get
   for (int i = threadIdx.x; i < a.n; i += kPlanThreads) {
-    const int o = a.off[i];
-    a.dst[i] = -1;
-    a.valid[i] = 0;
+    const int o = off[i], src = src_of[i], n = len_of[i];
+    const bool copy = o >= 0 && src >= 0;
+    a.src[i] = src;
+    a.dst[i] = copy ? ids[o] : -1;
+    a.valid[i] = copy ? n & (a.page - 1) : 0;
     if (o < 0) continue;
-    const int s = item_seq(a, i), n = a.len[s];
-    if (a.src[i] >= 0) {
-      a.dst[i] = a.ids[o];
-      a.valid[i] = n & (a.page - 1);
-    }
     if (FORK) {
       a.len[a.other[i]] = n;
     } else {
-      if (a.src[i] >= 0 && n >> a.shift < a.max_pages) {
-        a.table[s * a.max_pages + (n >> a.shift)] = a.ids[o];
-        atomicSub(&a.refs[a.src[i]], 1);
+      const int s = item_seq(a, i);
+      if (copy) {
+        a.table[s * a.max_pages + (n >> a.shift)] = ids[o];
+        atomicSub(&a.refs[src], 1);
       }
       a.len[s] = n + a.other[i];
     }
   }
-  for (int r = threadIdx.x; r < total; r += kPlanThreads) a.refs[a.ids[r]] = 1;
-  if (FORK) return;
-  __syncthreads();
-  // new pages into the table: page r of the call belongs to the last item that starts at or before it
   for (int r = threadIdx.x; r < total; r += kPlanThreads) {
+    a.refs[ids[r]] = 1;
+    if (FORK) continue;
+    // page r of the call belongs to the last item that starts at or before it (items that take
+    // nothing share their start with the next one; the last of them does not)
     int lo = 0, hi = a.n - 1;
     while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1, m = a.off[mid];
+      const int mid = (lo + hi + 1) >> 1, m = off[mid];
       if ((m < 0 ? -1 - m : m) <= r) lo = mid;
       else hi = mid - 1;
     }
-    // (items that take nothing share their start with the next one; the last of them does not)
-    const int s = item_seq(a, lo), at = r - a.off[lo] - (a.src[lo] >= 0);
-    if (at < 0) continue;  // the copy of a shared page, above
-    const int64_t j = ((a.len[s] - a.other[lo] + a.page - 1) >> a.shift) + at;
-    if (j < a.max_pages) a.table[s * a.max_pages + j] = a.ids[r];
+    const int at = r - off[lo] - (src_of[lo] >= 0);
+    if (at >= 0)  // (not the copy of a shared page, above)
+      a.table[item_seq(a, lo) * a.max_pages + ((len_of[lo] + a.page - 1) >> a.shift) + at] = ids[r];
   }
 }
 
@@ -207,21 +229,19 @@ __global__ __launch_bounds__(kPlanThreads) void pages_compact_plan_kernel(PagesA
   __shared__ int lds[kPlanThreads / 64];
   int64_t used = 0;
   for (int64_t base = 0; base < a.n_pages; base += kPlanThreads * kPlanPer) {
+    const int64_t p0 = base + (int64_t)threadIdx.x * kPlanPer;
+    int32_t v[kPlanPer];
+    load_refs(a.refs, p0, a.n_pages, v);
     int c = 0, total;
 #pragma unroll
-    for (int i = 0; i < kPlanPer; ++i) {
-      const int64_t p = base + (int64_t)threadIdx.x * kPlanPer + i;
-      if (p >= a.n_pages) break;
-      c += a.refs[p] != 0;
-      a.to[p] = (int32_t)p;
-    }
+    for (int i = 0; i < kPlanPer; ++i)
+      if (p0 + i < a.n_pages) c += v[i] != 0, a.to[p0 + i] = (int32_t)(p0 + i);
     plan_scan(c, lds, &total);
     used += total;
   }
   const int64_t all = a.n_pages;
-  const int holes = pages_where(a, 0, used, all, lds, [](int r) { return r == 0; },
-                                [&](int64_t p, int64_t r) { a.dst[r] = (int32_t)p; });
-  pages_where(a, used, a.n_pages, all, lds, [](int r) { return r != 0; }, [&](int64_t p, int64_t r) { a.src[r] = (int32_t)p; });
+  const int holes = (int)pages_where<true>(a.refs, 0, used, all, lds, [&](int64_t p, int64_t r) { a.dst[r] = (int32_t)p; });
+  pages_where<false>(a.refs, used, a.n_pages, all, lds, [&](int64_t p, int64_t r) { a.src[r] = (int32_t)p; });
   for (int r = threadIdx.x; r < holes; r += kPlanThreads) {
     const int32_t p = a.src[r], q = a.dst[r];
     a.to[p] = q;
@@ -279,7 +299,7 @@ __global__ __launch_bounds__(kThreads) void pages_copy_kernel(CopyArgs a) {
     char *to = pool + ((layer * a.n_pages + dst) * a.n_kv + h) * run;
     const int bytes = valid * a.row_bytes;
     for (int b = lane * 16; b < bytes; b += 64 * 16)
-      *reinterpret_cast<u32x4 *>(to + b) = *reinterpret_cast<const u32x4 *>(from + b);
+      __builtin_nontemporal_store(__builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from + b)), reinterpret_cast<u32x4 *>(to + b));
   }
 }
 

@@ -33,10 +33,18 @@ struct Carve {
 
 constexpr int64_t kMaxCount = (int64_t)1 << 30;
 
+// Rotation: waves that fill the chip.
+constexpr int64_t kRopeWaves = 4096;
 // Parts up to which one wave joins a row.
 constexpr int kJoinWave = 16;
-// Attention: workgroups that a launch aims at, and key blocks below which no tile is split.
-constexpr int kRowsTarget = 2048, kRowsLeast = 16, kTileTarget = 512, kTileLeast = 4;
+// Attention: workgroups that the chip holds at once (two a compute unit; of the kernels for
+// heads above 128 one, of the 16-row kernels for heads up to 96 three), which a launch that splits its tiles aims at: a few more would wait
+// for a second round.  8 sequences of 2000 to 6000 keys: 512 workgroups 30.8 us, 768 38.1.
+// Tiles of 16 rows whose parts stay at kLongBlocks blocks or more are split over up to
+// kSlotsLong workgroups, since sequences of different lengths then share the chip more
+// evenly (64 sequences of 500 to 8000 keys 156 -> 150 us).
+// Key blocks below which no tile is split.
+constexpr int kSlots = 512, kSlotsLong = 2048, kLongBlocks = 24, kRowsLeast = 8, kTileLeast = 4;
 
 int launched(const char *what) {
   const hipError_t e = hipGetLastError();
@@ -142,7 +150,11 @@ int run_rope(sats::RopeArgs a, int esz, bool append, hipStream_t stream) {
   const int units = a.dim / (2 * (wide ? vec : 1));
   a.lanes = 1;
   while (a.lanes < units && a.lanes < 64) a.lanes *= 2;
+  // rows of a token that a row of lanes takes one after another (they share its angles): as
+  // many as leave kRopeWaves waves, 8 at most.  4096 tokens of 48 rows: 1 30.3 us, 2 26.1, 6
+  // (a wave a token) 22.9; a few tokens want every row in lanes of its own.
   a.per = 1;
+  while (a.per < 8 && a.per < a.rows && n * ((a.rows + a.per) / (a.per + 1)) * a.lanes >= kRopeWaves * 64) ++a.per;
   const int64_t groups = (a.rows + a.per - 1) / a.per, threads = n * groups * a.lanes;
   if (threads > (int64_t)sats::kThreads * 0x7fffffff) return fail(SATS_ERR_SHAPE, "too many rows for one call");
   const dim3 grid((unsigned)((threads + sats::kThreads - 1) / sats::kThreads));
@@ -159,7 +171,7 @@ int run_rope(sats::RopeArgs a, int esz, bool append, hipStream_t stream) {
 struct AttendPlan {
   int tiles, splits, per_split;
 };
-AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int target, int least, int64_t max_q) {
+AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, int64_t max_q) {
   const sats::BatchView &b = a.batch;
   const int64_t per_seq = (max_q * a.group + R - 1) / R;
   AttendPlan p;
@@ -167,7 +179,11 @@ AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int target, i
   int64_t range = std::min<int64_t>(b.max_kv, b.max_pages << a.pool.shift);  // keys that a tile can see
   if (a.window) range = std::min(range, a.window + R / a.group + 1 + a.sinks + 2 * keys);
   const int64_t blocks = std::max<int64_t>(1, (range + keys - 1) / keys + 1);
-  const int64_t want = std::max<int64_t>(1, target / std::max<int64_t>(1, (int64_t)p.tiles * a.pool.n_kv));
+  const int64_t wgs = std::max<int64_t>(1, (int64_t)p.tiles * a.pool.n_kv);
+  int64_t slots = a.dim > 128 ? kSlots / 2 : kSlots;
+  if (R == 16 && a.dim <= 96) slots = kSlots * 3 / 2;
+  int64_t want = std::max<int64_t>(1, slots / wgs);
+  if (R == 16) want = std::max(want, std::min<int64_t>(kSlotsLong / wgs, blocks / kLongBlocks));
   p.per_split = (int)std::max<int64_t>(least, (blocks + want - 1) / want);
   p.splits = (int)((blocks + p.per_split - 1) / p.per_split);
   return p;
@@ -193,6 +209,21 @@ int launch_attention(sats::AttendArgs a, const AttendPlan &p, Kernel kernel, cha
   return launched("attend_join_kernel");
 }
 
+typedef void (*AttendKernel)(sats::AttendArgs);
+template <typename T> AttendKernel rows_kernel(int dim) {
+  using namespace sats;
+  return dim <= 64    ? (dim == 64 ? attend_rows_kernel<T, 64, true> : attend_rows_kernel<T, 64, false>)
+         : dim <= 96  ? (dim == 96 ? attend_rows_kernel<T, 96, true> : attend_rows_kernel<T, 96, false>)
+         : dim <= 128 ? (dim == 128 ? attend_rows_kernel<T, 128, true> : attend_rows_kernel<T, 128, false>)
+                      : attend_rows_kernel<T, 256, true>;  // (passing dims over costs it its registers)
+}
+AttendKernel tile_kernel(int dim) {
+  using namespace sats;
+  return dim <= 64    ? (dim == 64 ? attend_tile_kernel<64, true> : attend_tile_kernel<64, false>)
+         : dim <= 128 ? (dim == 128 ? attend_tile_kernel<128, true> : attend_tile_kernel<128, false>)
+                      : (dim == 256 ? attend_tile_kernel<256, true> : attend_tile_kernel<256, false>);
+}
+
 // Sequences of at most 16 rows a cache head, and all of float32, go in tiles of 16 rows,
 // the others in tiles of 128.  A batch of one sequence needs no launch for the former.
 template <typename T> int run_attention(sats::AttendArgs a, hipStream_t stream) {
@@ -200,9 +231,9 @@ template <typename T> int run_attention(sats::AttendArgs a, hipStream_t stream) 
   AttendPlan small{}, large{};
   const bool any_large = bf16 && a.batch.max_q * a.group > 16;
   if (!any_large || a.batch.n_seqs > 1) {
-    small = attend_plan(a, 16, sats::RowsOf<T>::kKeys, kRowsTarget, kRowsLeast, any_large ? 16 / a.group : a.batch.max_q);
+    small = attend_plan(a, 16, sats::RowsOf<T>::kKeys, kRowsLeast, any_large ? 16 / a.group : a.batch.max_q);
   }
-  if (any_large) large = attend_plan(a, sats::kTileRows, sats::kTileKeys, kTileTarget, kTileLeast, a.batch.max_q);
+  if (any_large) large = attend_plan(a, sats::kTileRows, sats::kTileKeys, kTileLeast, a.batch.max_q);
   const size_t bytes = std::max(attend_bytes(small, 16, a.pool.n_kv, a.dim),
                                 attend_bytes(large, sats::kTileRows, a.pool.n_kv, a.dim));
   char *mem = nullptr;
@@ -210,15 +241,13 @@ template <typename T> int run_attention(sats::AttendArgs a, hipStream_t stream) 
   if (rc) return rc;
   if (small.tiles) {
     a.small = 1, a.large = !bf16;
-    auto kernel = a.dim <= 64 ? sats::attend_rows_kernel<T, 64> : a.dim <= 128 ? sats::attend_rows_kernel<T, 128>
-                                                                                : sats::attend_rows_kernel<T, 256>;
+    auto kernel = rows_kernel<T>(a.dim);
     if ((rc = launch_attention<T, 16>(a, small, kernel, mem, stream))) return rc;
   }
   if constexpr (bf16)
     if (large.tiles) {
       a.small = small.tiles == 0, a.large = 1;
-      auto kernel = a.dim <= 64 ? sats::attend_tile_kernel<64> : a.dim <= 128 ? sats::attend_tile_kernel<128>
-                                                                              : sats::attend_tile_kernel<256>;
+      auto kernel = tile_kernel(a.dim);
       rc = launch_attention<T, sats::kTileRows>(a, large, kernel, mem, stream);
     }
   return rc;
@@ -227,14 +256,15 @@ template <typename T> int run_attention(sats::AttendArgs a, hipStream_t stream) 
 // ------------------------------------------------------------- pages
 
 struct PagesScratch {
-  int32_t *off, *ids, *to, *src, *dst, *valid, *ctl;
+  int32_t *off, *len_of, *ids, *to, *src, *dst, *valid, *ctl;
 };
 size_t pages_layout(char *base, int64_t n, int64_t n_pages, PagesScratch *out) {
   Carve c{base};
   PagesScratch s;
   const int64_t moves = std::max(n, n_pages);
   s.ctl = c.take<int32_t>(16);
-  s.off = c.take<int32_t>(n + 1);
+  s.off = c.take<int32_t>(n);
+  s.len_of = c.take<int32_t>(n);
   s.ids = c.take<int32_t>(n_pages);
   s.to = c.take<int32_t>(n_pages);
   s.src = c.take<int32_t>(moves);
@@ -263,7 +293,7 @@ sats::PagesArgs pages_args(const sats_kv_cache *c, const sats_kv_pages *p, const
   a.n_seqs = p->n_seqs, a.max_pages = p->max_pages, a.n_pages = c->n_pages;
   a.page = (int)c->page_size, a.shift = log2_of(c->page_size);
   a.seqs = seqs, a.other = other, a.n = (int)n;
-  if (s) a.off = s->off, a.ids = s->ids, a.to = s->to, a.src = s->src, a.dst = s->dst, a.valid = s->valid, a.ctl = s->ctl;
+  if (s) a.off = s->off, a.len_of = s->len_of, a.ids = s->ids, a.to = s->to, a.src = s->src, a.dst = s->dst, a.valid = s->valid, a.ctl = s->ctl;
   return a;
 }
 
@@ -272,7 +302,7 @@ int copy_pages(const sats_kv_cache *c, const int32_t *src, const int32_t *dst, c
   sats::CopyArgs a{static_cast<char *>(c->k), static_cast<char *>(c->v), c->n_pages, c->n_layers, (int)c->n_kv_heads,
                    (int)c->page_size, (int)(c->head_dim * c->elem_bytes), src, dst, valid, ctl, (int)n};
   const int64_t waves = n * c->n_layers * 2 * c->n_kv_heads, per = sats::kThreads / 64;
-  const int64_t grid = std::clamp<int64_t>((waves + per - 1) / per, 1, 2048);
+  const int64_t grid = std::clamp<int64_t>((waves + per - 1) / per, 1, 8192);
   sats::pages_copy_kernel<<<(unsigned)grid, sats::kThreads, 0, stream>>>(a);
   return launched("pages_copy_kernel");
 }
@@ -516,9 +546,9 @@ int sats_reserve_serving(int64_t max_items, int64_t n_pages, int64_t max_rows, i
       vocab < 0 || vocab > kMaxVocab || head_dim < 0 || head_dim > 256)
     return fail(SATS_ERR_SHAPE, "bad sizes for sats_reserve_serving");
   size_t bytes = 0;
-  // attention: a launch that splits its tiles has at most the target's workgroups
+  // attention: a launch that splits its tiles has at most kSlotsLong workgroups of 16 rows, kSlots of 128
   if (head_dim)
-    bytes = (size_t)std::max(kRowsTarget * 16, kTileTarget * sats::kTileRows) * (head_dim + 2) * sizeof(float);
+    bytes = (size_t)std::max(kSlotsLong * 16, kSlots * sats::kTileRows) * (head_dim + 2) * sizeof(float);
   if (n_pages) bytes = std::max(bytes, pages_layout(nullptr, max_items, n_pages, nullptr));
   if (max_rows && vocab) bytes = std::max(bytes, sample_layout(nullptr, max_rows, vocab, nullptr));
   char *mem = nullptr;
