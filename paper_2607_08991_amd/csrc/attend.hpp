@@ -54,6 +54,10 @@ struct AttendArgs {
 };
 
 __device__ u32x4 attend_zeros[64];  // a row of zeros
+constexpr uint32_t kNoRow = 0x80000000u;  // an offset past every buffer: the load returns zeros
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const char *base) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), (short)0, 0x7fffffff, 0x00020000);
+}
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -275,8 +279,32 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
   auto page_of = [&](int b) {  // of key lane % kKeys of a block
     return b < b_end ? key_page(a, t, kb, block_key(kb, b, kKeys) + (lane & (kKeys - 1))) : -1;
   };
-  auto load = [&](int b, int page) {
+  auto load = [&](int b, int page, uint32_t there) {
     const int j0 = (int)(block_key(kb, b, kKeys) & (a.pool.page - 1));  // (blocks and pages are powers of two)
+    if (a.pool.shift >= 4) {
+      // 16 keys are in one page: one address for them, and offsets that read zeros (past the
+      // buffer's end) for keys and dims that are not there
+#pragma unroll
+      for (int kt = 0; kt < kTiles; ++kt) {
+        const uint32_t here = there >> (16 * kt) & 0xffffu;
+        const int64_t p = here ? __builtin_amdgcn_readlane(page, 16 * kt + __builtin_ctz(here)) : 0;
+        const int64_t at = p * page_bytes + ((j0 + 16 * kt) & (a.pool.page - 1)) * row_bytes;
+        const __amdgpu_buffer_rsrc_t rk = rows_rsrc(kp + at), rv = rows_rsrc(vp + at);
+        const uint32_t k_off = here >> row & 1 ? row * row_bytes + g * 16 : kNoRow;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+          kr[kt * kSteps + s] = __builtin_bit_cast(
+              u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                         rk, FULL || (4 * s + g) * kVec < a.dim ? k_off + 64 * s : kNoRow, 0, 0));
+#pragma unroll
+        for (int i = 0; i < kLoads / kTiles; ++i) {
+          const int r = (i * 64 + lane) / kChunks, c = (i * 64 + lane) % kChunks;
+          const uint32_t off = (here >> r & 1) && (FULL || c * kVec < a.dim) ? r * row_bytes + c * 16 : kNoRow;
+          vr[kt * (kLoads / kTiles) + i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0));
+        }
+      }
+      return;
+    }
     // address of piece c of key i's row
     auto addr = [&](const char *base, int i, int c) {
       const int p = __shfl(page, i);
@@ -303,15 +331,16 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
 
   int b = z * a.per_split + w;
   int page = page_of(b);
-  if (b < b_end) load(b, page);
+  uint32_t there = (uint32_t)__ballot(page >= 0);
+  if (b < b_end) load(b, page, there);
   int page_next = page_of(b + 4);
   for (; b < b_end; b += 4) {
     const int64_t j0 = block_key(kb, b, kKeys);
-    const uint64_t there = __ballot(page >= 0);
-    const bool whole = (uint32_t)there == (uint32_t)((1ull << kKeys) - 1) && j0 + kKeys - 1 <= kb.low &&
+    const uint32_t here = there & (uint32_t)((1ull << kKeys) - 1);
+    const bool whole = here == (uint32_t)((1ull << kKeys) - 1) && j0 + kKeys - 1 <= kb.low &&
                        (!a.window || kb.high - j0 < a.window || j0 + kKeys <= a.sinks);
     // scores: lane (row, keys 16 kt + 4 g + i)
-    f32x4 s[kTiles];
+    f32x4 s[kTiles], s2 = {0, 0, 0, 0};  // (s2: float32's second chain of products)
 #pragma unroll
     for (int kt = 0; kt < kTiles; ++kt) {
       s[kt] = f32x4{0, 0, 0, 0};
@@ -323,12 +352,14 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
                                                           __builtin_bit_cast(bf16x8_t, qv[st]), s[kt], 0, 0, 0);
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            s[kt] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[kt * kSteps + st][e]),
-                                                         __uint_as_float(qv[st][e]), s[kt], 0, 0, 0);
+          for (int e = 0; e < 4; ++e) {
+            f32x4 &to = e & 1 ? s2 : s[0];
+            to = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[st][e]), __uint_as_float(qv[st][e]), to, 0, 0, 0);
+          }
         }
       }
     }
+    if constexpr (sizeof(T) == 4) s[0] += s2;
     // V to LDS, and the next block's loads
     bool odd = false;
     if (several && !whole) {
@@ -342,20 +373,21 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
       *reinterpret_cast<u32x4 *>(mine + r * kPitch + at % kChunks * 16) = vr[i];
     }
     page = page_next;
+    there = (uint32_t)__ballot(page >= 0);
     if (b + 4 < b_end) {
-      load(b + 4, page);
+      load(b + 4, page, there);
       page_next = page_of(b + 8);
     }
 #pragma unroll
     for (int kt = 0; kt < kTiles; ++kt) s[kt] *= scale2;
     if (!whole) {
       const Sight sight = sight_of(a, place, j0);
-      const uint32_t here = (uint32_t)there >> (4 * g);
+      const uint32_t mine = here >> (4 * g);
 #pragma unroll
       for (int kt = 0; kt < kTiles; ++kt)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          s[kt][i] = ((here >> (16 * kt + i) & 1) != 0) & sight.sees(16 * kt + 4 * g + i) ? s[kt][i] : -INFINITY;
+          s[kt][i] = ((mine >> (16 * kt + i) & 1) != 0) & sight.sees(16 * kt + 4 * g + i) ? s[kt][i] : -INFINITY;
     }
     float top = -INFINITY;
 #pragma unroll
@@ -483,9 +515,7 @@ template <int OFF> __device__ __forceinline__ void load_to_lds(const char *src, 
 }
 // The same from base + off, base the same for the whole wave.
 template <int OFF> __device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint8_t *dst) {
-  const __amdgpu_buffer_rsrc_t r =
-      __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), (short)0, 0x7fffffff, 0x00020000);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)dst, 16, (int)off, 0, OFF, 0);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rows_rsrc(base), (__attribute__((address_space(3))) void *)dst, 16, (int)off, 0, OFF, 0);
 }
 
 // Every load of this wave has landed, and every wave is here.
@@ -768,7 +798,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
           load_to_lds<i % 4 * 1024>(from + i / 4 * 4096, off ^ (place(i * kStep, 0) * 16), to + i / 4 * 4096);
         } else {
           const int c = place(i * kStep + r0, x);
-          load_to_lds<0>(from, c * 8 < a.dim ? (uint32_t)((i * kStep + r0) * row_bytes + c * 16) : 0x80000000u, to + i * 1024);
+          load_to_lds<0>(from, c * 8 < a.dim ? (uint32_t)((i * kStep + r0) * row_bytes + c * 16) : kNoRow, to + i * 1024);
         }
       };
       load(Const<0>{}), load(Const<1>{});
