@@ -530,9 +530,9 @@ int sats_sample(const void *logits, int elem_bytes, int64_t stride, int64_t n, i
   a.tokens = tokens, a.prob = prob, a.n_kept = n_kept;
   a.cmax = s.cmax, a.cid = s.cid, a.hsum = s.hsum, a.hcnt = s.hcnt, a.csum = s.csum, a.ccnt = s.ccnt;
   a.list = s.list, a.n_list = s.n_list, a.arrived = s.arrived, a.cuts = s.cuts;
-  // chunks of a workgroup: about a workgroup per compute unit
+  // chunks of a workgroup: about two workgroups per compute unit
   a.span = 1;
-  while (a.span < sats::kSampSpan && n * a.chunks > 256 * a.span) a.span *= 2;
+  while (a.span < sats::kSampSpan && n * a.chunks > kSlots * a.span) a.span *= 2;
   const bool wide = on16(logits) && stride * elem_bytes % 16 == 0;
   if (elem_bytes == 2) launch_sample<uint16_t>(a, wide, stream);
   else launch_sample<float>(a, wide, stream);
