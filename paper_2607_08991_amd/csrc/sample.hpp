@@ -12,7 +12,8 @@
 // and the first one always; the id drawn is the first, in the order of ids, whose
 // running sum of kept weights exceeds u times their total.
 //
-// Nothing is sorted.  Four launches, each over chunks of the rows but the last:
+// Nothing is sorted.  Either one launch, a workgroup per row that does all of it
+// (sample_row_kernel), or four, each over chunks of the rows but the last:
 //   max     the row's largest logit;
 //   hist    weights (for p) and counts (for k) by bins of (max - l) / T; the row's last
 //           workgroup finds the bins in which k and p can end;
@@ -137,14 +138,10 @@ __device__ __forceinline__ float row_max(const SampleArgs &a, int r, int32_t *id
   return m;
 }
 
-// Calls f(logit, id) for this thread's ids of a workgroup's span: a wave takes a share of
-// consecutive ids, which are of one chunk, V consecutive ones a lane and step.
+// Calls f(logit, id) for this lane's ids of lo .. hi - 1 (lo a multiple of V, hi the row's end
+// or a multiple of V), V consecutive ones a step, rising.
 template <typename T, int V, typename F>
-__device__ __forceinline__ void for_span(const SampleArgs &a, int r, F f) {
-  const T *row = (const T *)a.logits + (int64_t)r * a.stride;
-  const int per = a.span * (kSampChunk / (kSampThreads / 64));
-  const int64_t lo = ((int64_t)blockIdx.x * (kSampThreads / 64) + (threadIdx.x >> 6)) * per;
-  const int64_t hi = lo + per < a.vocab ? lo + per : a.vocab;
+__device__ __forceinline__ void for_range(const T *row, int64_t lo, int64_t hi, F f) {
 #pragma unroll 4
   for (int64_t i = lo + (threadIdx.x & 63) * V; i < hi; i += 64 * V) {
     if (i + V <= hi) {
@@ -158,6 +155,14 @@ __device__ __forceinline__ void for_span(const SampleArgs &a, int r, F f) {
     }
   }
 }
+// ... of a workgroup's span: a wave takes a share of consecutive ids, which are of one chunk.
+template <typename T, int V, typename F>
+__device__ __forceinline__ void for_span(const SampleArgs &a, int r, F f) {
+  const int per = a.span * (kSampChunk / (kSampThreads / 64));
+  const int64_t lo = ((int64_t)blockIdx.x * (kSampThreads / 64) + (threadIdx.x >> 6)) * per;
+  for_range<T, V>((const T *)a.logits + (int64_t)r * a.stride, lo, lo + per < a.vocab ? lo + per : a.vocab, f);
+}
+
 template <typename T, int V>
 __global__ __launch_bounds__(kSampThreads) void sample_max_kernel(SampleArgs a) {
   constexpr int kWaves = kSampThreads / 64;
@@ -190,22 +195,18 @@ __global__ __launch_bounds__(kSampThreads) void sample_max_kernel(SampleArgs a) 
   }
 }
 
-// Finds a row's cut from its bins, by the first 256 threads of a workgroup (8 bins each).
-__device__ __forceinline__ void row_cut(const SampleArgs &a, int r, const RowRule &q, u64 *lds_s, uint32_t *lds_c,
-                                        RowCut *out) {
+// Finds a row's cut from its bins (sum(b), count(b)), by the first 256 threads of a
+// workgroup (8 bins each).
+template <typename Sum, typename Count>
+__device__ __forceinline__ void row_cut(const RowRule &q, Sum sum, Count count_of, u64 *lds_s, uint32_t *lds_c, RowCut *out) {
   constexpr int kPer = kSampBins / kThreads;
   u64 s[kPer], inc_s = 0;
   uint32_t c[kPer], inc_c = 0;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool on = tid < kThreads;
   if (on) {
-    const u64 *hs = a.hsum + (int64_t)r * kSampBins + tid * kPer;
-    const uint32_t *hc = a.hcnt + (int64_t)r * kSampBins + tid * kPer;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {  // (added by other workgroups of this launch)
-      s[i] = __hip_atomic_load(hs + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      c[i] = __hip_atomic_load(hc + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
+    for (int i = 0; i < kPer; ++i) s[i] = sum(tid * kPer + i), c[i] = count_of(tid * kPer + i);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) inc_s += s[i], inc_c += c[i];
   }
@@ -303,7 +304,12 @@ __global__ __launch_bounds__(kSampThreads) void sample_hist_kernel(SampleArgs a)
     if (hc[b]) atomicAdd(&a.hcnt[(int64_t)r * kSampBins + b], hc[b]);
   }
   if (!arrive_last(a.arrived + r, gridDim.x, &last)) return;
-  row_cut(a, r, q, ls, lc, &cut);
+  // (the bins were added by other workgroups of this launch)
+  const u64 *hsum = a.hsum + (int64_t)r * kSampBins;
+  const uint32_t *hcnt = a.hcnt + (int64_t)r * kSampBins;
+  row_cut(
+      q, [&](int b) { return __hip_atomic_load(hsum + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); },
+      [&](int b) { return __hip_atomic_load(hcnt + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }, ls, lc, &cut);
   if (threadIdx.x == 0) a.cuts[r] = cut;
 }
 
@@ -619,6 +625,165 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
       if (a.n_kept) a.n_kept[r] = (int32_t)count;
     }
     x += w[i];
+  }
+}
+
+// A row by one workgroup: the same steps, one after the other, bins and list in LDS.  A row
+// of the four launches costs the chip less, but they are four, and pass through the caches:
+// the host takes this one where its rounds over the chip are shorter.
+template <typename T, int V>
+__global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) {
+  constexpr int kWaves = kPickThreads / 64;
+  __shared__ PickLds l;
+  __shared__ u64 hs[kSampBins];
+  __shared__ uint32_t hc[kSampBins];
+  __shared__ RowCut cut;
+  __shared__ float wave_top[kWaves];
+  __shared__ int32_t wave_id[kWaves];
+  __shared__ u64 end_lds, wave_sum_lds[kWaves];
+  __shared__ uint32_t n_keys, n_sure;
+  const int r = blockIdx.x, tid = threadIdx.x, w = tid >> 6;
+  const T *row = (const T *)a.logits + (int64_t)r * a.stride;
+  const int64_t share = ((a.vocab + kWaves - 1) / kWaves + 7) / 8 * 8;  // ids of a wave
+  const int64_t lo = w * share < a.vocab ? w * share : a.vocab, hi = lo + share < a.vocab ? lo + share : a.vocab;
+  const RowRule q = row_rule(a, r);
+  for (int b = tid; b < kSampBins; b += kPickThreads) hs[b] = 0, hc[b] = 0;
+  if (tid == 0) n_keys = 0, n_sure = 0;
+  // the largest logit and its lowest id
+  float top = -INFINITY;
+  int32_t id = 0x7fffffff;
+  for_range<T, V>(row, lo, hi, [&](float x, uint32_t i) {
+    if (x > top) top = x, id = (int32_t)i;
+  });
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    const float x = __shfl_xor(top, d);
+    const int32_t y = __shfl_xor(id, d);
+    if (x > top || (x == top && y < id)) top = x, id = y;
+  }
+  if ((tid & 63) == 0) wave_top[w] = top, wave_id[w] = id;
+  __syncthreads();
+  top = wave_top[0], id = wave_id[0];
+#pragma unroll
+  for (int i = 1; i < kWaves; ++i)
+    if (wave_top[i] > top) top = wave_top[i], id = wave_id[i];  // (the waves' ids rise)
+  if (q.first || !(top > -INFINITY)) {
+    const bool some = top > -INFINITY;
+    if (tid == 0) {
+      a.tokens[r] = some ? id : -1;
+      if (a.prob) a.prob[r] = some ? 1.0f : 0.0f;
+      if (a.n_kept) a.n_kept[r] = some;
+    }
+    return;
+  }
+  int sure = kSampBins, maybe = -1, k_bin = -1;
+  if (q.by_k || q.by_p) {
+    for_range<T, V>(row, lo, hi, [&](float x, uint32_t) {
+      const float z = below(x, top, q.inv_t);
+      if (!(z > -30.0f)) return;
+      const int b = bin_of(z);
+      if (q.by_p) {
+        const u64 wt = weight_of(share_of(z));
+        if (!wt) return;
+        atomicAdd(&hs[b], wt);
+        if (q.by_k) atomicAdd(&hc[b], 1u);
+      } else if (weighs(z)) {
+        atomicAdd(&hc[b], 1u);
+      }
+    });
+    __syncthreads();
+    row_cut(q, [&](int b) { return hs[b]; }, [&](int b) { return hc[b]; }, l.scan, l.cnt, &cut);
+    k_bin = cut.k_bin;
+    if (q.by_p) sure = cut.p_lo, maybe = cut.p_hi;
+    else sure = k_bin;
+  }
+  // the list, and the weights kept for certain
+  u64 *list = a.list + (int64_t)r * a.vocab;
+  u64 sum = 0;
+  uint32_t cnt = 0;
+  for_range<T, V>(row, lo, hi, [&](float x, uint32_t i) {
+    const float z = below(x, top, q.inv_t);
+    if (!(z > -30.0f)) return;
+    const int b = bin_of(z);
+    const bool listed = ((b >= sure) & (b <= maybe)) | (b == k_bin);
+    if (b < sure || listed) {
+      const float sh = share_of(z);
+      const u64 wt = weight_of(sh);
+      if (listed) {
+        if (!wt) return;
+        const uint32_t at = atomicAdd(&n_keys, 1u);
+        if (at < kPickList) l.keys[at] = key_of(x, i);
+        else list[at] = key_of(x, i);
+      } else if (sh >= q.min_p) {
+        sum += wt, cnt += wt != 0;
+      }
+    }
+  });
+  sum = wave_sum(sum);
+  const u64 c = wave_sum((u64)cnt);
+  if ((tid & 63) == 0) wave_sum_lds[w] = sum, atomicAdd(&n_sure, (uint32_t)c);
+  __syncthreads();
+  u64 last = ~0ull, kept = 0;
+  const uint32_t n = n_keys;
+  if (n) {
+    PickKeys k{list, nullptr, n, top, q.inv_t, 0, 0};
+    if (n <= kPickList) {
+      for (uint32_t i = tid; i < n; i += kPickThreads) l.weights[i] = k.weigh(l.keys[i]);
+      k.list = l.keys, k.weights = l.weights;
+    } else {
+      for (uint32_t i = tid; i < kPickList; i += kPickThreads) list[i] = l.keys[i];
+    }
+    __syncthreads();
+    if (n <= kPickWave) {
+      if (tid < 64) {
+        const u64 end = pick_last<64>(q, cut, k, l);
+        if (tid == 0) end_lds = end;
+      }
+      __syncthreads();
+      last = end_lds;
+    } else {
+      last = pick_last<kPickThreads>(q, cut, k, l);
+    }
+    __syncthreads();
+    for (uint32_t i = tid; i < n; i += kPickThreads) {
+      const u64 key = k.list[i];
+      if (key > last) continue;
+      const float sh = share_of(below(key_logit(key), top, q.inv_t));
+      if (sh >= q.min_p) atomicAdd(&wave_sum_lds[(uint32_t)key / (uint32_t)share], weight_of(sh)), ++kept;
+    }
+  }
+  u64 count;
+  (void)pick_scan(kept, l.scan, &count);
+  // the wave's share that holds the draw, then the thread's, then the id
+  u64 total = 0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) total += wave_sum_lds[i];
+  const double u = (double)fmaxf(a.u[r], 0.0f);
+  u64 at = (u64)fmin(u * (double)total, 0x1p63);
+  at = at < total ? at : total - 1;
+  u64 base = 0;
+  int from = 0;
+  for (; from < kWaves - 1 && at >= base + wave_sum_lds[from]; ++from) base += wave_sum_lds[from];
+  const int64_t per = (share + kPickThreads - 1) / kPickThreads;
+  const int64_t t0 = from * share + tid * per, s_end = (from + 1) * share < a.vocab ? (from + 1) * share : a.vocab;
+  const int64_t t1 = t0 + per < s_end ? t0 + per : s_end;
+  auto weight_at = [&](int64_t i) -> u64 {
+    const float x = Elem<T>::get(row + i), sh = share_of(below(x, top, q.inv_t));
+    return sh >= q.min_p && key_of(x, (uint32_t)i) <= last ? weight_of(sh) : 0;
+  };
+  u64 own = 0, unused;
+  for (int64_t i = t0; i < t1; ++i) own += weight_at(i);
+  u64 x = base + pick_scan(own, l.scan, &unused);
+  if (at < x || at >= x + own) return;
+  for (int64_t i = t0; i < t1; ++i) {
+    const u64 wt = weight_at(i);
+    if (at < x + wt) {
+      a.tokens[r] = (int32_t)i;
+      if (a.prob) a.prob[r] = (float)((double)wt / (double)total);
+      if (a.n_kept) a.n_kept[r] = (int32_t)(count + n_sure);
+      return;
+    }
+    x += wt;
   }
 }
 

@@ -335,11 +335,24 @@ size_t sample_layout(char *base, int64_t n, int64_t vocab, SampleScratch *out) {
   return c.off;
 }
 
+// One launch, a workgroup a row, or four over chunks of the rows.  Measured (us, rows of
+// bf16): 1 x 8000 13.4, 23.5; 1 x 32000 30.5, 24.2; 64 x 8000 21.5, 36.0; 64 x 32000 48.4,
+// 41.2; 256 x 64000 74.0, 75.9; 256 x 128256 120.5, 112.4: about 17 + 0.75 for 1000 ids of
+// each round over the compute units, and 33 + 2.4 for a million ids of all rows.
+bool sample_by_rows(int64_t n, int64_t vocab) {
+  return 0.75e-3 * vocab * std::max(1.0, n / 256.0) < 16.0 + 2.4e-6 * n * vocab;
+}
+
 constexpr int64_t kMaxVocab = (int64_t)sats::kSampChunk * sats::kPickThreads;
 
 template <typename T> void launch_sample(const sats::SampleArgs &a, bool wide, hipStream_t stream) {
   const dim3 grid((unsigned)((a.chunks + a.span - 1) / a.span), (unsigned)a.n);
   constexpr int V = 16 / sizeof(T);
+  if (sample_by_rows(a.n, a.vocab)) {
+    auto kernel = wide ? sats::sample_row_kernel<T, V> : sats::sample_row_kernel<T, 1>;
+    kernel<<<(unsigned)a.n, sats::kPickThreads, 0, stream>>>(a);
+    return;
+  }
   if (wide) {
     sats::sample_max_kernel<T, V><<<grid, sats::kSampThreads, 0, stream>>>(a);
     sats::sample_hist_kernel<T, V><<<grid, sats::kSampThreads, 0, stream>>>(a);

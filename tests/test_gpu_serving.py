@@ -708,3 +708,17 @@ def test_a_decode_step_in_a_graph(sats):
             assert torch.equal(x, y), i
         torch.randn(1000, device="cuda").sum().item()
     sats.sats_release()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,vocab", [(1, 21000), (1, 22000), (5, 40000), (300, 700), (2, 100003)])
+def test_sampling_on_both_sides_of_the_launches(sats, dtype, n, vocab):
+    """Sizes at which a workgroup takes a row and at which chunks of the rows are shared out,
+    aligned and not, with lists that pass what LDS holds (few distinct values)."""
+    r = random.Random(vocab + n)
+    x = (torch.randn((n, vocab), generator=gen(vocab), device="cuda") * 2).to(dt_of(dtype))
+    x[::3] = (x[::3] * 2).round() / 2
+    check_sample(sats, x, [r.random() for _ in range(n)], **rules(r, n, vocab))
+    odd = torch.empty((n, vocab + 1), device="cuda", dtype=x.dtype)
+    odd[:, 1:] = x
+    check_sample(sats, odd[:, 1:], [r.random() for _ in range(n)], **rules(r, n, vocab))
