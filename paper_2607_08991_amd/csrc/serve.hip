@@ -111,6 +111,12 @@ bool overlap(const void *a, int64_t na, const void *b, int64_t nb) {
   return na > 0 && nb > 0 && x < y + nb && y < x + na;
 }
 
+// Whether n bytes at p touch the cache's arrays.
+bool in_cache(const void *p, int64_t n, const sats_kv_cache *c) {
+  const int64_t all = (int64_t)pool_bytes(c);
+  return overlap(p, n, c->k, all) || overlap(p, n, c->v, all);
+}
+
 // ------------------------------------------------------------- norm and rotation
 
 int run_rope(sats::RopeArgs a, int esz, bool append, hipStream_t stream) {
@@ -343,6 +349,8 @@ bool sample_by_rows(int64_t n, int64_t vocab) {
   return 0.75e-3 * vocab * std::max(1.0, n / 256.0) < 16.0 + 2.4e-6 * n * vocab;
 }
 
+// Rows of a pass: their lists are as long as the vocabulary.
+constexpr int64_t kSampleRows = 512;
 constexpr int64_t kMaxVocab = (int64_t)sats::kSampChunk * sats::kPickThreads;
 
 template <typename T> void launch_sample(const sats::SampleArgs &a, bool wide, hipStream_t stream) {
@@ -410,6 +418,8 @@ int sats_qkv_append(const void *q, int64_t q_stride, const void *k, int64_t k_st
   a.n_tokens = batch->n_tokens;
   a.k_pool = layer_of(cache->k, cache, layer), a.v_pool = layer_of(cache->v, cache, layer);
   a.batch = batch_view(batch), a.pool = pool_view(cache);
+  const int64_t qs = span(batch->n_tokens, q_out_stride, n_q_heads * cache->head_dim, cache->elem_bytes);
+  if (q_out && in_cache(q_out, qs, cache)) return fail(SATS_ERR_ARG, "q_out overlaps the cache");
   return run_rope(a, cache->elem_bytes, true, stream);
 }
 
@@ -430,7 +440,10 @@ int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *c
   const int64_t row = n_q_heads * cache->head_dim, n = batch->n_tokens;
   if (q_stride < row) return fail(SATS_ERR_SHAPE, "q_stride is below the token's row");
   if (!on16(q) || !on16(out) || q_stride * esz % 16) return fail(SATS_ERR_ARG, "q, out and the rows of q must be 16-byte aligned");
-  if (overlap(out, n * row * esz, q, span(n, q_stride, row, esz))) return fail(SATS_ERR_ARG, "out overlaps q");
+  if (overlap(out, n * row * esz, q, span(n, q_stride, row, esz)) || in_cache(out, n * row * esz, cache))
+    return fail(SATS_ERR_ARG, "out overlaps q or the cache");
+  if (std::min(batch->max_q_len, n) * (n_q_heads / cache->n_kv_heads) > 0x7fffff00)
+    return fail(SATS_ERR_SHAPE, "too many rows for one call");
   sats::AttendArgs a{};
   a.q = q, a.q_stride = q_stride, a.out = out, a.lse = lse;
   a.k = layer_of(cache->k, cache, layer), a.v = layer_of(cache->v, cache, layer);
@@ -533,23 +546,30 @@ int sats_sample(const void *logits, int elem_bytes, int64_t stride, int64_t n, i
   if (stride < vocab) return fail(SATS_ERR_SHAPE, "stride is below vocab");
   char *mem = nullptr;
   SampleScratch s;
-  int rc = sats_host::serve_workspace(stream, sample_layout(nullptr, n, vocab, nullptr), &mem);
+  const int64_t pass = std::min(n, kSampleRows);
+  int rc = sats_host::serve_workspace(stream, sample_layout(nullptr, pass, vocab, nullptr), &mem);
   if (rc) return rc;
-  sample_layout(mem, n, vocab, &s);
+  sample_layout(mem, pass, vocab, &s);
   sats::SampleArgs a{};
-  a.logits = logits, a.stride = stride, a.vocab = vocab, a.n = (int)n;
+  a.stride = stride, a.vocab = vocab;
   a.chunks = (int)((vocab + sats::kSampChunk - 1) / sats::kSampChunk);
-  a.temperature = temperature, a.top_k = top_k, a.top_p = top_p, a.min_p = min_p, a.u = u;
-  a.tokens = tokens, a.prob = prob, a.n_kept = n_kept;
   a.cmax = s.cmax, a.cid = s.cid, a.hsum = s.hsum, a.hcnt = s.hcnt, a.csum = s.csum, a.ccnt = s.ccnt;
   a.list = s.list, a.n_list = s.n_list, a.arrived = s.arrived, a.cuts = s.cuts;
-  // chunks of a workgroup: about two workgroups per compute unit
-  a.span = 1;
-  while (a.span < sats::kSampSpan && n * a.chunks > kSlots * a.span) a.span *= 2;
   const bool wide = on16(logits) && stride * elem_bytes % 16 == 0;
-  if (elem_bytes == 2) launch_sample<uint16_t>(a, wide, stream);
-  else launch_sample<float>(a, wide, stream);
-  return launched("sample kernels");
+  for (int64_t r = 0; r < n && !rc; r += pass) {
+    auto at = [r](auto *p) { return p ? p + r : p; };
+    a.logits = static_cast<const char *>(logits) + r * stride * elem_bytes;
+    a.n = (int)std::min(pass, n - r);
+    a.temperature = at(temperature), a.top_k = at(top_k), a.top_p = at(top_p), a.min_p = at(min_p), a.u = at(u);
+    a.tokens = at(tokens), a.prob = at(prob), a.n_kept = at(n_kept);
+    // chunks of a workgroup: about two workgroups per compute unit
+    a.span = 1;
+    while (a.span < sats::kSampSpan && a.n * a.chunks > kSlots * a.span) a.span *= 2;
+    if (elem_bytes == 2) launch_sample<uint16_t>(a, wide, stream);
+    else launch_sample<float>(a, wide, stream);
+    rc = launched("sample kernels");
+  }
+  return rc;
 }
 
 int sats_reserve_serving(int64_t max_items, int64_t n_pages, int64_t max_rows, int64_t vocab, int64_t head_dim,
@@ -563,7 +583,7 @@ int sats_reserve_serving(int64_t max_items, int64_t n_pages, int64_t max_rows, i
   if (head_dim)
     bytes = (size_t)std::max(kSlotsLong * 16, kSlots * sats::kTileRows) * (head_dim + 2) * sizeof(float);
   if (n_pages) bytes = std::max(bytes, pages_layout(nullptr, max_items, n_pages, nullptr));
-  if (max_rows && vocab) bytes = std::max(bytes, sample_layout(nullptr, max_rows, vocab, nullptr));
+  if (max_rows && vocab) bytes = std::max(bytes, sample_layout(nullptr, std::min(max_rows, kSampleRows), vocab, nullptr));
   char *mem = nullptr;
   return sats_host::serve_workspace(stream, bytes, &mem);
 }

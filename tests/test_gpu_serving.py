@@ -722,3 +722,22 @@ def test_sampling_on_both_sides_of_the_launches(sats, dtype, n, vocab):
     odd = torch.empty((n, vocab + 1), device="cuda", dtype=x.dtype)
     odd[:, 1:] = x
     check_sample(sats, odd[:, 1:], [r.random() for _ in range(n)], **rules(r, n, vocab))
+
+
+def test_sampling_more_rows_than_a_pass(sats):
+    """Rows past the 512 that share scratch memory, both forms of the launches."""
+    for vocab, n in ((50, 1100), (30011, 515)):
+        x = torch.randn((n, vocab), generator=gen(n), device="cuda") * 2
+        rows = [0, 1, 511, 512, 513, n - 2, n - 1]
+        u, k = torch.rand(n, generator=gen(5), device="cuda"), torch.full((n,), 40, dtype=torch.int32, device="cuda")
+        p = torch.full((n,), 0.9, device="cuda")
+        tok, kept = (torch.zeros(n, dtype=torch.int32, device="cuda") for _ in range(2))
+        sats.sats_sample(x, u, tok, top_k=k, top_p=p, n_kept=kept)
+        one, kept1 = (torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(2))
+        for r in rows:
+            s = slice(r, r + 1)
+            sats.sats_sample(x[s], u[s], one, top_k=k[s], top_p=p[s], n_kept=kept1)
+            assert int(tok[r]) == int(one) and int(kept[r]) == int(kept1)
+        want = ref.sample(f64(x[n - 1]), shares_of(x[n - 1:], torch.ones(1, device="cuda")).cpu().numpy()[0],
+                          float(u[n - 1]), top_k=40, top_p=float(p[n - 1]))
+        assert int(tok[n - 1]) == want[0] and int(kept[n - 1]) == want[2]

@@ -56,7 +56,8 @@ def attend(no_cache=False, no_batch=False, **kw):
     (ARG, dict(elem_bytes=3)), (ARG, dict(k=P + 8)), (ARG, dict(v=P + 2)), (ARG, dict(scale=float("nan"))),
     (ARG, dict(scale=float("inf"))), (ARG, dict(window=-1)), (ARG, dict(sinks=-1)), (ARG, dict(sinks=4)),
     (ARG, dict(n_tokens=1, q=P + 2)), (ARG, dict(n_tokens=1, out=BIG + 4)), (ARG, dict(n_tokens=1, q_stride=257)),
-    (ARG, dict(n_tokens=1, out=P + 16)),
+    (ARG, dict(n_tokens=1, out=P + 16)), (ARG, dict(n_tokens=1, k=BIG)), (ARG, dict(n_tokens=1, v=BIG + 256)),
+    (SHAPE, dict(n_tokens=1 << 29, max_q_len=1 << 29, heads=16, q_stride=1024, q=BIG << 4, out=BIG << 8)),
     (SHAPE, dict(page_size=0)), (SHAPE, dict(page_size=24)), (SHAPE, dict(page_size=8192)), (SHAPE, dict(head_dim=0)),
     (SHAPE, dict(head_dim=12)), (SHAPE, dict(head_dim=264)), (SHAPE, dict(n_pages=0)), (SHAPE, dict(n_kv_heads=0)),
     (SHAPE, dict(n_layers=0)), (SHAPE, dict(layer=2)), (SHAPE, dict(layer=-1)), (SHAPE, dict(heads=3)),
@@ -90,7 +91,7 @@ def append(no_cache=False, no_batch=False, **kw):
     (SHAPE, dict(n_tokens=1, vs=100)), (SHAPE, dict(n_tokens=1, os=255)),
     (ARG, dict(eps=-1.0)), (ARG, dict(eps=float("nan"))), (ARG, dict(eps=float("inf"))), (ARG, dict(pairs=2)),
     (ARG, dict(n_tokens=2, out=P + 16)), (ARG, dict(n_tokens=2, out=2 * P + 16)), (ARG, dict(n_tokens=2, out=3 * P)),
-    (ARG, dict(n_tokens=2, out=P, os=512)), (OK, dict()),
+    (ARG, dict(n_tokens=2, out=P, os=512)), (ARG, dict(n_tokens=1, out=P + 8192)), (OK, dict()),
 ])
 def test_append_refuses(want, kw):
     assert append(**kw) == want, sats.sats_last_error()
@@ -179,7 +180,7 @@ class Pages(ctypes.Structure):
     _fields_ = [("table", P), ("len", P), ("refs", P), ("seqs", I), ("width", I)]
 def A(k): return P(PTR * k)
 def attend(seqs, tokens, max_q, max_kv, heads=32, kv=8, dim=128, esz=2, window=0):
-    c = Cache(PTR, PTR * 2, 1, 1 << 20, kv, 16, dim, esz)
+    c = Cache(PTR * 32, PTR * 64, 1, 1 << 20, kv, 16, dim, esz)
     b = Batch(PTR * 3, PTR * 4, PTR * 5, seqs, (max_kv + 15) // 16, tokens, max_q, max_kv)
     return lib.sats_paged_attention(A(6), I(heads * dim), ctypes.byref(c), I(0), ctypes.byref(b), I(heads),
                                     ctypes.c_float(0.1), I(window), I(0), A(7), P(0), P(0))
