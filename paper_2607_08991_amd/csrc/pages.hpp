@@ -41,6 +41,7 @@ struct CopyArgs {
   const int32_t *src, *dst, *valid;  // valid null: whole pages
   const int32_t *ctl;           // or null: n moves
   int n;
+  int table_wgs;                // the launch's first workgroups, which see to the table
 };
 
 // Exclusive prefix over the workgroup of one number per thread; *total its sum.
@@ -255,11 +256,14 @@ __global__ __launch_bounds__(kPlanThreads) void pages_compact_plan_kernel(PagesA
   }
 }
 
-// Table rows of a fork: the source's full pages shared, its part page replaced by the copy.
-__global__ __launch_bounds__(kThreads) void pages_fork_rows_kernel(PagesArgs a) {
-  const int i = blockIdx.y;
-  const int64_t j = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (!a.ctl[0] || j >= a.max_pages || a.off[i] < 0) return;
+// What a call does to the table beside the moves of contents, by the first workgroups of
+// their launch, an entry a thread.
+enum { PAGES_ONLY = 0, PAGES_FORK = 1, PAGES_REMAP = 2 };
+// A row of a fork: the source's full pages shared, its part page replaced by the copy.
+__device__ __forceinline__ void fork_entry(const PagesArgs &a, int64_t e) {
+  const int i = (int)(e / a.max_pages);
+  const int64_t j = e - i * a.max_pages;
+  if (i >= a.n || a.off[i] < 0) return;
   const int64_t s = item_seq(a, i), o = a.other[i], n = a.len[s];
   int32_t p = -1;
   if (j < n >> a.shift) {
@@ -271,23 +275,28 @@ __global__ __launch_bounds__(kThreads) void pages_fork_rows_kernel(PagesArgs a) 
   }
   a.table[o * a.max_pages + j] = p;
 }
-
-__global__ __launch_bounds__(kThreads) void pages_remap_kernel(PagesArgs a) {
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= a.n_seqs * a.max_pages) return;
-  const int32_t p = a.table[i];
-  if (p >= 0 && p < a.n_pages) a.table[i] = a.to[p];
+__device__ __forceinline__ void remap_entry(const PagesArgs &a, int64_t e) {
+  if (e >= a.n_seqs * a.max_pages) return;
+  const int32_t p = a.table[e];
+  if (p >= 0 && p < a.n_pages) a.table[e] = a.to[p];
 }
 
 // Moves the pages' contents: a wave takes the tokens of one (move, layer, keys or
 // values, head), which are contiguous, in 16-byte pieces.
-__global__ __launch_bounds__(kThreads) void pages_copy_kernel(CopyArgs a) {
+template <int TABLE>
+__global__ __launch_bounds__(kThreads) void pages_copy_kernel(CopyArgs a, PagesArgs t) {
   if (a.ctl && !a.ctl[0]) return;
+  if (TABLE != PAGES_ONLY && (int)blockIdx.x < a.table_wgs) {
+    const int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (TABLE == PAGES_FORK) fork_entry(t, e);
+    else remap_entry(t, e);
+    return;
+  }
+  const int wg = (int)blockIdx.x - a.table_wgs, wgs = (int)gridDim.x - a.table_wgs;
   const int n = a.ctl ? a.ctl[1] : a.n;
   const int lane = threadIdx.x & 63;
   const int64_t per = a.layers * 2 * a.n_kv, units = per * n;
-  for (int64_t u = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 6; u < units;
-       u += (int64_t)gridDim.x * (kThreads / 64)) {
+  for (int64_t u = ((int64_t)wg * kThreads + threadIdx.x) >> 6; u < units; u += (int64_t)wgs * (kThreads / 64)) {
     const int64_t m = u / per;
     const int x = (int)(u - m * per), h = x % a.n_kv, kv = x / a.n_kv % 2;
     const int64_t layer = x / a.n_kv / 2, src = a.src[m], dst = a.dst[m];

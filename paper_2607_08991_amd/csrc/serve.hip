@@ -303,13 +303,17 @@ sats::PagesArgs pages_args(const sats_kv_cache *c, const sats_kv_pages *p, const
   return a;
 }
 
+// Moves of contents, and with them `entries` of the table (TABLE, t).
+template <int TABLE>
 int copy_pages(const sats_kv_cache *c, const int32_t *src, const int32_t *dst, const int32_t *valid, const int32_t *ctl,
-               int64_t n, hipStream_t stream) {
-  sats::CopyArgs a{static_cast<char *>(c->k), static_cast<char *>(c->v), c->n_pages, c->n_layers, (int)c->n_kv_heads,
-                   (int)c->page_size, (int)(c->head_dim * c->elem_bytes), src, dst, valid, ctl, (int)n};
+               int64_t n, const sats::PagesArgs &t, int64_t entries, hipStream_t stream) {
+  const int64_t table = (entries + sats::kThreads - 1) / sats::kThreads;
   const int64_t waves = n * c->n_layers * 2 * c->n_kv_heads, per = sats::kThreads / 64;
   const int64_t grid = std::clamp<int64_t>((waves + per - 1) / per, 1, 8192);
-  sats::pages_copy_kernel<<<(unsigned)grid, sats::kThreads, 0, stream>>>(a);
+  if (table + grid > 0x7fffffff) return fail(SATS_ERR_SHAPE, "the page table is too large");
+  sats::CopyArgs a{static_cast<char *>(c->k), static_cast<char *>(c->v), c->n_pages, c->n_layers, (int)c->n_kv_heads,
+                   (int)c->page_size, (int)(c->head_dim * c->elem_bytes), src, dst, valid, ctl, (int)n, (int)table};
+  sats::pages_copy_kernel<TABLE><<<(unsigned)(table + grid), sats::kThreads, 0, stream>>>(a, t);
   return launched("pages_copy_kernel");
 }
 
@@ -479,7 +483,7 @@ int sats_cache_extend(const sats_kv_cache *cache, const sats_kv_pages *pages, co
   a.status = status;
   sats::pages_plan_kernel<false><<<1, sats::kPlanThreads, 0, stream>>>(a);
   if ((rc = launched("pages_plan_kernel"))) return rc;
-  return copy_pages(cache, s.src, s.dst, s.valid, s.ctl, n, stream);
+  return copy_pages<sats::PAGES_ONLY>(cache, s.src, s.dst, s.valid, s.ctl, n, a, 0, stream);
 }
 
 int sats_cache_fork(const sats_kv_cache *cache, const sats_kv_pages *pages, const int32_t *src, const int32_t *dst,
@@ -496,12 +500,7 @@ int sats_cache_fork(const sats_kv_cache *cache, const sats_kv_pages *pages, cons
   a.status = status;
   sats::pages_plan_kernel<true><<<1, sats::kPlanThreads, 0, stream>>>(a);
   if ((rc = launched("pages_plan_kernel"))) return rc;
-  if (pages->max_pages) {
-    const dim3 grid((unsigned)((pages->max_pages + sats::kThreads - 1) / sats::kThreads), (unsigned)n);
-    sats::pages_fork_rows_kernel<<<grid, sats::kThreads, 0, stream>>>(a);
-    if ((rc = launched("pages_fork_rows_kernel"))) return rc;
-  }
-  return copy_pages(cache, s.src, s.dst, s.valid, s.ctl, n, stream);
+  return copy_pages<sats::PAGES_FORK>(cache, s.src, s.dst, s.valid, s.ctl, n, a, n * pages->max_pages, stream);
 }
 
 int sats_cache_compact(const sats_kv_cache *cache, const sats_kv_pages *pages, int32_t *n_used, hipStream_t stream) {
@@ -516,12 +515,8 @@ int sats_cache_compact(const sats_kv_cache *cache, const sats_kv_pages *pages, i
   a.n_used = n_used;
   sats::pages_compact_plan_kernel<<<1, sats::kPlanThreads, 0, stream>>>(a);
   if ((rc = launched("pages_compact_plan_kernel"))) return rc;
-  const int64_t entries = pages->n_seqs * pages->max_pages;
-  if (entries) {
-    sats::pages_remap_kernel<<<(unsigned)((entries + sats::kThreads - 1) / sats::kThreads), sats::kThreads, 0, stream>>>(a);
-    if ((rc = launched("pages_remap_kernel"))) return rc;
-  }
-  return copy_pages(cache, s.src, s.dst, nullptr, s.ctl, std::max<int64_t>(cache->n_pages / 2, 1), stream);
+  return copy_pages<sats::PAGES_REMAP>(cache, s.src, s.dst, nullptr, s.ctl, std::max<int64_t>(cache->n_pages / 2, 1), a,
+                                       pages->n_seqs * pages->max_pages, stream);
 }
 
 int sats_cache_copy(const sats_kv_cache *cache, const int32_t *src_pages, const int32_t *dst_pages, int64_t n,
@@ -532,7 +527,7 @@ int sats_cache_copy(const sats_kv_cache *cache, const int32_t *src_pages, const 
   if (n < 0 || n > kMaxCount) return fail(SATS_ERR_SHAPE, "n must be >= 0, at most 2^30");
   if (n == 0) return SATS_OK;
   if (!src_pages || !dst_pages) return fail(SATS_ERR_NULL, "src_pages and dst_pages must be non-null");
-  return copy_pages(cache, src_pages, dst_pages, nullptr, nullptr, n, stream);
+  return copy_pages<sats::PAGES_ONLY>(cache, src_pages, dst_pages, nullptr, nullptr, n, sats::PagesArgs{}, 0, stream);
 }
 
 int sats_sample(const void *logits, int elem_bytes, int64_t stride, int64_t n, int64_t vocab, const float *temperature,
