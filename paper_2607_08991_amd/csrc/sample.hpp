@@ -31,7 +31,7 @@ namespace sats {
 typedef unsigned long long u64;
 
 constexpr int kSampChunk = 4096;  // ids of a chunk
-constexpr int kSampThreads = 512; // (one row of 128256 bf16: 24.7 us, of 1024 27.1, of 256 26.2; 64 float32 rows 59.3, 57.8, 64.4)
+constexpr int kSampThreads = 512; // (when chosen, with 512, 1024, 256: 1 x 128256 bf16 24.7, 27.1, 26.2 us; 64 float32 rows 59.3, 57.8, 64.4)
 constexpr int kSampSpan = 8;      // chunks that a workgroup takes, at most (a power of two, no more than its waves)
 constexpr int kSampBins = 2048;
 constexpr float kSampScale = 70.0f;   // bins per unit of (max - l) / T: weights past bin 2047 round to 0
@@ -97,9 +97,8 @@ __device__ __forceinline__ float share_of(float x, float top, float inv_t, float
   *z = below(x, top, inv_t);
   return share_of(*z);
 }
-__device__ __forceinline__ u64 weight_of(float share) {  // round(2^40 share), in two parts of 32 bits
-  const float f = share * 1099511627776.0f, high = truncf(f * 0x1p-20f);
-  return (u64)(uint32_t)high * (1u << 20) + (uint32_t)rintf(fmaf(high, -0x1p20f, f));
+__device__ __forceinline__ u64 weight_of(float share) {  // round(2^40 share): the low bits of 2^52 + it in float64
+  return (u64)__double_as_longlong(fma((double)share, 0x1p40, 0x1p52)) & ((1ull << 52) - 1);
 }
 // Whether an id at z has a weight (2^40 exp(-28) rounds to 1).
 __device__ __forceinline__ bool weighs(float z) { return z > -28.0f || weight_of(share_of(z)) != 0; }
@@ -120,13 +119,21 @@ __device__ __forceinline__ u64 wave_sum(u64 v) {
   return v;
 }
 
-// Largest logit of a row from its chunks, and its lowest id (any wave, all lanes).
+// Largest logit of a row from its chunks (any wave, all lanes), and its lowest id.
+__device__ __forceinline__ float row_max(const SampleArgs &a, int r) {
+  float m = -INFINITY;
+  for (int c = threadIdx.x & 63; c < a.chunks; c += 64) m = fmaxf(m, a.cmax[(int64_t)r * a.chunks + c]);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+  return m;
+}
 __device__ __forceinline__ float row_max(const SampleArgs &a, int r, int32_t *id) {
   float m = -INFINITY;
   int32_t at = 0x7fffffff;
   for (int c = threadIdx.x & 63; c < a.chunks; c += 64) {
     const float x = a.cmax[(int64_t)r * a.chunks + c];
-    if (x > m) m = x, at = a.cid[(int64_t)r * a.chunks + c];
+    const int32_t y = a.cid[(int64_t)r * a.chunks + c];
+    if (x > m) m = x, at = y;
   }
 #pragma unroll
   for (int d = 32; d; d >>= 1) {
@@ -139,28 +146,64 @@ __device__ __forceinline__ float row_max(const SampleArgs &a, int r, int32_t *id
 }
 
 // Calls f(logit, id) for this lane's ids of lo .. hi - 1 (lo a multiple of V, hi the row's end
-// or a multiple of V), V consecutive ones a step, rising.
+// or a multiple of V), rising, and for ids past the end with a logit of NaN.  The next kAhead loads are under way while those before are
+// looked at.  One is enough where it brings eight ids: more of them cost the time to fetch the
+// longer code (16 rows of 2000 bf16: 15.5 us with one, 17.4 with two, 21.2 with four;
+// 256 of 128256 95.4, 93.6, 94.9; float32 13.7, 14.7, 16.5 and 117.1, 107.3, 106.1).
 template <typename T, int V, typename F>
-__device__ __forceinline__ void for_range(const T *row, int64_t lo, int64_t hi, F f) {
-#pragma unroll 4
-  for (int64_t i = lo + (threadIdx.x & 63) * V; i < hi; i += 64 * V) {
-    if (i + V <= hi) {
-      float x[V];
-      load_vec_cached<T, V>(row + i, x);
+__device__ __forceinline__ void for_range(const T *row, int lo, int hi, F f) {
+  constexpr int kAhead = V == 1 ? 8 : V == 4 ? 2 : 1, kStep = 64 * V;
+  const int lane = threadIdx.x & 63;
+  if (lo >= hi) return;
+  if constexpr (V == 1) {
+    float x[kAhead], y[kAhead];
+    auto load = [&](float(&to)[kAhead], int from) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) f(x[j], (uint32_t)(i + j));
-    } else {
-      for (int j = 0; j < V; ++j)
-        if (i + j < hi) f(Elem<T>::get(row + i + j), (uint32_t)(i + j));
+      for (int s = 0; s < kAhead; ++s) {
+        to[s] = NAN;
+        if (from + s * kStep + lane < hi) to[s] = Elem<T>::get(row + from + s * kStep + lane);
+      }
+    };
+    load(x, lo);
+    for (int i = lo; i < hi; i += kAhead * kStep) {
+      load(y, i + kAhead * kStep);
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) f(x[s], (uint32_t)(i + s * kStep + lane));
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) x[s] = y[s];
     }
+  } else {
+    const int end = hi - hi % V;
+    const uint32_t none = sizeof(T) == 2 ? 0x7fc07fc0u : 0x7fc00000u;
+    u32x4 x[kAhead], y[kAhead];
+    auto load = [&](u32x4(&to)[kAhead], int from) {
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) {
+        to[s] = u32x4{none, none, none, none};
+        const int i = from + s * kStep + lane * V;
+        if (i < end) to[s] = *reinterpret_cast<const u32x4 *>(row + i);
+      }
+    };
+    load(x, lo);
+    for (int i = lo; i < end; i += kAhead * kStep) {
+      load(y, i + kAhead * kStep);
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) f(unpack<T>(x[s], j), (uint32_t)(i + s * kStep + lane * V + j));
+      }
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) x[s] = y[s];
+    }
+    if (end < hi) f(end + lane < hi ? Elem<T>::get(row + end + lane) : NAN, (uint32_t)(end + lane));
   }
 }
 // ... of a workgroup's span: a wave takes a share of consecutive ids, which are of one chunk.
 template <typename T, int V, typename F>
 __device__ __forceinline__ void for_span(const SampleArgs &a, int r, F f) {
-  const int per = a.span * (kSampChunk / (kSampThreads / 64));
-  const int64_t lo = ((int64_t)blockIdx.x * (kSampThreads / 64) + (threadIdx.x >> 6)) * per;
-  for_range<T, V>((const T *)a.logits + (int64_t)r * a.stride, lo, lo + per < a.vocab ? lo + per : a.vocab, f);
+  const int per = a.span * (kSampChunk / (kSampThreads / 64)), vocab = (int)a.vocab;
+  const int lo = (int)(blockIdx.x * (kSampThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * per;
+  for_range<T, V>((const T *)a.logits + (int64_t)r * a.stride, lo, lo + per < vocab ? lo + per : vocab, f);
 }
 
 template <typename T, int V>
@@ -267,10 +310,41 @@ __device__ __forceinline__ void row_cut(const RowRule &q, Sum sum, Count count_o
   __syncthreads();
 }
 
+// Calls go(f), f(logit, id) adding an id to the bins that the row's rule looks at: without a
+// branch, so that the ids of a load overlap (what has no weight goes to a bin of the lane's
+// past the last; from -29 on weights are 0).
+constexpr int kSampBinsAll = kSampBins + 64;
+template <typename Go>
+__device__ __forceinline__ void with_bins(const RowRule &q, float top, u64 *hs, uint32_t *hc, Go go) {
+  const int none = kSampBins + (threadIdx.x & 63);
+  if (!q.by_p) {
+    go([&](float x, uint32_t) {
+      const float z = fmaxf(below(x, top, q.inv_t), -29.0f);
+      atomicAdd(&hc[weight_of(expf(z)) ? (int)(-z * kSampScale) : none], 1u);
+    });
+  } else {
+    const bool by_k = q.by_k;
+    go([&](float x, uint32_t) {
+      const float z = fmaxf(below(x, top, q.inv_t), -29.0f);
+      const u64 w = weight_of(expf(z));
+      const int b = z > -29.0f ? (int)(-z * kSampScale) : none;
+      atomicAdd(&hs[b], w);
+      if (by_k) atomicAdd(&hc[b], (uint32_t)(w != 0));
+    });
+  }
+}
+
+// Only ids whose (l - max) / T is above this can be kept or listed: those in bins below `reach`,
+// where k or p set it, or above min_p where neither did.
+__device__ __forceinline__ float least_z(const RowRule &q, int reach) {
+  if (q.by_k || q.by_p) return reach < kSampBins ? -1.00001f / kSampScale * (float)reach : -30.0f;
+  return q.min_p > 0.0f ? fmaxf(-30.0f, 1.00001f * logf(q.min_p) - 0.00001f) : -30.0f;
+}
+
 template <typename T, int V>
 __global__ __launch_bounds__(kSampThreads) void sample_hist_kernel(SampleArgs a) {
-  __shared__ u64 hs[kSampBins];
-  __shared__ uint32_t hc[kSampBins];
+  __shared__ u64 hs[kSampBinsAll];
+  __shared__ uint32_t hc[kSampBinsAll];
   __shared__ u64 ls[8];
   __shared__ uint32_t lc[4];
   __shared__ RowCut cut;
@@ -278,26 +352,10 @@ __global__ __launch_bounds__(kSampThreads) void sample_hist_kernel(SampleArgs a)
   const int r = blockIdx.y;
   const RowRule q = row_rule(a, r);
   if (!q.by_k && !q.by_p) return;
-  int32_t id;
-  const float top = row_max(a, r, &id);
+  const float top = row_max(a, r);
   for (int b = threadIdx.x; b < kSampBins; b += kSampThreads) hs[b] = 0, hc[b] = 0;
   __syncthreads();
-  if (q.by_p) {
-    for_span<T, V>(a, r, [&](float x, uint32_t) {
-      float z;
-      const u64 w = weight_of(share_of(x, top, q.inv_t, &z));
-      if (w) {
-        const int b = bin_of(z);
-        atomicAdd(&hs[b], w);
-        if (q.by_k) atomicAdd(&hc[b], 1u);
-      }
-    });
-  } else {
-    for_span<T, V>(a, r, [&](float x, uint32_t) {
-      const float z = below(x, top, q.inv_t);
-      if (weighs(z)) atomicAdd(&hc[bin_of(z)], 1u);
-    });
-  }
+  with_bins(q, top, hs, hc, [&](auto f) { for_span<T, V>(a, r, f); });
   __syncthreads();
   for (int b = threadIdx.x; b < kSampBins; b += kSampThreads) {
     if (hs[b]) atomicAdd(&a.hsum[(int64_t)r * kSampBins + b], hs[b]);
@@ -322,8 +380,7 @@ __global__ __launch_bounds__(kSampThreads) void sample_cut_kernel(SampleArgs a) 
   const int r = blockIdx.y;
   const RowRule q = row_rule(a, r);
   if (q.first) return;
-  int32_t id;
-  const float top = row_max(a, r, &id);
+  const float top = row_max(a, r);
   // bins below `sure` are kept whole (but for k_bin), those up to `maybe`, and k_bin, go to the list
   int sure = kSampBins, maybe = -1, k_bin = -1;
   if (q.by_k || q.by_p) {
@@ -341,9 +398,10 @@ __global__ __launch_bounds__(kSampThreads) void sample_cut_kernel(SampleArgs a) 
   u64 sum = 0;
   uint32_t cnt = 0;
   u64 *list = a.list + (int64_t)r * a.vocab;
-  for_span<T, V>(a, r, [&](float x, uint32_t i) {
+  const float least = least_z(q, max(sure, max(maybe, k_bin) + 1));
+  auto take = [&](float x, uint32_t i) {
     const float z = below(x, top, q.inv_t);
-    if (!(z > -30.0f)) return;
+    if (!(z > least)) return;
     const int b = bin_of(z);
     const bool listed = ((b >= sure) & (b <= maybe)) | (b == k_bin);
     if (b < sure || listed) {
@@ -358,7 +416,8 @@ __global__ __launch_bounds__(kSampThreads) void sample_cut_kernel(SampleArgs a) 
         sum += w, cnt += w != 0;
       }
     }
-  });
+  };
+  for_span<T, V>(a, r, take);
   sum = wave_sum(sum);
   const u64 c = wave_sum((u64)cnt);
   if ((threadIdx.x & 63) == 0) ls[threadIdx.x >> 6] = sum, lc[threadIdx.x >> 6] = (uint32_t)c;
@@ -378,15 +437,17 @@ __global__ __launch_bounds__(kSampThreads) void sample_cut_kernel(SampleArgs a) 
 
 constexpr int kPickList = 2048;  // keys of the list that are held in LDS
 constexpr int kPickWave = 2048;  // ... that one wave looks through
+constexpr int kPickFew = 256;    // ... whose ranks are counted
 
 struct PickLds {
-  u64 sum[256];
+  u64 sum[256], rank[256];
   uint32_t cnt[256];
   u64 key_and, key_or, base, weight, found;
   int64_t left;
   uint32_t one;
   u64 scan[kPickThreads / 64];
   u64 chunk[kPickThreads];
+  u64 few_p[256], few_k[256];
   u64 keys[kPickList], weights[kPickList];  // (weights: in the low 48 bits, the bin above)
 };
 
@@ -439,12 +500,12 @@ struct PickKeys {
   }
 };
 
-// The key at which the kept ids end: the `left`-th smallest (BY_COUNT), or the last one
+// The key at which the kept ids end: the `left`-th smallest (by_count), or the last one
 // whose weights before it, from `base` on, are below `limit`.  Each step splits the keys
 // that are left by the 8 highest bits in which they differ and goes on with one part.
 // *upto: base and the weights up to it.  By the whole workgroup or by its first wave.
-template <bool BY_COUNT, int THREADS>
-__device__ u64 pick_end(const PickKeys &k, int64_t left, u64 base, double limit, PickLds &l, u64 *upto) {
+template <int THREADS>
+__device__ __forceinline__ u64 pick_end(const PickKeys &k, bool by_count, int64_t left, u64 base, double limit, PickLds &l, u64 *upto) {
   u64 fixed = 0, value = 0;  // bits that are decided, and what they are
   const int tid = threadIdx.x;
   auto meet = [] {
@@ -493,7 +554,7 @@ __device__ u64 pick_end(const PickKeys &k, int64_t left, u64 base, double limit,
       uint32_t size = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (c[i] && (BY_COUNT ? cb < left : (double)before < limit)) part = 4 * tid + i, at = before, cat = cb, size = c[i];
+        if (c[i] && (by_count ? cb < left : (double)before < limit)) part = 4 * tid + i, at = before, cat = cb, size = c[i];
         before += s[i], cb += c[i];
       }
       const u64 any = __ballot(part >= 0);
@@ -523,14 +584,62 @@ __device__ u64 pick_end(const PickKeys &k, int64_t left, u64 base, double limit,
 // The key at which a row's kept ids end.
 template <int THREADS>
 __device__ __forceinline__ u64 pick_last(const RowRule &q, const RowCut &cut, PickKeys k, PickLds &l) {
-  u64 all = cut.k_before, end = ~0ull, unused;
-  if (cut.k_bin < kSampBins) {
-    k.lo = k.hi = cut.k_bin;
-    end = pick_end<true, THREADS>(k, cut.k_left, cut.k_before, 0.0, l, &all);
+  u64 all = cut.k_before, end = ~0ull;
+  // (one loop for k and for p: code that runs once costs its fetch)
+#pragma unroll 1
+  for (int step = 0; step < 2; ++step) {
+    const bool by_k = step == 0;
+    if (by_k ? cut.k_bin >= kSampBins : !q.by_p) continue;
+    k.lo = by_k ? cut.k_bin : cut.p_lo, k.hi = by_k ? cut.k_bin : cut.p_hi;
+    end = pick_end<THREADS>(k, by_k, cut.k_left, by_k ? cut.k_before : cut.p_before, q.p * (double)all, l, &all);
   }
-  if (!q.by_p) return end;
-  k.lo = cut.p_lo, k.hi = cut.p_hi;
-  return pick_end<false, THREADS>(k, 0, cut.p_before, q.p * (double)all, l, &unused);
+  return end;
+}
+
+// The same where the keys are few: every key against every other.
+__device__ __forceinline__ u64 pick_few(const RowRule &q, const RowCut &cut, const PickKeys &k, PickLds &l) {
+  static_assert(kPickFew == 256 && kPickThreads % 256 == 0, "");
+  constexpr u64 kOne = 1ull << 50;  // (256 weights sum to less)
+  const int tid = threadIdx.x, i = tid & 255;
+  const int n = (int)k.n;
+  if (tid < 256) {
+    u64 p = 0, of_k = 0;
+    if (tid < n) {
+      const u64 both = l.weights[tid], w = both & ((1ull << 48) - 1);
+      const int b = (int)(both >> 48);
+      p = b >= cut.p_lo && b <= cut.p_hi ? w : 0;
+      of_k = b == cut.k_bin ? w | kOne : 0;
+    }
+    l.few_p[tid] = p, l.few_k[tid] = of_k, l.sum[tid] = 0, l.rank[tid] = 0;
+  }
+  if (tid == 0) l.base = cut.k_before, l.found = ~0ull, l.weight = 0;
+  __syncthreads();
+  const u64 key = i < n ? l.keys[i] : 0;
+  const bool by_k = cut.k_bin < kSampBins;
+  if (i < n) {
+    u64 p = 0, of_k = 0;
+    if (by_k) {
+      for (int j = tid >> 8; j < n; j += kPickThreads / 256) {
+        const bool less = l.keys[j] < key;
+        p += less ? l.few_p[j] : 0, of_k += less ? l.few_k[j] : 0;
+      }
+      atomicAdd(&l.rank[i], of_k);
+    } else {
+      for (int j = tid >> 8; j < n; j += kPickThreads / 256) p += l.keys[j] < key ? l.few_p[j] : 0;
+    }
+    atomicAdd(&l.sum[i], p);
+  }
+  __syncthreads();
+  if (by_k) {
+    if (tid < n && l.few_k[tid] && (int64_t)(l.rank[tid] / kOne) == cut.k_left - 1)
+      l.found = key, l.base = cut.k_before + ((l.rank[tid] + l.few_k[tid]) & (kOne - 1));
+    __syncthreads();
+  }
+  if (!q.by_p) return l.found;
+  const double limit = q.p * (double)l.base;
+  if (tid < n && l.few_p[tid] && (double)(cut.p_before + l.sum[tid]) < limit) atomicMax(&l.weight, key);
+  __syncthreads();
+  return l.weight;
 }
 
 template <typename T>
@@ -544,6 +653,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   const uint32_t ccnt = mine_there ? a.ccnt[(int64_t)r * a.chunks + tid] : 0, n = a.n_list[r];
   const RowCut cut = a.cuts[r];
   const RowRule q = row_rule(a, r);
+  const double u = (double)fmaxf(a.u[r], 0.0f);
   int32_t id;
   const float top = row_max(a, r, &id);
   if (q.first || !(top > -INFINITY)) {
@@ -570,7 +680,9 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
       k.list = l.keys, k.weights = l.weights;
     }
     __syncthreads();
-    if (n <= kPickWave) {
+    if (n <= kPickFew) {
+      last = pick_few(q, cut, k, l);
+    } else if (n <= kPickWave) {
       if (tid < 64) {
         const u64 end = pick_last<64>(q, cut, k, l);
         if (tid == 0) end_lds = end;
@@ -594,7 +706,6 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   const u64 mine = tid < a.chunks ? l.chunk[tid] : 0, before = pick_scan(mine, l.scan, &total);
   if (tid == 0) l.found = 0, l.base = 0;
   (void)pick_scan(kept, l.scan, &count);
-  const double u = (double)fmaxf(a.u[r], 0.0f);
   u64 at = (u64)fmin(u * (double)total, 0x1p63);
   at = at < total ? at : total - 1;
   if (at >= before && at < before + mine) l.found = (u64)tid, l.base = before;
@@ -635,17 +746,17 @@ template <typename T, int V>
 __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) {
   constexpr int kWaves = kPickThreads / 64;
   __shared__ PickLds l;
-  __shared__ u64 hs[kSampBins];
-  __shared__ uint32_t hc[kSampBins];
+  __shared__ u64 hs[kSampBinsAll];
+  __shared__ uint32_t hc[kSampBinsAll];
   __shared__ RowCut cut;
   __shared__ float wave_top[kWaves];
   __shared__ int32_t wave_id[kWaves];
   __shared__ u64 end_lds, wave_sum_lds[kWaves];
   __shared__ uint32_t n_keys, n_sure;
-  const int r = blockIdx.x, tid = threadIdx.x, w = tid >> 6;
+  const int r = blockIdx.x, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const T *row = (const T *)a.logits + (int64_t)r * a.stride;
-  const int64_t share = ((a.vocab + kWaves - 1) / kWaves + 7) / 8 * 8;  // ids of a wave
-  const int64_t lo = w * share < a.vocab ? w * share : a.vocab, hi = lo + share < a.vocab ? lo + share : a.vocab;
+  const int vocab = (int)a.vocab, share = ((vocab + kWaves - 1) / kWaves + 7) / 8 * 8;  // ids of a wave
+  const int lo = min(w * share, vocab), hi = min(lo + share, vocab);
   const RowRule q = row_rule(a, r);
   for (int b = tid; b < kSampBins; b += kPickThreads) hs[b] = 0, hc[b] = 0;
   if (tid == 0) n_keys = 0, n_sure = 0;
@@ -678,19 +789,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
   }
   int sure = kSampBins, maybe = -1, k_bin = -1;
   if (q.by_k || q.by_p) {
-    for_range<T, V>(row, lo, hi, [&](float x, uint32_t) {
-      const float z = below(x, top, q.inv_t);
-      if (!(z > -30.0f)) return;
-      const int b = bin_of(z);
-      if (q.by_p) {
-        const u64 wt = weight_of(share_of(z));
-        if (!wt) return;
-        atomicAdd(&hs[b], wt);
-        if (q.by_k) atomicAdd(&hc[b], 1u);
-      } else if (weighs(z)) {
-        atomicAdd(&hc[b], 1u);
-      }
-    });
+    with_bins(q, top, hs, hc, [&](auto f) { for_range<T, V>(row, lo, hi, f); });
     __syncthreads();
     row_cut(q, [&](int b) { return hs[b]; }, [&](int b) { return hc[b]; }, l.scan, l.cnt, &cut);
     k_bin = cut.k_bin;
@@ -701,9 +800,10 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
   u64 *list = a.list + (int64_t)r * a.vocab;
   u64 sum = 0;
   uint32_t cnt = 0;
-  for_range<T, V>(row, lo, hi, [&](float x, uint32_t i) {
+  const float least = least_z(q, max(sure, max(maybe, k_bin) + 1));
+  auto take = [&](float x, uint32_t i) {
     const float z = below(x, top, q.inv_t);
-    if (!(z > -30.0f)) return;
+    if (!(z > least)) return;
     const int b = bin_of(z);
     const bool listed = ((b >= sure) & (b <= maybe)) | (b == k_bin);
     if (b < sure || listed) {
@@ -718,7 +818,8 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
         sum += wt, cnt += wt != 0;
       }
     }
-  });
+  };
+  for_range<T, V>(row, lo, hi, take);
   sum = wave_sum(sum);
   const u64 c = wave_sum((u64)cnt);
   if ((tid & 63) == 0) wave_sum_lds[w] = sum, atomicAdd(&n_sure, (uint32_t)c);
@@ -734,7 +835,9 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
       for (uint32_t i = tid; i < kPickList; i += kPickThreads) list[i] = l.keys[i];
     }
     __syncthreads();
-    if (n <= kPickWave) {
+    if (n <= kPickFew) {
+      last = pick_few(q, cut, k, l);
+    } else if (n <= kPickWave) {
       if (tid < 64) {
         const u64 end = pick_last<64>(q, cut, k, l);
         if (tid == 0) end_lds = end;
@@ -764,18 +867,17 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
   u64 base = 0;
   int from = 0;
   for (; from < kWaves - 1 && at >= base + wave_sum_lds[from]; ++from) base += wave_sum_lds[from];
-  const int64_t per = (share + kPickThreads - 1) / kPickThreads;
-  const int64_t t0 = from * share + tid * per, s_end = (from + 1) * share < a.vocab ? (from + 1) * share : a.vocab;
-  const int64_t t1 = t0 + per < s_end ? t0 + per : s_end;
-  auto weight_at = [&](int64_t i) -> u64 {
+  const int per = (share + kPickThreads - 1) / kPickThreads;
+  const int t0 = from * share + tid * per, t1 = min(t0 + per, min((from + 1) * share, vocab));
+  auto weight_at = [&](int i) -> u64 {
     const float x = Elem<T>::get(row + i), sh = share_of(below(x, top, q.inv_t));
     return sh >= q.min_p && key_of(x, (uint32_t)i) <= last ? weight_of(sh) : 0;
   };
   u64 own = 0, unused;
-  for (int64_t i = t0; i < t1; ++i) own += weight_at(i);
+  for (int i = t0; i < t1; ++i) own += weight_at(i);
   u64 x = base + pick_scan(own, l.scan, &unused);
   if (at < x || at >= x + own) return;
-  for (int64_t i = t0; i < t1; ++i) {
+  for (int i = t0; i < t1; ++i) {
     const u64 wt = weight_at(i);
     if (at < x + wt) {
       a.tokens[r] = (int32_t)i;

@@ -346,11 +346,11 @@ size_t sample_layout(char *base, int64_t n, int64_t vocab, SampleScratch *out) {
 }
 
 // One launch, a workgroup a row, or four over chunks of the rows.  Measured (us, rows of
-// bf16): 1 x 8000 13.4, 23.5; 1 x 32000 30.5, 24.2; 64 x 8000 21.5, 36.0; 64 x 32000 48.4,
-// 41.2; 256 x 64000 74.0, 75.9; 256 x 128256 120.5, 112.4: about 17 + 0.75 for 1000 ids of
-// each round over the compute units, and 33 + 2.4 for a million ids of all rows.
+// bf16): 1 x 8000 11.2, 21.0; 1 x 32000 19.0, 21.7; 1 x 64000 29.1, 22.6; 64 x 8000 16.5, 30.4;
+// 64 x 32000 32.4, 38.7; 64 x 64000 50.9, 43.1; 256 x 128256 96.3, 102.2: about 0.5 for 1000 ids
+// of each round over the compute units, and 16 + 2.3 for a million ids of all rows.
 bool sample_by_rows(int64_t n, int64_t vocab) {
-  return 0.75e-3 * vocab * std::max(1.0, n / 256.0) < 16.0 + 2.4e-6 * n * vocab;
+  return 0.5e-3 * vocab * std::max(1.0, n / 256.0) < 16.0 + 2.3e-6 * n * vocab;
 }
 
 // Rows of a pass: their lists are as long as the vocabulary.
