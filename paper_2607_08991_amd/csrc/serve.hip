@@ -175,17 +175,19 @@ int run_rope(sats::RopeArgs a, int esz, bool append, hipStream_t stream) {
 // The split of a launch: row tiles of R rows, their number at most, and over how many
 // workgroups a tile's blocks of `keys` keys go.
 struct AttendPlan {
-  int tiles, splits, per_split;
+  int64_t tiles;
+  int splits, per_split;
 };
 AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, int64_t max_q) {
   const sats::BatchView &b = a.batch;
   const int64_t per_seq = (max_q * a.group + R - 1) / R;
   AttendPlan p;
-  p.tiles = (int)std::min<int64_t>(b.n_seqs * per_seq, b.n_tokens * a.group / R + b.n_seqs);
+  p.tiles = b.n_tokens * a.group / R + b.n_seqs;
+  if (b.n_seqs && per_seq <= p.tiles / b.n_seqs) p.tiles = b.n_seqs * per_seq;
   int64_t range = std::min<int64_t>(b.max_kv, b.max_pages << a.pool.shift);  // keys that a tile can see
   if (a.window) range = std::min(range, a.window + R / a.group + 1 + a.sinks + 2 * keys);
   const int64_t blocks = std::max<int64_t>(1, (range + keys - 1) / keys + 1);
-  const int64_t wgs = std::max<int64_t>(1, (int64_t)p.tiles * a.pool.n_kv);
+  const int64_t wgs = std::max<int64_t>(1, p.tiles * a.pool.n_kv);
   int64_t slots = a.dim > 128 ? kSlots / 2 : kSlots;
   if (R == 16 && a.dim <= 96) slots = kSlots * 3 / 2;
   int64_t want = std::max<int64_t>(1, slots / wgs);
@@ -201,9 +203,9 @@ size_t attend_bytes(const AttendPlan &p, int R, int n_kv, int dim) {
 
 template <typename T, int R, typename Kernel>
 int launch_attention(sats::AttendArgs a, const AttendPlan &p, Kernel kernel, char *mem, hipStream_t stream) {
-  const int64_t grid_x = (int64_t)p.tiles * a.pool.n_kv;
+  const int64_t grid_x = p.tiles * a.pool.n_kv;
   if (grid_x > 0x7fffffff || p.splits > 65535) return fail(SATS_ERR_SHAPE, "too many rows for one call");
-  a.tiles = p.tiles, a.splits = p.splits, a.per_split = p.per_split;
+  a.tiles = (int)p.tiles, a.splits = p.splits, a.per_split = p.per_split;
   a.part = reinterpret_cast<float *>(mem);
   a.part_ml = a.part + grid_x * p.splits * R * a.dim;
   kernel<<<dim3((unsigned)grid_x, (unsigned)p.splits), 256, 0, stream>>>(a);
@@ -453,7 +455,8 @@ int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *c
   a.k = layer_of(cache->k, cache, layer), a.v = layer_of(cache->v, cache, layer);
   a.batch = batch_view(batch), a.pool = pool_view(cache);
   a.n_q = (int)n_q_heads, a.group = (int)(n_q_heads / cache->n_kv_heads), a.dim = (int)cache->head_dim;
-  a.scale = scale, a.window = window, a.sinks = n_sinks;
+  // (places are below 2^31)
+  a.scale = scale, a.window = std::min(window, (int64_t)1 << 31), a.sinks = std::min(n_sinks, (int64_t)1 << 31);
   if (batch->max_q_len == 0) return SATS_OK;
   return esz == 2 ? run_attention<uint16_t>(a, stream) : run_attention<float>(a, stream);
 }

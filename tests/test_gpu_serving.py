@@ -286,6 +286,14 @@ def test_attention(sats, dtype, shape):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window,sinks", [((1 << 63) - 1, 0), ((1 << 63) - 1, (1 << 63) - 1), (1 << 31, 3), (5, 1 << 40)])
+def test_windows_past_every_length(sats, dtype, window, sinks):
+    b = Batch(sats, dt_of(dtype), [70, 1, 40], [900, 3000, 40], 4, 2, 64, 16, seed=9)
+    out, lse, scale = run_attention(sats, b, dt_of(dtype), window=window, sinks=sinks)
+    check_attention(b, out, lse, 1, scale, window, sinks, dtype, set(range(0, 110, 13)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("q_len,kv_len,window,sinks", [([1], [77], 0, 0), ([70, 1, 3], [77, 200, 131], 0, 0),
                                                        ([1, 40], [500, 300], 60, 3)])
 def test_what_is_not_seen_may_hold_anything(sats, dtype, q_len, kv_len, window, sinks):

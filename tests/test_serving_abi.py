@@ -58,6 +58,7 @@ def attend(no_cache=False, no_batch=False, **kw):
     (ARG, dict(n_tokens=1, q=P + 2)), (ARG, dict(n_tokens=1, out=BIG + 4)), (ARG, dict(n_tokens=1, q_stride=257)),
     (ARG, dict(n_tokens=1, out=P + 16)), (ARG, dict(n_tokens=1, k=BIG)), (ARG, dict(n_tokens=1, v=BIG + 256)),
     (SHAPE, dict(n_tokens=1 << 29, max_q_len=1 << 29, heads=16, q_stride=1024, q=BIG << 4, out=BIG << 8)),
+    (SHAPE, dict(n_tokens=1 << 30, n_seqs=1 << 30, max_q_len=1 << 29, out=BIG << 8)),
     (SHAPE, dict(page_size=0)), (SHAPE, dict(page_size=24)), (SHAPE, dict(page_size=8192)), (SHAPE, dict(head_dim=0)),
     (SHAPE, dict(head_dim=12)), (SHAPE, dict(head_dim=264)), (SHAPE, dict(n_pages=0)), (SHAPE, dict(n_kv_heads=0)),
     (SHAPE, dict(n_layers=0)), (SHAPE, dict(layer=2)), (SHAPE, dict(layer=-1)), (SHAPE, dict(heads=3)),
