@@ -5,7 +5,12 @@
 // ones in ascending order, so what a call does follows from the state alone.  The plan of
 // a call (which items are sound, how many pages they need, which ones they get) is made
 // by one workgroup: it is a prefix sum over a few thousand numbers, and a second
-// kernel over the whole chip moves the data and writes the table rows.
+// kernel over the whole chip moves the data, and writes the table rows of a fork and the
+// numbers that a compaction changes.
+//
+// The plans are latency: 256 extensions 8.5 us (15 us the call, with the free before it), 64
+// forks 6.5, a compaction of 768 pages 8.7.  The moves are a copy: 64 pages of 2 MB 34 us (part
+// pages: 128 MB read and written), 805 MB of a compaction 155 us, 5.2 TB/s.
 #pragma once
 
 #include "paged.hpp"

@@ -7,6 +7,10 @@
 // Both in float32 on registers, rounded once.  A row (a token's head) is held by
 // `lanes` lanes, each with V elements and the V that they are rotated with, so that the
 // rotation moves nothing between lanes and the mean square is a sum over `lanes` lanes.
+//
+// Bound by memory where there are tokens: 4096 of 32 + 8 + 8 heads of 128 with norms (bf16,
+// 102.8 MB in and out) take 23.2 us, 4.4 TB/s, where a large copy reaches 4.9.  One token is
+// the launch: 3.8 us of kernel in 11.2 us of a call from Python.
 #pragma once
 
 #include "elem.hpp"

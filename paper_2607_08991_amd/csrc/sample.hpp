@@ -20,7 +20,14 @@
 //   cut     the ids of those bins go to a list, the weights of the bins before them to a
 //           sum per chunk;
 //   pick    a workgroup per row: k and p end at an element of the list, found by its
-//           (logit, id) key 8 bits at a time; then the chunk, then the id, of the draw.
+//           (logit, id) key against the others, or 8 bits at a time where the list is long;
+//           then the chunk, then the id, of the draw.
+//
+// The logits are read four times, from the caches after the first.  64 rows of 128256 float32
+// (32.8 MB) take 54.6 us: max 8.5 (3.9 TB/s), hist 17.5, cut 14.2, pick 17.  hist is 31 vector
+// instructions an id, a third of its time, and waits for the rest: the chain of a row's
+// maximum, its bins and its last workgroup.  One row is latency and the fetch of code that
+// runs once: 128256 bf16 21.2 us in four launches, 2000 10.9 in one.
 #pragma once
 
 #include "elem.hpp"

@@ -38,8 +38,8 @@ constexpr int64_t kRopeWaves = 4096;
 // Parts up to which one wave joins a row.
 constexpr int kJoinWave = 16;
 // Attention: workgroups that the chip holds at once (two a compute unit; of the kernels for
-// heads above 128 one, of the 16-row kernels for heads up to 96 three), which a launch that splits its tiles aims at: a few more would wait
-// for a second round.  8 sequences of 2000 to 6000 keys: 512 workgroups 30.8 us, 768 38.1.
+// heads above 128 one, of the 16-row kernels for heads up to 96 three), which a launch that
+// splits its tiles aims at: a few more would wait for a second round.  8 sequences of 2000 to 6000 keys: 512 workgroups 30.8 us, 768 38.1.
 // Tiles of 16 rows whose parts stay at kLongBlocks blocks or more are split over up to
 // kSlotsLong workgroups, since sequences of different lengths then share the chip more
 // evenly (64 sequences of 500 to 8000 keys 156 -> 150 us).
