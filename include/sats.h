@@ -455,7 +455,8 @@ int sats_qkv_append(const void *q, int64_t q_stride, const void *k, int64_t k_st
  * elements a token; out the same, dense; lse [n_tokens][n_q_heads] (float32, or
  * NULL) the logarithm of the sum of exp(scale q . k_j).  A token that sees
  * nothing gives zeros and -inf.  What a key that is not seen holds (NaN,
- * infinities) does not matter.  q, out and rows of q on 16 bytes.
+ * infinities) does not matter.  q, out and rows of q on 16 bytes; q, out, lse and
+ * the cache must not overlap.
  */
 int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *cache, int64_t layer,
                          const sats_kv_batch *batch, int64_t n_q_heads, float scale, int64_t window, int64_t n_sinks,

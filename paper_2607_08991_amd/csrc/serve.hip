@@ -448,6 +448,10 @@ int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *c
   if (!on16(q) || !on16(out) || q_stride * esz % 16) return fail(SATS_ERR_ARG, "q, out and the rows of q must be 16-byte aligned");
   if (overlap(out, n * row * esz, q, span(n, q_stride, row, esz)) || in_cache(out, n * row * esz, cache))
     return fail(SATS_ERR_ARG, "out overlaps q or the cache");
+  const int64_t lse_bytes = lse ? n * n_q_heads * (int64_t)sizeof(float) : 0;
+  if (reinterpret_cast<uintptr_t>(lse) % sizeof(float) || overlap(lse, lse_bytes, q, span(n, q_stride, row, esz)) ||
+      overlap(lse, lse_bytes, out, n * row * esz) || in_cache(lse, lse_bytes, cache))
+    return fail(SATS_ERR_ARG, "lse must be 4-byte aligned, apart from q, out and the cache");
   if (std::min(batch->max_q_len, n) * (n_q_heads / cache->n_kv_heads) > 0x7fffff00)
     return fail(SATS_ERR_SHAPE, "too many rows for one call");
   sats::AttendArgs a{};

@@ -71,6 +71,15 @@ def test_attention_refuses(want, kw):
     assert bool(sats.sats_last_error()) == (want != OK)
 
 
+@pytest.mark.parametrize("lse", [BIG, BIG + 508, BIG - 12, P, P + 508, 4 * P + 8, 8 * P + 2])
+def test_attention_refuses_an_lse_over_its_arrays(lse):
+    """One token of 4 heads of 64 bf16: q at P and out at BIG take 512 bytes, the sums 16."""
+    kw = dict(n_tokens=1, k=4 * P, v=6 * P, max_q_len=0)
+    assert attend(lse=lse, **kw) == ARG and "lse" in sats.sats_last_error()
+    for apart in (None, BIG + 512, BIG - 16, P + 512, P - 16, 8 * P):
+        assert attend(lse=apart, **kw) == OK, sats.sats_last_error()
+
+
 def append(no_cache=False, no_batch=False, **kw):
     a = dict(q=P, qs=256, k=2 * P, ks=128, v=3 * P, vs=128, qn=None, kn=None, eps=1e-6, rope=P, n_pos=5, pos=None,
              out=BIG, os=256, layer=0, heads=4, rot=64, pairs=0)
