@@ -241,10 +241,13 @@ template <typename T> struct RowsOf {
   static constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;  // keys of a block
 };
 
-// FULL: heads of DT dims; else products of dims that a head has not are passed over.
+// FULL: heads of DT dims.  Else every load leaves out the dims that a head has not (they are the
+// next slot's, or lie behind the cache), and up to DT = 128 the products do too.  Of 256 they
+// multiply zeros there: leaving them out spills 989 registers (bf16; 683 float32), all of them none.
 template <typename T, int DT, bool FULL>
 __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_rows_kernel(AttendArgs a) {
   constexpr int kKeys = RowsOf<T>::kKeys, kVec = Elem<T>::kVec, kRow = DT * (int)sizeof(T), kChunks = kRow / 16;
+  constexpr bool kSkip = !FULL && DT <= 128;
   constexpr int kTiles = kKeys / 16, kSteps = kChunks / 4, kLoads = kKeys * kChunks / 64, kOut = DT / 16;
   // V's rows lie a little apart, so that the rows that are read together (bf16: 32 bytes of 8
   // rows; float32: 64 bytes of 4 rows, 4 apart) are in different banks
@@ -353,7 +356,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
       s[kt] = f32x4{0, 0, 0, 0};
 #pragma unroll
       for (int st = 0; st < kSteps; ++st) {
-        if (!FULL && st * 4 * kVec >= a.dim) break;
+        if (kSkip && st * 4 * kVec >= a.dim) break;
         if constexpr (sizeof(T) == 2) {
           s[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kr[kt * kSteps + st]),
                                                           __builtin_bit_cast(bf16x8_t, qv[st]), s[kt], 0, 0, 0);
@@ -425,7 +428,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
         for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[e >> 2][e & 3];
 #pragma unroll
         for (int o = 0; o < kOut; ++o) {
-          if (!FULL && 16 * o >= a.dim) break;
+          if (kSkip && 16 * o >= a.dim) break;
           i16x4_t v2[2];
 #pragma unroll
           for (int kt = 0; kt < 2; ++kt) {
@@ -440,7 +443,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
       } else {
 #pragma unroll
         for (int o = 0; o < kOut; ++o) {
-          if (!FULL && 16 * o >= a.dim) break;
+          if (kSkip && 16 * o >= a.dim) break;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float v = *reinterpret_cast<const float *>(mine + (4 * g + i) * kPitch + (16 * o + row) * 4);

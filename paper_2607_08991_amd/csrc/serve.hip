@@ -217,13 +217,15 @@ int launch_attention(sats::AttendArgs a, const AttendPlan &p, Kernel kernel, cha
   return launched("attend_join_kernel");
 }
 
+// The second argument is true for heads of exactly the first one's dims only: such a kernel
+// loads rows of that width.
 typedef void (*AttendKernel)(sats::AttendArgs);
 template <typename T> AttendKernel rows_kernel(int dim) {
   using namespace sats;
   return dim <= 64    ? (dim == 64 ? attend_rows_kernel<T, 64, true> : attend_rows_kernel<T, 64, false>)
          : dim <= 96  ? (dim == 96 ? attend_rows_kernel<T, 96, true> : attend_rows_kernel<T, 96, false>)
          : dim <= 128 ? (dim == 128 ? attend_rows_kernel<T, 128, true> : attend_rows_kernel<T, 128, false>)
-                      : attend_rows_kernel<T, 256, true>;  // (passing dims over costs it its registers)
+                      : (dim == 256 ? attend_rows_kernel<T, 256, true> : attend_rows_kernel<T, 256, false>);
 }
 AttendKernel tile_kernel(int dim) {
   using namespace sats;

@@ -749,3 +749,34 @@ def test_sampling_more_rows_than_a_pass(sats):
         want = ref.sample(f64(x[n - 1]), shares_of(x[n - 1:], torch.ones(1, device="cuda")).cpu().numpy()[0],
                           float(u[n - 1]), top_k=40, top_p=float(p[n - 1]))
         assert int(tok[n - 1]) == want[0] and int(kept[n - 1]) == want[2]
+
+
+# ------------------------------------------------------------------ heads of every width
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [4, 16, 64])
+@pytest.mark.parametrize("dim", [8, 24, 72, 80, 96, 104, 120, 136, 160, 192, 248, 256])
+def test_heads_of_every_width_read_their_own_rows(sats, dtype, dim, page):
+    """Single tokens, short and long chunks together and a chunk alone, over a cache with NaN behind
+    its last slot, in every slot that nobody sees and then infinities in all of the next head."""
+    dt = dt_of(dtype)
+    for q_len, kv_len, window, sinks in (([1], [64], 0, 0), ([1, 3, 1, 40, 2], [2 * 64, 70, 1, 64, 200], 0, 0),
+                                         ([50], [128], 0, 0), ([1, 20], [300, 150], 60, 3)):
+        b = Batch(sats, dt, q_len, kv_len, 4, 2, dim, page, seed=dim + page, spare=0)
+        for name in ("k", "v"):
+            x = getattr(b, name)
+            flat = torch.full((x.numel() + 2048,), math.nan, dtype=dt, device="cuda")
+            setattr(b, name, flat[:x.numel()].view(x.shape).copy_(x))
+        used = torch.zeros(b.k.shape[1], page, dtype=torch.bool)
+        for s, n in enumerate(kv_len):
+            for j in range(n):
+                used[b.rows[s][j // page], j % page] = True
+        for pool in (b.k, b.v):
+            pool.permute(1, 3, 0, 2, 4)[~used.cuda()] = math.nan
+        b.cache = sats.KVCache(b.k, b.v)
+        out, lse, scale = run_attention(sats, b, dt, window=window, sinks=sinks)
+        check_attention(b, out, lse, 1, scale, window, sinks, dtype, {0, 1, 33})
+        for pool in (b.k, b.v):
+            pool[:, :, 1] = math.inf
+        got, got_lse, _ = run_attention(sats, b, dt, window=window, sinks=sinks)
+        assert torch.equal(got[:, :2], out[:, :2]) and torch.equal(got_lse[:, :2], lse[:, :2])

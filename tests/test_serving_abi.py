@@ -266,3 +266,24 @@ print(json.dumps(out))""")
     assert kinds[0] == ["rows", "join"] and kinds[1] == ["rows", "join"] and kinds[2] == ["rows"]
     assert kinds[3] == ["tile"] and kinds[4][0] == "rows" and "tile" in kinds[4]
     assert kinds[5] == ["tile", "join"] and kinds[6][0] == "rows" and "tile" not in kinds[6]
+
+
+def test_kernels_of_whole_heads_are_for_heads_of_their_width(run):
+    """The instances that load whole rows (second argument true) read DT dims of each key: a narrower
+    head's rows would run into the next slot, or past the cache's end."""
+    import re
+    got = run("""
+out = []
+for dim in range(8, 257, 8):
+    for esz in (2, 4):
+        for a in ((3, 3, 1, 100), (1, 200, 200, 300), (4, 200, 180, 300)):
+            assert attend(*a, dim=dim, esz=esz) == 0
+            out += [[dim, esz, n] for n in launches(log()) if "join" not in n]
+print(json.dumps(out))""")
+    kinds = set()
+    for dim, esz, name in got:
+        width, whole = re.search(r"attend_(?:rows|tile)_kernelI.*?Li(\d+)ELb([01])E", name).groups()
+        assert int(width) >= dim and (whole == "0" or int(width) == dim), (dim, esz, name)
+        kinds.add((width, whole, "rows" in name))
+    assert {w for w, _, rows in kinds if rows} == {"64", "96", "128", "256"}
+    assert {w for w, _, rows in kinds if not rows} == {"64", "128", "256"}
