@@ -60,7 +60,11 @@
  * (see sats_reserve), with results that agree within rounding.
  *
  * Concurrency: calls on different streams use different workspaces and may
- * overlap.  Calls on one stream are ordered by the stream.
+ * overlap.  Calls on one stream are ordered by the stream; they may come from
+ * several threads, each call's work is enqueued as a whole.  A graph that
+ * recorded a call uses the workspace of the stream it was recorded on: a
+ * replay must not overlap that stream's calls, nor replays of other graphs
+ * recorded there.
  */
 #ifndef SATS_H
 #define SATS_H
@@ -527,8 +531,9 @@ int sats_reserve_serving(int64_t max_items, int64_t n_pages, int64_t max_rows, i
                          hipStream_t stream);
 
 /* Free every workspace of the calling process, and the kept buffers of the
- * routing-table construction and of the calibration (synchronises each
- * device). */
+ * routing-table construction and of the calibration (waits for calls that
+ * other threads are issuing, and synchronises each device).  Graphs that
+ * recorded a call of the library must not be replayed afterwards. */
 int sats_release(void);
 
 /* Thread-local text of the last error returned on this thread ("" if none). */

@@ -5,6 +5,8 @@
 
 #include <stddef.h>
 
+#include <mutex>
+
 #include "../../include/sats.h"
 
 namespace sats_host {
@@ -16,10 +18,15 @@ void clear_error();
 // Compute units of the current device (0 on an error).
 int device_cus();
 
-// The serving operators' scratch memory of (current device, stream): at least `bytes`,
-// grown where it is smaller (SATS_ERR_WORKSPACE under stream capture or for want of
-// memory; what is there then stays).
-int serve_workspace(hipStream_t stream, size_t bytes, char **mem);
+// Calls on one stream may come from several threads, and a call is several launches that
+// hand each other results in the stream's workspace: a call holds the stream's turn from
+// before it looks at the workspace until its last launch is enqueued.
+typedef std::unique_lock<std::mutex> Turn;
+
+// Takes the turn of (current device, stream), and the serving operators' scratch memory
+// of it: at least `bytes`, grown where it is smaller (SATS_ERR_WORKSPACE under stream capture
+// or for want of memory; what is there then stays).
+int serve_workspace(hipStream_t stream, size_t bytes, char **mem, Turn *turn);
 
 }  // namespace sats_host
 

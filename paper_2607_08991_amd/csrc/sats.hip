@@ -506,8 +506,26 @@ struct Workspace {
 };
 constexpr size_t kPfCounterBytes = (kPfCounters * sizeof(unsigned) + 255) / 256 * 256;
 
+// Taken after a stream's turn where a call holds one.
 std::mutex g_ws_mu;
 std::map<std::pair<int, hipStream_t>, Workspace> g_ws;
+
+// The streams' turns (host.hpp).  They stay when the workspaces go: a thread may be waiting for one.
+using sats_host::Turn;
+std::mutex g_turns_mu;
+std::map<std::pair<int, hipStream_t>, std::mutex> g_turns;
+
+int take_turn(hipStream_t stream, Turn *turn) {
+  int dev = 0;
+  HIP_TRY(hipGetDevice(&dev));
+  std::mutex *m;
+  {
+    std::lock_guard<std::mutex> lk(g_turns_mu);
+    m = &g_turns[{dev, stream}];
+  }
+  *turn = Turn(*m);
+  return SATS_OK;
+}
 
 // Whether the stream records a graph (or another does and forbids calls here).
 bool stream_captures(hipStream_t stream) {
@@ -1315,9 +1333,10 @@ int run_lora(const Call &c, bool vec_ok) {
     return fail(SATS_ERR_SHAPE, "LoRA: B_down slices of the second reduction stage do not fit LDS");
   const Plan p = make_plan(c.d, c.d_ff, esz, vec_ok, 1);
   const size_t bytes = layout(nullptr, p, 1, c.d, c.d_ff, esz, c.L, dp, nullptr);
+  Turn turn;
   Workspace *ws = nullptr;
-  int rc = ensure_workspace(c.stream, bytes, counter_count(p, 1, dp), &ws);
-  if (rc) return rc;
+  int rc = take_turn(c.stream, &turn);
+  if (rc || (rc = ensure_workspace(c.stream, bytes, counter_count(p, 1, dp), &ws))) return rc;
   Buffers b{};
   layout(ws->mem, p, 1, c.d, c.d_ff, esz, c.L, dp, &b);
   for (int64_t i = 0; i < c.n; ++i) {
@@ -1366,6 +1385,9 @@ int run(const Call &c) {
     if (rc) return rc;
     if (!lora_batched(c, esz, vec_ok)) return run_lora<T>(c, vec_ok);
   }
+  Turn turn;
+  int rc = c.noalloc ? SATS_OK : take_turn(c.stream, &turn);  // (the fixed array is no stream's)
+  if (rc) return rc;
   const int64_t lrank = c.Ag ? c.rank : 0;
   // single-token path: one token, vector layout, h fits the LDS copy
   bool decode = c.n == 1 && vec_d && g_opt.single_token != SATS_SINGLE_OFF;
@@ -1381,7 +1403,6 @@ int run(const Call &c) {
   }
   Workspace *ws = nullptr;
   Workspace fixed{};
-  int rc = 0;
   if (c.Ag ? lora_tiled(c, esz, vec_ok) : pf_ok(esz, vec_d, c.n, c.d, c.d_ff)) {
     const size_t need = pf_bytes(c.n, c.d, c.d_ff, esz, lrank);
     char *mem = nullptr;
@@ -2102,9 +2123,10 @@ int fail(int code, const char *fmt, ...) {
 void clear_error() { g_err.clear(); }
 int device_cus() { return ::device_cus(); }
 
-int serve_workspace(hipStream_t stream, size_t bytes, char **mem) try {
+int serve_workspace(hipStream_t stream, size_t bytes, char **mem, Turn *turn) try {
   int dev = 0, rc = 0;
   HIP_TRY(hipGetDevice(&dev));
+  if ((rc = take_turn(stream, turn))) return rc;
   std::lock_guard<std::mutex> lk(g_ws_mu);
   Workspace &w = g_ws[{dev, stream}];
   const bool capturing = stream_captures(stream);
@@ -2259,8 +2281,10 @@ int sats_reserve(int64_t max_tokens, int64_t d, int64_t d_ff, int64_t n_layers, 
                                        elem_bytes == 2 ? sats::kLoraMaxRank : 0));
         nc = std::max(nc, counter_count(p, pass, dp));
       }
+  Turn turn;
   Workspace *ws = nullptr;
-  int rc = ensure_workspace(stream, bytes, nc, &ws);
+  int rc = take_turn(stream, &turn);
+  if (!rc) rc = ensure_workspace(stream, bytes, nc, &ws);
   // the tiled products' buffers, whatever the options are now: up to 64 tokens and beyond
   for (const int64_t n : {std::min<int64_t>(max_tokens, kMaxPass), max_tokens})
     if (!rc && pf_shape(elem_bytes, true, n, d, d_ff)) rc = reserve_tiled(stream, n, d, d_ff, elem_bytes);
@@ -2269,20 +2293,26 @@ int sats_reserve(int64_t max_tokens, int64_t d, int64_t d_ff, int64_t n_layers, 
 
 int sats_release(void) {
   g_err.clear();
-  std::lock_guard<std::mutex> lk(g_ws_mu);
   int cur = 0;
   HIP_TRY(hipGetDevice(&cur));
-  for (auto &kv : g_ws) {
-    HIP_TRY(hipSetDevice(kv.first.first));
-    HIP_TRY(hipDeviceSynchronize());
-    if (kv.second.mem) HIP_TRY(hipFree(kv.second.mem));
-    if (kv.second.counters) HIP_TRY(hipFree(kv.second.counters));
-    for (const Workspace::Tiled &t : kv.second.tiled)
-      if (t.mem) HIP_TRY(hipFree(t.mem));
-    if (kv.second.serve) HIP_TRY(hipFree(kv.second.serve));
-    for (void *t : kv.second.kept) HIP_TRY(hipFree(t));
+  {
+    // every stream's turn: no call is about to launch on what goes
+    std::lock_guard<std::mutex> lt(g_turns_mu);
+    std::vector<Turn> turns;
+    for (auto &kv : g_turns) turns.emplace_back(kv.second);
+    std::lock_guard<std::mutex> lk(g_ws_mu);
+    for (auto &kv : g_ws) {
+      HIP_TRY(hipSetDevice(kv.first.first));
+      HIP_TRY(hipDeviceSynchronize());
+      if (kv.second.mem) HIP_TRY(hipFree(kv.second.mem));
+      if (kv.second.counters) HIP_TRY(hipFree(kv.second.counters));
+      for (const Workspace::Tiled &t : kv.second.tiled)
+        if (t.mem) HIP_TRY(hipFree(t.mem));
+      if (kv.second.serve) HIP_TRY(hipFree(kv.second.serve));
+      for (void *t : kv.second.kept) HIP_TRY(hipFree(t));
+    }
+    g_ws.clear();
   }
-  g_ws.clear();
   HIP_TRY(hipSetDevice(cur));
   int rc = route_release_all();
   if (!rc) rc = cal_release_all();
@@ -2377,6 +2407,8 @@ int sats_device_status(hipStream_t stream) {
   HIP_TRY(hipGetDevice(&dev));
   HIP_TRY(hipStreamSynchronize(stream));
   // the flags of this stream's workspace and of the device's allocation-free scratch
+  Turn turn;
+  if (const int rc = take_turn(stream, &turn)) return rc;
   std::vector<unsigned *> flags;
   {
     std::lock_guard<std::mutex> lk(g_ws_mu);

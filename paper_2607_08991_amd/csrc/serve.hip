@@ -16,6 +16,7 @@ namespace {
 
 using sats_host::clear_error;
 using sats_host::fail;
+using sats_host::Turn;
 
 bool on16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -247,7 +248,8 @@ template <typename T> int run_attention(sats::AttendArgs a, hipStream_t stream) 
   const size_t bytes = std::max(attend_bytes(small, 16, a.pool.n_kv, a.dim),
                                 attend_bytes(large, sats::kTileRows, a.pool.n_kv, a.dim));
   char *mem = nullptr;
-  int rc = bytes ? sats_host::serve_workspace(stream, bytes, &mem) : SATS_OK;
+  Turn turn;
+  int rc = bytes ? sats_host::serve_workspace(stream, bytes, &mem, &turn) : SATS_OK;
   if (rc) return rc;
   if (small.tiles) {
     a.small = 1, a.large = !bf16;
@@ -485,8 +487,9 @@ int sats_cache_extend(const sats_kv_cache *cache, const sats_kv_pages *pages, co
   if (rc || n == 0) return rc;
   if (!add) return fail(SATS_ERR_NULL, "add must be non-null");
   char *mem = nullptr;
+  Turn turn;
   PagesScratch s;
-  if ((rc = sats_host::serve_workspace(stream, pages_layout(nullptr, n, cache->n_pages, nullptr), &mem))) return rc;
+  if ((rc = sats_host::serve_workspace(stream, pages_layout(nullptr, n, cache->n_pages, nullptr), &mem, &turn))) return rc;
   pages_layout(mem, n, cache->n_pages, &s);
   sats::PagesArgs a = pages_args(cache, pages, seqs, add, n, &s);
   a.status = status;
@@ -502,8 +505,9 @@ int sats_cache_fork(const sats_kv_cache *cache, const sats_kv_pages *pages, cons
   if (rc || n == 0) return rc;
   if (!src || !dst) return fail(SATS_ERR_NULL, "src and dst must be non-null");
   char *mem = nullptr;
+  Turn turn;
   PagesScratch s;
-  if ((rc = sats_host::serve_workspace(stream, pages_layout(nullptr, n, cache->n_pages, nullptr), &mem))) return rc;
+  if ((rc = sats_host::serve_workspace(stream, pages_layout(nullptr, n, cache->n_pages, nullptr), &mem, &turn))) return rc;
   pages_layout(mem, n, cache->n_pages, &s);
   sats::PagesArgs a = pages_args(cache, pages, src, dst, n, &s);
   a.status = status;
@@ -517,8 +521,9 @@ int sats_cache_compact(const sats_kv_cache *cache, const sats_kv_pages *pages, i
   int rc = check_pages(cache, pages, 0, true);
   if (rc) return rc;
   char *mem = nullptr;
+  Turn turn;
   PagesScratch s;
-  if ((rc = sats_host::serve_workspace(stream, pages_layout(nullptr, 0, cache->n_pages, nullptr), &mem))) return rc;
+  if ((rc = sats_host::serve_workspace(stream, pages_layout(nullptr, 0, cache->n_pages, nullptr), &mem, &turn))) return rc;
   pages_layout(mem, 0, cache->n_pages, &s);
   sats::PagesArgs a = pages_args(cache, pages, nullptr, nullptr, 0, &s);
   a.n_used = n_used;
@@ -549,9 +554,10 @@ int sats_sample(const void *logits, int elem_bytes, int64_t stride, int64_t n, i
   if (!logits || !u || !tokens) return fail(SATS_ERR_NULL, "logits, u and tokens must be non-null");
   if (stride < vocab) return fail(SATS_ERR_SHAPE, "stride is below vocab");
   char *mem = nullptr;
+  Turn turn;
   SampleScratch s;
   const int64_t pass = std::min(n, kSampleRows);
-  int rc = sats_host::serve_workspace(stream, sample_layout(nullptr, pass, vocab, nullptr), &mem);
+  int rc = sats_host::serve_workspace(stream, sample_layout(nullptr, pass, vocab, nullptr), &mem, &turn);
   if (rc) return rc;
   sample_layout(mem, pass, vocab, &s);
   sats::SampleArgs a{};
@@ -589,7 +595,8 @@ int sats_reserve_serving(int64_t max_items, int64_t n_pages, int64_t max_rows, i
   if (n_pages) bytes = std::max(bytes, pages_layout(nullptr, max_items, n_pages, nullptr));
   if (max_rows && vocab) bytes = std::max(bytes, sample_layout(nullptr, std::min(max_rows, kSampleRows), vocab, nullptr));
   char *mem = nullptr;
-  return sats_host::serve_workspace(stream, bytes, &mem);
+  Turn turn;
+  return sats_host::serve_workspace(stream, bytes, &mem, &turn);
 }
 
 }  // extern "C"
