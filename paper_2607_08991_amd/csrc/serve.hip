@@ -33,6 +33,9 @@ struct Carve {
 };
 
 constexpr int64_t kMaxCount = (int64_t)1 << 30;
+// Workgroups of 256 threads in a row of a launch, at most: HIP takes less than 2^32 threads there.
+constexpr int64_t kMaxGrid = ((int64_t)1 << 24) - 1;
+static_assert(sats::kThreads == 256, "");
 
 // Rotation: waves that fill the chip.
 constexpr int64_t kRopeWaves = 4096;
@@ -163,7 +166,7 @@ int run_rope(sats::RopeArgs a, int esz, bool append, hipStream_t stream) {
   a.per = 1;
   while (a.per < 8 && a.per < a.rows && n * ((a.rows + a.per) / (a.per + 1)) * a.lanes >= kRopeWaves * 64) ++a.per;
   const int64_t groups = (a.rows + a.per - 1) / a.per, threads = n * groups * a.lanes;
-  if (threads > (int64_t)sats::kThreads * 0x7fffffff) return fail(SATS_ERR_SHAPE, "too many rows for one call");
+  if (threads > sats::kThreads * kMaxGrid) return fail(SATS_ERR_SHAPE, "too many rows for one call");
   const dim3 grid((unsigned)((threads + sats::kThreads - 1) / sats::kThreads));
   auto go = [&](auto fn) { fn<<<grid, sats::kThreads, 0, stream>>>(a); };
   if (esz == 2) wide ? go(sats::rope_kernel<uint16_t, 8, 1>) : go(sats::rope_kernel<uint16_t, 1, 2>);
@@ -205,7 +208,6 @@ size_t attend_bytes(const AttendPlan &p, int R, int n_kv, int dim) {
 template <typename T, int R, typename Kernel>
 int launch_attention(sats::AttendArgs a, const AttendPlan &p, Kernel kernel, char *mem, hipStream_t stream) {
   const int64_t grid_x = p.tiles * a.pool.n_kv;
-  if (grid_x > 0x7fffffff || p.splits > 65535) return fail(SATS_ERR_SHAPE, "too many rows for one call");
   a.tiles = (int)p.tiles, a.splits = p.splits, a.per_split = p.per_split;
   a.part = reinterpret_cast<float *>(mem);
   a.part_ml = a.part + grid_x * p.splits * R * a.dim;
@@ -245,6 +247,8 @@ template <typename T> int run_attention(sats::AttendArgs a, hipStream_t stream) 
     small = attend_plan(a, 16, sats::RowsOf<T>::kKeys, kRowsLeast, any_large ? 16 / a.group : a.batch.max_q);
   }
   if (any_large) large = attend_plan(a, sats::kTileRows, sats::kTileKeys, kTileLeast, a.batch.max_q);
+  for (const AttendPlan *p : {&small, &large})
+    if (p->tiles * a.pool.n_kv > kMaxGrid || p->splits > 65535) return fail(SATS_ERR_SHAPE, "too many rows for one call");
   const size_t bytes = std::max(attend_bytes(small, 16, a.pool.n_kv, a.dim),
                                 attend_bytes(large, sats::kTileRows, a.pool.n_kv, a.dim));
   char *mem = nullptr;
@@ -309,14 +313,21 @@ sats::PagesArgs pages_args(const sats_kv_cache *c, const sats_kv_pages *p, const
   return a;
 }
 
+// Workgroups that write `entries` of a table beside the moves of contents (kCopyGrid at most).
+// Whether the launch takes them is asked before the plan, which changes the pages' state.
+constexpr int64_t kCopyGrid = 8192;
+int64_t table_grid(int64_t entries) { return (entries + sats::kThreads - 1) / sats::kThreads; }
+int check_table(int64_t entries) {
+  return table_grid(entries) + kCopyGrid <= kMaxGrid ? SATS_OK : fail(SATS_ERR_SHAPE, "the page table is too large for one call");
+}
+
 // Moves of contents, and with them `entries` of the table (TABLE, t).
 template <int TABLE>
 int copy_pages(const sats_kv_cache *c, const int32_t *src, const int32_t *dst, const int32_t *valid, const int32_t *ctl,
                int64_t n, const sats::PagesArgs &t, int64_t entries, hipStream_t stream) {
-  const int64_t table = (entries + sats::kThreads - 1) / sats::kThreads;
+  const int64_t table = table_grid(entries);
   const int64_t waves = n * c->n_layers * 2 * c->n_kv_heads, per = sats::kThreads / 64;
-  const int64_t grid = std::clamp<int64_t>((waves + per - 1) / per, 1, 8192);
-  if (table + grid > 0x7fffffff) return fail(SATS_ERR_SHAPE, "the page table is too large");
+  const int64_t grid = std::clamp<int64_t>((waves + per - 1) / per, 1, kCopyGrid);
   sats::CopyArgs a{static_cast<char *>(c->k), static_cast<char *>(c->v), c->n_pages, c->n_layers, (int)c->n_kv_heads,
                    (int)c->page_size, (int)(c->head_dim * c->elem_bytes), src, dst, valid, ctl, (int)n, (int)table};
   sats::pages_copy_kernel<TABLE><<<(unsigned)(table + grid), sats::kThreads, 0, stream>>>(a, t);
@@ -504,6 +515,7 @@ int sats_cache_fork(const sats_kv_cache *cache, const sats_kv_pages *pages, cons
   int rc = check_pages(cache, pages, n, true);
   if (rc || n == 0) return rc;
   if (!src || !dst) return fail(SATS_ERR_NULL, "src and dst must be non-null");
+  if ((rc = check_table(n * pages->max_pages))) return rc;
   char *mem = nullptr;
   Turn turn;
   PagesScratch s;
@@ -519,7 +531,7 @@ int sats_cache_fork(const sats_kv_cache *cache, const sats_kv_pages *pages, cons
 int sats_cache_compact(const sats_kv_cache *cache, const sats_kv_pages *pages, int32_t *n_used, hipStream_t stream) {
   clear_error();
   int rc = check_pages(cache, pages, 0, true);
-  if (rc) return rc;
+  if (rc || (rc = check_table(pages->n_seqs * pages->max_pages))) return rc;
   char *mem = nullptr;
   Turn turn;
   PagesScratch s;

@@ -287,3 +287,38 @@ print(json.dumps(out))""")
         kinds.add((width, whole, "rows" in name))
     assert {w for w, _, rows in kinds if rows} == {"64", "96", "128", "256"}
     assert {w for w, _, rows in kinds if not rows} == {"64", "128", "256"}
+
+
+def test_tables_past_a_launch_are_refused_before_the_state_changes(run):
+    """A launch takes less than 2^32 threads in a row, an entry each for a fork's or a compaction's
+    table: what is too large is refused with nothing enqueued."""
+    got = run("""
+def call(what, n, seqs, width):
+    c = Cache(PTR, PTR * 2, 1, 500, 1, 16, 8, 2)
+    p = Pages(PTR * 3, PTR * 4, PTR * 5, seqs, width)
+    log()
+    if what == "fork":
+        rc = lib.sats_cache_fork(ctypes.byref(c), ctypes.byref(p), A(6), A(7), I(n), P(0), P(0))
+    else:
+        rc = lib.sats_cache_compact(ctypes.byref(c), ctypes.byref(p), P(0), P(0))
+    return [rc] + [[l[1], int(l[2].split("x")[0])] for l in log() if l[0] == "launch"]
+out = [call("fork", 65535, 64, 1 << 26), call("fork", 1 << 14, 1 << 14, 1 << 18), call("compact", 0, 1 << 12, 1 << 24),
+       call("compact", 0, 1 << 8, 1 << 24), call("fork", 1 << 14, 1 << 14, (1 << 18) - 256), call("compact", 0, 255, 1 << 24)]
+print(json.dumps(out))""")
+    assert got[:4] == [[SHAPE]] * 4
+    for rc, *launches in got[4:]:
+        assert rc == OK and len(launches) == 2 and launches[1][1] * 256 < 1 << 32
+
+
+def test_rows_past_a_launch_are_refused(run):
+    """... before the launch for a batch's short sequences, and before any scratch memory."""
+    kw = dict(n_tokens=1 << 30, max_q_len=1 << 28, n_seqs=4, q=BIG << 4, out=BIG << 8)
+    assert attend(**kw) == SHAPE and "rows" in sats.sats_last_error()
+    assert rope(n=1 << 30, hq=64, qs=4096, qos=4096, q=BIG << 3, k=BIG << 6, qo=BIG << 9, ko=BIG << 12) == SHAPE
+    rc, lines = run("""
+c = Cache(PTR, PTR * 2, 1, 500, 2, 16, 64, 2)
+b = Batch(PTR * 3, PTR * 4, PTR * 5, 4, 4, 1 << 30, 1 << 28, 64)
+rc = lib.sats_paged_attention(P(PTR << 4), I(256), ctypes.byref(c), I(0), ctypes.byref(b), I(4), ctypes.c_float(0.1),
+                              I(0), I(0), P(PTR << 12), P(0), P(0))
+print(json.dumps([rc, log()]))""")
+    assert rc == SHAPE and lines == []
