@@ -431,8 +431,9 @@ typedef struct {
  * rot_dim / 2 cosines of a position, then the sines.  Rows of heads are dense;
  * the strides are elements from one token to the next, so q, k and v may be
  * parts of one projection's output.  An output may be its own input (same
- * pointer and stride); other overlap is rejected.  Arrays and strides on 16
- * bytes, with head_dim and rot_dim multiples of 32 bytes' worth of elements,
+ * pointer and stride); other overlap is rejected (rows of one stride may lie
+ * between each other), and so are inputs or q_out in the cache.  Arrays and
+ * strides on 16 bytes, with head_dim and rot_dim multiples of 32 bytes' worth of elements,
  * move in 16-byte pieces, others element by element.
  *
  * sats_qk_norm_rope: positions [n_tokens] (device; cut off to 0 .. n_pos - 1).

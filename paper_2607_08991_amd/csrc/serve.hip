@@ -115,6 +115,22 @@ bool overlap(const void *a, int64_t na, const void *b, int64_t nb) {
   return na > 0 && nb > 0 && x < y + nb && y < x + na;
 }
 
+// n rows of `row` elements at a stride (none: a null pointer, or no elements).
+struct Rows {
+  const void *p;
+  int64_t stride, row;
+};
+bool same_rows(const Rows &a, const Rows &b) { return a.p == b.p && a.stride == b.stride; }
+// Whether any of n rows of a touches one of b.  Rows of one stride may lie between each other (parts
+// of one projection's output); of different strides they are apart where their spans are.
+bool rows_overlap(const Rows &a, const Rows &b, int64_t n, int esz) {
+  if (!a.p || !b.p || !a.row || !b.row || !overlap(a.p, span(n, a.stride, a.row, esz), b.p, span(n, b.stride, b.row, esz))) return false;
+  if (n == 1 || a.stride != b.stride) return true;
+  const int64_t s = a.stride * esz, off = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p));
+  const int64_t d = (off % s + s) % s;  // from a row of a to the next one of b
+  return d < a.row * esz || d + b.row * esz > s;
+}
+
 // Whether n bytes at p touch the cache's arrays.
 bool in_cache(const void *p, int64_t n, const sats_kv_cache *c) {
   const int64_t all = (int64_t)pool_bytes(c);
@@ -123,7 +139,9 @@ bool in_cache(const void *p, int64_t n, const sats_kv_cache *c) {
 
 // ------------------------------------------------------------- norm and rotation
 
-int run_rope(sats::RopeArgs a, int esz, bool append, hipStream_t stream) {
+// (cache: where keys and values go, or null)
+int run_rope(sats::RopeArgs a, int esz, const sats_kv_cache *cache, hipStream_t stream) {
+  const bool append = cache != nullptr;
   const int64_t n = a.n_tokens;
   if (n < 0 || n > kMaxCount || a.n_q < 0 || a.n_kv < 0 || a.n_q > 4096 || a.n_kv > 1024)
     return fail(SATS_ERR_SHAPE, "n_tokens, n_q_heads or n_kv_heads out of range");
@@ -140,18 +158,18 @@ int run_rope(sats::RopeArgs a, int esz, bool append, hipStream_t stream) {
   const int64_t qrow = (int64_t)a.n_q * a.dim, krow = (int64_t)a.n_kv * a.dim;
   if (a.q_stride < qrow || a.q_out_stride < qrow || a.k_stride < krow || (append ? a.v_stride : a.k_out_stride) < krow)
     return fail(SATS_ERR_SHAPE, "a token stride is below the token's row");
-  // outputs over inputs: the same rows, or apart
-  const int64_t sq = span(n, a.q_stride, qrow, esz), sk = span(n, a.k_stride, krow, esz);
-  const int64_t sqo = span(n, a.q_out_stride, qrow, esz), sko = append ? 0 : span(n, a.k_out_stride, krow, esz);
-  const bool q_same = a.q_out == a.q && a.q_out_stride == a.q_stride;
-  const bool k_same = !append && a.k_out == a.k && a.k_out_stride == a.k_stride;
-  const int64_t sv = append ? span(n, a.v_stride, krow, esz) : 0;
-  if (!q_same && (overlap(a.q_out, sqo, a.q, sq) || overlap(a.q_out, sqo, a.k, sk) || overlap(a.q_out, sqo, a.v, sv)))
+  // an output's rows: those of its own input, or apart from every input's and the other output's
+  const Rows q{a.q, a.q_stride, qrow}, k{a.k, a.k_stride, krow}, v{append ? a.v : nullptr, a.v_stride, krow};
+  const Rows qo{a.q_out, a.q_out_stride, qrow}, ko{append ? nullptr : a.k_out, a.k_out_stride, krow};
+  if ((!same_rows(qo, q) && rows_overlap(qo, q, n, esz)) || rows_overlap(qo, k, n, esz) || rows_overlap(qo, v, n, esz))
     return fail(SATS_ERR_ARG, "q_out overlaps the inputs without being q itself");
-  if (!append && !k_same && (overlap(a.k_out, sko, a.k, sk) || overlap(a.k_out, sko, a.q, sq)))
+  if ((!same_rows(ko, k) && rows_overlap(ko, k, n, esz)) || rows_overlap(ko, q, n, esz))
     return fail(SATS_ERR_ARG, "k_out overlaps the inputs without being k itself");
-  if (!append && !(q_same && k_same) && overlap(a.q_out, sqo, a.k_out, sko))
-    return fail(SATS_ERR_ARG, "q_out and k_out overlap");
+  if (rows_overlap(qo, ko, n, esz)) return fail(SATS_ERR_ARG, "q_out and k_out overlap");
+  if (append)
+    for (const Rows &r : {q, k, v, qo})
+      if (r.p && r.row && in_cache(r.p, span(n, r.stride, r.row, esz), cache))
+        return fail(SATS_ERR_ARG, "q, k, v or q_out overlaps the cache");
   const int vec = 16 / esz;
   const bool wide = a.dim % (2 * vec) == 0 && a.rot % (2 * vec) == 0 && on16(a.q) && on16(a.k) && on16(a.v) &&
                     on16(a.q_norm) && on16(a.k_norm) && on16(a.rope) && on16(a.q_out) && on16(a.k_out) &&
@@ -415,7 +433,7 @@ int sats_qk_norm_rope(const void *q, int64_t q_stride, const void *k, int64_t k_
   a.q_out = q_out, a.k_out = k_out, a.q_out_stride = q_out_stride, a.k_out_stride = k_out_stride;
   a.n_q = (int)n_q_heads, a.n_kv = (int)n_kv_heads, a.dim = (int)head_dim, a.rot = (int)rot_dim, a.pairs = interleaved;
   a.n_tokens = n_tokens;
-  return run_rope(a, elem_bytes, false, stream);
+  return run_rope(a, elem_bytes, nullptr, stream);
 }
 
 int sats_qkv_append(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
@@ -439,9 +457,7 @@ int sats_qkv_append(const void *q, int64_t q_stride, const void *k, int64_t k_st
   a.n_tokens = batch->n_tokens;
   a.k_pool = layer_of(cache->k, cache, layer), a.v_pool = layer_of(cache->v, cache, layer);
   a.batch = batch_view(batch), a.pool = pool_view(cache);
-  const int64_t qs = span(batch->n_tokens, q_out_stride, n_q_heads * cache->head_dim, cache->elem_bytes);
-  if (q_out && in_cache(q_out, qs, cache)) return fail(SATS_ERR_ARG, "q_out overlaps the cache");
-  return run_rope(a, cache->elem_bytes, true, stream);
+  return run_rope(a, cache->elem_bytes, cache, stream);
 }
 
 int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *cache, int64_t layer,

@@ -322,3 +322,39 @@ rc = lib.sats_paged_attention(P(PTR << 4), I(256), ctypes.byref(c), I(0), ctypes
                               I(0), I(0), P(PTR << 12), P(0), P(0))
 print(json.dumps([rc, log()]))""")
     assert rc == SHAPE and lines == []
+
+
+# ------------------------------------------------------------------ rows that touch each other
+
+@pytest.mark.parametrize("what", ["q", "k", "v"])
+def test_append_refuses_inputs_in_the_cache(what):
+    """Other tokens' keys and values are written there while the inputs are read."""
+    size = 2 * 10 * 2 * 16 * 64 * 2  # bytes of the cache's k, at P; v is there too
+    kw = dict(n_tokens=3, q=4 * P, k=5 * P, v=6 * P)
+    for at in (P, P + size - 16, P - 16):
+        bad = dict(kw, **{what: at})
+        assert append(**bad) == ARG and "cache" in sats.sats_last_error(), at
+    for at in (P + size, P - 3 * 512):
+        assert append(**dict(kw, **{what: at})) != ARG, sats.sats_last_error()
+
+
+def fused(n=3, **at):
+    """q, k and their outputs as parts of rows of 1024 bf16: offsets in elements, heads of 64."""
+    a = dict(q=0, k=256, qo=0, ko=256)
+    a.update(at)
+    return rope(n=n, hq=4, hk=2, **{x: P + 2 * o for x, o in a.items()}, qs=1024, ks=1024, qos=1024, kos=1024)
+
+
+@pytest.mark.parametrize("n", [1, 3])
+def test_rotation_in_place_refuses_parts_that_overlap(n):
+    for bad in (dict(k=192, ko=192), dict(k=192, ko=512), dict(q=64, qo=64, k=0, ko=0), dict(qo=128, q=0), dict(qo=640, ko=768),
+                dict(qo=300), dict(ko=320), dict(ko=128)):
+        assert fused(n, **bad) == ARG, bad
+
+
+@pytest.mark.parametrize("n", [1, 3])
+def test_rotation_takes_parts_of_one_row_that_lie_apart(n):
+    for good in (dict(), dict(qo=512, ko=768), dict(qo=384), dict(ko=384), dict(qo=768, ko=384), dict(q=768, qo=768)):
+        assert fused(n, **good) != ARG, (good, sats.sats_last_error())
+    assert fused(3, q=900, qo=900, k=1024 + 140, ko=1024 + 140) != ARG  # a row that ends where the next begins
+    assert fused(3, q=900, qo=900, k=1024 + 128, ko=1024 + 128) == ARG
