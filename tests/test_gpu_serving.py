@@ -780,3 +780,53 @@ def test_heads_of_every_width_read_their_own_rows(sats, dtype, dim, page):
             pool[:, :, 1] = math.inf
         got, got_lse, _ = run_attention(sats, b, dt, window=window, sinks=sinks)
         assert torch.equal(got[:, :2], out[:, :2]) and torch.equal(got_lse[:, :2], lse[:, :2])
+
+
+# ------------------------------------------------------------------ the weights' bits
+
+def weights_between_bf16(sats, q_len, n, value, page=16, dim=128):
+    """Sequences of n keys of one direction: key 0 weighs 1 (values 0), the others 0.5 + 0.49 * 2^-8
+    (values `value` [dim]), which bfloat16 rounds to 0.5; the (out, o, lse) of every new token."""
+    w = 0.5 + 0.49 * 2.0 ** -8
+    b = Batch(sats, torch.bfloat16, q_len, [n] * len(q_len), 8, 2, dim, page, seed=1)
+    b.q.zero_(), b.k.zero_()
+    b.q[:, :, 0], b.k[..., 0] = 1.0, -1.0
+    b.v.copy_(value)
+    for s in range(len(q_len)):
+        b.k[:, b.rows[s][0], :, 0] = 0.0
+        b.v[:, b.rows[s][0], :, 0] = 0.0
+    out, lse, scale = run_attention(sats, b, torch.bfloat16, scale=-math.log(w))
+    w = math.exp(-np.float64(np.float32(scale)))
+    place = np.array([n - m + i for m in q_len for i in range(m)])[:, None]
+    keys = np.maximum(place, 0).astype(np.float64)  # besides key 0 (a place below 0 sees nothing)
+    return f64(out), f64(value) * keys * w / (1 + keys * w), f64(lse), np.where(place < 0, -math.inf, np.log1p(keys * w))
+
+
+@pytest.mark.parametrize("n", [2, 33, 500, 3000])
+@pytest.mark.parametrize("q_len", [[1], [1] * 5, [4, 1, 2]])
+def test_decoding_keeps_the_weights_bits(sats, n, q_len):
+    """bf16 tokens of at most 16 rows a cache head: before its rounding a result is off by d, 16 bits of
+    each weight (2^-16, and 2^-20 that keep the rest of one above 0) and the float32 sums, and so at
+    most 2 d farther from o than the bfloat16 nearest to o.  With the weights' first 8 bits alone d
+    would be up to 2^-8."""
+    value = (1 + torch.rand(128, generator=gen(n), device="cuda")).to(torch.bfloat16)
+    got, o, got_lse, lse = weights_between_bf16(sats, q_len, n, value)
+    d = (2.0 ** -16 + 2.0 ** -20 + (n + 64 + 2 * 8) * 2.0 ** -24) * np.abs(o[:, None])
+    nearest = f64(torch.from_numpy(o).to(torch.bfloat16))[:, None]
+    assert (np.abs(got - o[:, None]) <= np.abs(nearest - o[:, None]) + 2 * d).all()
+    assert ((got_lse == lse) | (np.abs(got_lse - lse) <= 2.0 ** -20 * np.maximum(lse, 1) + 2.0 ** -20)).all()
+
+
+@pytest.mark.parametrize("q_len", [[1], [4, 1], [40]])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_an_infinity_that_is_seen_stays_one(sats, q_len, sign):
+    """Whatever the bits of its weight: 1, 0.5 (nothing after the first bits) and in between."""
+    for scale in (math.log(2.0), 0.69, 0.0, 3.0):
+        b = Batch(sats, torch.bfloat16, q_len, [90] * len(q_len), 8, 2, 64, 16, seed=2)
+        b.q.zero_(), b.k.zero_()
+        b.q[:, :, 0] = 1.0
+        for s in range(len(q_len)):
+            b.k[:, b.rows[s][0], :, 5, 0] = -1.0
+            b.v[:, b.rows[s][0], 0, 5] = sign * math.inf
+        out, _, _ = run_attention(sats, b, torch.bfloat16, scale=scale)
+        assert (out[:, :4] == sign * math.inf).all() and torch.isfinite(out[:, 4:]).all()
