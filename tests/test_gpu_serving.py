@@ -830,3 +830,58 @@ def test_an_infinity_that_is_seen_stays_one(sats, q_len, sign):
             b.v[:, b.rows[s][0], 0, 5] = sign * math.inf
         out, _, _ = run_attention(sats, b, torch.bfloat16, scale=scale)
         assert (out[:, :4] == sign * math.inf).all() and torch.isfinite(out[:, 4:]).all()
+
+
+# ------------------------------------------------------------------ pages whose every element differs
+
+class MarkedWorld(PageWorld):
+    """... with contents that differ in every layer, head, slot and dim."""
+
+    def __init__(self, sats, n_pages, page, n_seqs, width, layers, heads, dim):
+        super().__init__(sats, n_pages, page, n_seqs, width, layers, heads, dim)
+        self.each = layers * heads * dim
+        assert n_pages * page * self.each < 1 << 23  # (whole numbers in float32, the values' doubled)
+        self.part = torch.arange(self.each, device="cuda", dtype=torch.float32).view(layers, 1, heads, 1, dim)
+        slots = torch.arange(n_pages * page, device="cuda", dtype=torch.float32).view(1, n_pages, 1, page, 1)
+        self.k.copy_(slots * self.each + self.part)
+        self.v.copy_(-2 * (slots * self.each + self.part))
+
+    def check(self):
+        m = self.model
+        assert self.refs.tolist() == m.refs and self.len.tolist() == m.len and self.table.tolist() == m.table
+        mark = torch.tensor([[p * m.page + i for p, i in row] for row in m.data], dtype=torch.float32, device="cuda")
+        want = mark.view(1, len(m.refs), 1, m.page, 1) * self.each + self.part
+        assert torch.equal(self.k, want) and torch.equal(self.v, -2 * want)
+
+
+@pytest.mark.parametrize("layers,heads,dim,page", [(3, 2, 8, 4), (2, 3, 24, 16), (1, 1, 256, 2), (5, 4, 72, 8)])
+def test_moves_of_pages_take_every_element_with_them(sats, layers, heads, dim, page):
+    w = MarkedWorld(sats, 40, page, 8, 10, layers, heads, dim)
+    part = page // 2 + 1 if page > 2 else 1
+    assert w.extend([0, 1, 2], [3 * page + part, part, 2 * page]) == (0, 0); w.check()
+    assert w.fork([0, 1, 0, 2], [3, 4, 5, 6]) == (0, 0); w.check()    # part pages are copied, full ones shared
+    w.free([3], [2 * page + 1]); w.check()                           # ends inside a shared page
+    assert w.extend([3, 0], [1, page]) == (0, 0); w.check()          # ... which it takes a copy of
+    w.free([0, 1]); w.check()
+    w.compact(); w.check()
+    w.free([5, 6]); w.compact(); w.check()
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_marked_pages_over_random_calls(sats, seed):
+    r = random.Random(100 + seed)
+    page = r.choice((2, 4, 8))
+    w = MarkedWorld(sats, r.randint(20, 100), page, 12, 8, r.randint(1, 3), r.choice((1, 3)), r.choice((8, 24)))
+    for _ in range(30):
+        some = r.sample(range(12), r.randint(2, 6))
+        what = r.choice(("extend", "extend", "fork", "fork", "cut", "compact"))
+        if what == "extend":
+            w.extend(some, [r.randint(0, 2 * page) for _ in some])
+        elif what == "fork":
+            w.free(some[len(some) // 2:])
+            w.fork(some[:len(some) // 2], some[len(some) // 2:2 * (len(some) // 2)])
+        elif what == "cut":
+            w.free(some, [r.randint(0, 8 * page) for _ in some])
+        else:
+            w.compact()
+        w.check()
