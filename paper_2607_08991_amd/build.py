@@ -14,7 +14,6 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libsats.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("sats.hip", "serve.hip")]
-DEPS = SOURCES + [os.path.join(CSRC, "kernels.hpp"), os.path.join(ROOT, "include", "sats.h")]
 ARCH = "gfx950"
 
 

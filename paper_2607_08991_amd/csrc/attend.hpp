@@ -45,7 +45,6 @@ struct AttendArgs {
   int n_q, group, dim;  // group: query heads of a cache head
   float scale;
   int64_t window, sinks;
-  int tiles;          // upper bound of the row tiles of the batch
   int splits;         // workgroups a tile's blocks are split over, at most
   int per_split;      // key blocks of a split
   int small, large;   // which sequences the launch takes: at most 16 rows a head, more

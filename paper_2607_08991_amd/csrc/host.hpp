@@ -15,9 +15,6 @@ namespace sats_host {
 int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 void clear_error();
 
-// Compute units of the current device (0 on an error).
-int device_cus();
-
 // Calls on one stream may come from several threads, and a call is several launches that
 // hand each other results in the stream's workspace: a call holds the stream's turn from
 // before it looks at the workspace until its last launch is enqueued.
@@ -29,9 +26,3 @@ typedef std::unique_lock<std::mutex> Turn;
 int serve_workspace(hipStream_t stream, size_t bytes, char **mem, Turn *turn);
 
 }  // namespace sats_host
-
-#define SATS_HIP_TRY(expr)                                                                                  \
-  do {                                                                                                      \
-    hipError_t e_ = (expr);                                                                                 \
-    if (e_ != hipSuccess) return sats_host::fail(SATS_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_));     \
-  } while (0)

@@ -107,8 +107,6 @@ __device__ __forceinline__ float share_of(float x, float top, float inv_t, float
 __device__ __forceinline__ u64 weight_of(float share) {  // round(2^40 share): the low bits of 2^52 + it in float64
   return (u64)__double_as_longlong(fma((double)share, 0x1p40, 0x1p52)) & ((1ull << 52) - 1);
 }
-// Whether an id at z has a weight (2^40 exp(-28) rounds to 1).
-__device__ __forceinline__ bool weighs(float z) { return z > -28.0f || weight_of(share_of(z)) != 0; }
 __device__ __forceinline__ int bin_of(float z) {
   const int b = (int)(-z * kSampScale);
   return b < kSampBins - 1 ? b : kSampBins - 1;

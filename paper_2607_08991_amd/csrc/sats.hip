@@ -2121,7 +2121,6 @@ int fail(int code, const char *fmt, ...) {
   return code;
 }
 void clear_error() { g_err.clear(); }
-int device_cus() { return ::device_cus(); }
 
 int serve_workspace(hipStream_t stream, size_t bytes, char **mem, Turn *turn) try {
   int dev = 0, rc = 0;

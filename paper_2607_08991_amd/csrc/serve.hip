@@ -226,7 +226,7 @@ size_t attend_bytes(const AttendPlan &p, int R, int n_kv, int dim) {
 template <typename T, int R, typename Kernel>
 int launch_attention(sats::AttendArgs a, const AttendPlan &p, Kernel kernel, char *mem, hipStream_t stream) {
   const int64_t grid_x = p.tiles * a.pool.n_kv;
-  a.tiles = (int)p.tiles, a.splits = p.splits, a.per_split = p.per_split;
+  a.splits = p.splits, a.per_split = p.per_split;
   a.part = reinterpret_cast<float *>(mem);
   a.part_ml = a.part + grid_x * p.splits * R * a.dim;
   kernel<<<dim3((unsigned)grid_x, (unsigned)p.splits), 256, 0, stream>>>(a);
