@@ -655,11 +655,13 @@ template <int DT, bool FULL> struct TileWave {
   }
 
   // The row's maximum moves to `top` (a lane's own), and the sums are scaled to it, only where a
-  // weight would pass 2^8.
+  // weight would pass 2^8.  (Each row for itself, so that its result does not depend on the others';
+  // a maximum that is NaN stays out, the weights are NaN then.)
   __device__ __forceinline__ void rescale(float top) {
     top = fmaxf(top, __shfl_xor(top, 32));
-    if (__any(!((top - m) * scale2 <= 8.0f))) {
-      const float mn = fmaxf(m, top), f = mn == m ? 1.0f : exp2_fast((m - mn) * scale2);
+    const bool past = (top - m) * scale2 > 8.0f;
+    if (__any(past)) {
+      const float mn = past ? top : m, f = past ? exp2_fast((m - mn) * scale2) : 1.0f;
       m = mn;
       l *= f;
 #pragma unroll

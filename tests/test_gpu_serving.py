@@ -885,3 +885,22 @@ def test_marked_pages_over_random_calls(sats, seed):
         else:
             w.compact()
         w.check()
+
+
+# ------------------------------------------------------------------ rows of a tile
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_len,kv_len,window", [([64], [1000], 0), ([150], [150], 0), ([70, 3], [4000, 90], 0),
+                                                 ([40], [2000], 300), ([4], [3000], 0)])
+def test_a_row_does_not_depend_on_the_others(sats, dtype, q_len, kv_len, window):
+    """Other queries of a tile that score far higher, or are NaN, change no bit of a row."""
+    dt = dt_of(dtype)
+    b = Batch(sats, dt, q_len, kv_len, 8, 2, 64, 16, seed=31)
+    want, want_lse, scale = run_attention(sats, b, dt, window=window)
+    for value in (40.0, -40.0, math.nan):
+        q = b.q.clone()
+        q[1::3, 2] *= value
+        got, lse, _ = run_attention(sats, b, dt, window=window, q=q)
+        same = torch.ones(b.n, 8, dtype=torch.bool, device="cuda")
+        same[1::3, 2] = False
+        assert torch.equal(got[same], want[same]) and torch.equal(lse[same], want_lse[same])
