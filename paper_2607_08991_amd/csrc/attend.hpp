@@ -965,9 +965,10 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   for (int z0 = w * per; z0 < parts; z0 += W * per) {
     const int z = z0 + sub < parts ? z0 + sub : parts - 1;
     const float *ml = a.part_ml + (at + (int64_t)z * R) * 2;
-    const float f = z0 + sub < parts ? exp2_fast(ml[0] - at0) : 0.0f;
+    const float lz = z0 + sub < parts ? ml[1] : 0.0f, f = exp2_fast(ml[0] - at0);
     const f32x4 x = *reinterpret_cast<const f32x4 *>(a.part + (at + (int64_t)z * R) * a.dim + dd);
-    if (f != 0.0f) l += ml[1] * f, o += x * f;  // (f is NaN where the row's maximum is an infinity)
+    // (a part that saw nothing has 0; one whose scores are NaN has no maximum, but NaN here)
+    if (lz != 0.0f) l += lz * f, o += x * f;
   }
   for (int m = lanes; m < 64; m <<= 1) {
     l += __shfl_xor(l, m);

@@ -904,3 +904,57 @@ def test_a_row_does_not_depend_on_the_others(sats, dtype, q_len, kv_len, window)
         same = torch.ones(b.n, 8, dtype=torch.bool, device="cuda")
         same[1::3, 2] = False
         assert torch.equal(got[same], want[same]) and torch.equal(lse[same], want_lse[same])
+
+
+# ------------------------------------------------------------------ NaN that is seen, in one part of a row
+
+LONG = [  # q_len, kv_len, which are split over workgroups
+    ([1], [5000]), ([1], [32000]), ([1, 1, 1], [3000, 40, 700]), ([70], [8000]), ([3, 40], [4000, 3000]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_len,kv_len", LONG)
+def test_nan_scores_are_not_lost(sats, dtype, q_len, kv_len):
+    """A query that is NaN, and then keys that are NaN for so long that a part of the row sees no
+    other: the rows that see them are NaN, every other one is what it was."""
+    dt = dt_of(dtype)
+    b = Batch(sats, dt, q_len, kv_len, 4, 2, 64, 16, seed=21)
+    clean, clean_lse, scale = run_attention(sats, b, dt)
+    q = b.q.clone()
+    q[-1, 1, 5] = math.nan
+    got, lse, _ = run_attention(sats, b, dt, q=q)
+    assert got[-1, 1].isnan().all() and lse[-1, 1].isnan()
+    got[-1, 1], lse[-1, 1] = clean[-1, 1], clean_lse[-1, 1]
+    assert torch.equal(got, clean) and torch.equal(lse, clean_lse)
+    for j in range(512, 1536):  # (of the first sequence, the second cache head: heads 2 and 3)
+        b.k[1, b.rows[0][j // 16], 1, j % 16, 3] = math.nan
+    got, lse, _ = run_attention(sats, b, dt)
+    own = slice(0, q_len[0])
+    assert got[own, 2:].isnan().all() and lse[own, 2:].isnan().all()
+    got[own, 2:], lse[own, 2:] = clean[own, 2:], clean_lse[own, 2:]
+    assert torch.equal(got, clean) and torch.equal(lse, clean_lse)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_len,kv_len", LONG)
+def test_a_value_that_is_not_finite_reaches_its_rows_from_any_part(sats, dtype, q_len, kv_len):
+    """NaN and infinities of one key's values, whatever the part of the row and its weight (to e^-200:
+    nothing in float32, where the product is NaN)."""
+    dt = dt_of(dtype)
+    for value in (math.nan, math.inf):
+        for small in (False, True):
+            b = Batch(sats, dt, q_len, kv_len, 4, 2, 64, 16, seed=22)
+            b.q.zero_()
+            b.q[:, :, 0] = 1.0
+            b.k[..., 0] = 0.0
+            if small:
+                for j in range(512, 1536):
+                    b.k[1, b.rows[0][j // 16], :, j % 16, 0] = -200.0
+            b.v[1, b.rows[0][1000 // 16], 0, 1000 % 16, 7] = value
+            got, _, _ = run_attention(sats, b, dt, scale=1.0)
+            own = slice(0, q_len[0])
+            assert not got[own, :2, 7].isfinite().any()
+            rest = got.clone()
+            rest[own, :2, 7] = 0
+            assert rest.isfinite().all()
