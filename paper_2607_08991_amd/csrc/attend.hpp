@@ -465,8 +465,10 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
       product(Plain{});
     } else {
       product(Odd{});
+      const Sight sight = sight_of(a, place, j0);
 #pragma unroll 1
       for (int k = 0; k < kKeys; ++k) {
+        const bool seen = ((here >> k & 1) != 0) & sight.sees(k);  // (its weight may have underflowed to 0)
         float p = 0.0f;
 #pragma unroll
         for (int kt = 0; kt < kTiles; ++kt)
@@ -480,7 +482,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
           for (int e = 0; e < 4; ++e) {
             const int d = 16 * o + 4 * g + e;
             const float v = Elem<T>::get(reinterpret_cast<const T *>(mine + k * kPitch) + d);
-            if (p != 0.0f && odd_of(v)) acc[o][e] += p * v;
+            if (seen && odd_of(v)) acc[o][e] += p * v;
           }
       }
     }
@@ -728,11 +730,15 @@ template <int DT, bool FULL> struct TileWave {
     }
     if (NEXT) *top = t;
   }
-  // ... and the infinities and NaN that it left out, where a row sees them.
-  __device__ __forceinline__ void add_odd(const f32x16_t (&s)[2], const uint8_t *vt) {
+  // ... and the infinities and NaN that it left out, where a row sees them (the block's keys from j0
+  // on, of which `there` are seen by some row of the tile).
+  __device__ __forceinline__ void add_odd(const AttendArgs &a, uint64_t there, int64_t j0, const f32x16_t (&s)[2],
+                                          const uint8_t *vt) {
     const int lane = threadIdx.x & 63, hf = lane >> 5;
+    const Sight sight = sight_of(a, place, j0);
 #pragma unroll 1
     for (int k = 0; k < kTileKeys; ++k) {
+      const bool seen = ((there >> k & 1) != 0) & sight.sees(k);  // (its weight may have underflowed to 0)
       float p = 0.0f;
 #pragma unroll
       for (int x = 0; x < 2; ++x)
@@ -746,7 +752,7 @@ template <int DT, bool FULL> struct TileWave {
         for (int e = 0; e < 16; ++e) {
           const int d = 32 * o + 8 * (e >> 2) + 4 * hf + (e & 3);
           const uint16_t v = reinterpret_cast<const uint16_t *>(vt + k * kRow + v_place(k, d >> 3) * 16)[d & 7];
-          if (p != 0.0f && odd_bits(v)) acc[o][e] += p * bf16_to_f32(v);
+          if (seen && odd_bits(v)) acc[o][e] += p * bf16_to_f32(v);
         }
     }
   }
@@ -857,7 +863,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
     f32x16_t sa[2], sb[2];
     held.first = -1;
     int page = page_of(b0), next = page_of(b0 + 1);
-    uint64_t there = __ballot(page >= 0), there_next = __ballot(next >= 0);
+    uint64_t there = __ballot(page >= 0), there_next = __ballot(next >= 0), here = there;  // (here: of the block at hand)
     issue_k(b0, page, there, k0);
     issue_v(b0, page, there, v0);
     if (b0 + 1 < b_end) issue_k(b0 + 1, next, there_next, k1);
@@ -883,21 +889,21 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
       if (some) wave.mask(a, there_next, j1, sn);
       if (kOdd && odd) {
         wave.template product<true, true>(s, vt, sn, &top);
-        wave.add_odd(s, vt);
+        wave.add_odd(a, here, block_key(kb, b, kTileKeys), s, vt);
       } else {
         wave.template product<false, true>(s, vt, sn, &top);
         again |= odd;
       }
       wave.rescale(top);
-      next = page, there_next = there;
+      next = page, here = there_next, there_next = there;
     };
-    auto last = [&](f32x16_t (&s)[2], uint8_t *vt) {
+    auto last = [&](int b, f32x16_t (&s)[2], uint8_t *vt) {
       stage_barrier();
       const bool odd = some && Wave::odd_block(vt);
       wave.template weights<false>(s, vt, s);
       if (kOdd && odd) {
         wave.template product<true, false>(s, vt, s, &top);
-        wave.add_odd(s, vt);
+        wave.add_odd(a, here, block_key(kb, b, kTileKeys), s, vt);
       } else {
         wave.template product<false, false>(s, vt, s, &top);
         again |= odd;
@@ -910,9 +916,9 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
     }
     if (b + 1 < b_end) {
       step(b, sa, sb, k0, k1, v0, v1);
-      last(sb, v1);
+      last(b + 1, sb, v1);
     } else {
-      last(sa, v0);
+      last(b, sa, v0);
     }
     return again;
   };

@@ -958,3 +958,28 @@ def test_a_value_that_is_not_finite_reaches_its_rows_from_any_part(sats, dtype, 
             rest = got.clone()
             rest[own, :2, 7] = 0
             assert rest.isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_len,kv_len", [([3], [40]), ([3, 1], [5000, 70]), ([40], [100]), ([100, 2], [3000, 50])])
+def test_a_value_that_is_not_finite_among_keys_on_which_rows_disagree(sats, dtype, q_len, kv_len):
+    """A key that all rows see, in the block of the last ones that only some see: whatever its weight
+    (e^-200: nothing in float32), its NaN reaches every row that sees it and no other."""
+    dt = dt_of(dtype)
+    for weight in (0.0, -200.0):
+        b = Batch(sats, dt, q_len, kv_len, 4, 2, 64, 16, seed=23)
+        b.q.zero_()
+        b.q[:, :, 0] = 1.0
+        b.k[..., 0] = 0.0
+        clean, clean_lse, _ = run_attention(sats, b, dt, scale=1.0)
+        n = kv_len[0]
+        for j, first in ((n - q_len[0] - 1, 0), (n - 1, q_len[0] - 1)):  # seen by all; by the last token alone
+            at = b.rows[0][j // 16], slice(None), j % 16
+            k0, v0 = b.k[(1, *at)].clone(), b.v[(1, *at)].clone()
+            b.k[(1, *at)][:, 0] = weight
+            b.v[(1, *at)][:, 7] = math.nan
+            got, _, _ = run_attention(sats, b, dt, scale=1.0)
+            assert got[first:q_len[0], :, 7].isnan().all()
+            assert got[:first].isfinite().all() and torch.equal(got[:first], clean[:first])
+            assert torch.equal(got[q_len[0]:], clean[q_len[0]:])
+            b.k[(1, *at)], b.v[(1, *at)] = k0, v0
