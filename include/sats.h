@@ -472,8 +472,9 @@ int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *c
  * seqs NULL: sequences 0 .. n - 1); a sequence may be in it once.
  *
  * sats_cache_extend: item i's sequence grows by add[i] tokens: its table gets
- * the pages that these need.  A last page that is not full and that other
- * sequences share is replaced by a copy of its own.
+ * the pages that these need (also the one that the sequence ends inside of, where
+ * it was given back).  A last page that is not full and that other sequences
+ * share is replaced by a copy of its own.
  * sats_cache_fork: sequence dst[i], which has to be empty, becomes a copy of
  * src[i] (no dst is a src): full pages are shared, a last page that is not full
  * is copied (its tokens, in every layer).

@@ -84,7 +84,9 @@ class Pages:
             part = self._part(s) if a else None
             copy = part is not None and self.refs[part] > 1
             up = lambda n: -(-n // self.page)  # noqa: E731
-            want.append((copy, part, up(self.len[s] + a) - up(self.len[s])))
+            # the first page that is missing: the one that the sequence ends inside of, where it is not there
+            first = self.len[s] // self.page if a and part is None else up(self.len[s])
+            want.append((copy, part, up(self.len[s] + a) - first, first))
         got, missing = self._take([0 if w is None else w[0] + w[2] for w in want])
         if got is None:
             return missing, left_out
@@ -99,8 +101,7 @@ class Pages:
                 self.refs[w[1]] -= 1
                 self.table[s][n // self.page] = ids[0]
                 ids = ids[1:]
-            first = -(-n // self.page)
-            self.table[s][first:first + len(ids)] = ids
+            self.table[s][w[3]:w[3] + len(ids)] = ids
             self.len[s] = n + a
         return 0, left_out
 

@@ -20,6 +20,7 @@ namespace sats {
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanPer = 16;  // refs that a thread looks at in one step of the free list's scan
 constexpr int kPlanItems = 1024, kPlanIds = 4096;  // items and new pages whose lists are held in LDS
+constexpr int kNoPart = -2;  // an item's page to copy: none, and the page that its sequence ends inside of is not there
 
 struct PagesArgs {
   int32_t *table, *len, *refs;
@@ -117,7 +118,7 @@ __device__ __forceinline__ int32_t part_page(const PagesArgs &a, int s, int n) {
 }
 
 // Plan of an extension (FORK false: item i's sequence grows by other[i] tokens; a shared
-// last page that it ends inside of is replaced by a copy) or of a fork (item i: sequence
+// last page that it ends inside of is replaced by a copy, one that is not there by a new one) or of a fork (item i: sequence
 // other[i], which has to be empty, becomes a copy of seqs[i]; its last page, where it is
 // not full, is copied).  All items or, for want of pages, none.
 template <bool FORK>
@@ -148,8 +149,10 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesArgs a) {
         ok = ok && o >= 0 && n + o <= a.max_pages << a.shift;
         if (ok && o > 0) {
           src = part_page(a, (int)s, (int)n);
-          if (src >= 0 && a.refs[src] <= 1) src = -1;
-          need = (int)(((n + o + a.page - 1) >> a.shift) - ((n + a.page - 1) >> a.shift)) + (src >= 0);
+          // (a sequence that was cut inside of pages that it had given back has no such page)
+          if (src < 0) src = n & (a.page - 1) ? kNoPart : -1;
+          else if (a.refs[src] <= 1) src = -1;
+          need = (int)(((n + o + a.page - 1) >> a.shift) - ((n + a.page - 1) >> a.shift)) + (src != -1);
         }
       }
       if (!ok) atomicAdd(&left_out, 1), need = -1;
@@ -203,8 +206,8 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesArgs a) {
       if ((m < 0 ? -1 - m : m) <= r) lo = mid;
       else hi = mid - 1;
     }
-    const int at = r - off[lo] - (src_of[lo] >= 0);
-    if (at >= 0)  // (not the copy of a shared page, above)
+    const int at = r - off[lo] - (src_of[lo] != -1);
+    if (at >= 0 || src_of[lo] == kNoPart)  // (not the copy of a shared page, above)
       a.table[item_seq(a, lo) * a.max_pages + ((len_of[lo] + a.page - 1) >> a.shift) + at] = ids[r];
   }
 }

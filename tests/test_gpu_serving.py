@@ -983,3 +983,38 @@ def test_a_value_that_is_not_finite_among_keys_on_which_rows_disagree(sats, dtyp
             assert got[:first].isfinite().all() and torch.equal(got[:first], clean[:first])
             assert torch.equal(got[q_len[0]:], clean[q_len[0]:])
             b.k[(1, *at)], b.v[(1, *at)] = k0, v0
+
+
+# ------------------------------------------------------------------ pages given back, then needed again
+
+def test_a_sequence_that_ends_in_pages_it_gave_back_gets_one_when_it_grows(sats):
+    w = PageWorld(sats, 6, 4, 4, 5)
+    assert w.extend([0, 1], [12, 3]) == (0, 0)
+    w.free([0], [0], [8]); w.check()
+    w.free([0], [6]); w.check()
+    assert w.extend([0, 1, 2], [3, 1, 2]) == (0, 0); w.check()
+    assert w.table[0].tolist() == [-1, 0, 1, -1, -1] and w.refs[:2].tolist() == [1, 1]
+    w.free([0], [0], [4]); w.free([0], [2])
+    assert w.fork([0], [3]) == (0, 0); w.check()              # nothing to copy, and nothing there
+    assert w.extend([3, 0], [1, 40]) == (0, 1); w.check()     # no room for the second
+    assert w.extend([3, 0], [18, 18])[0] > 0; w.check()       # not enough pages: nothing changes
+    assert w.extend([3, 0], [1, 7]) == (0, 0); w.check()
+    assert (w.table[3, 0] >= 0) and (w.table[0, :3] >= 0).all()
+
+
+def test_what_is_appended_after_such_a_cut_is_there(sats):
+    """The tokens' keys and values, read back by attention."""
+    cache = sats.KVCache(torch.zeros((1, 6, 1, 4, 8), device="cuda"), torch.zeros((1, 6, 1, 4, 8), device="cuda"))
+    table, ln, refs = ints([[-1] * 4]), ints([0]), ints([0] * 6)
+    pages = sats.KVPages(table, ln, refs)
+    sats.sats_cache_extend(cache, pages, None, ints([12]))
+    sats.sats_cache_free(cache, pages, ints([0]), ints([0]), ints([8]))
+    sats.sats_cache_free(cache, pages, ints([0]), ints([5]))
+    sats.sats_cache_extend(cache, pages, None, ints([2]))
+    batch = sats.KVBatch(table, ints([0, 2]), ln, 2, 2, 16)
+    q, k = torch.ones((2, 1, 8), device="cuda"), torch.ones((2, 1, 8), device="cuda")
+    v = torch.arange(1.0, 17.0, device="cuda").view(2, 1, 8)
+    out, lse = torch.empty_like(q), torch.empty((2, 1), device="cuda")
+    sats.sats_qkv_append(q, k, v, None, q, cache, 0, batch)
+    sats.sats_paged_attention(q, cache, 0, batch, out, 1.0, window=2, lse=lse)
+    assert torch.equal(out[1, 0], (v[0, 0] + v[1, 0]) / 2) and abs(float(lse[1]) - 8 - math.log(2)) < 1e-5

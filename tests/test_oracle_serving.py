@@ -115,3 +115,16 @@ def test_sampling_limits_by_hand():
     ties = np.zeros(5)
     assert ref.sample(ties, np.ones(5, np.float32), 0.99, top_k=2)[::2] == (1, 2)
     assert ref.sample(np.full(3, -np.inf), np.ones(3), 0.5) == (-1, 0.0, 0)
+
+
+def test_extension_of_a_sequence_that_ends_in_pages_it_gave_back():
+    """12 tokens in pages of 4; the first 8 are given back, and the sequence is cut to 6: tokens 6 and 7
+    need a page again."""
+    p = ref.Pages(8, 4, 2, 5)
+    assert p.extend([0, 1], [12, 3]) == (0, 0)
+    p.free([0], [0], [8])
+    p.free([0], [6])
+    assert p.table[0] == [-1] * 5 and p.len[0] == 6 and p.refs == [0, 0, 0, 1, 0, 0, 0, 0]
+    assert p.extend([0], [0]) == (0, 0) and p.table[0] == [-1] * 5
+    assert p.extend([0, 1], [3, 1]) == (0, 0)
+    assert p.table[0] == [-1, 0, 1, -1, -1] and p.len[0] == 9 and p.refs[:4] == [1, 1, 0, 1]
