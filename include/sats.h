@@ -527,7 +527,11 @@ int sats_sample(const void *logits, int elem_bytes, int64_t stride, int64_t n, i
  * of up to max_items items over n_pages pages, sampling of max_rows rows of vocab
  * logits, attention of any batch with heads of head_dim (zeros: none).
  * Without it a call allocates what it needs, once; a call under stream capture that
- * would have to allocate returns SATS_ERR_WORKSPACE.
+ * would have to allocate returns SATS_ERR_WORKSPACE.  A stream's scratch memory is as
+ * large as the largest of these needs (grown, at least twice as large where there is
+ * that much) and kept until sats_release: sampling 8 bytes a logit and 24 KB a row, of
+ * 512 rows at most (525 MB for 512 x 128256); attention 256 KB x (head_dim + 2); pages
+ * 16 bytes a page and 20 an item.
  */
 int sats_reserve_serving(int64_t max_items, int64_t n_pages, int64_t max_rows, int64_t vocab, int64_t head_dim,
                          hipStream_t stream);

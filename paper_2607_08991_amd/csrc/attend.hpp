@@ -232,8 +232,14 @@ struct Odd { static constexpr bool kOdd = true; };
 //
 // Bound by the cache's bytes: 64 sequences of 500 to 8000 keys (8 heads of 128, four rows each,
 // bf16, 711 MB) take 151 us with the join, 4.7 TB/s (counters: 712 MB fetched, no bank
-// conflicts); one sequence of 32768 keys (134 MB) 30.6 us in this kernel, 4.4 TB/s, and 8 in
-// the join.  16 rows are what a matrix instruction has columns for.  Of float32 it is eight
+// conflicts); one sequence of 32768 keys (134 MB) 29.7 us in this kernel, 4.5 TB/s, and 8.3 in
+// the join.  Of other widths the same sequences reach, in TB/s, 4.2 (64), 3.8 (80), 3.3 (96, which
+// spills registers at three waves a SIMD), 3.0 (136) to 4.3 (256: one workgroup a compute unit);
+// float32 4.8 at 128.  Few keys are latency, not products: 12 heads of 80 on 4 (float32), a token
+// alone on 16 keys takes 6.6 us, the sequence, the table, the keys and the end, each after the
+// other; six sequences in 208 tiles with a window of 16 9.2, and from there 3.3 us for each block of
+// a wave (window 512, three blocks: 22.2; 1024, six: 32.2), of which its 40 products are 1.3.
+// 16 rows are what a matrix instruction has columns for.  Of float32 it is eight
 // products of 16 x 16 x 4 where bf16 has one of 16 x 16 x 32: a chunk of 512 tokens on 1000
 // earlier ones (32 heads of 128) runs at 56 TFLOP/s, a third of a large float32 product's 154.
 template <typename T> struct RowsOf {
@@ -523,15 +529,23 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
 
 // Prompts and chunks of bf16: four waves of 32 rows, blocks of 64 keys that the workgroup
 // loads into LDS straight from memory, one block ahead.  Rows of K and V lie in LDS
-// with their 16-byte pieces exchanged, so that the 8 lanes that a cycle serves (K: the
-// same piece of 8 rows; V: two pieces of 4 rows) read different banks.
+// with their 16-byte pieces exchanged: the same piece of 16 rows of K is in 16 different places
+// of a row's 256 bytes, and two pieces of 4 rows of V are in eight.  For V that is not enough:
+// the counters show two cycles of bank conflicts for each read of V, whatever the width (heads of
+// 128: 64 for each wave and block, a third of the LDS's cycles), as where a cycle serves 32 lanes and
+// with them four pieces of 4 rows, of which two rows' coincide.
 //
 // Bound by issue: a chunk of 2048 tokens on 4096 earlier ones (32 heads of 128, 172 Gflop) takes
-// 196 us, 877 TFLOP/s, where a large bf16 product reaches 1140.  Without its loads it took 181
+// 199 us in calls one after another, 863 TFLOP/s, where a large bf16 product reaches 1140 (221
+// where each call is waited for, 217 to 245 under a tracer).  Without its loads it took 181
 // us and without the exponentials 192 (scratch builds, when it took 206): what is left is the
 // matrix and the vector instructions of a wave that do not overlap.  32 rows a wave fill the
 // 32 x 32 x 16 instruction; 256 rows a workgroup were slower (one workgroup a compute unit
 // leaves nothing to run at its barriers).
+// Other widths, the same chunk, with 4096 dims in all but 80 and 96 (32 heads): 64 662 TFLOP/s, as
+// many matrix cycles and 1.8 x the vector instructions (half the products for an exponential);
+// 80 574 and 96 676, whose rows lie in LDS, and are read, as if of 128; 256 619, one workgroup a
+// compute unit (131 KB of LDS), so nothing runs at its barriers.
 constexpr int kTileRows = 128, kTileKeys = 64;
 
 // 16 bytes of each lane into LDS at dst + OFF + 16 * lane, from src + OFF (dst the same for

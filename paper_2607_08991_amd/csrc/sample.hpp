@@ -24,10 +24,18 @@
 //           then the chunk, then the id, of the draw.
 //
 // The logits are read four times, from the caches after the first.  64 rows of 128256 float32
-// (32.8 MB) take 54.6 us: max 8.5 (3.9 TB/s), hist 17.5, cut 14.2, pick 17.  hist is 31 vector
-// instructions an id, a third of its time, and waits for the rest: the chain of a row's
-// maximum, its bins and its last workgroup.  One row is latency and the fetch of code that
-// runs once: 128256 bf16 21.2 us in four launches, 2000 10.9 in one.
+// (32.8 MB), each with its own limits, take 55.4 us: max 8.4 (3.9 TB/s), hist 17.6, cut 14.2, pick 17.
+// max is bound by its bytes.  hist and pick are chains: with top-k and top-p, 16, 32, 64 and 128
+// rows take 20.2, 19.6, 21.1 and 29.6 us in hist, 9.8, 9.9, 10.1 and 10.3 in pick.  hist's is the row's
+// maximum, the bins in LDS, their addition to the row's in memory by every workgroup, and the cut
+// by the last one; one row of 32 workgroups takes 9.5.  What it works on, 31 vector instructions an
+// id, shows above 64 rows only (8.5 us for 8.2 million ids).  cut reads as max does where k leaves
+// out most ids by their bin (8.1 us), and forms every id's weight where there is no limit
+// (14.8) or p alone, which leaves most of the weight in (14.6).  pick's chain is longer where p
+// ends among many ids: 8.4 us without limits, 10.4 with k, 12.5 with p.
+// One row is latency and the fetch of code that runs once: 128256 bf16 in four launches 17.5 us
+// with min-p, 18.5 without limits, 25.3 with k, 27.1 with k and p, 30.8 with p, 13.1 for
+// the largest logit alone; 2000 10.9 in one.
 #pragma once
 
 #include "elem.hpp"

@@ -39,15 +39,21 @@ static_assert(sats::kThreads == 256, "");
 
 // Rotation: waves that fill the chip.
 constexpr int64_t kRopeWaves = 4096;
-// Parts up to which one wave joins a row.
+// Parts up to which one wave joins a row, four above.  us where the limit is 8, 16, 32, 64: a sequence
+// of 4000 keys (16 parts) 12.2, 13.3, 13.3, 13.3; of 6000 12.6, 12.6, 14.5, 14.5; of 16000 (63) 22.5, 22.5,
+// 22.5, 34.3; 128 new tokens on 4000, whose tiles have 128 rows, 38.9, 35.4, 35.3, 35.3.
 constexpr int kJoinWave = 16;
 // Attention: workgroups that the chip holds at once (two a compute unit; of the kernels for
 // heads above 128 one, of the 16-row kernels for heads up to 96 three), which a launch that
-// splits its tiles aims at: a few more would wait for a second round.  8 sequences of 2000 to 6000 keys: 512 workgroups 30.8 us, 768 38.1.
+// splits its tiles aims at: a few more would wait for a second round.  8 sequences of 2000 to 6000
+// keys: 512 workgroups 30.8 us, 768 38.1.
 // Tiles of 16 rows whose parts stay at kLongBlocks blocks or more are split over up to
 // kSlotsLong workgroups, since sequences of different lengths then share the chip more
 // evenly (64 sequences of 500 to 8000 keys 156 -> 150 us).
-// Key blocks below which no tile is split.
+// Key blocks of a part, at least, of 16 rows and of 128.  us for 4, 8, 16 blocks of 16 rows: a sequence
+// of 500 keys 10.1, 11.8, 14.8; of 2000 11.5, 12.5, 16.4; of 4000 10.7, 13.3, 16.7; of 8000 16.0, 14.2, 20.1.
+// For 2, 4, 8 blocks of 128: 64 new tokens on 500 18.8, 21.2, 26.6; on 2000 25.5, 23.6, 28.2; 256 on 1000
+// 34.5, 34.2, 31.5; 512 alone 31.8, 31.0, 32.6.
 constexpr int kSlots = 512, kSlotsLong = 2048, kLongBlocks = 24, kRowsLeast = 8, kTileLeast = 4;
 
 int launched(const char *what) {
