@@ -28,15 +28,22 @@ namespace {
 
 thread_local std::string g_err;
 
+// (without host memory for its text, an error keeps its code)
+void set_error(const char *text) try { g_err = text; } catch (const std::exception &) {
+}
+
 int fail(int code, const char *fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
-  g_err = buf;
+  set_error(buf);
   return code;
 }
+
+// A call that ran out of host memory: nothing is thrown through the C entry points.
+int no_host_memory() { return fail(SATS_ERR_WORKSPACE, "out of host memory"); }
 
 #define HIP_TRY(expr)                                                                   \
   do {                                                                                  \
@@ -515,7 +522,7 @@ using sats_host::Turn;
 std::mutex g_turns_mu;
 std::map<std::pair<int, hipStream_t>, std::mutex> g_turns;
 
-int take_turn(hipStream_t stream, Turn *turn) {
+int take_turn(hipStream_t stream, Turn *turn) try {
   int dev = 0;
   HIP_TRY(hipGetDevice(&dev));
   std::mutex *m;
@@ -525,6 +532,8 @@ int take_turn(hipStream_t stream, Turn *turn) {
   }
   *turn = Turn(*m);
   return SATS_OK;
+} catch (const std::exception &) {
+  return no_host_memory();
 }
 
 // Whether the stream records a graph (or another does and forbids calls here).
@@ -1355,7 +1364,7 @@ int run_lora(const Call &c, bool vec_ok) {
 }
 
 template <typename T>
-int run(const Call &c) {
+int run(const Call &c) try {
   if (!c.x || !c.Wg || !c.Wu || !c.Wd || !c.out) return fail(SATS_ERR_NULL, "x, weights and out must be non-null");
   if (c.route_mode != sats::ROUTE_BASE && !c.thr) return fail(SATS_ERR_NULL, "thresholds must be non-null");
   if (c.route_mode == sats::ROUTE_LUT && !c.ids) return fail(SATS_ERR_NULL, "token_ids must be non-null when route_lut is given");
@@ -1462,6 +1471,8 @@ int run(const Call &c) {
     if (rc) return rc;
   }
   return SATS_OK;
+} catch (const std::exception &) {
+  return no_host_memory();
 }
 
 Call make_call(const void *x, const int32_t *ids, const void *Wg, const void *Wu, const void *Wd,
@@ -2117,7 +2128,7 @@ int fail(int code, const char *fmt, ...) {
   va_start(ap, fmt);
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
-  g_err = buf;
+  set_error(buf);
   return code;
 }
 void clear_error() { g_err.clear(); }
@@ -2143,8 +2154,8 @@ int serve_workspace(hipStream_t stream, size_t bytes, char **mem, Turn *turn) tr
   if (capturing) w.serve_captured = true;
   *mem = w.serve;
   return SATS_OK;
-} catch (const std::exception &) {  // (host memory: nothing is thrown through the C entry points)
-  return SATS_ERR_WORKSPACE;
+} catch (const std::exception &) {
+  return no_host_memory();
 }
 
 }  // namespace sats_host
@@ -2253,14 +2264,16 @@ int sats_mlp_forward_lora_f32(const float *x, const int32_t *token_ids, const fl
 
 int sats_route_table(const float *loss_base, const float *loss_sparse, const int32_t *token_ids, int64_t n_tokens,
                      const int32_t *heldout_ids, int64_t n_heldout, int64_t vocab, double r_tar,
-                     uint8_t *route_lut, double *scores, double *tau_out, double *realized_out, hipStream_t stream) {
+                     uint8_t *route_lut, double *scores, double *tau_out, double *realized_out, hipStream_t stream) try {
   g_err.clear();
   return route_build(loss_base, loss_sparse, token_ids, n_tokens, heldout_ids, n_heldout, vocab, r_tar, route_lut,
                      scores, tau_out, realized_out, stream);
+} catch (const std::exception &) {
+  return no_host_memory();
 }
 
 int sats_reserve(int64_t max_tokens, int64_t d, int64_t d_ff, int64_t n_layers, int elem_bytes,
-                 hipStream_t stream) {
+                 hipStream_t stream) try {
   g_err.clear();
   if (elem_bytes != 2 && elem_bytes != 4) return fail(SATS_ERR_ARG, "elem_bytes must be 2 or 4");
   if (d < 1 || d_ff < 1 || max_tokens < 1 || n_layers < 1 || d > (1 << 24) || d_ff > (1 << 24))
@@ -2288,9 +2301,11 @@ int sats_reserve(int64_t max_tokens, int64_t d, int64_t d_ff, int64_t n_layers, 
   for (const int64_t n : {std::min<int64_t>(max_tokens, kMaxPass), max_tokens})
     if (!rc && pf_shape(elem_bytes, true, n, d, d_ff)) rc = reserve_tiled(stream, n, d, d_ff, elem_bytes);
   return rc;
+} catch (const std::exception &) {
+  return no_host_memory();
 }
 
-int sats_release(void) {
+int sats_release(void) try {
   g_err.clear();
   int cur = 0;
   HIP_TRY(hipGetDevice(&cur));
@@ -2317,12 +2332,14 @@ int sats_release(void) {
   if (!rc) rc = cal_release_all();
   HIP_TRY(hipSetDevice(cur));
   return rc;
+} catch (const std::exception &) {
+  return no_host_memory();
 }
 
 int sats_calibration_curves(const sats_bf16 *h, const sats_bf16 *W_gate, const sats_bf16 *W_up_T,
                             const sats_bf16 *W_down, int64_t n, int64_t d, int64_t d_ff, const double *levels,
                             int64_t n_levels, float *t_out, double *err_out, double *sp_out, float *err_rows,
-                            hipStream_t stream) {
+                            hipStream_t stream) try {
   g_err.clear();
   if (!h || !W_gate || !W_up_T || !W_down || !levels || !t_out || !err_out || !sp_out)
     return fail(SATS_ERR_NULL, "h, weights, levels and the outputs must be non-null");
@@ -2340,12 +2357,14 @@ int sats_calibration_curves(const sats_bf16 *h, const sats_bf16 *W_gate, const s
   const hipError_t se = hipStreamSynchronize(stream);  // also on an error: the next call reuses the buffers
   if (!rc && se != hipSuccess) return fail(SATS_ERR_HIP, "%s", hipGetErrorString(se));
   return rc;
+} catch (const std::exception &) {
+  return no_host_memory();
 }
 
 int sats_calibrate_sats(const sats_bf16 *x_cal, int64_t n_cal, const sats_bf16 *W_gate, const sats_bf16 *W_up_T,
                         const sats_bf16 *W_down, int64_t d, int64_t d_ff, int64_t n_layers, double s_tar,
                         double coarse_step, double fine_step, int guardrail, float *thresholds_out,
-                        double *budget_out, double *realized_out, hipStream_t stream) {
+                        double *budget_out, double *realized_out, hipStream_t stream) try {
   g_err.clear();
   if (!x_cal || !W_gate || !W_up_T || !W_down || !thresholds_out)
     return fail(SATS_ERR_NULL, "x_cal, weights and thresholds_out must be non-null");
@@ -2353,6 +2372,8 @@ int sats_calibrate_sats(const sats_bf16 *x_cal, int64_t n_cal, const sats_bf16 *
                            guardrail, thresholds_out, budget_out, realized_out, stream);
   if (!rc) HIP_TRY(hipStreamSynchronize(stream));
   return rc;
+} catch (const std::exception &) {
+  return no_host_memory();
 }
 
 const char *sats_last_error(void) { return g_err.c_str(); }
@@ -2400,7 +2421,7 @@ int sats_query_path(int64_t n_tokens, int64_t d, int64_t d_ff, int elem_bytes, i
   return SATS_OK;
 }
 
-int sats_device_status(hipStream_t stream) {
+int sats_device_status(hipStream_t stream) try {
   g_err.clear();
   int dev = 0;
   HIP_TRY(hipGetDevice(&dev));
@@ -2431,9 +2452,11 @@ int sats_device_status(hipStream_t stream) {
   }
   if (raised) return fail(SATS_ERR_DEVICE, "a bounded device-side wait gave up (results of the affected call are invalid)");
   return SATS_OK;
+} catch (const std::exception &) {
+  return no_host_memory();
 }
 
-int sats_timing_begin(int kind, int capacity) {
+int sats_timing_begin(int kind, int capacity) try {
   g_err.clear();
   if (kind < 0 || kind >= SATS_K_COUNT || capacity < 1) return fail(SATS_ERR_ARG, "bad timing request");
   std::lock_guard<std::mutex> lk(g_timer_mu);
@@ -2449,6 +2472,8 @@ int sats_timing_begin(int kind, int capacity) {
   t.used = 0;
   t.armed = true;
   return SATS_OK;
+} catch (const std::exception &) {
+  return no_host_memory();
 }
 
 int sats_timing_end(int kind, double *total_ms, int64_t *count) {

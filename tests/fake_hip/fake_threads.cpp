@@ -22,7 +22,9 @@
 #undef __hipPopCallConfiguration
 
 #include <chrono>
+#include <cstdlib>
 #include <mutex>
+#include <new>
 #include <thread>
 
 namespace {
@@ -43,7 +45,20 @@ int launch_by(const void *f, Dim grid) {
 }
 }  // namespace
 
+// Host memory that runs out: while fake_no_memory is set, nothing can be allocated with `new`.
+namespace {
+bool g_no_memory = false;
+}
+void *operator new(size_t n) {
+  void *p = g_no_memory ? nullptr : malloc(n ? n : 1);
+  if (!p) throw std::bad_alloc();
+  return p;
+}
+void operator delete(void *p) noexcept { free(p); }
+void operator delete(void *p, size_t) noexcept { free(p); }
+
 extern "C" {
+void fake_no_memory(int on) { g_no_memory = on; }
 void fake_thread(int k) { g_thread = k; }
 int hipLaunchKernel(const void *f, Dim grid, Dim, void **, size_t, void *) { return launch_by(f, grid); }
 int hipExtLaunchKernel(const void *f, Dim grid, Dim, void **, size_t, void *, void *, void *, int) {

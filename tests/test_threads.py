@@ -1,6 +1,6 @@
-"""Calls on one stream from several threads, without a GPU: the launches of a call hand
-each other results in the stream's workspace, so another thread's come before or after
-them, and a buffer is freed when nobody is about to use it."""
+"""Calls on one stream from several threads, and calls without host memory, on a stand-in
+runtime: the launches of a call hand each other results in the stream's workspace, so another
+thread's come before or after them, and a buffer is freed when nobody is about to use it."""
 import os
 import subprocess
 
@@ -121,3 +121,34 @@ print(json.dumps(together(lambda: on(8, 1, 100000), lambda: on(16, 1, 100000), e
     assert len(got) == 64
     with pytest.raises(AssertionError):
         runs(got, [4, 4])
+
+
+WS = -4
+CALLS = {"extend": "extend(8, 500)", "sample": "sample(2, 100000)", "attend": "attend(2, 2, 1, 30000)",
+         "batch": "fwd(8, 512, 1024, L=3)", "token": "fwd(1, 512, 1024)", "float32": "fwd(5, 512, 1024, 'f32')",
+         "reserve": "reserve(8, 512, 1024)", "serving": "lib.sats_reserve_serving(I(8), I(500), I(0), I(0), I(128), P(0))",
+         "release": "lib.sats_release()"}
+
+
+@pytest.mark.parametrize("what", sorted(CALLS))
+def test_without_host_memory_a_call_is_refused_and_works_again(run, what):
+    """Nothing is thrown through the C entry points, no lock stays held, and the next call is as ever."""
+    before, rc, after = run(f"""
+call = lambda: {CALLS[what]}
+rcs = [call()]
+{"assert fwd(8, 512, 1024, L=3) == 0" if what == "release" else "lib.sats_release()"}
+fake.fake_no_memory(1)
+rc = call()
+fake.fake_no_memory(0)
+assert b"memory" in lib.sats_last_error() or not lib.sats_last_error()
+print(json.dumps([rcs[0], rc, call()]))""")
+    assert (before, rc, after) == (0, WS, 0)
+
+
+def test_without_host_memory_a_refusal_keeps_its_code(run):
+    rcs = run("""
+fake.fake_no_memory(1)
+rcs = [sample(-1, 100), sample(1, 0), attend(1, 1, 1, 1 << 40), fwd(-1, 512, 1024)]
+fake.fake_no_memory(0)
+print(json.dumps(rcs))""")
+    assert rcs == [-2] * 4
