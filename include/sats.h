@@ -378,7 +378,7 @@ int sats_query_path(int64_t n_tokens, int64_t d, int64_t d_ff, int elem_bytes, i
 
 /*
  * Serving: what a token passes between two MLPs, and from the last one to the
- * next id.  bf16 or float32 throughout (elem_bytes 2 or 4), sums and softmax
+ * next id.  bf16 or float32 throughout (elem_bytes 2 or 4; a cache also 8 bits), sums and softmax
  * statistics in float32 or wider, each result rounded once.
  *
  * Keys and values are kept in pages of page_size tokens.  A cache holds them
@@ -416,6 +416,42 @@ typedef struct {
   const int32_t *table, *q_start, *kv_len; /* device */
   int64_t n_seqs, max_pages, n_tokens, max_q_len, max_kv_len;
 } sats_kv_batch;
+
+/*
+ * A cache of 8 bits: every call that takes a cache takes &c8.kv, whose elem_bytes says
+ * the format.  k and v hold codes, a byte each, and the scale arrays (of any alignment) a byte b for
+ * each row of head_dim codes (a token's head):
+ *   k_scale, v_scale   [n_layers][n_pages][n_kv_heads][page_size]
+ * Code c stands for c 2^(b - 127), and for NaN where b is 255.  Codes are E4M3 numbers (4 bits
+ * of exponent, 3 of mantissa, 448 at most, 0x7f and 0xff NaN) or whole numbers from -127 to 127.
+ * A row is written with the smallest b from 1 to 254 for which its largest magnitude is
+ * within the codes, each value to the nearest code, ties to even (at most, one that does not
+ * read as an infinity); a row that holds an infinity or NaN as zeros under 255.  Values are
+ * attended to, and read, as bf16 holds them, which is exactly (below 2^-126: cut off or rounded to its
+ * step).
+ * page_size is at least 16 and head_dim a multiple of 16.  q_elem_bytes (2 or 4) is the
+ * type of what is appended and of the queries and results of an attention over the cache.
+ */
+enum { SATS_KV_E4M3 = 17, SATS_KV_INT8 = 18 }; /* elem_bytes of a sats_kv_cache8's kv */
+typedef struct {
+  sats_kv_cache kv;
+  uint8_t *k_scale, *v_scale;
+  int32_t q_elem_bytes;
+} sats_kv_cache8;
+
+/*
+ * Groups of a batch's sequences that share a prefix (sats_prefix_attention): the sequences seq_start[g] ..
+ * seq_start[g + 1] - 1 (which follow each other in the batch) have their first len[g] tokens
+ * in common (as far as each has them), as after sats_cache_fork.  seq_start [n_groups + 1] and len [n_groups]
+ * are device data; sequences outside of every group, and groups of one or with no
+ * prefix, are fine.  max_tokens (new tokens of a group), max_len (of a prefix) and max_own (of
+ * any sequence's tokens behind its prefix, the new ones included) are upper bounds on the host:
+ * what is beyond them is cut off.
+ */
+typedef struct {
+  const int32_t *seq_start, *len; /* device */
+  int64_t n_groups, max_tokens, max_len, max_own;
+} sats_kv_prefix;
 
 typedef struct {
   int32_t *table, *len, *refs; /* device */
@@ -466,6 +502,26 @@ int sats_qkv_append(const void *q, int64_t q_stride, const void *k, int64_t k_st
 int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *cache, int64_t layer,
                          const sats_kv_batch *batch, int64_t n_q_heads, float scale, int64_t window, int64_t n_sinks,
                          void *out, float *lse, hipStream_t stream);
+
+/*
+ * The same attention for a batch whose sequences share prefixes: the keys of a
+ * prefix are read once for all rows of its group (from the pages of the first of its
+ * sequences that is as long; shorter ones see of it what they have), the others from each sequence's own.  Results agree with sats_paged_attention's
+ * within rounding.  Scratch memory as said at sats_reserve_prefix.
+ */
+int sats_prefix_attention(const void *q, int64_t q_stride, const sats_kv_cache *cache, int64_t layer,
+                          const sats_kv_batch *batch, const sats_kv_prefix *prefix, int64_t n_q_heads, float scale,
+                          int64_t window, int64_t n_sinks, void *out, float *lse, hipStream_t stream);
+
+/*
+ * Keys and values of the batch's tokens as they are in `layer` of the cache (of any format):
+ * token t's go to row t of k_out and v_out, [n_tokens][n_kv_heads][head_dim] of elem_bytes (2 or
+ * 4) at strides in elements; either may be NULL.  With q_start the running sums of kv_len that
+ * reads whole sequences.  A token whose page is not there reads zeros; rows that are of
+ * no sequence stay as they were.  The outputs may not overlap each other or the cache.
+ */
+int sats_cache_read(const sats_kv_cache *cache, int64_t layer, const sats_kv_batch *batch, void *k_out, int64_t k_stride,
+                    void *v_out, int64_t v_stride, int elem_bytes, hipStream_t stream);
 
 /*
  * Bookkeeping of the pages, on the device.  A call takes n items (up to 65535;
@@ -521,6 +577,47 @@ int sats_cache_copy(const sats_kv_cache *cache, const int32_t *src_pages, const 
 int sats_sample(const void *logits, int elem_bytes, int64_t stride, int64_t n, int64_t vocab, const float *temperature,
                 const int32_t *top_k, const float *top_p, const float *min_p, const float *u, int32_t *tokens,
                 float *prob, int32_t *n_kept, hipStream_t stream);
+
+/*
+ * Rules on logits, ahead of sats_sample: out = logits [n][vocab] after, in this order and in float32,
+ *   l <- l / repetition (l > 0) or l repetition (else)   ids among the row's ids so far
+ *   l <- l - frequency count - presence [count > 0]      count: of the id in the answer
+ *   l <- l + the sum of the id's biases, in their order
+ *   l <- -infinity                                       ids without a bit in the row's mask
+ * each rounded once to the type of out (elem_bytes and out_elem_bytes: 2 or 4; strides in elements).
+ * out may be logits itself (same stride and type): logits that no rule changes are then not touched;
+ * other overlap is rejected.  All arrays are on the device; max_history, n_bias or n_masks 0: no such rule:
+ *   history        [n_seqs][history_stride] ids so far, the prompt first: of row i the first history_len[s] of row
+ *                  s = seqs[i] (seqs NULL: i), at most max_history; from prompt_len[s] on (NULL: 0) they are
+ *                  the answer
+ *   repetition, frequency, presence   [n], a number a row (NULL: 1, 0, 0)
+ *   bias_ids, bias [n_bias] ids and what is added to them, of row i from bias_start[i] to bias_start[i + 1] - 1
+ *   masks          [n_masks][mask_stride] bits, id x in bit x % 32 of word x / 32; row i has mask
+ *                  mask_of[i] (NULL: i), none where that is no mask
+ * Ids outside the vocabulary are passed over, lengths cut off to their arrays.  vocab <= 2^22, n < 65536.
+ */
+typedef struct {
+  const int32_t *seqs, *history, *history_len, *prompt_len;
+  int64_t n_seqs, history_stride, max_history;
+  const float *repetition, *frequency, *presence;
+  const int32_t *bias_start, *bias_ids;
+  const float *bias;
+  int64_t n_bias;
+  const uint32_t *masks;
+  const int32_t *mask_of;
+  int64_t n_masks, mask_stride;
+} sats_logit_rules;
+int sats_adjust_logits(const void *logits, int elem_bytes, int64_t stride, const sats_logit_rules *rules, void *out,
+                       int out_elem_bytes, int64_t out_stride, int64_t n, int64_t vocab, hipStream_t stream);
+
+/*
+ * Allocate the scratch memory of (current device, stream) for sats_prefix_attention calls with these
+ * sizes (of cache, batch and prefix; their pointers may be NULL): the batch's rows, n_q_heads a
+ * token, in each of the parts that a launch splits their keys into, head_dim + 2 floats each.  Else as
+ * sats_reserve_serving, which covers the other calls; a stream's scratch memory is one for all.
+ */
+int sats_reserve_prefix(const sats_kv_cache *cache, const sats_kv_batch *batch, const sats_kv_prefix *prefix, int64_t n_q_heads,
+                        hipStream_t stream);
 
 /*
  * Allocate the scratch memory of (current device, stream) for serving calls: page calls

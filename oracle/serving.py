@@ -1,5 +1,6 @@
-"""The serving operators in 64 bits: head norms and rotation, attention over a paged
-cache, the bookkeeping of its pages, and sampling from given numbers."""
+"""The serving operators in 64 bits: head norms and rotation, the rows of a cache of 8 bits,
+attention over a paged cache, the bookkeeping of its pages, rules on logits, and sampling from
+given numbers."""
 from __future__ import annotations
 
 import math
@@ -46,6 +47,84 @@ def attend_row(q, keys, values, seen, scale):
     with np.errstate(all="ignore"):
         return (p @ v, float(top + np.log(np.exp(s - top).sum())), p @ np.abs(v),
                 float(abs(scale) * (np.abs(k) @ np.abs(np.asarray(q, np.float64))).max()))
+
+
+def e4m3_values():
+    """The numbers of the codes 0 .. 255 (NaN for 0x7f and 0xff)."""
+    c = np.arange(256)
+    e, m = c >> 3 & 15, c & 7
+    v = np.where(e > 0, (8.0 + m) * 2.0 ** (e - 10.0), m * 2.0 ** -9)
+    v[(c & 127) == 127] = np.nan
+    return np.where(c >= 128, -v, v)
+
+
+def code_values(form):
+    """The numbers that the bytes 0 .. 255 stand for under a scale of 1."""
+    return e4m3_values() if form == "e4m3" else np.arange(256).astype(np.int8).astype(np.float64)
+
+
+def row_byte(top, form):
+    """The scale byte of a row whose largest magnitude is `top`."""
+    if not np.isfinite(top):
+        return 255
+    most, b = (448.0 if form == "e4m3" else 127.0), 1
+    while top > most * 2.0 ** (b - 127):
+        b += 1
+    return b
+
+
+def quantise(x, form):
+    """Rows x [..][dim] as (codes, scale bytes): the nearest code of each number, ties to even."""
+    x = np.asarray(x, np.float64)
+    flat = x.reshape(-1, x.shape[-1])
+    values = code_values(form)
+    up = np.nonzero(~np.isnan(values) & ((values > 0) | (np.arange(256) == 0)))[0]  # codes from 0 up
+    if form == "int8":
+        up = np.arange(128)
+    codes, scale = np.zeros(flat.shape, np.uint8), np.zeros(len(flat), np.uint8)
+    for i, row in enumerate(flat):
+        b = row_byte(np.abs(row).max(), form) if not np.isnan(row).any() else 255
+        scale[i] = b
+        if b == 255:
+            continue
+        unit = 2.0 ** (b - 127)
+        ok = up[values[up] * unit < 2.0 ** 128]  # (what reads as an infinity is not taken)
+        v, y = values[ok] * unit, np.abs(row)
+        hi = np.clip(np.searchsorted(v, y), 1, len(v) - 1)
+        lo = hi - 1
+        below, above = y - v[lo], v[hi] - y
+        pick = np.where((below < above) | ((below == above) & (ok[lo] % 2 == 0)), ok[lo], ok[hi])
+        if form == "e4m3":
+            codes[i] = np.where(np.signbit(row), pick | 128, pick)
+        else:
+            codes[i] = np.where(row < 0, -pick, pick).astype(np.int8).view(np.uint8)
+    return codes.reshape(x.shape), scale.reshape(x.shape[:-1])
+
+
+def dequantise(codes, scale, form):
+    """What codes [..][dim] under scale bytes [..] stand for."""
+    scale = np.asarray(scale, np.float64)
+    unit = np.where(scale == 255, np.nan, 2.0 ** (scale - 127.0))
+    return code_values(form)[codes] * unit[..., None]
+
+
+def adjust_logits(x, told=(), prompt=0, repetition=1.0, frequency=0.0, presence=0.0, biases=(), mask=None):
+    """A row of logits under its rules; told: the ids so far; biases: (id, number) pairs; mask: ids allowed (or None)."""
+    x = np.array(x, np.float64)
+    count = {}
+    for i, t in enumerate(told):
+        if 0 <= t < len(x):
+            count[t] = count.get(t, 0) + (i >= prompt)
+    for t, c in count.items():
+        x[t] = x[t] / repetition if x[t] > 0 else x[t] * repetition
+        if c:
+            x[t] -= frequency * c + presence
+    for t, v in biases:
+        if 0 <= t < len(x):
+            x[t] += v
+    if mask is not None:
+        x[~np.asarray(mask, bool)] = -math.inf
+    return x
 
 
 class Pages:

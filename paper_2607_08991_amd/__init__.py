@@ -17,4 +17,6 @@ from ._lib import (  # noqa: F401
     SATS_K_DEC_REDUCE, SATS_K_DENSE_DOWN, SATS_K_DEC_REDUCE_LORA, SATS_K_ROUTE_MERGE,
     KVCache, KVBatch, KVPages, sats_qk_norm_rope, sats_qkv_append, sats_paged_attention, sats_cache_extend,
     sats_cache_fork, sats_cache_free, sats_cache_compact, sats_cache_copy, sats_sample, sats_reserve_serving,
+    KVPrefix, LogitRules, sats_prefix_attention, sats_cache_read, sats_adjust_logits, sats_reserve_prefix,
+    SATS_KV_E4M3, SATS_KV_INT8,
 )

@@ -26,6 +26,7 @@ SATS_K_ROUTE_MERGE = 14
 SATS_BATCH_AUTO, SATS_BATCH_MFMA, SATS_BATCH_SPLIT, SATS_BATCH_COMPACT = 0, 1, 2, 3
 SATS_SINGLE_AUTO, SATS_SINGLE_OFF = 0, 1
 SATS_PATH_SINGLE_TOKEN, SATS_PATH_BATCH_MFMA, SATS_PATH_BATCH_SPLIT, SATS_PATH_BATCH_COMPACT = 1, 2, 3, 4
+SATS_KV_E4M3, SATS_KV_INT8 = 17, 18
 
 
 class SatsOptions(ctypes.Structure):
@@ -41,6 +42,13 @@ class SatsKvCache(ctypes.Structure):
                 ("head_dim", ctypes.c_int64), ("elem_bytes", ctypes.c_int32)]
 
 
+class SatsKvCache8(ctypes.Structure):
+    """sats_kv_cache8 of include/sats.h."""
+    _anonymous_ = ("kv",)
+    _fields_ = [("kv", SatsKvCache), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("q_elem_bytes", ctypes.c_int32)]
+
+
 class SatsKvBatch(ctypes.Structure):
     """sats_kv_batch of include/sats.h."""
     _fields_ = [("table", ctypes.c_void_p), ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
@@ -52,6 +60,22 @@ class SatsKvPages(ctypes.Structure):
     """sats_kv_pages of include/sats.h."""
     _fields_ = [("table", ctypes.c_void_p), ("len", ctypes.c_void_p), ("refs", ctypes.c_void_p),
                 ("n_seqs", ctypes.c_int64), ("max_pages", ctypes.c_int64)]
+
+
+class SatsKvPrefix(ctypes.Structure):
+    """sats_kv_prefix of include/sats.h."""
+    _fields_ = [("seq_start", ctypes.c_void_p), ("len", ctypes.c_void_p), ("n_groups", ctypes.c_int64),
+                ("max_tokens", ctypes.c_int64), ("max_len", ctypes.c_int64), ("max_own", ctypes.c_int64)]
+
+
+class SatsLogitRules(ctypes.Structure):
+    """sats_logit_rules of include/sats.h."""
+    _fields_ = [("seqs", ctypes.c_void_p), ("history", ctypes.c_void_p), ("history_len", ctypes.c_void_p),
+                ("prompt_len", ctypes.c_void_p), ("n_seqs", ctypes.c_int64), ("history_stride", ctypes.c_int64),
+                ("max_history", ctypes.c_int64), ("repetition", ctypes.c_void_p), ("frequency", ctypes.c_void_p),
+                ("presence", ctypes.c_void_p), ("bias_start", ctypes.c_void_p), ("bias_ids", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p), ("n_bias", ctypes.c_int64), ("masks", ctypes.c_void_p),
+                ("mask_of", ctypes.c_void_p), ("n_masks", ctypes.c_int64), ("mask_stride", ctypes.c_int64)]
 
 
 # exported symbols and their argument types (p = pointer, i = int64, s = stream, n = int32)
@@ -90,6 +114,10 @@ SIGNATURES = {
     "sats_cache_copy": ([_P] * 3 + [_I, _S], _N),
     "sats_sample": ([_P, _N, _I, _I, _I] + [_P] * 8 + [_S], _N),
     "sats_reserve_serving": ([_I] * 5 + [_S], _N),
+    "sats_prefix_attention": ([_P, _I, _P, _I, _P, _P, _I, _F, _I, _I, _P, _P, _S], _N),
+    "sats_cache_read": ([_P, _I, _P, _P, _I, _P, _I, _N, _S], _N),
+    "sats_adjust_logits": ([_P, _N, _I, _P, _P, _N, _I, _I, _I, _S], _N),
+    "sats_reserve_prefix": ([_P, _P, _P, _I, _S], _N),
     "sats_calibrate_sats": ([_P, _I] + [_P] * 3 + [_I] * 3 + [ctypes.c_double] * 3 + [_N] + [_P] * 3 + [_S], _N),
 }
 
@@ -396,16 +424,38 @@ def _heads(t, dtype, name, shape):
 
 
 class KVCache:
-    """Keys and values of every layer in pages: k, v [n_layers][n_pages][n_kv_heads][page_size][head_dim]."""
+    """Keys and values of every layer in pages: k, v [n_layers][n_pages][n_kv_heads][page_size][head_dim].
 
-    __slots__ = ("k", "v", "dtype", "c", "ref")
+    In bfloat16 or float32; or in 8 bits, k and v being float8_e4m3fn or int8 codes with a scale byte a
+    row (k_scale, v_scale uint8 [n_layers][n_pages][n_kv_heads][page_size]), and dtype (bfloat16 or float32)
+    the type of what is appended and of queries and results.
+    """
 
-    def __init__(self, k, v):
-        shape, esz = k.shape, _elem_bytes(k)
+    __slots__ = ("k", "v", "k_scale", "v_scale", "dtype", "c", "ref")
+
+    def __init__(self, k, v, k_scale=None, v_scale=None, dtype=None):
+        shape = k.shape
         if len(shape) != 5 or shape != v.shape or k.dtype is not v.dtype:
             raise ValueError("k and v must be alike: [n_layers][n_pages][n_kv_heads][page_size][head_dim]")
-        self.k, self.v, self.dtype = k, v, k.dtype
-        self.c = SatsKvCache(_ptr(k), _ptr(v), *shape, esz)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        if k_scale is None and v_scale is None:
+            esz = _elem_bytes(k)
+            if dtype is not None and dtype is not k.dtype:
+                raise ValueError("dtype is that of k and v, or of an 8-bit cache's queries")
+            self.dtype = k.dtype
+            self.c = SatsKvCache(_ptr(k), _ptr(v), *shape, esz)
+        else:
+            torch = _torch or _setup()
+            form = SATS_KV_E4M3 if k.dtype is torch.float8_e4m3fn else SATS_KV_INT8 if k.dtype is torch.int8 else None
+            if form is None or k_scale is None or v_scale is None:
+                raise ValueError("k and v of float8_e4m3fn or int8 have scales, k_scale and v_scale")
+            if k_scale.shape != shape[:4] or v_scale.shape != shape[:4]:
+                raise ValueError("k_scale and v_scale must be [n_layers][n_pages][n_kv_heads][page_size]")
+            self.dtype = dtype or torch.bfloat16
+            if self.dtype is not torch.bfloat16 and self.dtype is not torch.float32:
+                raise ValueError(f"bfloat16 or float32 is required, got {dtype}")
+            self.c = SatsKvCache8(SatsKvCache(_ptr(k), _ptr(v), *shape, form), _array(k_scale, torch.uint8, None, "k_scale"),
+                                  _array(v_scale, torch.uint8, None, "v_scale"), 2 if self.dtype is torch.bfloat16 else 4)
         self.ref = ctypes.byref(self.c)
 
 
@@ -440,6 +490,77 @@ class KVPages:
         self.n_pages = refs.numel()
         self.c = SatsKvPages(_i32(table, None, "table"), _i32(len, n, "len"), _i32(refs, self.n_pages, "refs"), n, width)
         self.ref = ctypes.byref(self.c)
+
+
+class KVPrefix:
+    """Groups of a batch's sequences that share a prefix (sats_kv_prefix).
+
+    Sequences seq_start[g] .. seq_start[g + 1] - 1 have their first len[g] tokens in common; both are device
+    int32, [n_groups + 1] and [n_groups].  max_tokens (new tokens of a group), max_len (of a prefix) and max_own
+    (a sequence's tokens behind its prefix) are upper bounds.
+    """
+
+    __slots__ = ("keep", "c", "ref")
+
+    def __init__(self, seq_start, len, max_tokens, max_len, max_own):
+        n = len.numel()
+        self.keep = (seq_start, len)
+        self.c = SatsKvPrefix(_i32(seq_start, n + 1, "seq_start"), _i32(len, n, "len"), n, max_tokens, max_len, max_own)
+        self.ref = ctypes.byref(self.c)
+
+
+class LogitRules:
+    """Rules on n rows of logits (sats_logit_rules); every array is on the device, None where a rule is not wanted.
+
+    history int32 [n_seqs][width] ids so far (rows may be strided), the first history_len[s] of row s = seqs[i] (i)
+    for row i, from prompt_len[s] on the answer's; repetition, frequency, presence float32 [n]; bias_start int32
+    [n + 1], bias_ids int32 and bias float32 [n_bias]; masks int32 [n_masks][words] (rows may be strided), a bit
+    an id, mask_of int32 [n] (no mask where it is none's number).
+    """
+
+    __slots__ = ("keep", "n", "vocab_words", "c", "ref")
+
+    def __init__(self, history=None, history_len=None, prompt_len=None, seqs=None, repetition=None, frequency=None,
+                 presence=None, bias_start=None, bias_ids=None, bias=None, masks=None, mask_of=None):
+        self.keep = (history, history_len, prompt_len, seqs, repetition, frequency, presence, bias_start, bias_ids, bias,
+                     masks, mask_of)
+        n = None  # rows, as far as the arrays say
+        for t, more in ((seqs, 0), (repetition, 0), (frequency, 0), (presence, 0), (mask_of, 0), (bias_start, 1)):
+            if t is not None:
+                if n is not None and t.numel() - more != n:
+                    raise ValueError("the rules' arrays of a number a row must have the same rows")
+                n = t.numel() - more
+        if history is None and any(t is not None for t in (history_len, prompt_len, repetition, frequency, presence)):
+            raise ValueError("penalties need history")
+        if (bias is None) != (bias_ids is None) or (bias is None) != (bias_start is None):
+            raise ValueError("biases need bias_start, bias_ids and bias")
+        if masks is None and mask_of is not None:
+            raise ValueError("mask_of needs masks")
+        hp, n_seqs, h_stride, width = _rows(history, "history")
+        mp, n_masks, m_stride, words = _rows(masks, "masks")
+        self.n, self.vocab_words = n, (words if masks is not None else None)
+        m = 0 if bias is None else bias.numel()
+        f = lambda t, name: _f32(t, n, name)  # noqa: E731
+        self.c = SatsLogitRules(
+            _i32(seqs, n, "seqs"), hp, _i32(history_len, n_seqs if history is not None else None, "history_len"),
+            _i32(prompt_len, n_seqs if history is not None else None, "prompt_len"), n_seqs, h_stride, width,
+            f(repetition, "repetition"), f(frequency, "frequency"), f(presence, "presence"),
+            _i32(bias_start, None, "bias_start"), _i32(bias_ids, m if bias is not None else None, "bias_ids"),
+            _f32(bias, None, "bias"), m, mp, _i32(mask_of, n, "mask_of"), n_masks, m_stride)
+        self.ref = ctypes.byref(self.c)
+
+
+def _rows(t, name):
+    """(pointer, rows, row stride, row length) of device int32 [rows][length] with dense rows."""
+    if t is None:
+        return None, 0, 0, 0
+    if t.dtype is not (_torch or _setup()).int32 or len(t.shape) != 2 or not t.is_cuda:
+        raise ValueError(f"{name}: a device int32 tensor of two dimensions is required")
+    n, m = t.shape
+    s0, s1 = t.stride()
+    if (m > 1 and s1 != 1) or (n > 1 and s0 < m):
+        raise ValueError(f"{name}: dense rows apart from each other are required")
+    return t.data_ptr(), n, (s0 if n > 1 else m), m
 
 
 def _table(table):
@@ -498,19 +619,47 @@ def sats_qkv_append(q, k, v, rope, q_out, cache, layer, batch, q_norm=None, k_no
           int(interleaved), _cur_stream(stream))
 
 
-def sats_paged_attention(q, cache, layer, batch, out, scale, window=0, n_sinks=0, lse=None, stream=None):
-    """Attention of a batch's new tokens over a layer of the cache (window 0: every earlier key)."""
+def _attend(q, cache, batch, out, lse):
+    """(pointer, token stride, heads) of q, with out and lse looked at."""
     shape, dt = q.shape, cache.dtype
     n, hq, d = shape
     if n != batch.n_tokens or d != cache.c.head_dim:
         raise ValueError("q must have the batch's tokens and the cache's head_dim")
     if out.shape != shape or out.dtype is not dt:
         raise ValueError("out must be like q")
-    qp, qs = _heads(q, dt, "q", shape)
     if lse is not None and lse.shape != (n, hq):
         raise ValueError("lse must be [n_tokens][n_q_heads]")
+    qp, qs = _heads(q, dt, "q", shape)
+    return qp, qs, hq
+
+
+def sats_paged_attention(q, cache, layer, batch, out, scale, window=0, n_sinks=0, lse=None, stream=None):
+    """Attention of a batch's new tokens over a layer of the cache (window 0: every earlier key)."""
+    qp, qs, hq = _attend(q, cache, batch, out, lse)
     _call("sats_paged_attention", qp, qs, cache.ref, layer, batch.ref, hq, scale, window, n_sinks, _ptr(out),
           _f32(lse, None, "lse"), _cur_stream(stream))
+
+
+def sats_prefix_attention(q, cache, layer, batch, prefix, out, scale, window=0, n_sinks=0, lse=None, stream=None):
+    """sats_paged_attention for a batch whose sequences share prefixes (KVPrefix), read once for each group."""
+    qp, qs, hq = _attend(q, cache, batch, out, lse)
+    _call("sats_prefix_attention", qp, qs, cache.ref, layer, batch.ref, prefix.ref, hq, scale, window, n_sinks, _ptr(out),
+          _f32(lse, None, "lse"), _cur_stream(stream))
+
+
+def sats_cache_read(cache, layer, batch, k_out, v_out, stream=None):
+    """Keys and values of a batch's tokens, as a layer of the cache holds them, in bfloat16 or float32.
+
+    k_out, v_out [n_tokens][n_kv_heads][head_dim] of one type (one of them may be None).
+    """
+    c = cache.c
+    shape = (batch.n_tokens, c.n_kv_heads, c.head_dim)
+    like = k_out if k_out is not None else v_out
+    if like is None:
+        raise ValueError("k_out or v_out is required")
+    kp, ks = (None, 0) if k_out is None else _heads(k_out, like.dtype, "k_out", shape)
+    vp, vs = (None, 0) if v_out is None else _heads(v_out, like.dtype, "v_out", shape)
+    _call("sats_cache_read", cache.ref, layer, batch.ref, kp, ks, vp, vs, _elem_bytes(like), _cur_stream(stream))
 
 
 def sats_cache_extend(cache, pages, seqs, add, status=None, stream=None):
@@ -562,6 +711,27 @@ def sats_sample(logits, u, tokens, temperature=None, top_k=None, top_p=None, min
           _f32(temperature, n, "temperature"), _i32(top_k, n, "top_k"), _f32(top_p, n, "top_p"),
           _f32(min_p, n, "min_p"), _f32(u, n, "u"), _i32(tokens, n, "tokens"), _f32(prob, n, "prob"),
           _i32(n_kept, n, "n_kept"), _cur_stream(stream))
+
+
+def sats_adjust_logits(logits, rules, out, stream=None):
+    """out = logits [n][vocab] under the rules (LogitRules); rows may be strided, out may be logits."""
+    n, vocab = logits.shape
+    if out.shape != logits.shape or not logits.is_cuda or not out.is_cuda:
+        raise ValueError("logits and out must be device tensors [n][vocab]")
+    if rules.n is not None and rules.n != n:
+        raise ValueError(f"the rules are for {rules.n} rows, the logits have {n}")
+    if rules.vocab_words is not None and rules.vocab_words * 32 < vocab:
+        raise ValueError("masks need a bit for every id")
+    (s0, s1), (o0, o1) = logits.stride(), out.stride()
+    if vocab > 1 and (s1 != 1 or o1 != 1):
+        raise ValueError("logits and out must have dense rows")
+    _call("sats_adjust_logits", logits.data_ptr(), _elem_bytes(logits), s0 if n > 1 else vocab, rules.ref, out.data_ptr(),
+          _elem_bytes(out), o0 if n > 1 else vocab, n, vocab, _cur_stream(stream))
+
+
+def sats_reserve_prefix(cache, batch, prefix, n_q_heads, stream=None):
+    """Scratch memory of sats_prefix_attention calls of these sizes, ahead of stream capture."""
+    _call("sats_reserve_prefix", cache.ref, batch.ref, prefix.ref, n_q_heads, _stream(stream))
 
 
 def sats_reserve_serving(max_items=0, n_pages=0, max_rows=0, vocab=0, head_dim=0, stream=None):

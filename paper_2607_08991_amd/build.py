@@ -8,12 +8,14 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libsats.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("sats.hip", "serve.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("sats.hip", "serve.hip", "attend.hip", "attend_prefix.hip", "attend8.hip")]
 ARCH = "gfx950"
 
 
@@ -31,15 +33,24 @@ def command(out: str = LIB):
             "-I", os.path.join(ROOT, "include"), "-o", out] + SOURCES
 
 
-def build(verbose: bool = True) -> str:
-    tmp = LIB + ".tmp"
-    cmd = command(tmp)
-    if verbose:
-        print(" ".join(cmd), flush=True)
+def _run(cmd) -> None:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         sys.stderr.write(r.stdout + r.stderr)
         raise RuntimeError(f"hipcc failed with exit code {r.returncode}")
+
+
+def build(verbose: bool = True) -> str:
+    """Each source on its own (side by side: the kernels' instances are most of the work), then the library."""
+    tmp = LIB + ".tmp"
+    flags = [a for a in command(tmp) if a not in SOURCES and a not in ("-shared", "-o", tmp)]
+    if verbose:
+        print(" ".join(command(tmp)), flush=True)
+    with tempfile.TemporaryDirectory() as folder:
+        objects = [os.path.join(folder, os.path.basename(s) + ".o") for s in SOURCES]
+        with ThreadPoolExecutor(len(SOURCES)) as pool:
+            list(pool.map(_run, [flags + ["-c", s, "-o", o] for s, o in zip(SOURCES, objects)]))
+        _run([hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp] + objects)
     os.replace(tmp, LIB)
     return LIB
 

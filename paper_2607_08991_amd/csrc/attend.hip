@@ -1,0 +1,238 @@
+// Host side of the attention over the paged cache: plans and launches, and the kernels of bf16 and
+// float32 caches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "attend_host.hpp"
+
+namespace sats_host {
+namespace {
+
+// Parts up to which one wave joins a row, four above.  us where the limit is 8, 16, 32, 64: a sequence
+// of 4000 keys (16 parts) 12.2, 13.3, 13.3, 13.3; of 6000 12.6, 12.6, 14.5, 14.5; of 16000 (63) 22.5, 22.5,
+// 22.5, 34.3; 128 new tokens on 4000, whose tiles have 128 rows, 38.9, 35.4, 35.3, 35.3.
+constexpr int kJoinWave = 16;
+// Attention: workgroups that the chip holds at once (two a compute unit; of the kernels for
+// heads above 128 one, of the 16-row kernels for heads up to 96 three), which a launch that
+// splits its tiles aims at: a few more would wait for a second round.  8 sequences of 2000 to 6000
+// keys: 512 workgroups 30.8 us, 768 38.1.
+// Tiles of 16 rows whose parts stay at kLongBlocks blocks or more are split over up to
+// kSlotsLong workgroups, since sequences of different lengths then share the chip more
+// evenly (64 sequences of 500 to 8000 keys 156 -> 150 us).
+// Key blocks of a part, at least, of 16 rows and of 128.  us for 4, 8, 16 blocks of 16 rows: a sequence
+// of 500 keys 10.1, 11.8, 14.8; of 2000 11.5, 12.5, 16.4; of 4000 10.7, 13.3, 16.7; of 8000 16.0, 14.2, 20.1.
+// For 2, 4, 8 blocks of 128: 64 new tokens on 500 18.8, 21.2, 26.6; on 2000 25.5, 23.6, 28.2; 256 on 1000
+// 34.5, 34.2, 31.5; 512 alone 31.8, 31.0, 32.6.
+constexpr int kSlots = 512, kSlotsLong = 2048, kLongBlocks = 24, kRowsLeast = 8, kTileLeast = 4;
+
+
+// The split of a launch: row tiles of R rows, their number at most, and over how many
+// workgroups a tile's blocks of `keys` keys go.
+struct AttendPlan {
+  int64_t tiles;
+  int splits, per_split;
+};
+// Tiles of `units` sequences or groups with up to max_q tokens each, which see `range` keys at most.
+AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, int64_t max_q, int64_t units, int64_t range) {
+  const sats::BatchView &b = a.batch;
+  const int64_t per_unit = (max_q * a.group + R - 1) / R;
+  AttendPlan p;
+  p.tiles = b.n_tokens * a.group / R + units;
+  if (units && per_unit <= p.tiles / units) p.tiles = units * per_unit;
+  range = std::min<int64_t>(range, std::min<int64_t>(b.max_kv, b.max_pages << a.pool.shift));  // keys that a tile can see
+  // (rows of several sequences have windows far from each other)
+  if (a.window && a.phase != sats::kShared) range = std::min(range, a.window + R / a.group + 1 + a.sinks + 2 * keys);
+  const int64_t blocks = std::max<int64_t>(1, (range + keys - 1) / keys + 1);
+  const int64_t wgs = std::max<int64_t>(1, p.tiles * a.pool.n_kv);
+  int64_t slots = a.dim > 128 ? kSlots / 2 : kSlots;
+  if (R == 16 && a.dim <= 96) slots = kSlots * 3 / 2;
+  int64_t want = std::max<int64_t>(1, slots / wgs);
+  if (R == 16) want = std::max(want, std::min<int64_t>(kSlotsLong / wgs, blocks / kLongBlocks));
+  p.per_split = (int)std::max<int64_t>(least, (blocks + want - 1) / want);
+  p.splits = (int)((blocks + p.per_split - 1) / p.per_split);
+  return p;
+}
+
+// The launches of a phase: of tiles of 16 rows and of 128 (tiles 0: none).  Units of at most 16 rows a cache
+// head, and all of float32, go in tiles of 16 rows, the others in tiles of 128.  A single unit needs no
+// launch for the former.
+struct PhasePlan {
+  AttendPlan small{}, large{};
+};
+PhasePlan phase_plan(const sats::AttendArgs &a, int form, int esz, int64_t max_q, int64_t units, int64_t range) {
+  PhasePlan p;
+  const bool any_large = esz == 2 && max_q * a.group > 16;
+  if (!any_large || units > 1)
+    p.small = attend_plan(a, 16, form || esz == 2 ? 32 : 16, kRowsLeast, any_large ? 16 / a.group : max_q, units, range);
+  if (any_large) p.large = attend_plan(a, sats::kTileRows, sats::kTileKeys, kTileLeast, max_q, units, range);
+  return p;
+}
+int check_plan(const sats::AttendArgs &a, const PhasePlan &p) {
+  for (const AttendPlan *x : {&p.small, &p.large})
+    if (x->tiles * a.pool.n_kv > kMaxGrid || x->splits > 65535) return fail(SATS_ERR_SHAPE, "too many rows for one call");
+  return SATS_OK;
+}
+
+size_t part_rows(const AttendPlan &p, int R, int n_kv) { return (size_t)p.tiles * n_kv * p.splits * R; }
+size_t attend_bytes(const AttendPlan &p, int R, int n_kv, int dim) {
+  return p.splits > 1 ? part_rows(p, R, n_kv) * (dim + 2) * sizeof(float) : 0;
+}
+// The parts of a launch at *mem, which moves past them.
+void place_parts(sats::AttendArgs &a, const AttendPlan &p, int R, char **mem) {
+  const size_t rows = part_rows(p, R, a.pool.n_kv);
+  a.splits = p.splits, a.per_split = p.per_split;
+  a.part = reinterpret_cast<float *>(*mem);
+  a.part_ml = a.part + rows * a.dim;
+  *mem += (rows * (a.dim + 2) * sizeof(float) + 255) & ~size_t(255);
+}
+
+int launch_tiles(const sats::AttendArgs &a, const AttendPlan &p, AttendKernel kernel, hipStream_t stream) {
+  kernel<<<dim3((unsigned)(p.tiles * a.pool.n_kv), (unsigned)p.splits), 256, 0, stream>>>(a);
+  return launched("attention kernel");
+}
+// A join of up to `parts` parts of each row, by one wave a row or (kernel4) by four.
+int launch_join(const sats::AttendArgs &a, const AttendPlan &p, int R, int parts, AttendKernel kernel1, AttendKernel kernel4,
+                hipStream_t stream) {
+  const unsigned grid_x = (unsigned)(p.tiles * a.pool.n_kv);
+  const int64_t rows = std::min<int64_t>(R, a.batch.max_q * a.group);
+  if (parts > kJoinWave) kernel4<<<dim3(grid_x, (unsigned)rows), 256, 0, stream>>>(a);
+  else kernel1<<<dim3(grid_x, (unsigned)((rows + 3) / 4)), 256, 0, stream>>>(a);
+  return launched("attention join");
+}
+
+// The second argument is true for heads of exactly the first one's dims only: such a kernel
+// loads rows of that width.
+template <typename T> AttendKernel rows_kernel(int dim) {
+  using namespace sats;
+  return dim <= 64    ? (dim == 64 ? attend_rows_kernel<T, 64, true> : attend_rows_kernel<T, 64, false>)
+         : dim <= 96  ? (dim == 96 ? attend_rows_kernel<T, 96, true> : attend_rows_kernel<T, 96, false>)
+         : dim <= 128 ? (dim == 128 ? attend_rows_kernel<T, 128, true> : attend_rows_kernel<T, 128, false>)
+                      : (dim == 256 ? attend_rows_kernel<T, 256, true> : attend_rows_kernel<T, 256, false>);
+}
+AttendKernel tile_kernel(int dim) {
+  using namespace sats;
+  return dim <= 64    ? (dim == 64 ? attend_tile_kernel<64, true> : attend_tile_kernel<64, false>)
+         : dim <= 128 ? (dim == 128 ? attend_tile_kernel<128, true> : attend_tile_kernel<128, false>)
+                      : (dim == 256 ? attend_tile_kernel<256, true> : attend_tile_kernel<256, false>);
+}
+// The join of tiles of R rows (those of 16 count blocks of the kernel's keys).
+AttendKernel join_kernel(int R, int esz, int form, bool four) {
+  using namespace sats;
+  if (R != 16) return four ? attend_join_kernel<uint16_t, kTileRows, 4, kTileKeys> : attend_join_kernel<uint16_t, kTileRows, 1, kTileKeys>;
+  if (esz == 2) return four ? attend_join_kernel<uint16_t, 16, 4, 32> : attend_join_kernel<uint16_t, 16, 1, 32>;
+  if (form) return four ? attend_join_kernel<float, 16, 4, 32> : attend_join_kernel<float, 16, 1, 32>;
+  return four ? attend_join_kernel<float, 16, 4, 16> : attend_join_kernel<float, 16, 1, 16>;
+}
+AttendKernel join_phases_kernel(int R, int esz, bool four) {
+  using namespace sats;
+  if (R != 16) return four ? attend_join_phases_kernel<uint16_t, kTileRows, 4> : attend_join_phases_kernel<uint16_t, kTileRows, 1>;
+  if (esz == 2) return four ? attend_join_phases_kernel<uint16_t, 16, 4> : attend_join_phases_kernel<uint16_t, 16, 1>;
+  return four ? attend_join_phases_kernel<float, 16, 4> : attend_join_phases_kernel<float, 16, 1>;
+}
+
+struct PrefixPlan {
+  PhasePlan pre, own;
+};
+PrefixPlan prefix_plan(sats::AttendArgs a, int form, int esz) {
+  PrefixPlan p;
+  a.phase = sats::kShared;
+  p.pre = phase_plan(a, form, esz, a.max_tokens, a.n_groups, a.max_len);
+  a.phase = sats::kOwn;
+  p.own = phase_plan(a, form, esz, a.batch.max_q, a.batch.n_seqs, a.max_own);
+  return p;
+}
+size_t prefix_bytes(const sats::AttendArgs &a, const PrefixPlan &p) {
+  sats::AttendArgs x = a;
+  char *mem = nullptr;
+  for (const PhasePlan *q : {&p.pre, &p.own}) {
+    place_parts(x, q->small, 16, &mem);
+    place_parts(x, q->large, sats::kTileRows, &mem);
+  }
+  return (size_t)mem;
+}
+
+}  // namespace
+
+int run_attention(sats::AttendArgs a, int form, int esz, hipStream_t stream) {
+  a.phase = sats::kWhole;
+  const PhasePlan p = phase_plan(a, form, esz, a.batch.max_q, a.batch.n_seqs, (int64_t)1 << 31);
+  int rc = check_plan(a, p);
+  if (rc) return rc;
+  const size_t bytes = std::max(attend_bytes(p.small, 16, a.pool.n_kv, a.dim),
+                                attend_bytes(p.large, sats::kTileRows, a.pool.n_kv, a.dim));
+  char *mem = nullptr;
+  Turn turn;
+  if (bytes && (rc = serve_workspace(stream, bytes, &mem, &turn))) return rc;
+  if (p.small.tiles) {
+    char *at = mem;
+    place_parts(a, p.small, 16, &at);
+    a.small = 1, a.large = esz != 2;
+    const AttendKernel kernel = form ? rows8_kernel(form, esz, a.dim) : esz == 2 ? rows_kernel<uint16_t>(a.dim) : rows_kernel<float>(a.dim);
+    if ((rc = launch_tiles(a, p.small, kernel, stream))) return rc;
+    if (p.small.splits > 1 && (rc = launch_join(a, p.small, 16, p.small.splits, join_kernel(16, esz, form, false),
+                                                join_kernel(16, esz, form, true), stream)))
+      return rc;
+  }
+  if (p.large.tiles) {
+    char *at = mem;
+    place_parts(a, p.large, sats::kTileRows, &at);
+    a.small = p.small.tiles == 0, a.large = 1;
+    if ((rc = launch_tiles(a, p.large, form ? tile8_kernel(form, a.dim) : tile_kernel(a.dim), stream))) return rc;
+    if (p.large.splits > 1)
+      rc = launch_join(a, p.large, sats::kTileRows, p.large.splits, join_kernel(sats::kTileRows, esz, form, false),
+                       join_kernel(sats::kTileRows, esz, form, true), stream);
+  }
+  return rc;
+}
+
+// The groups' tiles, the sequences' tiles, and the joins of the latter's rows with both.
+int run_prefix_attention(sats::AttendArgs a, int form, int esz, hipStream_t stream) {
+  if (a.n_groups == 0 || a.max_len == 0 || a.max_tokens == 0) return run_attention(a, form, esz, stream);
+  size_t bytes = 0;
+  int rc = prefix_scratch(a, form, esz, &bytes);
+  if (rc) return rc;
+  const PrefixPlan plan = prefix_plan(a, form, esz);
+  char *mem = nullptr;
+  Turn turn;
+  if ((rc = serve_workspace(stream, bytes, &mem, &turn))) return rc;
+  const AttendKernel rows = form ? rows8_kernel(form, esz, a.dim) : phase_rows_kernel(esz, a.dim);
+  const AttendKernel tile = form ? tile8_kernel(form, a.dim) : phase_tile_kernel(a.dim);
+  sats::AttendArgs own[2];
+  for (int phase : {sats::kShared, sats::kOwn}) {
+    const PhasePlan &p = phase == sats::kShared ? plan.pre : plan.own;
+    for (int large = 0; large < 2; ++large) {
+      const AttendPlan &x = large ? p.large : p.small;
+      if (!x.tiles) continue;
+      a.phase = phase;
+      place_parts(a, x, large ? sats::kTileRows : 16, &mem);
+      a.small = !large || p.small.tiles == 0, a.large = large || esz != 2;
+      if ((rc = launch_tiles(a, x, large ? tile : rows, stream))) return rc;
+      if (phase == sats::kShared) a.pre[large] = {a.part, a.part_ml, a.splits, a.small, a.large, x.tiles};
+      else own[large] = a;
+    }
+  }
+  const int pre = std::max(plan.pre.small.splits, plan.pre.large.splits);
+  for (int large = 0; large < 2; ++large) {
+    const AttendPlan &x = large ? plan.own.large : plan.own.small;
+    const int R = large ? sats::kTileRows : 16;
+    if (x.tiles && (rc = launch_join(own[large], x, R, pre + x.splits, join_phases_kernel(R, esz, false),
+                                     join_phases_kernel(R, esz, true), stream)))
+      return rc;
+  }
+  return rc;
+}
+
+size_t attention_scratch(int64_t head_dim) {
+  // a launch that splits its tiles has at most kSlotsLong workgroups of 16 rows, kSlots of 128
+  return (size_t)std::max(kSlotsLong * 16, kSlots * sats::kTileRows) * (head_dim + 2) * sizeof(float);
+}
+int prefix_scratch(const sats::AttendArgs &a, int form, int esz, size_t *bytes) {
+  const PrefixPlan p = prefix_plan(a, form, esz);
+  int rc = check_plan(a, p.pre);
+  if (rc || (rc = check_plan(a, p.own))) return rc;
+  *bytes = prefix_bytes(a, p);
+  return SATS_OK;
+}
+
+}  // namespace sats_host

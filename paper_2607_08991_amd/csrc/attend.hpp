@@ -23,13 +23,16 @@
 // first row's window on.  The blocks of a tile can be split over several workgroups
 // (`per_split` each); their partial results are joined by a second launch in a fixed
 // order.
+//
+// Where sequences of a batch share a prefix, the work is in two phases (KeyPhase): the shared keys of a
+// group for the rows of all its sequences, which are one tile's rows there, and then each sequence's
+// own keys.  Every part of a row is kept, and joined as the parts of a split tile are.
 #pragma once
 
-#include "paged.hpp"
+#include "cache8.hpp"
 
 namespace sats {
 
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) i16x4_t lds_i16x4;
@@ -50,9 +53,20 @@ struct AttendArgs {
   int small, large;   // which sequences the launch takes: at most 16 rows a head, more
   float *part;        // [tiles * n_kv][splits][rows of a tile][dim]
   float *part_ml;     // [tiles * n_kv][splits][rows of a tile][2]
+  const uint8_t *k_scale, *v_scale;  // of the layer, 8-bit caches
+  // shared prefixes: sequences seq_start[g] .. seq_start[g + 1] - 1 have their first shared[g] tokens in common
+  int phase, n_groups;
+  const int32_t *seq_start, *shared;
+  int64_t max_tokens, max_len, max_own;  // of a group's new tokens, of a prefix, of a sequence's other keys
+  struct {            // parts of the groups' tiles of 16 rows and of 128, as above
+    const float *part, *part_ml;
+    int splits, small, large;
+    int64_t tiles;
+  } pre[2];
 };
+enum : int { kWhole = 0, kShared = 1, kOwn = 2 };  // phase: all keys, those of the groups, those of a sequence alone
 
-__device__ u32x4 attend_zeros[64];  // a row of zeros
+static __device__ u32x4 attend_zeros[64];  // a row of zeros
 constexpr uint32_t kNoRow = 0x80000000u;  // an offset past every buffer: the load returns zeros
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const char *base) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), (short)0, 0x7fffffff, 0x00020000);
@@ -66,15 +80,135 @@ struct RowTile {
   int seq;          // -1: none
   int first, count;
   int64_t start, place0, len;  // sequence's first token; place of its first new token; length
+  // (in phases) the first key that counts; the group's sequences, whose tokens the tile's rows are (seq: the one
+  // whose pages are read)
+  int64_t lo;
+  int seq0, seq_end;
 };
 
 __device__ __forceinline__ bool takes(const AttendArgs &a, int rows) { return rows <= 16 ? a.small : a.large; }
 
-// Tile `t` of the batch (rows in tiles of R; a sequence's last rows, which see most keys, first).
-template <int R>
-__device__ __forceinline__ RowTile find_tile(const AttendArgs &a, int t) {
+// Group g: its sequences, its tokens and the length of its prefix, in range.
+struct GroupView {
+  int s0, s1, n;
+  int64_t start, len;
+};
+__device__ __forceinline__ GroupView group_view(const AttendArgs &a, int g) {
+  const int lo = a.seq_start[g], hi = a.seq_start[g + 1];
+  GroupView v;
+  v.s0 = lo < 0 ? 0 : lo > a.batch.n_seqs ? a.batch.n_seqs : lo;
+  v.s1 = hi < v.s0 ? v.s0 : hi > a.batch.n_seqs ? a.batch.n_seqs : hi;
+  const int64_t n = a.batch.n_tokens, t0 = a.batch.q_start[v.s0], t1 = a.batch.q_start[v.s1];
+  v.start = t0 < 0 ? 0 : t0 > n ? n : t0;
+  const int64_t end = t1 < v.start ? v.start : t1 > n ? n : t1;
+  v.n = v.s0 == v.s1 ? 0 : (int)(end - v.start < a.max_tokens ? end - v.start : a.max_tokens);
+  int64_t top = a.batch.max_kv < a.batch.max_pages << a.pool.shift ? a.batch.max_kv : a.batch.max_pages << a.pool.shift;
+  if (a.max_len < top) top = a.max_len;
+  const int64_t p = a.shared[g];
+  v.len = p < 0 ? 0 : p > top ? top : p;
+  return v;
+}
+// The first group that sequence s is in, or -1.  (All lanes of a wave call it.)
+__device__ __forceinline__ int group_of(const AttendArgs &a, int s) {
+  const int lane = threadIdx.x & 63;
+  for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
+    const int g = g0 + lane;
+    const uint64_t in = __ballot(g < a.n_groups && a.seq_start[g < a.n_groups ? g : 0] <= s &&
+                                 a.seq_start[g < a.n_groups ? g + 1 : 0] > s);
+    if (in) return __builtin_amdgcn_readfirstlane(g0 + __builtin_ctzll(in));
+  }
+  return -1;
+}
+// The first sequence of a group that is as long as its prefix (where none is: that is as long as any), whose
+// pages are read for all of them.  (All lanes call it.)
+__device__ __forceinline__ int group_leader(const AttendArgs &a, const GroupView &v) {
+  const int lane = threadIdx.x & 63;
+  int most = 0;
+  for (int s = v.s0 + lane; s < v.s1; s += 64) most = a.batch.kv_len[s] > most ? a.batch.kv_len[s] : most;
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    const int o = __shfl_xor(most, d);
+    most = o > most ? o : most;
+  }
+  if (most > v.len) most = (int)v.len;
+  for (int base = v.s0; base < v.s1; base += 64) {
+    const uint64_t long_enough = __ballot(base + lane < v.s1 && a.batch.kv_len[base + lane < v.s1 ? base + lane : v.s0] >= most);
+    if (long_enough) return __builtin_amdgcn_readfirstlane(base + __builtin_ctzll(long_enough));
+  }
+  return v.s0;
+}
+// The place of token `tok` in the one of sequences s0 .. s1 - 1 that it is of (-1: of none).  (All lanes call it.)
+__device__ __forceinline__ int64_t group_place(const AttendArgs &a, int s0, int s1, int64_t tok) {
+  const int lane = threadIdx.x & 63;
+  int64_t place = -1;
+  bool done = false;
+  for (int base = s0; base < s1; base += 64) {
+    const bool in = base + lane < s1;
+    const int end = in ? a.batch.q_start[base + lane + 1] : 0x7fffffff, kv = in ? a.batch.kv_len[base + lane] : 0;
+    int at = 0;  // the first of these sequences that ends behind the token
+#pragma unroll
+    for (int d = 32; d; d >>= 1) at += __shfl(end, at + d - 1) <= tok ? d : 0;
+    const int e = __shfl(end, at), n = __shfl(kv, at);
+    if (!done && e > tok && base + at < s1) place = (int64_t)n - e + tok, done = true;
+    if (__all(done)) break;
+  }
+  return place;
+}
+
+// Tiles of the groups, in their order: tile `t` of those that a launch takes.
+template <int R> __device__ __forceinline__ RowTile find_group_tile(const AttendArgs &a, int t) {
   RowTile o;
   o.seq = -1;
+  int g = -1, idx = 0;
+  if (a.max_tokens * a.group <= R) {  // a tile per group
+    if (t < a.n_groups) g = t;
+  } else {
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
+      int n = 0;
+      if (g0 + lane < a.n_groups) {
+        const int rows = group_view(a, g0 + lane).n * a.group;
+        if (takes(a, rows)) n = (rows + R - 1) / R;
+      }
+      int inc = n;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int x = __shfl_up(inc, d);
+        if (lane >= d) inc += x;
+      }
+      const uint64_t past = __ballot(base + inc > t);
+      if (past) {
+        const int at = __builtin_ctzll(past);
+        g = g0 + at;
+        idx = t - base - (__shfl(inc, at) - __shfl(n, at));
+        break;
+      }
+      base += __shfl(inc, 63);
+    }
+  }
+  if (g < 0) return o;
+  g = __builtin_amdgcn_readfirstlane(g);
+  idx = __builtin_amdgcn_readfirstlane(idx);
+  const GroupView v = group_view(a, g);
+  if (!v.n || !takes(a, v.n * a.group)) return o;
+  o.seq = group_leader(a, v), o.seq0 = v.s0, o.seq_end = v.s1;
+  o.first = idx * R;
+  const int rows = v.n * a.group - o.first;
+  o.count = rows < R ? rows : R;
+  o.start = v.start;
+  o.place0 = 0;
+  o.lo = 0, o.len = v.len;
+  return o;
+}
+
+// Tile `t` of the batch (rows in tiles of R; a sequence's last rows, which see most keys, first).
+template <int R, bool PHASED = false>
+__device__ __forceinline__ RowTile find_tile(const AttendArgs &a, int t) {
+  if (PHASED && a.phase == kShared) return find_group_tile<R>(a, t);
+  RowTile o;
+  o.seq = -1;
+  o.lo = 0;
   const int lane = threadIdx.x & 63;
   int base = 0, idx = 0, n = 0;
   if (a.batch.max_q * a.group <= R) {  // a tile per sequence
@@ -119,7 +253,44 @@ __device__ __forceinline__ RowTile find_tile(const AttendArgs &a, int t) {
   // (as token_place counts: from the length as it is given)
   o.place0 = (int64_t)a.batch.kv_len[o.seq] - (a.batch.q_start[o.seq + 1] - v.start);
   o.len = v.len;
+  if (PHASED && a.phase == kOwn) {
+    const int g = group_of(a, o.seq);
+    if (g >= 0) o.lo = group_view(a, g).len;
+    if (o.len - o.lo > a.max_own) o.len = o.lo + a.max_own;
+  }
   return o;
+}
+
+// (Phases) the places of a tile's rows, row r in lane r % 64; they are those of one sequence, or of the
+// sequences of a group.
+template <int R> struct RowPlaces {
+  static constexpr int kPer = (R + 63) / 64;
+  int64_t p[kPer];
+  __device__ __forceinline__ void find(const AttendArgs &a, const RowTile &t) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int r = (threadIdx.x & 63) + 64 * i, in = t.first + (r < t.count ? r : t.count - 1);
+      p[i] = a.phase == kShared ? group_place(a, t.seq0, t.seq_end, t.start + in / a.group) : t.place0 + in / a.group;
+    }
+  }
+  __device__ __forceinline__ int64_t of(int r) const {
+    int64_t v = __shfl(p[0], r & 63);
+    if constexpr (kPer > 1) {
+      const int64_t w = __shfl(p[1], r & 63);
+      v = r < 64 ? v : w;
+    }
+    return v;
+  }
+};
+// The smallest and largest of a number of each of N lanes (a power of two).
+template <int N> __device__ __forceinline__ void range_of(int64_t v, int64_t *low, int64_t *high) {
+  int64_t lo = v, hi = v;
+#pragma unroll
+  for (int d = 1; d < N; d <<= 1) {
+    const int64_t x = __shfl_xor(lo, d), y = __shfl_xor(hi, d);
+    lo = x < lo ? x : lo, hi = y > hi ? y : hi;
+  }
+  *low = lo, *high = hi;
 }
 
 // The blocks of B keys that a tile's rows see.
@@ -128,23 +299,46 @@ struct KeyBlocks {
   int n_sink;         // blocks of sinks before the window
   int64_t first;      // first block of the window
   int n;              // all
+  int64_t lo, sink0;  // (phases) the first key, and its block
 };
+template <int B> __device__ __forceinline__ void count_blocks(const AttendArgs &a, int64_t lo, int64_t len, KeyBlocks &k) {
+  const int64_t end = k.high + 1 < len ? k.high + 1 : len;
+  int64_t from = a.window ? k.low - a.window + 1 : 0;
+  from = from < lo ? lo : from;
+  k.first = from / B;
+  k.lo = lo, k.sink0 = lo / B;
+  const int64_t last = end > 0 ? (end + B - 1) / B : 0, sink = a.window ? (a.sinks + B - 1) / B : 0;
+  int64_t s = sink < k.first ? sink : k.first;
+  if (s > last) s = last;
+  k.n_sink = (int)(s > k.sink0 ? s - k.sink0 : 0);
+  k.n = k.n_sink + (int)(last > k.first ? last - k.first : 0);
+}
 template <int B> __device__ __forceinline__ KeyBlocks key_blocks(const AttendArgs &a, const RowTile &t) {
   KeyBlocks k;
   k.low = t.place0 + t.first / a.group;
   k.high = t.place0 + (t.first + t.count - 1) / a.group;
-  const int64_t end = k.high + 1 < t.len ? k.high + 1 : t.len;
-  int64_t from = a.window ? k.low - a.window + 1 : 0;
-  from = from < 0 ? 0 : from;
-  k.first = from / B;
-  const int64_t last = end > 0 ? (end + B - 1) / B : 0, sink = a.window ? (a.sinks + B - 1) / B : 0;
-  k.n_sink = (int)(sink < k.first ? sink : k.first);
-  if (k.n_sink > last) k.n_sink = (int)last;
-  k.n = k.n_sink + (int)(last > k.first ? last - k.first : 0);
+  count_blocks<B>(a, 0, t.len, k);
+  return k;
+}
+// (Phases: all lanes of a wave call it.)
+template <int B, int R> __device__ __forceinline__ KeyBlocks key_blocks(const AttendArgs &a, const RowTile &t, const RowPlaces<R> &p) {
+  KeyBlocks k;
+  if (a.phase == kShared) {
+    range_of<64>(p.p[0], &k.low, &k.high);
+    if constexpr (RowPlaces<R>::kPer > 1) {
+      int64_t low, high;
+      range_of<64>(p.p[1], &low, &high);
+      k.low = low < k.low ? low : k.low, k.high = high > k.high ? high : k.high;
+    }
+  } else {
+    k.low = t.place0 + t.first / a.group;
+    k.high = t.place0 + (t.first + t.count - 1) / a.group;
+  }
+  count_blocks<B>(a, t.lo, t.len, k);
   return k;
 }
 __device__ __forceinline__ int64_t block_key(const KeyBlocks &k, int b, int keys) {
-  return (b < k.n_sink ? b : k.first + (b - k.n_sink)) * keys;
+  return (b < k.n_sink ? k.sink0 + b : k.first + (b - k.n_sink)) * keys;
 }
 
 // Which keys of the block from j0 on the token at `place` sees: key j0 + i where
@@ -160,13 +354,15 @@ __device__ __forceinline__ Sight sight_of(const AttendArgs &a, int64_t place, in
   return {cut_off(place - j0), a.window ? cut_off(place - j0 - a.window + 1) : 0, cut_off(a.sinks - j0)};
 }
 // Whether any row of a tile at places low .. high sees key j.
+template <bool PHASED = false>
 __device__ __forceinline__ bool any_sees(const AttendArgs &a, const KeyBlocks &k, int64_t len, int64_t j) {
-  return j < len && j <= k.high && (!a.window || k.low - j < a.window || j < a.sinks);
+  return j < len && (!PHASED || j >= k.lo) && j <= k.high && (!a.window || k.low - j < a.window || j < a.sinks);
 }
 
 // Page of key j where some row sees it, else -1.
+template <bool PHASED = false>
 __device__ __forceinline__ int key_page(const AttendArgs &a, const RowTile &t, const KeyBlocks &k, int64_t j) {
-  if (!any_sees(a, k, t.len, j)) return -1;
+  if (!any_sees<PHASED>(a, k, t.len, j)) return -1;
   const int p = a.batch.table[t.seq * a.batch.max_pages + (j >> a.pool.shift)];
   return p >= 0 && p < a.pool.n_pages ? p : -1;
 }
@@ -197,6 +393,13 @@ __device__ __forceinline__ void put_row(const AttendArgs &a, const RowTile &t, i
 __device__ __forceinline__ void put_part(const AttendArgs &a, int64_t at, int d, const f32x4 &o, float m, float l) {
   if (d < a.dim) *reinterpret_cast<f32x4 *>(a.part + at * a.dim + d) = o;
   if (d == 0) a.part_ml[at * 2] = m, a.part_ml[at * 2 + 1] = l;
+}
+
+// (Phases) split z of a tile has nothing to add: its part is empty.
+template <int R> __device__ __forceinline__ void put_nothing(const AttendArgs &a, const RowTile &t, int z) {
+  if (a.phase == kWhole || (int)threadIdx.x >= t.count) return;
+  const int64_t at = ((int64_t)blockIdx.x * a.splits + z) * R + threadIdx.x;
+  a.part_ml[at * 2] = -INFINITY, a.part_ml[at * 2 + 1] = 0.0f;
 }
 
 template <typename T> __device__ __forceinline__ bool odd_value(const u32x4 &q) {  // an infinity or NaN among them
@@ -246,10 +449,46 @@ template <typename T> struct RowsOf {
   static constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;  // keys of a block
 };
 
+// The end of a tile of 16 rows: the sums of its four waves (row lane % 16; m, l: of this lane's group's keys)
+// into results, or into split z's part.  `lds`: 4 x 16 x DT floats.
+template <typename T, int DT>
+__device__ __forceinline__ void finish_rows(const AttendArgs &a, const RowTile &t, int kvh, int z, bool split, float m, float l,
+                                            const f32x4 (&acc)[DT / 16], uint8_t *lds, float (&ml)[4][16][2]) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, row = lane & 15, g = lane >> 4;
+  // a row's sums: over the four lane groups, then over the waves
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (g == 0) ml[w][row][0] = m, ml[w][row][1] = l;
+  __syncthreads();
+  float top = -INFINITY, fw[4], total = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = fmaxf(top, ml[i][row][0]);
+  const float at0 = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    fw[i] = exp2_fast(ml[i][row][0] - at0);
+    total += ml[i][row][1] * fw[i];
+  }
+  // each wave's sums, scaled to the common maximum: [wave][dim / 4][row][4]
+  float *sums = reinterpret_cast<float *>(lds);
+#pragma unroll
+  for (int o = 0; o < DT / 16; ++o)
+    *reinterpret_cast<f32x4 *>(sums + ((w * (DT / 4) + 4 * o + g) * 16 + row) * 4) = acc[o] * fw[w];
+  __syncthreads();
+  for (int i = threadIdx.x >> 4; i < DT / 4; i += 16) {
+    f32x4 o = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) o += *reinterpret_cast<const f32x4 *>(sums + ((x * (DT / 4) + i) * 16 + row) * 4);
+    if (row >= t.count) continue;
+    if (split) put_part(a, ((int64_t)blockIdx.x * a.splits + z) * 16 + row, 4 * i, o, top, total);
+    else put_row<T>(a, t, row, kvh, 4 * i, o, top, total);
+  }
+}
+
 // FULL: heads of DT dims.  Else every load leaves out the dims that a head has not (they are the
 // next slot's, or lie behind the cache), and up to DT = 128 the products do too.  Of 256 they
 // multiply zeros there: leaving them out spills 989 registers (bf16; 683 float32), all of them none.
-template <typename T, int DT, bool FULL>
+template <typename T, int DT, bool FULL, bool PHASED = false>
 __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_rows_kernel(AttendArgs a) {
   constexpr int kKeys = RowsOf<T>::kKeys, kVec = Elem<T>::kVec, kRow = DT * (int)sizeof(T), kChunks = kRow / 16;
   constexpr bool kSkip = !FULL && DT <= 128;
@@ -262,14 +501,23 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
   __shared__ float ml[4][16][2];
 
   const int kvh = blockIdx.x % a.pool.n_kv, z = blockIdx.y;
-  const RowTile t = find_tile<16>(a, blockIdx.x / a.pool.n_kv);
+  const RowTile t = find_tile<16, PHASED>(a, blockIdx.x / a.pool.n_kv);
   if (t.seq < 0) return;
-  const KeyBlocks kb = key_blocks<kKeys>(a, t);
+  RowPlaces<16> places;
+  if constexpr (PHASED) places.find(a, t);
+  KeyBlocks kb;
+  if constexpr (PHASED) kb = key_blocks<kKeys>(a, t, places);
+  else kb = key_blocks<kKeys>(a, t);
   const int parts = kb.n > a.per_split ? (kb.n + a.per_split - 1) / a.per_split : 1;
-  if (z >= parts) return;
+  if (z >= parts) {
+    if constexpr (PHASED) put_nothing<16>(a, t, z);
+    return;
+  }
   const int b_end = kb.n < (z + 1) * a.per_split ? kb.n : (z + 1) * a.per_split;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, row = lane & 15, g = lane >> 4;
-  const int64_t place = t.place0 + (t.first + (row < t.count ? row : t.count - 1)) / a.group;
+  int64_t place;
+  if constexpr (PHASED) place = places.of(row);
+  else place = t.place0 + (t.first + (row < t.count ? row : t.count - 1)) / a.group;
   const bool several = kb.low != kb.high;
 
   // Q as the second operand: this lane's row, its pieces of k
@@ -292,7 +540,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
 
   u32x4 kr[kLoads], vr[kLoads];
   auto page_of = [&](int b) {  // of key lane % kKeys of a block
-    return b < b_end ? key_page(a, t, kb, block_key(kb, b, kKeys) + (lane & (kKeys - 1))) : -1;
+    return b < b_end ? key_page<PHASED>(a, t, kb, block_key(kb, b, kKeys) + (lane & (kKeys - 1))) : -1;
   };
   auto load = [&](int b, int page, uint32_t there) {
     const int j0 = (int)(block_key(kb, b, kKeys) & (a.pool.page - 1));  // (blocks and pages are powers of two)
@@ -494,35 +742,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
     }
   }
 
-  // a row's sums: over the four lane groups, then over the waves
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-  if (g == 0) ml[w][row][0] = m, ml[w][row][1] = l;
-  __syncthreads();
-  float top = -INFINITY, fw[4], total = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) top = fmaxf(top, ml[i][row][0]);
-  const float at0 = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    fw[i] = exp2_fast(ml[i][row][0] - at0);
-    total += ml[i][row][1] * fw[i];
-  }
-  // each wave's sums, scaled to the common maximum: [wave][dim / 4][row][4]
-  float *sums = reinterpret_cast<float *>(lds);
-#pragma unroll
-  for (int o = 0; o < kOut; ++o)
-    *reinterpret_cast<f32x4 *>(sums + ((w * (DT / 4) + 4 * o + g) * 16 + row) * 4) = acc[o] * fw[w];
-  __syncthreads();
-  const bool split = parts > 1;
-  for (int i = threadIdx.x >> 4; i < DT / 4; i += 16) {
-    f32x4 o = f32x4{0, 0, 0, 0};
-#pragma unroll
-    for (int x = 0; x < 4; ++x) o += *reinterpret_cast<const f32x4 *>(sums + ((x * (DT / 4) + i) * 16 + row) * 4);
-    if (row >= t.count) continue;
-    if (split) put_part(a, ((int64_t)blockIdx.x * a.splits + z) * 16 + row, 4 * i, o, top, total);
-    else put_row<T>(a, t, row, kvh, 4 * i, o, top, total);
-  }
+  finish_rows<T, DT>(a, t, kvh, z, parts > 1 || (PHASED && a.phase != kWhole), m, l, acc, &lds[0][0], ml);
 }
 
 // ------------------------------------------------------------------ tiles of 128 rows
@@ -621,6 +841,48 @@ template <int DT, bool FULL> struct TileWave {
     bf16x8_t v8;
     __builtin_memcpy(&v8, v2, 16);
     return v8;
+  }
+
+  // The places of this lane's row (r_in of the tile) and of the wave's first and last row.
+  __device__ __forceinline__ void take_places(const AttendArgs &a, const RowTile &t, int w, int r_in) {
+    place = t.place0 + (t.first + r_in) / a.group;
+    low = t.place0 + (t.first + (32 * w < t.count ? 32 * w : t.count - 1)) / a.group;
+    high = t.place0 + (t.first + (32 * w + 31 < t.count ? 32 * w + 31 : t.count - 1)) / a.group;
+  }
+  __device__ __forceinline__ void take_places(const RowPlaces<kTileRows> &p, int w, int col) {
+    place = p.of(32 * w + col);
+    range_of<32>(place, &low, &high);
+  }
+  __device__ __forceinline__ void take_rows(const AttendArgs &a, const RowTile &t, int kvh, int r_in) {
+    dim = a.dim;
+    scale2 = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;
+    // q with the scale's sign (zeros for a scale of 0), so that the largest product is the largest score
+    const int r = t.first + r_in;
+    const uint16_t *qr = (const uint16_t *)a.q + (t.start + r / a.group) * a.q_stride +
+                         (int64_t)(kvh * a.group + r % a.group) * a.dim;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int c = 2 * s + ((threadIdx.x & 63) >> 5);
+      u32x4 x = c * 8 < a.dim && a.scale != 0.0f ? *reinterpret_cast<const u32x4 *>(qr + c * 8) : u32x4{0, 0, 0, 0};
+      if (a.scale < 0.0f) x ^= 0x80008000u;
+      q[s] = __builtin_bit_cast(bf16x8_t, x);
+    }
+  }
+  // This lane's results: the row's, or split z's part of it.
+  __device__ __forceinline__ void put(const AttendArgs &a, const RowTile &t, int kvh, int row, int z, bool split) {
+    float sum = l;
+    sum += __shfl_xor(sum, 32);
+    if (row >= t.count) return;
+    const float top = m * scale2;
+#pragma unroll
+    for (int o = 0; o < kOut; ++o)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x4 v = {acc[o][4 * e], acc[o][4 * e + 1], acc[o][4 * e + 2], acc[o][4 * e + 3]};
+        const int d = 32 * o + 8 * e + 4 * ((threadIdx.x & 63) >> 5);
+        if (split) put_part(a, ((int64_t)blockIdx.x * a.splits + z) * kTileRows + row, d, v, top, sum);
+        else put_row<uint16_t>(a, t, row, kvh, d, v, top, sum);
+      }
   }
 
   __device__ __forceinline__ void clear() {
@@ -772,7 +1034,7 @@ template <int DT, bool FULL> struct TileWave {
   }
 };
 
-template <int DT, bool FULL>
+template <int DT, bool FULL, bool PHASED = false>
 __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a) {
   using Wave = TileWave<DT, FULL>;
   constexpr int kRow = Wave::kRow, kChunks = Wave::kChunks, kLoads = kTileKeys * kChunks / 256;
@@ -780,33 +1042,26 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
   __shared__ __align__(16) uint8_t k0[kTileKeys * kRow], k1[kTileKeys * kRow], v0[kTileKeys * kRow], v1[kTileKeys * kRow];
 
   const int kvh = blockIdx.x % a.pool.n_kv, z = blockIdx.y;
-  const RowTile t = find_tile<kTileRows>(a, blockIdx.x / a.pool.n_kv);
+  const RowTile t = find_tile<kTileRows, PHASED>(a, blockIdx.x / a.pool.n_kv);
   if (t.seq < 0) return;
-  const KeyBlocks kb = key_blocks<kTileKeys>(a, t);
+  RowPlaces<kTileRows> places;
+  if constexpr (PHASED) places.find(a, t);
+  KeyBlocks kb;
+  if constexpr (PHASED) kb = key_blocks<kTileKeys>(a, t, places);
+  else kb = key_blocks<kTileKeys>(a, t);
   const int parts = kb.n > a.per_split ? (kb.n + a.per_split - 1) / a.per_split : 1;
-  if (z >= parts) return;
+  if (z >= parts) {
+    if constexpr (PHASED) put_nothing<kTileRows>(a, t, z);
+    return;
+  }
   const int b0 = z * a.per_split, b_end = kb.n < b0 + a.per_split ? kb.n : b0 + a.per_split;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, hf = lane >> 5;
   const int row = 32 * w + col, r_in = row < t.count ? row : t.count - 1;  // (rows past the last repeat it)
 
   Wave wave;
-  wave.dim = a.dim;
-  wave.place = t.place0 + (t.first + r_in) / a.group;
-  wave.low = t.place0 + (t.first + (32 * w < t.count ? 32 * w : t.count - 1)) / a.group;
-  wave.high = t.place0 + (t.first + (32 * w + 31 < t.count ? 32 * w + 31 : t.count - 1)) / a.group;
-  wave.scale2 = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;
-  {  // q with the scale's sign (zeros for a scale of 0), so that the largest product is the largest score
-    const int r = t.first + r_in;
-    const uint16_t *q = (const uint16_t *)a.q + (t.start + r / a.group) * a.q_stride +
-                        (int64_t)(kvh * a.group + r % a.group) * a.dim;
-#pragma unroll
-    for (int s = 0; s < Wave::kSteps; ++s) {
-      const int c = 2 * s + hf;
-      u32x4 x = c * 8 < a.dim && a.scale != 0.0f ? *reinterpret_cast<const u32x4 *>(q + c * 8) : u32x4{0, 0, 0, 0};
-      if (a.scale < 0.0f) x ^= 0x80008000u;
-      wave.q[s] = __builtin_bit_cast(bf16x8_t, x);
-    }
-  }
+  if constexpr (PHASED) wave.take_places(places, w, col);
+  else wave.take_places(a, t, w, r_in);
+  wave.take_rows(a, t, kvh, r_in);
   const char *zeros = reinterpret_cast<const char *>(attend_zeros);
   const int64_t head_bytes = ((int64_t)kvh << a.pool.shift) * a.dim * 2;
   const int64_t page_bytes = ((int64_t)a.pool.n_kv << a.pool.shift) * a.dim * 2;
@@ -825,9 +1080,9 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
       held.page = p >= 0 && p < a.pool.n_pages ? p : -1;
     }
     const int p = __shfl(held.page, (int)(((j0 + lane) >> a.pool.shift) - held.first));
-    const bool inside = j0 + kTileKeys <= t.len && j0 + kTileKeys - 1 <= kb.high &&
+    const bool inside = j0 + kTileKeys <= t.len && (!PHASED || j0 >= kb.lo) && j0 + kTileKeys - 1 <= kb.high &&
                         (!a.window || kb.low - j0 < a.window || j0 + kTileKeys <= a.sinks);
-    return inside || any_sees(a, kb, t.len, j0 + lane) ? p : -1;
+    return inside || any_sees<PHASED>(a, kb, t.len, j0 + lane) ? p : -1;
   };
   // wave w loads rows 16 w .. 16 w + 15 of a block of K or V; where all of them are there, in
   // one page and whole, from one address and fixed offsets
@@ -938,37 +1193,24 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
   };
   if (__syncthreads_or(run(Plain{}))) run(Odd{});
 
-  float l = wave.l;
-  l += __shfl_xor(l, 32);
-  if (row >= t.count) return;
-  const float m = wave.m * wave.scale2;
-#pragma unroll
-  for (int o = 0; o < Wave::kOut; ++o)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const f32x4 v = {wave.acc[o][4 * e], wave.acc[o][4 * e + 1], wave.acc[o][4 * e + 2], wave.acc[o][4 * e + 3]};
-      const int d = 32 * o + 8 * e + 4 * hf;
-      if (parts > 1) put_part(a, ((int64_t)blockIdx.x * a.splits + z) * kTileRows + row, d, v, m, l);
-      else put_row<uint16_t>(a, t, row, kvh, d, v, m, l);
-    }
+  wave.put(a, t, kvh, row, z, parts > 1 || (PHASED && a.phase != kWhole));
 }
 
 // ------------------------------------------------------------------ join
 
-// Joins the parts of a tile's rows where it was split: W waves per row, each part of a row
+// Joins the parts of a tile's rows where it was split (into blocks of KEYS keys): W waves per row, each part of a row
 // held by `lanes` lanes, so that a wave adds 64 / lanes parts at a time and the W waves'
 // loads are all in flight.  The order of a row's sum depends on the batch's bounds alone.
 // Latency: two dependent loads and the launch, 5.7 us for 64 sequences in 4 parts each, 8.2 us
 // for one sequence in 61.
-template <typename T, int R, int W>
+template <typename T, int R, int W, int KEYS>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-  constexpr int kKeys = R == 16 ? RowsOf<T>::kKeys : kTileKeys;
   __shared__ float ls[W > 1 ? W : 1];
   __shared__ f32x4 os[W > 1 ? W : 1][64];
   const RowTile t = find_tile<R>(a, blockIdx.x / a.pool.n_kv);
   const int wave = threadIdx.x >> 6, r = blockIdx.y * (4 / W) + wave / W, w = wave % W, lane = threadIdx.x & 63;
   if (t.seq < 0 || (W > 1 ? (int)blockIdx.y : r) >= t.count) return;  // (W > 1: a row a workgroup)
-  const KeyBlocks kb = key_blocks<kKeys>(a, t);
+  const KeyBlocks kb = key_blocks<KEYS>(a, t);
   const int parts = kb.n > a.per_split ? (kb.n + a.per_split - 1) / a.per_split : 1;
   if (parts == 1) return;
   const int64_t at = (int64_t)blockIdx.x * a.splits * R + r;  // part z's row is at + z * R
@@ -1005,6 +1247,96 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
     for (int i = 0; i < W; ++i) o += os[i][lane], l += ls[i];
   }
   if (lane < lanes && d < a.dim) put_row<T>(a, t, r, blockIdx.x % a.pool.n_kv, d, o, top, l);
+}
+
+// The same where sequences share prefixes: a row's parts are those of its own tile (of R rows) and those
+// of its group's tile.  Every split of these has left a part, an empty one too, so that no block of
+// keys is counted here again.
+template <typename T, int R, int W>
+__global__ __launch_bounds__(256) void attend_join_phases_kernel(AttendArgs a) {
+  __shared__ float ls[W > 1 ? W : 1];
+  __shared__ f32x4 os[W > 1 ? W : 1][64];
+  const int kvh = blockIdx.x % a.pool.n_kv;
+  const RowTile t = find_tile<R, true>(a, blockIdx.x / a.pool.n_kv);
+  const int wave = threadIdx.x >> 6, r = blockIdx.y * (4 / W) + wave / W, w = wave % W, lane = threadIdx.x & 63;
+  if (t.seq < 0 || (W > 1 ? (int)blockIdx.y : r) >= t.count) return;  // (W > 1: a row a workgroup)
+  // where the row's parts are: of its own keys, and of the prefix
+  const float *part[2] = {a.part, nullptr}, *ml[2] = {a.part_ml, nullptr};
+  int64_t at[2] = {(int64_t)blockIdx.x * a.splits * R + r, 0};  // part z's row is at + z * rows
+  int splits[2] = {a.splits, 0}, rows[2] = {R, 0};
+  const int g = group_of(a, t.seq);
+  if (g >= 0) {
+    const GroupView v = group_view(a, g);
+    const int in = (int)(t.start - v.start) * a.group + t.first + r, n = v.n * a.group;
+    const int c = n <= 16 ? !a.pre[0].small : a.pre[1].large;  // which launch took the group
+    const int tall = c ? kTileRows : 16;
+    if (in >= 0 && in < n) {
+      int tile = g;
+      if (a.max_tokens * a.group > tall) {
+        tile = in / tall;
+        for (int g0 = 0; g0 < g; g0 += 64) {
+          int m = 0;
+          if (g0 + lane < g) {
+            const int of = group_view(a, g0 + lane).n * a.group;
+            if (of <= 16 ? a.pre[c].small : a.pre[c].large) m = (of + tall - 1) / tall;
+          }
+#pragma unroll
+          for (int d = 32; d; d >>= 1) m += __shfl_xor(m, d);
+          tile += m;
+        }
+      }
+      if (tile < a.pre[c].tiles) {  // (groups that overlap may have more tiles than a launch has)
+        part[1] = a.pre[c].part, ml[1] = a.pre[c].part_ml;
+        splits[1] = a.pre[c].splits, rows[1] = tall;
+        at[1] = ((int64_t)tile * a.pool.n_kv + kvh) * splits[1] * tall + in % tall;
+      }
+    }
+  }
+  float top = -INFINITY;
+  int used[2] = {0, 0};  // parts up to the last that holds anything
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+    for (int z0 = 0; z0 < splits[x]; z0 += 64) {
+      const int z = z0 + lane;
+      const float *p = ml[x] + (at[x] + (int64_t)(z < splits[x] ? z : 0) * rows[x]) * 2;
+      const float m = p[0], l = p[1];
+      if (z < splits[x]) top = fmaxf(top, m);
+      const uint64_t some = __ballot(z < splits[x] && l != 0.0f);
+      if (some) used[x] = z0 + 64 - __builtin_clzll(some);
+    }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float at0 = top == -INFINITY ? 0.0f : top;
+  const int lanes = a.dim <= 64 ? 16 : a.dim <= 128 ? 32 : 64, sub = lane / lanes, per = 64 / lanes;
+  const int d = lane % lanes * 4, dd = d < a.dim ? d : 0;
+  float l = 0.0f;
+  f32x4 o = f32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+#pragma unroll 4
+    for (int z0 = w * per; z0 < used[x]; z0 += W * per) {
+      const int z = z0 + sub < used[x] ? z0 + sub : used[x] - 1;
+      const float *p = ml[x] + (at[x] + (int64_t)z * rows[x]) * 2;
+      const float lz = z0 + sub < used[x] ? p[1] : 0.0f, f = exp2_fast(p[0] - at0);
+      const f32x4 v = *reinterpret_cast<const f32x4 *>(part[x] + (at[x] + (int64_t)z * rows[x]) * a.dim + dd);
+      if (lz != 0.0f) l += lz * f, o += v * f;
+    }
+  }
+  for (int m = lanes; m < 64; m <<= 1) {
+    l += __shfl_xor(l, m);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], m);
+  }
+  if constexpr (W > 1) {
+    os[w][lane] = o;
+    if (lane == 0) ls[w] = l;
+    __syncthreads();
+    if (w) return;
+    o = f32x4{0, 0, 0, 0}, l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) o += os[i][lane], l += ls[i];
+  }
+  if (lane < lanes && d < a.dim) put_row<T>(a, t, r, kvh, d, o, top, l);
 }
 
 }  // namespace sats

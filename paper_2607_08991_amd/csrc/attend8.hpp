@@ -1,0 +1,428 @@
+// Attention over a cache of 8 bits (gfx950): the tiles, masks, softmax and parts of attend.hpp with
+// other loads.  Codes become bf16 numbers in registers (exactly: their scales are powers of two), those
+// of E4M3 with the scale in the converting instruction, and multiply as those of a bf16 cache do.
+// Queries of float32 go in as three bf16 pieces (24 bits), weights for them too, so that float32
+// callers lose nothing but what the cache has lost.
+//
+// Pages have 16 tokens or more here, so that 16 keys have one address.  A kernel serves every phase.
+#pragma once
+
+#include "attend.hpp"
+
+namespace sats {
+
+// ------------------------------------------------------------------ tiles of 16 rows
+
+template <typename T, int F, int DT, bool FULL>
+__global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_rows8_kernel(AttendArgs a) {
+  constexpr int kKeys = 32, kTiles = 2, kOut = DT / 16, kChunks = DT / 16, kSteps = DT / 64;
+  constexpr int kLoads = kKeys * kChunks / 64, kPer = kLoads / kTiles, kPieces = sizeof(T) == 2 ? 1 : 3;
+  constexpr bool kSkip = !FULL && DT <= 128;
+  constexpr int kPitch = DT * 2 + 32;
+  constexpr int kPart = kKeys * kPitch > 16 * DT * 4 ? kKeys * kPitch : 16 * DT * 4;
+  __shared__ __align__(16) uint8_t lds[4][kPart];
+  __shared__ float ml[4][16][2];
+
+  const int kvh = blockIdx.x % a.pool.n_kv, z = blockIdx.y;
+  const RowTile t = find_tile<16, true>(a, blockIdx.x / a.pool.n_kv);
+  if (t.seq < 0) return;
+  RowPlaces<16> places;
+  places.find(a, t);
+  const KeyBlocks kb = key_blocks<kKeys>(a, t, places);
+  const int parts = kb.n > a.per_split ? (kb.n + a.per_split - 1) / a.per_split : 1;
+  if (z >= parts) {
+    put_nothing<16>(a, t, z);
+    return;
+  }
+  const int b_end = kb.n < (z + 1) * a.per_split ? kb.n : (z + 1) * a.per_split;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, row = lane & 15, g = lane >> 4;
+  const int64_t place = places.of(row);
+  const bool several = kb.low != kb.high;
+
+  // Q as the second operand: of this lane's row the dims 16 (g + 4 s) .. + 15, as a lane has a key's codes
+  u32x4 qv[kPieces][kSteps][2];
+  {
+    const int r = t.first + (row < t.count ? row : t.count - 1);
+    const T *q = (const T *)a.q + (t.start + r / a.group) * a.q_stride + (int64_t)(kvh * a.group + r % a.group) * a.dim;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int d = 16 * (g + 4 * s) + 8 * y;
+        if constexpr (sizeof(T) == 2) {
+          qv[0][s][y] = d < a.dim ? *reinterpret_cast<const u32x4 *>(q + d) : u32x4{0, 0, 0, 0};
+        } else {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; i += 4) {
+            const f32x4 v = d < a.dim ? *reinterpret_cast<const f32x4 *>(q + d + i) : f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[i + j] = v[j];
+          }
+#pragma unroll
+          for (int p = 0; p < kPieces; ++p) {
+            bf16x8_t piece;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float top = odd_of(x[i]) ? x[i] : __uint_as_float(__float_as_uint(x[i]) & 0xffff0000u);
+              piece[i] = (__bf16)top;
+              x[i] = odd_of(x[i]) ? 0.0f : x[i] - top;  // (what is infinite or NaN is so in its first piece)
+            }
+            qv[p][s][y] = __builtin_bit_cast(u32x4, piece);
+          }
+        }
+      }
+  }
+  const float scale2 = a.scale * kLog2e;
+  const int64_t head_bytes = ((int64_t)kvh << a.pool.shift) * a.dim, head_rows = (int64_t)kvh << a.pool.shift;
+  const int64_t page_bytes = ((int64_t)a.pool.n_kv << a.pool.shift) * a.dim, page_rows = (int64_t)a.pool.n_kv << a.pool.shift;
+  const char *kp = (const char *)a.k + head_bytes, *vp = (const char *)a.v + head_bytes;
+  const char *ksp = (const char *)a.k_scale + head_rows, *vsp = (const char *)a.v_scale + head_rows;
+
+  u32x4 kr[kTiles][kSteps], vr[kLoads];
+  uint8_t ks[kTiles], vs[kLoads];
+  auto page_of = [&](int b) {  // of key lane % 32 of a block
+    return b < b_end ? key_page<true>(a, t, kb, block_key(kb, b, kKeys) + (lane & (kKeys - 1))) : -1;
+  };
+  auto load = [&](int b, int page, uint32_t there) {
+    const int j0 = (int)(block_key(kb, b, kKeys) & (a.pool.page - 1));
+#pragma unroll
+    for (int kt = 0; kt < kTiles; ++kt) {
+      const uint32_t here = there >> (16 * kt) & 0xffffu;
+      const int64_t p = here ? __builtin_amdgcn_readlane(page, 16 * kt + __builtin_ctz(here)) : 0;
+      const int slot = (j0 + 16 * kt) & (a.pool.page - 1);
+      const int64_t at = p * page_bytes + slot * a.dim, at_s = p * page_rows + slot;
+      const __amdgpu_buffer_rsrc_t rk = rows_rsrc(kp + at), rv = rows_rsrc(vp + at);
+      const __amdgpu_buffer_rsrc_t rks = rows_rsrc(ksp + at_s), rvs = rows_rsrc(vsp + at_s);
+      const bool k_here = here >> row & 1;
+      const uint32_t k_off = k_here ? row * a.dim + g * 16 : kNoRow;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+        kr[kt][s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                  rk, FULL || (4 * s + g) * 16 < a.dim ? k_off + 64 * s : kNoRow, 0, 0));
+      ks[kt] = __builtin_amdgcn_raw_buffer_load_b8(rks, k_here ? row : kNoRow, 0, 0);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int r = (i * 64 + lane) / kChunks, c = (i * 64 + lane) % kChunks;
+        const bool v_here = here >> r & 1;
+        vr[kt * kPer + i] = __builtin_bit_cast(
+            u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, v_here && (FULL || c * 16 < a.dim) ? r * a.dim + c * 16 : kNoRow, 0, 0));
+        vs[kt * kPer + i] = __builtin_amdgcn_raw_buffer_load_b8(rvs, v_here ? r : kNoRow, 0, 0);
+      }
+    }
+  };
+
+  f32x4 acc[kOut];
+#pragma unroll
+  for (int i = 0; i < kOut; ++i) acc[i] = f32x4{0, 0, 0, 0};
+  float m = -INFINITY, l = 0.0f;
+  uint8_t *mine = lds[w];
+
+  int b = z * a.per_split + w;
+  int page = page_of(b);
+  uint32_t there = (uint32_t)__ballot(page >= 0);
+  if (b < b_end) load(b, page, there);
+  int page_next = page_of(b + 4);
+  for (; b < b_end; b += 4) {
+    const int64_t j0 = block_key(kb, b, kKeys);
+    const uint32_t here = there;
+    const bool whole = here == ~0u && j0 + kKeys - 1 <= kb.low &&
+                       (!a.window || kb.high - j0 < a.window || j0 + kKeys <= a.sinks);
+    // scores: lane (row, keys 16 kt + 4 g + i)
+    f32x4 s[kTiles];
+#pragma unroll
+    for (int kt = 0; kt < kTiles; ++kt) {
+      s[kt] = f32x4{0, 0, 0, 0};
+      const float f = scale_of(ks[kt]);
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st) {
+        if (kSkip && st * 64 >= a.dim) break;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const bf16x8_t k8 = __builtin_bit_cast(bf16x8_t, decode8<F>(kr[kt][st][2 * y], kr[kt][st][2 * y + 1], f));
+#pragma unroll
+          for (int p = kPieces - 1; p >= 0; --p)
+            s[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, __builtin_bit_cast(bf16x8_t, qv[p][st][y]), s[kt], 0, 0, 0);
+        }
+      }
+    }
+    // V to LDS, and the next block's loads
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = (i * 64 + lane) / kChunks, c = (i * 64 + lane) % kChunks;  // (16 rows a tile: kPer loads)
+      const float f = scale_of(vs[i]);
+      uint8_t *to = mine + r * kPitch + c * 32;
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const u32x4 v = decode8<F>(vr[i][2 * y], vr[i][2 * y + 1], f);
+        if (several && !whole) odd |= odd_value<uint16_t>(v);
+        *reinterpret_cast<u32x4 *>(to + 16 * y) = v;
+      }
+    }
+    odd = __any(odd);
+    page = page_next;
+    there = (uint32_t)__ballot(page >= 0);
+    if (b + 4 < b_end) {
+      load(b + 4, page, there);
+      page_next = page_of(b + 8);
+    }
+#pragma unroll
+    for (int kt = 0; kt < kTiles; ++kt) s[kt] *= scale2;
+    if (!whole) {
+      const Sight sight = sight_of(a, place, j0);
+      const uint32_t mine = here >> (4 * g);
+#pragma unroll
+      for (int kt = 0; kt < kTiles; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          s[kt][i] = ((mine >> (16 * kt + i) & 1) != 0) & sight.sees(16 * kt + 4 * g + i) ? s[kt][i] : -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int kt = 0; kt < kTiles; ++kt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, s[kt][i]);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float mn = fmaxf(m, top), at0 = mn == -INFINITY ? 0.0f : mn, f = exp2_fast(m - at0);
+    m = mn;
+    float sum = 0.0f;
+#pragma unroll
+    for (int kt = 0; kt < kTiles; ++kt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[kt][i] = exp2_fast(s[kt][i] - at0);
+        sum += s[kt][i];
+      }
+    l = l * f + sum;
+#pragma unroll
+    for (int i = 0; i < kOut; ++i) acc[i] *= f;
+    auto product = [&](auto kind) {
+      constexpr bool kOdd = decltype(kind)::kOdd;
+      // a weight in two pieces of 8 bits (the second as attend_rows_kernel has it), for float32 in three
+      constexpr int kWeights = kPieces == 1 ? 2 : 3;
+      bf16x8_t p[kWeights];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float x = s[e >> 2][e & 3];
+#pragma unroll
+        for (int i = 0; i < kWeights - 1; ++i) {
+          const float top = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+          p[i][e] = (__bf16)top;
+          x = kWeights == 2 ? fmaf(x, 1.0f + 0x1p-20f, -top) : x - top;
+        }
+        p[kWeights - 1][e] = (__bf16)x;
+      }
+#pragma unroll
+      for (int o = 0; o < kOut; ++o) {
+        if (kSkip && 16 * o >= a.dim) break;
+        i16x4_t v2[2];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+          const int r = 16 * kt + 4 * g + (row >> 2);
+          v2[kt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(mine + r * kPitch + 32 * o + (row & 3) * 8));
+          if (kOdd) v2[kt] = sane(v2[kt]);
+        }
+        bf16x8_t v8;
+        __builtin_memcpy(&v8, v2, 16);
+#pragma unroll
+        for (int i = kWeights - 1; i >= 0; --i) acc[o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, p[i], acc[o], 0, 0, 0);
+      }
+    };
+    if (!odd) {
+      product(Plain{});
+    } else {
+      product(Odd{});
+      const Sight sight = sight_of(a, place, j0);
+#pragma unroll 1
+      for (int k = 0; k < kKeys; ++k) {
+        const bool seen = ((here >> k & 1) != 0) & sight.sees(k);
+        float p = 0.0f;
+#pragma unroll
+        for (int kt = 0; kt < kTiles; ++kt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if ((k >> 4) == kt && (k & 3) == i) p = s[kt][i];
+        p = __shfl(p, row + 16 * ((k >> 2) & 3));
+#pragma unroll
+        for (int o = 0; o < kOut; ++o)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint16_t v = reinterpret_cast<const uint16_t *>(mine + k * kPitch)[16 * o + 4 * g + e];
+            if (seen && odd_bits(v)) acc[o][e] += p * bf16_to_f32(v);
+          }
+      }
+    }
+  }
+  finish_rows<T, DT>(a, t, kvh, z, parts > 1 || a.phase != kWhole, m, l, acc, &lds[0][0], ml);
+}
+
+// ------------------------------------------------------------------ tiles of 128 rows
+
+// As attend_tile_kernel, whose blocks come from memory straight into LDS: here a wave's codes of a block
+// are in registers for the length of a step, and become bf16 rows in LDS at the start of the next.
+template <int F, int DT, bool FULL>
+__global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile8_kernel(AttendArgs a) {
+  using Wave = TileWave<DT, FULL>;
+  constexpr int kRow = Wave::kRow, kCodes = DT / 16, kLoads = 16 * kCodes / 64;  // (a wave's 16 rows of a block)
+  __shared__ __align__(16) uint8_t k0[kTileKeys * kRow], k1[kTileKeys * kRow], v0[kTileKeys * kRow], v1[kTileKeys * kRow];
+
+  const int kvh = blockIdx.x % a.pool.n_kv, z = blockIdx.y;
+  const RowTile t = find_tile<kTileRows, true>(a, blockIdx.x / a.pool.n_kv);
+  if (t.seq < 0) return;
+  RowPlaces<kTileRows> places;
+  places.find(a, t);
+  const KeyBlocks kb = key_blocks<kTileKeys>(a, t, places);
+  const int parts = kb.n > a.per_split ? (kb.n + a.per_split - 1) / a.per_split : 1;
+  if (z >= parts) {
+    put_nothing<kTileRows>(a, t, z);
+    return;
+  }
+  const int b0 = z * a.per_split, b_end = kb.n < b0 + a.per_split ? kb.n : b0 + a.per_split;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31;
+  const int row = 32 * w + col, r_in = row < t.count ? row : t.count - 1;  // (rows past the last repeat it)
+
+  Wave wave;
+  wave.take_places(places, w, col);
+  wave.take_rows(a, t, kvh, r_in);
+  const int64_t head_rows = (int64_t)kvh << a.pool.shift, page_rows = (int64_t)a.pool.n_kv << a.pool.shift;
+  const char *kp = (const char *)a.k + head_rows * a.dim, *vp = (const char *)a.v + head_rows * a.dim;
+  const char *ksp = (const char *)a.k_scale + head_rows, *vsp = (const char *)a.v_scale + head_rows;
+  const int32_t *table = a.batch.table + t.seq * a.batch.max_pages;
+
+  HeldPages held;
+  auto page_of = [&](int b) {
+    if (b >= b_end) return -1;
+    const int64_t j0 = block_key(kb, b, kTileKeys), p0 = j0 >> a.pool.shift, p1 = (j0 + kTileKeys - 1) >> a.pool.shift;
+    if (held.first < 0 || p0 < held.first || p1 >= held.first + 64) {
+      held.first = p0;
+      const int p = p0 + lane < a.batch.max_pages ? table[p0 + lane] : -1;
+      held.page = p >= 0 && p < a.pool.n_pages ? p : -1;
+    }
+    const int p = __shfl(held.page, (int)(((j0 + lane) >> a.pool.shift) - held.first));
+    const bool inside = j0 + kTileKeys <= t.len && j0 >= kb.lo && j0 + kTileKeys - 1 <= kb.high &&
+                        (!a.window || kb.low - j0 < a.window || j0 + kTileKeys <= a.sinks);
+    return inside || any_sees<true>(a, kb, t.len, j0 + lane) ? p : -1;
+  };
+  // wave w's 16 rows of a block: load i holds rows i * (64 / kCodes) .., piece lane % kCodes
+  struct Codes {
+    u32x4 c[kLoads];
+    uint8_t s[kLoads];
+  };
+  Codes kc, vc;
+  const int r0 = lane / kCodes, c0 = lane % kCodes;
+  auto fetch = [&](int b, int page, uint64_t there, const char *pool, const char *scales, Codes &to) {
+    const int slot = ((int)(block_key(kb, b, kTileKeys) & (a.pool.page - 1)) + 16 * w) & (a.pool.page - 1);
+    const uint32_t here = (uint32_t)(there >> (16 * w)) & 0xffffu;
+    const int64_t p = here ? __builtin_amdgcn_readlane(page, 16 * w + __builtin_ctz(here)) : 0;
+    const __amdgpu_buffer_rsrc_t rc = rows_rsrc(pool + (p * page_rows + slot) * a.dim), rs = rows_rsrc(scales + p * page_rows + slot);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = i * (64 / kCodes) + r0;
+      const bool in = here >> r & 1;
+      to.c[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                              rc, in && (FULL || c0 * 16 < a.dim) ? r * a.dim + c0 * 16 : kNoRow, 0, 0));
+      to.s[i] = __builtin_amdgcn_raw_buffer_load_b8(rs, in ? r : kNoRow, 0, 0);
+    }
+  };
+  auto put = [&](const Codes &from, uint8_t *to, auto place) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = 16 * w + i * (64 / kCodes) + r0;
+      const float f = scale_of(from.s[i]);
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+        *reinterpret_cast<u32x4 *>(to + r * kRow + place(r, 2 * c0 + y) * 16) = decode8<F>(from.c[i][2 * y], from.c[i][2 * y + 1], f);
+    }
+  };
+  auto put_k = [&](uint8_t *to) { put(kc, to, Wave::k_place); };
+  auto put_v = [&](uint8_t *to) { put(vc, to, Wave::v_place); };
+
+  // K of block b is in buffer (b - b0) % 2, V likewise.  At the barrier of step b every wave's rows (K of
+  // b + 1, V of b) are in LDS, and K of b and V of b - 1 have been read by all; the codes of K of
+  // b + 2 and V of b + 1 are in registers, or on their way.
+  auto run = [&](auto kind) {
+    constexpr bool kOdd = decltype(kind)::kOdd;
+    wave.clear();
+    bool again = false;
+    if (b0 >= b_end) return again;
+    f32x16_t sa[2], sb[2];
+    held.first = -1;
+    int page = page_of(b0);
+    uint64_t here = __ballot(page >= 0), there_next, there;  // (of the block at hand, of the next, of the one after)
+    fetch(b0, page, here, kp, ksp, kc);
+    fetch(b0, page, here, vp, vsp, vc);
+    put_k(k0);
+    put_v(v0);
+    int next = page_of(b0 + 1);
+    there_next = __ballot(next >= 0);
+    if (b0 + 1 < b_end) {
+      fetch(b0 + 1, next, there_next, kp, ksp, kc);
+      fetch(b0 + 1, next, there_next, vp, vsp, vc);
+      put_k(k1);
+    }
+    page = page_of(b0 + 2);
+    there = __ballot(page >= 0);
+    if (b0 + 2 < b_end) fetch(b0 + 2, page, there, kp, ksp, kc);
+    stage_barrier();
+    wave.scores(k0, sa);
+    bool some = !wave.whole(a, here, block_key(kb, b0, kTileKeys));  // rows disagree on a key of the block at hand
+    if (some) wave.mask(a, here, block_key(kb, b0, kTileKeys), sa);
+    float top = sa[0][0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) top = fmaxf(top, sa[i >> 4][i & 15]);
+    wave.rescale(top);
+    auto step = [&](int b, f32x16_t (&s)[2], f32x16_t (&sn)[2], uint8_t *kt, uint8_t *kn, uint8_t *vt, uint8_t *vn) {
+      stage_barrier();
+      if (b + 2 < b_end) put_k(kt);
+      put_v(vn);
+      if (b + 2 < b_end) fetch(b + 2, page, there, vp, vsp, vc);
+      const int after = page_of(b + 3);
+      const uint64_t there_after = __ballot(after >= 0);
+      if (b + 3 < b_end) fetch(b + 3, after, there_after, kp, ksp, kc);
+      const bool odd = some && Wave::odd_block(vt);
+      wave.template weights<true>(s, kn, sn);
+      const int64_t j1 = block_key(kb, b + 1, kTileKeys);
+      some = !wave.whole(a, there_next, j1);
+      if (some) wave.mask(a, there_next, j1, sn);
+      if (kOdd && odd) {
+        wave.template product<true, true>(s, vt, sn, &top);
+        wave.add_odd(a, here, block_key(kb, b, kTileKeys), s, vt);
+      } else {
+        wave.template product<false, true>(s, vt, sn, &top);
+        again |= odd;
+      }
+      wave.rescale(top);
+      here = there_next, there_next = there, there = there_after, page = after;
+    };
+    auto last = [&](int b, f32x16_t (&s)[2], uint8_t *vt) {
+      stage_barrier();
+      const bool odd = some && Wave::odd_block(vt);
+      wave.template weights<false>(s, vt, s);
+      if (kOdd && odd) {
+        wave.template product<true, false>(s, vt, s, &top);
+        wave.add_odd(a, here, block_key(kb, b, kTileKeys), s, vt);
+      } else {
+        wave.template product<false, false>(s, vt, s, &top);
+        again |= odd;
+      }
+    };
+    int b = b0;
+    for (; b + 2 < b_end; b += 2) {
+      step(b, sa, sb, k0, k1, v0, v1);
+      step(b + 1, sb, sa, k1, k0, v1, v0);
+    }
+    if (b + 1 < b_end) {
+      step(b, sa, sb, k0, k1, v0, v1);
+      last(b + 1, sb, v1);
+    } else {
+      last(b, sa, v0);
+    }
+    return again;
+  };
+  if (__syncthreads_or(run(Plain{}))) run(Odd{});
+  wave.put(a, t, kvh, row, z, parts > 1 || a.phase != kWhole);
+}
+
+}  // namespace sats

@@ -43,6 +43,7 @@ struct PagesArgs {
 
 struct CopyArgs {
   char *k, *v;                  // the pools of every layer
+  uint8_t *k_scale, *v_scale;   // of 8-bit caches, or null
   int64_t n_pages, layers;
   int n_kv, page, row_bytes;    // row: a token's head
   const int32_t *src, *dst, *valid;  // valid null: whole pages
@@ -315,6 +316,11 @@ __global__ __launch_bounds__(kThreads) void pages_copy_kernel(CopyArgs a, PagesA
     const int64_t run = (int64_t)a.page * a.row_bytes;
     const char *from = pool + ((layer * a.n_pages + src) * a.n_kv + h) * run;
     char *to = pool + ((layer * a.n_pages + dst) * a.n_kv + h) * run;
+    if (a.k_scale) {
+      uint8_t *scale = kv ? a.v_scale : a.k_scale;
+      const int64_t s = ((layer * a.n_pages + src) * a.n_kv + h) * a.page, d = ((layer * a.n_pages + dst) * a.n_kv + h) * a.page;
+      for (int i = lane; i < valid; i += 64) scale[d + i] = scale[s + i];
+    }
     const int bytes = valid * a.row_bytes;
     for (int b = lane * 16; b < bytes; b += 64 * 16)
       __builtin_nontemporal_store(__builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from + b)), reinterpret_cast<u32x4 *>(to + b));

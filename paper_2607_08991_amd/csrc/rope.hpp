@@ -35,12 +35,14 @@ struct RopeArgs {
   int per;                           // rows of a token that a row of lanes takes
   // the cache (null k_pool: keys go to k_out)
   void *k_pool, *v_pool;             // of the layer
+  uint8_t *k_scale, *v_scale;        // of the layer, 8-bit caches
   BatchView batch;
   PoolView pool;
 };
 
-// NU: units of 2 V elements that a lane holds (1, or 2 for scalar loads of long rows).
-template <typename T, int V, int NU>
+// NU: units of 2 V elements that a lane holds (1, or 2 for scalar loads of long rows).  F: the format
+// of the cache's rows.
+template <typename T, int V, int NU, int F>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
   const int lane = threadIdx.x & (a.lanes - 1);
   const int groups = (a.rows + a.per - 1) / a.per;  // rows of lanes per token
@@ -123,14 +125,17 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
           if (on[u]) x[u][i] *= f * wx[u][i], y[u][i] *= f * wy[u][i];
     }
     T *dst = nullptr;
-    if (live) {
+    uint8_t *codes = nullptr;
+    if (live && F != kPlain && !is_q) {
+      if (dst_row >= 0) codes = (uint8_t *)(is_v ? a.v_pool : a.k_pool) + (dst_row + (int64_t)h * a.pool.page) * a.dim;
+    } else if (live) {
       if (is_q) dst = (T *)a.q_out + t * a.q_out_stride + (int64_t)h * a.dim;
       else if (!a.k_pool) dst = (T *)a.k_out + t * a.k_out_stride + (int64_t)h * a.dim;
       else if (dst_row >= 0) dst = (T *)(is_v ? a.v_pool : a.k_pool) + (dst_row + (int64_t)h * a.pool.page) * a.dim;
     }
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
-      if (!on[u] || !dst) continue;
+      if (!on[u] || !(dst || codes)) continue;
       T o0[V], o1[V];
       if (turn[u] && !is_v) {
         if (!a.pairs) {
@@ -156,10 +161,32 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
           }
         }
       }
+      if (F != kPlain && codes) continue;
 #pragma unroll
       for (int i = 0; i < V; ++i) o0[i] = Elem<T>::round(x[u][i]), o1[i] = Elem<T>::round(y[u][i]);
       store_vec<T, V>(dst + e0[u], o0);
       store_vec<T, V>(dst + e1[u], o1);
+    }
+    if constexpr (F != kPlain) {
+      if (is_q) continue;
+      uint32_t top = 0;  // bits of a magnitude are ordered as it is, NaN above all
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const uint32_t p = __float_as_uint(x[u][i]) & 0x7fffffffu, q = __float_as_uint(y[u][i]) & 0x7fffffffu;
+          if (on[u]) top = top > p ? top : p, top = top > q ? top : q;
+        }
+      for (int m = a.lanes >> 1; m; m >>= 1) {
+        const uint32_t o = __shfl_xor(top, m);
+        top = top > o ? top : o;
+      }
+      const RowScale rs = row_scale<F>(top);
+      if (!codes) continue;
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+        if (on[u]) store_codes<F, V>(codes + e0[u], x[u], rs), store_codes<F, V>(codes + e1[u], y[u], rs);
+      if (lane == 0) (is_v ? a.v_scale : a.k_scale)[dst_row + (int64_t)h * a.pool.page] = (uint8_t)rs.byte;
     }
   }
 }

@@ -2143,7 +2143,7 @@ int serve_workspace(hipStream_t stream, size_t bytes, char **mem, Turn *turn) tr
   if (w.serve_bytes < bytes) {
     if (capturing)
       return ::fail(SATS_ERR_WORKSPACE, "%zu bytes of scratch memory are not there under stream capture: call "
-                    "sats_reserve_serving first", bytes);
+                    "sats_reserve_serving (sats_reserve_prefix) first", bytes);
     size_t got = 0;
     char *m = alloc_or(std::max(bytes, 2 * w.serve_bytes), bytes, &got);
     if (!m) return ::fail(SATS_ERR_WORKSPACE, "workspace allocation of %zu bytes failed", bytes);

@@ -4,10 +4,12 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "host.hpp"
 
-#include "attend.hpp"
+#include "attend_host.hpp"
+#include "logits.hpp"
 #include "pages.hpp"
 #include "rope.hpp"
 #include "sample.hpp"
@@ -32,45 +34,41 @@ struct Carve {
   }
 };
 
+using sats_host::kMaxGrid;
+using sats_host::launched;
+
 constexpr int64_t kMaxCount = (int64_t)1 << 30;
-// Workgroups of 256 threads in a row of a launch, at most: HIP takes less than 2^32 threads there.
-constexpr int64_t kMaxGrid = ((int64_t)1 << 24) - 1;
-static_assert(sats::kThreads == 256, "");
 
 // Rotation: waves that fill the chip.
 constexpr int64_t kRopeWaves = 4096;
-// Parts up to which one wave joins a row, four above.  us where the limit is 8, 16, 32, 64: a sequence
-// of 4000 keys (16 parts) 12.2, 13.3, 13.3, 13.3; of 6000 12.6, 12.6, 14.5, 14.5; of 16000 (63) 22.5, 22.5,
-// 22.5, 34.3; 128 new tokens on 4000, whose tiles have 128 rows, 38.9, 35.4, 35.3, 35.3.
-constexpr int kJoinWave = 16;
-// Attention: workgroups that the chip holds at once (two a compute unit; of the kernels for
-// heads above 128 one, of the 16-row kernels for heads up to 96 three), which a launch that
-// splits its tiles aims at: a few more would wait for a second round.  8 sequences of 2000 to 6000
-// keys: 512 workgroups 30.8 us, 768 38.1.
-// Tiles of 16 rows whose parts stay at kLongBlocks blocks or more are split over up to
-// kSlotsLong workgroups, since sequences of different lengths then share the chip more
-// evenly (64 sequences of 500 to 8000 keys 156 -> 150 us).
-// Key blocks of a part, at least, of 16 rows and of 128.  us for 4, 8, 16 blocks of 16 rows: a sequence
-// of 500 keys 10.1, 11.8, 14.8; of 2000 11.5, 12.5, 16.4; of 4000 10.7, 13.3, 16.7; of 8000 16.0, 14.2, 20.1.
-// For 2, 4, 8 blocks of 128: 64 new tokens on 500 18.8, 21.2, 26.6; on 2000 25.5, 23.6, 28.2; 256 on 1000
-// 34.5, 34.2, 31.5; 512 alone 31.8, 31.0, 32.6.
-constexpr int kSlots = 512, kSlotsLong = 2048, kLongBlocks = 24, kRowsLeast = 8, kTileLeast = 4;
+// Compute units, twice over.
+constexpr int kSlots = 512;
 
-int launched(const char *what) {
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? SATS_OK : fail(SATS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+// The format of a cache's rows, the bytes of one of its elements, its 8-bit part (or null), and the
+// type of what is quantised into it and attends over it.
+int form_of(const sats_kv_cache *c) {
+  return c->elem_bytes == SATS_KV_E4M3 ? sats::kE4m3 : c->elem_bytes == SATS_KV_INT8 ? sats::kInt8 : sats::kPlain;
 }
+int stored_bytes(const sats_kv_cache *c) { return form_of(c) ? 1 : c->elem_bytes; }
+const sats_kv_cache8 *cache8_of(const sats_kv_cache *c) {
+  return form_of(c) ? reinterpret_cast<const sats_kv_cache8 *>(c) : nullptr;
+}
+int outer_bytes(const sats_kv_cache *c) { return form_of(c) ? cache8_of(c)->q_elem_bytes : c->elem_bytes; }
 
-// Bytes of an array of keys (or values) of every layer.
-double pool_bytes(const sats_kv_cache *c) {
-  return (double)c->n_layers * (double)c->n_pages * (double)c->n_kv_heads * (double)c->page_size * (double)c->head_dim *
-         c->elem_bytes;
+// Rows (of a token's head) of every layer, and bytes of an array of keys (or values) of every layer.
+double pool_rows(const sats_kv_cache *c) {
+  return (double)c->n_layers * (double)c->n_pages * (double)c->n_kv_heads * (double)c->page_size;
 }
+double pool_bytes(const sats_kv_cache *c) { return pool_rows(c) * (double)c->head_dim * stored_bytes(c); }
 
 int check_cache(const sats_kv_cache *c, bool data) {
   if (!c) return fail(SATS_ERR_NULL, "cache must be non-null");
   if (data && (!c->k || !c->v)) return fail(SATS_ERR_NULL, "the cache's k and v must be non-null");
-  if (c->elem_bytes != 2 && c->elem_bytes != 4) return fail(SATS_ERR_ARG, "elem_bytes must be 2 or 4");
+  const sats_kv_cache8 *c8 = cache8_of(c);
+  if (!c8 && c->elem_bytes != 2 && c->elem_bytes != 4)
+    return fail(SATS_ERR_ARG, "elem_bytes must be 2, 4, SATS_KV_E4M3 or SATS_KV_INT8");
+  if (c8 && data && (!c8->k_scale || !c8->v_scale)) return fail(SATS_ERR_NULL, "the cache's k_scale and v_scale must be non-null");
+  if (c8 && c8->q_elem_bytes != 2 && c8->q_elem_bytes != 4) return fail(SATS_ERR_ARG, "q_elem_bytes must be 2 or 4");
   if (c->n_layers < 1 || c->n_pages < 1 || c->n_kv_heads < 1 || c->n_layers > 4096 || c->n_pages > kMaxCount ||
       c->n_kv_heads > 1024)
     return fail(SATS_ERR_SHAPE, "a cache has 1 to 4096 layers, 1 to 2^30 pages and 1 to 1024 heads");
@@ -78,6 +76,8 @@ int check_cache(const sats_kv_cache *c, bool data) {
     return fail(SATS_ERR_SHAPE, "page_size must be a power of two up to 4096");
   if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8)
     return fail(SATS_ERR_SHAPE, "head_dim must be a multiple of 8 from 8 to 256");
+  if (c8 && (c->page_size < 16 || c->head_dim % 16))
+    return fail(SATS_ERR_SHAPE, "a cache of 8 bits has pages of at least 16 tokens, and heads of a multiple of 16 dims");
   if (pool_bytes(c) > 1e18) return fail(SATS_ERR_SHAPE, "the cache is too large");
   if (data && (!on16(c->k) || !on16(c->v))) return fail(SATS_ERR_ARG, "the cache's k and v must be 16-byte aligned");
   return SATS_OK;
@@ -110,7 +110,10 @@ sats::BatchView batch_view(const sats_kv_batch *b) {
 }
 
 char *layer_of(void *pool, const sats_kv_cache *c, int64_t layer) {
-  return static_cast<char *>(pool) + layer * c->n_pages * c->n_kv_heads * c->page_size * c->head_dim * c->elem_bytes;
+  return static_cast<char *>(pool) + layer * c->n_pages * c->n_kv_heads * c->page_size * c->head_dim * stored_bytes(c);
+}
+uint8_t *layer_scales(uint8_t *scales, const sats_kv_cache *c, int64_t layer) {
+  return scales + layer * c->n_pages * c->n_kv_heads * c->page_size;
 }
 
 // Bytes from a row's start to the last row's end, for n rows of `row` elements at a stride.
@@ -139,8 +142,10 @@ bool rows_overlap(const Rows &a, const Rows &b, int64_t n, int esz) {
 
 // Whether n bytes at p touch the cache's arrays.
 bool in_cache(const void *p, int64_t n, const sats_kv_cache *c) {
-  const int64_t all = (int64_t)pool_bytes(c);
-  return overlap(p, n, c->k, all) || overlap(p, n, c->v, all);
+  const int64_t all = (int64_t)pool_bytes(c), rows = (int64_t)pool_rows(c);
+  const sats_kv_cache8 *c8 = cache8_of(c);
+  return overlap(p, n, c->k, all) || overlap(p, n, c->v, all) ||
+         (c8 && (overlap(p, n, c8->k_scale, rows) || overlap(p, n, c8->v_scale, rows)));
 }
 
 // ------------------------------------------------------------- norm and rotation
@@ -193,104 +198,16 @@ int run_rope(sats::RopeArgs a, int esz, const sats_kv_cache *cache, hipStream_t 
   if (threads > sats::kThreads * kMaxGrid) return fail(SATS_ERR_SHAPE, "too many rows for one call");
   const dim3 grid((unsigned)((threads + sats::kThreads - 1) / sats::kThreads));
   auto go = [&](auto fn) { fn<<<grid, sats::kThreads, 0, stream>>>(a); };
-  if (esz == 2) wide ? go(sats::rope_kernel<uint16_t, 8, 1>) : go(sats::rope_kernel<uint16_t, 1, 2>);
-  else wide ? go(sats::rope_kernel<float, 4, 1>) : go(sats::rope_kernel<float, 1, 2>);
+  auto of = [&](auto f) {
+    constexpr int F = decltype(f)::value;
+    if (esz == 2) wide ? go(sats::rope_kernel<uint16_t, 8, 1, F>) : go(sats::rope_kernel<uint16_t, 1, 2, F>);
+    else wide ? go(sats::rope_kernel<float, 4, 1, F>) : go(sats::rope_kernel<float, 1, 2, F>);
+  };
+  const int form = cache ? form_of(cache) : sats::kPlain;
+  if (form == sats::kE4m3) of(std::integral_constant<int, sats::kE4m3>{});
+  else if (form == sats::kInt8) of(std::integral_constant<int, sats::kInt8>{});
+  else of(std::integral_constant<int, sats::kPlain>{});
   return launched("rope_kernel");
-}
-
-// ------------------------------------------------------------- attention
-
-// The split of a launch: row tiles of R rows, their number at most, and over how many
-// workgroups a tile's blocks of `keys` keys go.
-struct AttendPlan {
-  int64_t tiles;
-  int splits, per_split;
-};
-AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, int64_t max_q) {
-  const sats::BatchView &b = a.batch;
-  const int64_t per_seq = (max_q * a.group + R - 1) / R;
-  AttendPlan p;
-  p.tiles = b.n_tokens * a.group / R + b.n_seqs;
-  if (b.n_seqs && per_seq <= p.tiles / b.n_seqs) p.tiles = b.n_seqs * per_seq;
-  int64_t range = std::min<int64_t>(b.max_kv, b.max_pages << a.pool.shift);  // keys that a tile can see
-  if (a.window) range = std::min(range, a.window + R / a.group + 1 + a.sinks + 2 * keys);
-  const int64_t blocks = std::max<int64_t>(1, (range + keys - 1) / keys + 1);
-  const int64_t wgs = std::max<int64_t>(1, p.tiles * a.pool.n_kv);
-  int64_t slots = a.dim > 128 ? kSlots / 2 : kSlots;
-  if (R == 16 && a.dim <= 96) slots = kSlots * 3 / 2;
-  int64_t want = std::max<int64_t>(1, slots / wgs);
-  if (R == 16) want = std::max(want, std::min<int64_t>(kSlotsLong / wgs, blocks / kLongBlocks));
-  p.per_split = (int)std::max<int64_t>(least, (blocks + want - 1) / want);
-  p.splits = (int)((blocks + p.per_split - 1) / p.per_split);
-  return p;
-}
-
-size_t attend_bytes(const AttendPlan &p, int R, int n_kv, int dim) {
-  return p.splits > 1 ? (size_t)p.tiles * n_kv * p.splits * R * (dim + 2) * sizeof(float) : 0;
-}
-
-template <typename T, int R, typename Kernel>
-int launch_attention(sats::AttendArgs a, const AttendPlan &p, Kernel kernel, char *mem, hipStream_t stream) {
-  const int64_t grid_x = p.tiles * a.pool.n_kv;
-  a.splits = p.splits, a.per_split = p.per_split;
-  a.part = reinterpret_cast<float *>(mem);
-  a.part_ml = a.part + grid_x * p.splits * R * a.dim;
-  kernel<<<dim3((unsigned)grid_x, (unsigned)p.splits), 256, 0, stream>>>(a);
-  int rc = launched("attention kernel");
-  if (rc || p.splits == 1) return rc;
-  const int64_t rows = std::min<int64_t>(R, a.batch.max_q * a.group);
-  if (p.splits > kJoinWave) sats::attend_join_kernel<T, R, 4><<<dim3((unsigned)grid_x, (unsigned)rows), 256, 0, stream>>>(a);
-  else sats::attend_join_kernel<T, R, 1><<<dim3((unsigned)grid_x, (unsigned)((rows + 3) / 4)), 256, 0, stream>>>(a);
-  return launched("attend_join_kernel");
-}
-
-// The second argument is true for heads of exactly the first one's dims only: such a kernel
-// loads rows of that width.
-typedef void (*AttendKernel)(sats::AttendArgs);
-template <typename T> AttendKernel rows_kernel(int dim) {
-  using namespace sats;
-  return dim <= 64    ? (dim == 64 ? attend_rows_kernel<T, 64, true> : attend_rows_kernel<T, 64, false>)
-         : dim <= 96  ? (dim == 96 ? attend_rows_kernel<T, 96, true> : attend_rows_kernel<T, 96, false>)
-         : dim <= 128 ? (dim == 128 ? attend_rows_kernel<T, 128, true> : attend_rows_kernel<T, 128, false>)
-                      : (dim == 256 ? attend_rows_kernel<T, 256, true> : attend_rows_kernel<T, 256, false>);
-}
-AttendKernel tile_kernel(int dim) {
-  using namespace sats;
-  return dim <= 64    ? (dim == 64 ? attend_tile_kernel<64, true> : attend_tile_kernel<64, false>)
-         : dim <= 128 ? (dim == 128 ? attend_tile_kernel<128, true> : attend_tile_kernel<128, false>)
-                      : (dim == 256 ? attend_tile_kernel<256, true> : attend_tile_kernel<256, false>);
-}
-
-// Sequences of at most 16 rows a cache head, and all of float32, go in tiles of 16 rows,
-// the others in tiles of 128.  A batch of one sequence needs no launch for the former.
-template <typename T> int run_attention(sats::AttendArgs a, hipStream_t stream) {
-  constexpr bool bf16 = sizeof(T) == 2;
-  AttendPlan small{}, large{};
-  const bool any_large = bf16 && a.batch.max_q * a.group > 16;
-  if (!any_large || a.batch.n_seqs > 1) {
-    small = attend_plan(a, 16, sats::RowsOf<T>::kKeys, kRowsLeast, any_large ? 16 / a.group : a.batch.max_q);
-  }
-  if (any_large) large = attend_plan(a, sats::kTileRows, sats::kTileKeys, kTileLeast, a.batch.max_q);
-  for (const AttendPlan *p : {&small, &large})
-    if (p->tiles * a.pool.n_kv > kMaxGrid || p->splits > 65535) return fail(SATS_ERR_SHAPE, "too many rows for one call");
-  const size_t bytes = std::max(attend_bytes(small, 16, a.pool.n_kv, a.dim),
-                                attend_bytes(large, sats::kTileRows, a.pool.n_kv, a.dim));
-  char *mem = nullptr;
-  Turn turn;
-  int rc = bytes ? sats_host::serve_workspace(stream, bytes, &mem, &turn) : SATS_OK;
-  if (rc) return rc;
-  if (small.tiles) {
-    a.small = 1, a.large = !bf16;
-    auto kernel = rows_kernel<T>(a.dim);
-    if ((rc = launch_attention<T, 16>(a, small, kernel, mem, stream))) return rc;
-  }
-  if constexpr (bf16)
-    if (large.tiles) {
-      a.small = small.tiles == 0, a.large = 1;
-      auto kernel = tile_kernel(a.dim);
-      rc = launch_attention<T, sats::kTileRows>(a, large, kernel, mem, stream);
-    }
-  return rc;
 }
 
 // ------------------------------------------------------------- pages
@@ -352,8 +269,10 @@ int copy_pages(const sats_kv_cache *c, const int32_t *src, const int32_t *dst, c
   const int64_t table = table_grid(entries);
   const int64_t waves = n * c->n_layers * 2 * c->n_kv_heads, per = sats::kThreads / 64;
   const int64_t grid = std::clamp<int64_t>((waves + per - 1) / per, 1, kCopyGrid);
-  sats::CopyArgs a{static_cast<char *>(c->k), static_cast<char *>(c->v), c->n_pages, c->n_layers, (int)c->n_kv_heads,
-                   (int)c->page_size, (int)(c->head_dim * c->elem_bytes), src, dst, valid, ctl, (int)n, (int)table};
+  const sats_kv_cache8 *c8 = cache8_of(c);
+  sats::CopyArgs a{static_cast<char *>(c->k), static_cast<char *>(c->v), c8 ? c8->k_scale : nullptr, c8 ? c8->v_scale : nullptr,
+                   c->n_pages, c->n_layers, (int)c->n_kv_heads, (int)c->page_size, (int)(c->head_dim * stored_bytes(c)),
+                   src, dst, valid, ctl, (int)n, (int)table};
   sats::pages_copy_kernel<TABLE><<<(unsigned)(table + grid), sats::kThreads, 0, stream>>>(a, t);
   return launched("pages_copy_kernel");
 }
@@ -418,6 +337,85 @@ template <typename T> void launch_sample(const sats::SampleArgs &a, bool wide, h
   sats::sample_pick_kernel<T><<<(unsigned)a.n, sats::kPickThreads, 0, stream>>>(a);
 }
 
+// ------------------------------------------------------------- attention
+
+// The arguments of an attention call, checked; *nothing where there is no row to compute.
+int attend_args(const void *q, int64_t q_stride, const sats_kv_cache *cache, int64_t layer, const sats_kv_batch *batch,
+                int64_t n_q_heads, float scale, int64_t window, int64_t n_sinks, void *out, float *lse, sats::AttendArgs *args,
+                bool *nothing) {
+  int rc = check_cache(cache, true);
+  if (rc || (rc = check_batch(batch))) return rc;
+  if (layer < 0 || layer >= cache->n_layers) return fail(SATS_ERR_SHAPE, "layer outside the cache");
+  if (n_q_heads < 1 || n_q_heads > 4096 || n_q_heads % cache->n_kv_heads)
+    return fail(SATS_ERR_SHAPE, "n_q_heads must be a multiple of the cache's heads, at most 4096");
+  if (window < 0 || n_sinks < 0 || (n_sinks && !window)) return fail(SATS_ERR_ARG, "window and n_sinks must be >= 0, sinks need a window");
+  if (!std::isfinite(scale)) return fail(SATS_ERR_ARG, "scale must be finite");
+  *nothing = batch->n_tokens == 0;
+  if (*nothing) return SATS_OK;
+  if (!q || !out) return fail(SATS_ERR_NULL, "q and out must be non-null");
+  const int esz = outer_bytes(cache);
+  const int64_t row = n_q_heads * cache->head_dim, n = batch->n_tokens;
+  if (q_stride < row) return fail(SATS_ERR_SHAPE, "q_stride is below the token's row");
+  if (!on16(q) || !on16(out) || q_stride * esz % 16) return fail(SATS_ERR_ARG, "q, out and the rows of q must be 16-byte aligned");
+  if (overlap(out, n * row * esz, q, span(n, q_stride, row, esz)) || in_cache(out, n * row * esz, cache))
+    return fail(SATS_ERR_ARG, "out overlaps q or the cache");
+  const int64_t lse_bytes = lse ? n * n_q_heads * (int64_t)sizeof(float) : 0;
+  if (reinterpret_cast<uintptr_t>(lse) % sizeof(float) || overlap(lse, lse_bytes, q, span(n, q_stride, row, esz)) ||
+      overlap(lse, lse_bytes, out, n * row * esz) || in_cache(lse, lse_bytes, cache))
+    return fail(SATS_ERR_ARG, "lse must be 4-byte aligned, apart from q, out and the cache");
+  if (std::min(batch->max_q_len, n) * (n_q_heads / cache->n_kv_heads) > 0x7fffff00)
+    return fail(SATS_ERR_SHAPE, "too many rows for one call");
+  sats::AttendArgs a{};
+  a.q = q, a.q_stride = q_stride, a.out = out, a.lse = lse;
+  a.k = layer_of(cache->k, cache, layer), a.v = layer_of(cache->v, cache, layer);
+  if (const sats_kv_cache8 *c8 = cache8_of(cache))
+    a.k_scale = layer_scales(c8->k_scale, cache, layer), a.v_scale = layer_scales(c8->v_scale, cache, layer);
+  a.batch = batch_view(batch), a.pool = pool_view(cache);
+  a.n_q = (int)n_q_heads, a.group = (int)(n_q_heads / cache->n_kv_heads), a.dim = (int)cache->head_dim;
+  // (places are below 2^31)
+  a.scale = scale, a.window = std::min(window, (int64_t)1 << 31), a.sinks = std::min(n_sinks, (int64_t)1 << 31);
+  *nothing = batch->max_q_len == 0;
+  *args = a;
+  return SATS_OK;
+}
+
+int check_prefix(const sats_kv_prefix *p) {
+  if (!p) return fail(SATS_ERR_NULL, "prefix must be non-null");
+  if (p->n_groups < 0 || p->max_tokens < 0 || p->max_len < 0 || p->max_own < 0 || p->n_groups > kMaxCount || p->max_tokens > kMaxCount ||
+      p->max_len >= (int64_t)1 << 31 || p->max_own >= (int64_t)1 << 31)
+    return fail(SATS_ERR_SHAPE, "a prefix's sizes must be >= 0, at most 2^30 (lengths below 2^31)");
+  if (p->n_groups > 0 && (!p->seq_start || !p->len)) return fail(SATS_ERR_NULL, "the prefix's seq_start and len must be non-null");
+  return SATS_OK;
+}
+void prefix_args(const sats_kv_prefix *p, sats::AttendArgs *a) {
+  a->n_groups = (int)p->n_groups, a->seq_start = p->seq_start, a->shared = p->len;
+  a->max_tokens = std::min(p->max_tokens, a->batch.n_tokens), a->max_len = p->max_len, a->max_own = p->max_own;
+}
+
+// ------------------------------------------------------------- logits
+
+int check_rules(const sats_logit_rules *r, int64_t n, int64_t vocab) {
+  if (!r) return fail(SATS_ERR_NULL, "rules must be non-null");
+  if (r->n_seqs < 0 || r->max_history < 0 || r->n_bias < 0 || r->n_masks < 0 || r->n_seqs > kMaxCount || r->n_masks > kMaxCount ||
+      r->max_history >= (int64_t)1 << 31 || r->n_bias >= (int64_t)1 << 31)
+    return fail(SATS_ERR_SHAPE, "the rules' sizes must be >= 0, at most 2^30 (lengths below 2^31)");
+  if (r->max_history > 0 && n > 0) {
+    if (!r->history) return fail(SATS_ERR_NULL, "history must be non-null");
+    if (!r->history_len) return fail(SATS_ERR_NULL, "history needs history_len");
+    if (r->history_stride < r->max_history) return fail(SATS_ERR_SHAPE, "history_stride is below max_history");
+    if (r->history_stride >= (int64_t)1 << 31) return fail(SATS_ERR_SHAPE, "history_stride must be below 2^31");
+    if (!r->seqs && r->n_seqs < n) return fail(SATS_ERR_SHAPE, "history has fewer rows than logits, and seqs is null");
+  }
+  if (r->n_bias > 0 && (!r->bias || !r->bias_ids || !r->bias_start)) return fail(SATS_ERR_NULL, "biases need bias_start, bias_ids and bias");
+  if (r->n_masks > 0) {
+    if (!r->masks) return fail(SATS_ERR_NULL, "masks must be non-null");
+    if (r->mask_stride < (vocab + 31) / 32) return fail(SATS_ERR_SHAPE, "mask_stride is below a bit an id");
+    if (r->mask_stride >= (int64_t)1 << 31) return fail(SATS_ERR_SHAPE, "mask_stride must be below 2^31");
+    if (!r->mask_of && r->n_masks < n) return fail(SATS_ERR_SHAPE, "fewer masks than rows, and mask_of is null");
+  }
+  return SATS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -462,44 +460,75 @@ int sats_qkv_append(const void *q, int64_t q_stride, const void *k, int64_t k_st
   a.pairs = interleaved;
   a.n_tokens = batch->n_tokens;
   a.k_pool = layer_of(cache->k, cache, layer), a.v_pool = layer_of(cache->v, cache, layer);
+  if (const sats_kv_cache8 *c8 = cache8_of(cache))
+    a.k_scale = layer_scales(c8->k_scale, cache, layer), a.v_scale = layer_scales(c8->v_scale, cache, layer);
   a.batch = batch_view(batch), a.pool = pool_view(cache);
-  return run_rope(a, cache->elem_bytes, cache, stream);
+  return run_rope(a, outer_bytes(cache), cache, stream);
 }
 
 int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *cache, int64_t layer,
                          const sats_kv_batch *batch, int64_t n_q_heads, float scale, int64_t window, int64_t n_sinks,
                          void *out, float *lse, hipStream_t stream) {
   clear_error();
+  sats::AttendArgs a{};
+  bool nothing = false;
+  const int rc = attend_args(q, q_stride, cache, layer, batch, n_q_heads, scale, window, n_sinks, out, lse, &a, &nothing);
+  return rc || nothing ? rc : sats_host::run_attention(a, form_of(cache), outer_bytes(cache), stream);
+}
+
+int sats_prefix_attention(const void *q, int64_t q_stride, const sats_kv_cache *cache, int64_t layer,
+                          const sats_kv_batch *batch, const sats_kv_prefix *prefix, int64_t n_q_heads, float scale,
+                          int64_t window, int64_t n_sinks, void *out, float *lse, hipStream_t stream) {
+  clear_error();
+  sats::AttendArgs a{};
+  bool nothing = false;
+  int rc = check_prefix(prefix);
+  if (rc || (rc = attend_args(q, q_stride, cache, layer, batch, n_q_heads, scale, window, n_sinks, out, lse, &a, &nothing)) || nothing)
+    return rc;
+  if (std::min(prefix->max_tokens, batch->n_tokens) * a.group > 0x7fffff00) return fail(SATS_ERR_SHAPE, "too many rows for one call");
+  prefix_args(prefix, &a);
+  return sats_host::run_prefix_attention(a, form_of(cache), outer_bytes(cache), stream);
+}
+
+int sats_cache_read(const sats_kv_cache *cache, int64_t layer, const sats_kv_batch *batch, void *k_out, int64_t k_stride,
+                    void *v_out, int64_t v_stride, int elem_bytes, hipStream_t stream) {
+  clear_error();
   int rc = check_cache(cache, true);
   if (rc || (rc = check_batch(batch))) return rc;
   if (layer < 0 || layer >= cache->n_layers) return fail(SATS_ERR_SHAPE, "layer outside the cache");
-  if (n_q_heads < 1 || n_q_heads > 4096 || n_q_heads % cache->n_kv_heads)
-    return fail(SATS_ERR_SHAPE, "n_q_heads must be a multiple of the cache's heads, at most 4096");
-  if (window < 0 || n_sinks < 0 || (n_sinks && !window)) return fail(SATS_ERR_ARG, "window and n_sinks must be >= 0, sinks need a window");
-  if (!std::isfinite(scale)) return fail(SATS_ERR_ARG, "scale must be finite");
-  if (batch->n_tokens == 0) return SATS_OK;
-  if (!q || !out) return fail(SATS_ERR_NULL, "q and out must be non-null");
-  const int esz = cache->elem_bytes;
-  const int64_t row = n_q_heads * cache->head_dim, n = batch->n_tokens;
-  if (q_stride < row) return fail(SATS_ERR_SHAPE, "q_stride is below the token's row");
-  if (!on16(q) || !on16(out) || q_stride * esz % 16) return fail(SATS_ERR_ARG, "q, out and the rows of q must be 16-byte aligned");
-  if (overlap(out, n * row * esz, q, span(n, q_stride, row, esz)) || in_cache(out, n * row * esz, cache))
-    return fail(SATS_ERR_ARG, "out overlaps q or the cache");
-  const int64_t lse_bytes = lse ? n * n_q_heads * (int64_t)sizeof(float) : 0;
-  if (reinterpret_cast<uintptr_t>(lse) % sizeof(float) || overlap(lse, lse_bytes, q, span(n, q_stride, row, esz)) ||
-      overlap(lse, lse_bytes, out, n * row * esz) || in_cache(lse, lse_bytes, cache))
-    return fail(SATS_ERR_ARG, "lse must be 4-byte aligned, apart from q, out and the cache");
-  if (std::min(batch->max_q_len, n) * (n_q_heads / cache->n_kv_heads) > 0x7fffff00)
-    return fail(SATS_ERR_SHAPE, "too many rows for one call");
-  sats::AttendArgs a{};
-  a.q = q, a.q_stride = q_stride, a.out = out, a.lse = lse;
+  if (elem_bytes != 2 && elem_bytes != 4) return fail(SATS_ERR_ARG, "elem_bytes must be 2 or 4");
+  const int64_t n = batch->n_tokens, row = cache->n_kv_heads * cache->head_dim;
+  if (n == 0 || (!k_out && !v_out)) return SATS_OK;
+  if ((k_out && k_stride < row) || (v_out && v_stride < row)) return fail(SATS_ERR_SHAPE, "a token stride is below the token's row");
+  const Rows k{k_out, k_stride, row}, v{v_out, v_stride, row};
+  if (rows_overlap(k, v, n, elem_bytes)) return fail(SATS_ERR_ARG, "k_out and v_out overlap");
+  for (const Rows &r : {k, v}) {
+    if (r.p && reinterpret_cast<uintptr_t>(r.p) % elem_bytes) return fail(SATS_ERR_ARG, "k_out and v_out must be aligned to their elements");
+    if (r.p && in_cache(r.p, span(n, r.stride, row, elem_bytes), cache)) return fail(SATS_ERR_ARG, "k_out or v_out overlaps the cache");
+  }
+  sats::ReadArgs a{};
   a.k = layer_of(cache->k, cache, layer), a.v = layer_of(cache->v, cache, layer);
+  if (const sats_kv_cache8 *c8 = cache8_of(cache))
+    a.k_scale = layer_scales(c8->k_scale, cache, layer), a.v_scale = layer_scales(c8->v_scale, cache, layer);
+  a.k_out = k_out, a.v_out = v_out, a.k_stride = k_stride, a.v_stride = v_stride;
   a.batch = batch_view(batch), a.pool = pool_view(cache);
-  a.n_q = (int)n_q_heads, a.group = (int)(n_q_heads / cache->n_kv_heads), a.dim = (int)cache->head_dim;
-  // (places are below 2^31)
-  a.scale = scale, a.window = std::min(window, (int64_t)1 << 31), a.sinks = std::min(n_sinks, (int64_t)1 << 31);
-  if (batch->max_q_len == 0) return SATS_OK;
-  return esz == 2 ? run_attention<uint16_t>(a, stream) : run_attention<float>(a, stream);
+  a.dim = (int)cache->head_dim, a.chunks = a.dim / 8;
+  const int64_t grid = (n * cache->n_kv_heads * a.chunks + sats::kThreads - 1) / sats::kThreads;
+  if (grid > kMaxGrid) return fail(SATS_ERR_SHAPE, "too many rows for one call");
+  const bool wide = on16(k_out) && on16(v_out) && k_stride * elem_bytes % 16 == 0 && v_stride * elem_bytes % 16 == 0;
+  auto go = [&](auto fn) { fn<<<(unsigned)grid, sats::kThreads, 0, stream>>>(a); };
+  auto of = [&](auto c, auto f) {
+    using C = decltype(c);
+    constexpr int F = decltype(f)::value;
+    if (elem_bytes == 2) wide ? go(sats::cache_read_kernel<C, F, uint16_t, true>) : go(sats::cache_read_kernel<C, F, uint16_t, false>);
+    else wide ? go(sats::cache_read_kernel<C, F, float, true>) : go(sats::cache_read_kernel<C, F, float, false>);
+  };
+  const int form = form_of(cache);
+  if (form == sats::kE4m3) of(uint8_t{}, std::integral_constant<int, sats::kE4m3>{});
+  else if (form == sats::kInt8) of(uint8_t{}, std::integral_constant<int, sats::kInt8>{});
+  else if (cache->elem_bytes == 2) of(uint16_t{}, std::integral_constant<int, sats::kPlain>{});
+  else of(float{}, std::integral_constant<int, sats::kPlain>{});
+  return launched("cache_read_kernel");
 }
 
 int sats_cache_free(const sats_kv_cache *cache, const sats_kv_pages *pages, const int32_t *seqs, const int32_t *begin,
@@ -616,16 +645,92 @@ int sats_sample(const void *logits, int elem_bytes, int64_t stride, int64_t n, i
   return rc;
 }
 
+int sats_adjust_logits(const void *logits, int elem_bytes, int64_t stride, const sats_logit_rules *rules, void *out,
+                       int out_elem_bytes, int64_t out_stride, int64_t n, int64_t vocab, hipStream_t stream) {
+  clear_error();
+  if ((elem_bytes != 2 && elem_bytes != 4) || (out_elem_bytes != 2 && out_elem_bytes != 4))
+    return fail(SATS_ERR_ARG, "elem_bytes must be 2 or 4");
+  if (n < 0 || n > 65535 || vocab < 1 || vocab > kMaxVocab) return fail(SATS_ERR_SHAPE, "need 0 <= n < 65536 and 1 <= vocab <= 2^22");
+  const int rc = check_rules(rules, n, vocab);
+  if (rc || n == 0) return rc;
+  if (!logits || !out) return fail(SATS_ERR_NULL, "logits and out must be non-null");
+  if (stride < vocab || out_stride < vocab || stride > (int64_t)1 << 40 || out_stride > (int64_t)1 << 40)
+    return fail(SATS_ERR_SHAPE, "a stride is below vocab, or too large");
+  if (reinterpret_cast<uintptr_t>(logits) % elem_bytes || reinterpret_cast<uintptr_t>(out) % out_elem_bytes)
+    return fail(SATS_ERR_ARG, "logits and out must be aligned to their elements");
+  const int64_t in_bytes = span(n, stride, vocab, elem_bytes), out_bytes = span(n, out_stride, vocab, out_elem_bytes);
+  const bool same = out == logits && (n == 1 || out_stride == stride) && out_elem_bytes == elem_bytes;
+  if (!same && overlap(out, out_bytes, logits, in_bytes)) return fail(SATS_ERR_ARG, "out overlaps logits without being logits");
+  sats_logit_rules r = *rules;
+  if (!r.max_history) r.seqs = r.history = r.history_len = r.prompt_len = nullptr;
+  if (!r.n_bias) r.bias_start = r.bias_ids = nullptr, r.bias = nullptr;
+  if (!r.n_masks) r.masks = nullptr, r.mask_of = nullptr;
+  const int64_t rows = r.seqs ? r.n_seqs : std::max(n, r.n_seqs);
+  const struct {
+    const void *p;
+    int64_t bytes;
+  } read[] = {{r.seqs, n * 4}, {r.history, r.history ? span(r.n_seqs, r.history_stride, r.max_history, 4) : 0}, {r.history_len, rows * 4},
+              {r.prompt_len, rows * 4}, {r.repetition, n * 4}, {r.frequency, n * 4}, {r.presence, n * 4}, {r.bias_start, (n + 1) * 4},
+              {r.bias_ids, r.n_bias * 4}, {r.bias, r.n_bias * 4}, {r.masks, r.n_masks * r.mask_stride * 4}, {r.mask_of, n * 4}};
+  for (const auto &x : read)
+    if (x.p && overlap(out, out_bytes, x.p, x.bytes)) return fail(SATS_ERR_ARG, "out overlaps the rules' arrays");
+  sats::LogitArgs a{};
+  a.logits = logits, a.out = out, a.stride = stride, a.out_stride = out_stride, a.vocab = vocab;
+  a.seqs = r.seqs, a.history = r.history, a.history_len = r.history_len, a.prompt_len = r.prompt_len;
+  a.n_seqs = r.n_seqs, a.history_stride = r.history_stride, a.max_history = r.max_history;
+  a.repetition = r.repetition, a.frequency = r.frequency, a.presence = r.presence;
+  a.bias_start = r.bias_start, a.bias_ids = r.bias_ids, a.bias = r.bias, a.n_bias = r.n_bias;
+  a.masks = r.masks, a.mask_of = r.mask_of, a.n_masks = r.n_masks, a.mask_stride = r.mask_stride;
+  a.in_place = same;
+  const bool wide = on16(logits) && on16(out) && (n == 1 || (stride * elem_bytes % 16 == 0 && out_stride * out_elem_bytes % 16 == 0));
+  const dim3 grid((unsigned)((vocab + sats::kLogitChunk - 1) / sats::kLogitChunk), (unsigned)n);
+  const size_t lds = ((r.history ? 1 : 0) + (r.bias ? 1 : 0)) * sats::kLogitChunk * sizeof(float);
+  auto go = [&](auto fn) { fn<<<grid, sats::kLogitThreads, lds, stream>>>(a); };
+  auto of = [&](auto t, auto o) {
+    using T = decltype(t);
+    using O = decltype(o);
+    wide ? go(sats::logits_kernel<T, O, 8>) : go(sats::logits_kernel<T, O, 1>);
+  };
+  if (elem_bytes == 2) out_elem_bytes == 2 ? of(uint16_t{}, uint16_t{}) : of(uint16_t{}, float{});
+  else out_elem_bytes == 2 ? of(float{}, uint16_t{}) : of(float{}, float{});
+  return launched("logits_kernel");
+}
+
+int sats_reserve_prefix(const sats_kv_cache *cache, const sats_kv_batch *batch, const sats_kv_prefix *prefix, int64_t n_q_heads,
+                        hipStream_t stream) {
+  clear_error();
+  int rc = check_cache(cache, false);
+  if (rc) return rc;
+  if (!batch) return fail(SATS_ERR_NULL, "batch must be non-null");
+  sats_kv_batch b = *batch;
+  b.table = b.q_start = b.kv_len = reinterpret_cast<const int32_t *>(16);  // (sizes alone count here)
+  if ((rc = check_batch(&b))) return rc;
+  if (!prefix) return fail(SATS_ERR_NULL, "prefix must be non-null");
+  sats_kv_prefix p = *prefix;
+  p.seq_start = p.len = b.table;
+  if ((rc = check_prefix(&p))) return rc;
+  if (n_q_heads < 1 || n_q_heads > 4096 || n_q_heads % cache->n_kv_heads)
+    return fail(SATS_ERR_SHAPE, "n_q_heads must be a multiple of the cache's heads, at most 4096");
+  sats::AttendArgs a{};
+  a.batch = batch_view(&b), a.pool = pool_view(cache);
+  a.n_q = (int)n_q_heads, a.group = (int)(n_q_heads / cache->n_kv_heads), a.dim = (int)cache->head_dim;
+  if (std::min(std::max(p.max_tokens, b.max_q_len), b.n_tokens) * a.group > 0x7fffff00) return fail(SATS_ERR_SHAPE, "too many rows for one call");
+  prefix_args(&p, &a);
+  size_t bytes = 0;
+  if ((rc = sats_host::prefix_scratch(a, form_of(cache), outer_bytes(cache), &bytes))) return rc;
+  bytes = std::max(bytes, sats_host::attention_scratch(cache->head_dim));
+  char *mem = nullptr;
+  Turn turn;
+  return sats_host::serve_workspace(stream, bytes, &mem, &turn);
+}
+
 int sats_reserve_serving(int64_t max_items, int64_t n_pages, int64_t max_rows, int64_t vocab, int64_t head_dim,
                          hipStream_t stream) {
   clear_error();
   if (max_items < 0 || max_items > 65535 || n_pages < 0 || n_pages > kMaxCount || max_rows < 0 || max_rows > 65535 ||
       vocab < 0 || vocab > kMaxVocab || head_dim < 0 || head_dim > 256)
     return fail(SATS_ERR_SHAPE, "bad sizes for sats_reserve_serving");
-  size_t bytes = 0;
-  // attention: a launch that splits its tiles has at most kSlotsLong workgroups of 16 rows, kSlots of 128
-  if (head_dim)
-    bytes = (size_t)std::max(kSlotsLong * 16, kSlots * sats::kTileRows) * (head_dim + 2) * sizeof(float);
+  size_t bytes = head_dim ? sats_host::attention_scratch(head_dim) : 0;
   if (n_pages) bytes = std::max(bytes, pages_layout(nullptr, max_items, n_pages, nullptr));
   if (max_rows && vocab) bytes = std::max(bytes, sample_layout(nullptr, std::min(max_rows, kSampleRows), vocab, nullptr));
   char *mem = nullptr;
