@@ -15,7 +15,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libsats.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("sats.hip", "serve.hip", "attend.hip", "attend_prefix.hip", "attend8.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("sats.hip", "serve.hip", "attend.hip", "attend_prefix.hip", "attend_e4m3.hip",
+                                              "attend_int8.hip")]
 ARCH = "gfx950"
 
 

@@ -24,6 +24,7 @@ constexpr int kJoinWave = 16;
 // of 500 keys 10.1, 11.8, 14.8; of 2000 11.5, 12.5, 16.4; of 4000 10.7, 13.3, 16.7; of 8000 16.0, 14.2, 20.1.
 // For 2, 4, 8 blocks of 128: 64 new tokens on 500 18.8, 21.2, 26.6; on 2000 25.5, 23.6, 28.2; 256 on 1000
 // 34.5, 34.2, 31.5; 512 alone 31.8, 31.0, 32.6.
+constexpr int kJoinRows = 16;
 constexpr int kSlots = 512, kSlotsLong = 2048, kLongBlocks = 24, kRowsLeast = 8, kTileLeast = 4;
 
 
@@ -124,7 +125,8 @@ AttendKernel join_kernel(int R, int esz, int form, bool four) {
   if (form) return four ? attend_join_kernel<float, 16, 4, 32> : attend_join_kernel<float, 16, 1, 32>;
   return four ? attend_join_kernel<float, 16, 4, 16> : attend_join_kernel<float, 16, 1, 16>;
 }
-AttendKernel join_phases_kernel(int R, int esz, bool four) {
+typedef void (*JoinPhasesKernel)(sats::AttendArgs, sats::PhaseArgs, int);
+JoinPhasesKernel join_phases_kernel(int R, int esz, bool four) {
   using namespace sats;
   if (R != 16) return four ? attend_join_phases_kernel<uint16_t, kTileRows, 4> : attend_join_phases_kernel<uint16_t, kTileRows, 1>;
   if (esz == 2) return four ? attend_join_phases_kernel<uint16_t, 16, 4> : attend_join_phases_kernel<uint16_t, 16, 1>;
@@ -142,14 +144,26 @@ PrefixPlan prefix_plan(sats::AttendArgs a, int form, int esz) {
   p.own = phase_plan(a, form, esz, a.batch.max_q, a.batch.n_seqs, a.max_own);
   return p;
 }
-size_t prefix_bytes(const sats::AttendArgs &a, const PrefixPlan &p) {
+// The parts of the four sets from mem on, and the bytes that they take.
+size_t place_sets(const sats::AttendArgs &a, const PrefixPlan &p, int esz, char *mem, sats::PhaseArgs *out) {
+  const AttendPlan *plans[4] = {&p.pre.small, &p.pre.large, &p.own.small, &p.own.large};
   sats::AttendArgs x = a;
-  char *mem = nullptr;
-  for (const PhasePlan *q : {&p.pre, &p.own}) {
-    place_parts(x, q->small, 16, &mem);
-    place_parts(x, q->large, sats::kTileRows, &mem);
+  char *at = mem;
+  for (int i = 0; i < 4; ++i) {
+    place_parts(x, *plans[i], i & 1 ? sats::kTileRows : 16, &at);
+    const bool there = plans[i]->tiles > 0;
+    out->set[i] = {x.part, x.part_ml, plans[i]->tiles, x.splits, x.per_split, there && (!(i & 1) || !plans[i - 1]->tiles),
+                   there && ((i & 1) || esz != 2)};
   }
-  return (size_t)mem;
+  out->chunk = kSlots / 2;
+  return (size_t)(at - mem);
+}
+
+// Workgroups of the launch of the four sets.
+int64_t phase_wgs(const sats::AttendArgs &a, const sats::PhaseArgs &p) {
+  double n = 0;
+  for (const sats::PhaseSet &s : p.set) n += (double)s.tiles * a.pool.n_kv * s.splits;
+  return (int64_t)std::min(n, 1e18);
 }
 
 }  // namespace
@@ -168,7 +182,9 @@ int run_attention(sats::AttendArgs a, int form, int esz, hipStream_t stream) {
     char *at = mem;
     place_parts(a, p.small, 16, &at);
     a.small = 1, a.large = esz != 2;
-    const AttendKernel kernel = form ? rows8_kernel(form, esz, a.dim) : esz == 2 ? rows_kernel<uint16_t>(a.dim) : rows_kernel<float>(a.dim);
+    const AttendKernel kernel = form == sats::kE4m3   ? e4m3_rows_kernel(esz, a.dim)
+                                : form == sats::kInt8 ? int8_rows_kernel(esz, a.dim)
+                                : esz == 2            ? rows_kernel<uint16_t>(a.dim) : rows_kernel<float>(a.dim);
     if ((rc = launch_tiles(a, p.small, kernel, stream))) return rc;
     if (p.small.splits > 1 && (rc = launch_join(a, p.small, 16, p.small.splits, join_kernel(16, esz, form, false),
                                                 join_kernel(16, esz, form, true), stream)))
@@ -178,7 +194,8 @@ int run_attention(sats::AttendArgs a, int form, int esz, hipStream_t stream) {
     char *at = mem;
     place_parts(a, p.large, sats::kTileRows, &at);
     a.small = p.small.tiles == 0, a.large = 1;
-    if ((rc = launch_tiles(a, p.large, form ? tile8_kernel(form, a.dim) : tile_kernel(a.dim), stream))) return rc;
+    const AttendKernel kernel = form == sats::kE4m3 ? e4m3_tile_kernel(a.dim) : form == sats::kInt8 ? int8_tile_kernel(a.dim) : tile_kernel(a.dim);
+    if ((rc = launch_tiles(a, p.large, kernel, stream))) return rc;
     if (p.large.splits > 1)
       rc = launch_join(a, p.large, sats::kTileRows, p.large.splits, join_kernel(sats::kTileRows, esz, form, false),
                        join_kernel(sats::kTileRows, esz, form, true), stream);
@@ -186,7 +203,7 @@ int run_attention(sats::AttendArgs a, int form, int esz, hipStream_t stream) {
   return rc;
 }
 
-// The groups' tiles, the sequences' tiles, and the joins of the latter's rows with both.
+// The groups' tiles and the sequences' tiles, and the joins of the latter's rows with both.
 int run_prefix_attention(sats::AttendArgs a, int form, int esz, hipStream_t stream) {
   if (a.n_groups == 0 || a.max_len == 0 || a.max_tokens == 0) return run_attention(a, form, esz, stream);
   size_t bytes = 0;
@@ -196,29 +213,24 @@ int run_prefix_attention(sats::AttendArgs a, int form, int esz, hipStream_t stre
   char *mem = nullptr;
   Turn turn;
   if ((rc = serve_workspace(stream, bytes, &mem, &turn))) return rc;
-  const AttendKernel rows = form ? rows8_kernel(form, esz, a.dim) : phase_rows_kernel(esz, a.dim);
-  const AttendKernel tile = form ? tile8_kernel(form, a.dim) : phase_tile_kernel(a.dim);
-  sats::AttendArgs own[2];
-  for (int phase : {sats::kShared, sats::kOwn}) {
-    const PhasePlan &p = phase == sats::kShared ? plan.pre : plan.own;
-    for (int large = 0; large < 2; ++large) {
-      const AttendPlan &x = large ? p.large : p.small;
-      if (!x.tiles) continue;
-      a.phase = phase;
-      place_parts(a, x, large ? sats::kTileRows : 16, &mem);
-      a.small = !large || p.small.tiles == 0, a.large = large || esz != 2;
-      if ((rc = launch_tiles(a, x, large ? tile : rows, stream))) return rc;
-      if (phase == sats::kShared) a.pre[large] = {a.part, a.part_ml, a.splits, a.small, a.large, x.tiles};
-      else own[large] = a;
-    }
-  }
+  sats::PhaseArgs p;
+  place_sets(a, plan, esz, mem, &p);
+  const bool large = p.set[sats::kSharedLarge].tiles || p.set[sats::kOwnLarge].tiles;
+  const PhasesKernel kernel = form == sats::kE4m3   ? e4m3_phases_kernel(esz, a.dim, large)
+                              : form == sats::kInt8 ? int8_phases_kernel(esz, a.dim, large)
+                                                    : phases_kernel(esz, a.dim, large);
+  kernel<<<(unsigned)phase_wgs(a, p), 256, 0, stream>>>(a, p);
+  if ((rc = launched("attention kernel"))) return rc;
   const int pre = std::max(plan.pre.small.splits, plan.pre.large.splits);
-  for (int large = 0; large < 2; ++large) {
-    const AttendPlan &x = large ? plan.own.large : plan.own.small;
-    const int R = large ? sats::kTileRows : 16;
-    if (x.tiles && (rc = launch_join(own[large], x, R, pre + x.splits, join_phases_kernel(R, esz, false),
-                                     join_phases_kernel(R, esz, true), stream)))
-      return rc;
+  for (int i : {sats::kOwnSmall, sats::kOwnLarge}) {
+    const sats::PhaseSet &x = p.set[i];
+    if (!x.tiles) continue;
+    const int R = i == sats::kOwnSmall ? 16 : sats::kTileRows;
+    const bool four = pre + x.splits > kJoinWave;
+    const int64_t rows = std::min<int64_t>(R, a.batch.max_q * a.group);
+    const int per = kJoinRows;
+    join_phases_kernel(R, esz, four)<<<dim3((unsigned)(x.tiles * a.pool.n_kv), (unsigned)((rows + per - 1) / per)), 256, 0, stream>>>(a, p, per);
+    if ((rc = launched("attention join"))) return rc;
   }
   return rc;
 }
@@ -231,7 +243,9 @@ int prefix_scratch(const sats::AttendArgs &a, int form, int esz, size_t *bytes) 
   const PrefixPlan p = prefix_plan(a, form, esz);
   int rc = check_plan(a, p.pre);
   if (rc || (rc = check_plan(a, p.own))) return rc;
-  *bytes = prefix_bytes(a, p);
+  sats::PhaseArgs args;
+  *bytes = place_sets(a, p, esz, nullptr, &args);
+  if (phase_wgs(a, args) > kMaxGrid) return fail(SATS_ERR_SHAPE, "too many rows for one call");
   return SATS_OK;
 }
 

@@ -58,13 +58,22 @@ struct AttendArgs {
   int phase, n_groups;
   const int32_t *seq_start, *shared;
   int64_t max_tokens, max_len, max_own;  // of a group's new tokens, of a prefix, of a sequence's other keys
-  struct {            // parts of the groups' tiles of 16 rows and of 128, as above
-    const float *part, *part_ml;
-    int splits, small, large;
-    int64_t tiles;
-  } pre[2];
 };
 enum : int { kWhole = 0, kShared = 1, kOwn = 2 };  // phase: all keys, those of the groups, those of a sequence alone
+
+// A call in phases: its tiles, of 16 rows and of 128, of the groups and of the sequences (kSets).  One launch
+// takes them all: `chunk` workgroups of the groups' and of the sequences' by turns, while there are both, since
+// the former are bound by products and the latter by memory.
+struct PhaseSet {
+  float *part, *part_ml;
+  int64_t tiles;
+  int splits, per_split, small, large;  // as in AttendArgs
+};
+enum : int { kSharedSmall = 0, kSharedLarge = 1, kOwnSmall = 2, kOwnLarge = 3 };
+struct PhaseArgs {
+  PhaseSet set[4];
+  int chunk;
+};
 
 static __device__ u32x4 attend_zeros[64];  // a row of zeros
 constexpr uint32_t kNoRow = 0x80000000u;  // an offset past every buffer: the load returns zeros
@@ -396,10 +405,35 @@ __device__ __forceinline__ void put_part(const AttendArgs &a, int64_t at, int d,
 }
 
 // (Phases) split z of a tile has nothing to add: its part is empty.
-template <int R> __device__ __forceinline__ void put_nothing(const AttendArgs &a, const RowTile &t, int z) {
-  if (a.phase == kWhole || (int)threadIdx.x >= t.count) return;
-  const int64_t at = ((int64_t)blockIdx.x * a.splits + z) * R + threadIdx.x;
+template <int R> __device__ __forceinline__ void put_nothing(const AttendArgs &a, const RowTile &t, int x, int z) {
+  if ((int)threadIdx.x >= t.count) return;
+  const int64_t at = ((int64_t)x * a.splits + z) * R + threadIdx.x;
   a.part_ml[at * 2] = -INFINITY, a.part_ml[at * 2 + 1] = 0.0f;
+}
+// The set of workgroup `block` of a call in phases, into a; its number there (tiles and heads first, then splits).
+__device__ __forceinline__ int take_set(AttendArgs &a, const PhaseArgs &p, int64_t block, int *x, int *z) {
+  const int64_t n_kv = a.pool.n_kv;
+  auto wgs = [&](int i) { return p.set[i].tiles * n_kv * p.set[i].splits; };
+  const int64_t shared = wgs(kSharedLarge) + wgs(kSharedSmall), own = wgs(kOwnLarge) + wgs(kOwnSmall), c = p.chunk;
+  const int64_t turns = (shared < own ? shared : own) / c, turn = block / c;  // whole chunks of both
+  int64_t at;
+  bool is_own;
+  if (turn < 2 * turns) {
+    is_own = turn & 1;
+    at = (turn >> 1) * c + block % c;
+  } else {
+    at = block - turns * c;
+    is_own = at >= shared;
+    if (is_own) at = block - shared;
+  }
+  int i = is_own ? kOwnLarge : kSharedLarge;
+  if (at >= wgs(i)) at -= wgs(i), --i;
+  const PhaseSet &s = p.set[i];
+  a.phase = is_own ? kOwn : kShared;
+  a.part = s.part, a.part_ml = s.part_ml, a.splits = s.splits, a.per_split = s.per_split, a.small = s.small, a.large = s.large;
+  const int64_t heads = s.tiles * n_kv;
+  *z = (int)(at / heads), *x = (int)(at % heads);
+  return i;
 }
 
 template <typename T> __device__ __forceinline__ bool odd_value(const u32x4 &q) {  // an infinity or NaN among them
@@ -450,10 +484,11 @@ template <typename T> struct RowsOf {
 };
 
 // The end of a tile of 16 rows: the sums of its four waves (row lane % 16; m, l: of this lane's group's keys)
-// into results, or into split z's part.  `lds`: 4 x 16 x DT floats.
+// into results, or into split z's part.  lds: 16 x DT floats for each wave.
 template <typename T, int DT>
-__device__ __forceinline__ void finish_rows(const AttendArgs &a, const RowTile &t, int kvh, int z, bool split, float m, float l,
-                                            const f32x4 (&acc)[DT / 16], uint8_t *lds, float (&ml)[4][16][2]) {
+__device__ __forceinline__ void finish_rows(const AttendArgs &a, const RowTile &t, int x, int z, bool split, float m, float l,
+                                            const f32x4 (&acc)[DT / 16], uint8_t *mine, uint8_t *const (&lds)[4], float (&ml)[4][16][2]) {
+  const int kvh = x % a.pool.n_kv;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, row = lane & 15, g = lane >> 4;
   // a row's sums: over the four lane groups, then over the waves
   l += __shfl_xor(l, 16);
@@ -469,18 +504,17 @@ __device__ __forceinline__ void finish_rows(const AttendArgs &a, const RowTile &
     fw[i] = exp2_fast(ml[i][row][0] - at0);
     total += ml[i][row][1] * fw[i];
   }
-  // each wave's sums, scaled to the common maximum: [wave][dim / 4][row][4]
-  float *sums = reinterpret_cast<float *>(lds);
+  // each wave's sums, scaled to the common maximum: [dim / 4][row][4]
 #pragma unroll
   for (int o = 0; o < DT / 16; ++o)
-    *reinterpret_cast<f32x4 *>(sums + ((w * (DT / 4) + 4 * o + g) * 16 + row) * 4) = acc[o] * fw[w];
+    *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(mine) + ((4 * o + g) * 16 + row) * 4) = acc[o] * fw[w];
   __syncthreads();
   for (int i = threadIdx.x >> 4; i < DT / 4; i += 16) {
     f32x4 o = f32x4{0, 0, 0, 0};
 #pragma unroll
-    for (int x = 0; x < 4; ++x) o += *reinterpret_cast<const f32x4 *>(sums + ((x * (DT / 4) + i) * 16 + row) * 4);
+    for (int y = 0; y < 4; ++y) o += *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(lds[y]) + (i * 16 + row) * 4);
     if (row >= t.count) continue;
-    if (split) put_part(a, ((int64_t)blockIdx.x * a.splits + z) * 16 + row, 4 * i, o, top, total);
+    if (split) put_part(a, ((int64_t)x * a.splits + z) * 16 + row, 4 * i, o, top, total);
     else put_row<T>(a, t, row, kvh, 4 * i, o, top, total);
   }
 }
@@ -488,20 +522,23 @@ __device__ __forceinline__ void finish_rows(const AttendArgs &a, const RowTile &
 // FULL: heads of DT dims.  Else every load leaves out the dims that a head has not (they are the
 // next slot's, or lie behind the cache), and up to DT = 128 the products do too.  Of 256 they
 // multiply zeros there: leaving them out spills 989 registers (bf16; 683 float32), all of them none.
-template <typename T, int DT, bool FULL, bool PHASED = false>
-__global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_rows_kernel(AttendArgs a) {
+// x: tile and cache head; z: split.  lds: kPart bytes for each wave.
+template <typename T, int DT> struct RowsPart {
+  // V's rows lie a little apart, so that the rows that are read together (bf16: 32 bytes of 8
+  // rows; float32: 64 bytes of 4 rows, 4 apart) are in different banks
+  static constexpr int kPitch = DT * (int)sizeof(T) + (sizeof(T) == 2 ? 32 : 16);
+  static constexpr int kV = RowsOf<T>::kKeys * kPitch;
+  static constexpr int kBytes = kV > 16 * DT * 4 ? kV : 16 * DT * 4;  // (the waves' sums are joined there)
+};
+template <typename T, int DT, bool FULL, bool PHASED>
+__device__ __forceinline__ void attend_rows(const AttendArgs &a, int x, int z, uint8_t *const (&lds)[4], float (&ml)[4][16][2]) {
   constexpr int kKeys = RowsOf<T>::kKeys, kVec = Elem<T>::kVec, kRow = DT * (int)sizeof(T), kChunks = kRow / 16;
   constexpr bool kSkip = !FULL && DT <= 128;
   constexpr int kTiles = kKeys / 16, kSteps = kChunks / 4, kLoads = kKeys * kChunks / 64, kOut = DT / 16;
-  // V's rows lie a little apart, so that the rows that are read together (bf16: 32 bytes of 8
-  // rows; float32: 64 bytes of 4 rows, 4 apart) are in different banks
-  constexpr int kPitch = kRow + (sizeof(T) == 2 ? 32 : 16);
-  constexpr int kPart = kKeys * kPitch > 16 * DT * 4 ? kKeys * kPitch : 16 * DT * 4;  // (the waves' sums are joined there)
-  __shared__ __align__(16) uint8_t lds[4][kPart];
-  __shared__ float ml[4][16][2];
+  constexpr int kPitch = RowsPart<T, DT>::kPitch;
 
-  const int kvh = blockIdx.x % a.pool.n_kv, z = blockIdx.y;
-  const RowTile t = find_tile<16, PHASED>(a, blockIdx.x / a.pool.n_kv);
+  const int kvh = x % a.pool.n_kv;
+  const RowTile t = find_tile<16, PHASED>(a, x / a.pool.n_kv);
   if (t.seq < 0) return;
   RowPlaces<16> places;
   if constexpr (PHASED) places.find(a, t);
@@ -510,7 +547,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
   else kb = key_blocks<kKeys>(a, t);
   const int parts = kb.n > a.per_split ? (kb.n + a.per_split - 1) / a.per_split : 1;
   if (z >= parts) {
-    if constexpr (PHASED) put_nothing<16>(a, t, z);
+    if constexpr (PHASED) put_nothing<16>(a, t, x, z);
     return;
   }
   const int b_end = kb.n < (z + 1) * a.per_split ? kb.n : (z + 1) * a.per_split;
@@ -590,7 +627,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
 #pragma unroll
   for (int i = 0; i < kOut; ++i) acc[i] = f32x4{0, 0, 0, 0};
   float m = -INFINITY, l = 0.0f;
-  uint8_t *mine = lds[w];
+  uint8_t *mine = w == 0 ? lds[0] : w == 1 ? lds[1] : w == 2 ? lds[2] : lds[3];
 
   int b = z * a.per_split + w;
   int page = page_of(b);
@@ -742,7 +779,25 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
     }
   }
 
-  finish_rows<T, DT>(a, t, kvh, z, parts > 1 || (PHASED && a.phase != kWhole), m, l, acc, &lds[0][0], ml);
+  finish_rows<T, DT>(a, t, x, z, parts > 1 || PHASED, m, l, acc, mine, lds, ml);
+}
+
+template <typename T, int DT, bool FULL>
+__global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_rows_kernel(AttendArgs a) {
+  __shared__ __align__(16) uint8_t lds[4][RowsPart<T, DT>::kBytes];
+  __shared__ float ml[4][16][2];
+  uint8_t *const part[4] = {lds[0], lds[1], lds[2], lds[3]};
+  attend_rows<T, DT, FULL, false>(a, blockIdx.x, blockIdx.y, part, ml);
+}
+// The same in phases, of tiles of 16 rows only.
+template <typename T, int DT, bool FULL>
+__global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_rows_phases_kernel(AttendArgs a, PhaseArgs p) {
+  __shared__ __align__(16) uint8_t lds[4][RowsPart<T, DT>::kBytes];
+  __shared__ float ml[4][16][2];
+  uint8_t *const part[4] = {lds[0], lds[1], lds[2], lds[3]};
+  int x, z;
+  take_set(a, p, blockIdx.x, &x, &z);
+  attend_rows<T, DT, FULL, true>(a, x, z, part, ml);
 }
 
 // ------------------------------------------------------------------ tiles of 128 rows
@@ -869,7 +924,7 @@ template <int DT, bool FULL> struct TileWave {
     }
   }
   // This lane's results: the row's, or split z's part of it.
-  __device__ __forceinline__ void put(const AttendArgs &a, const RowTile &t, int kvh, int row, int z, bool split) {
+  __device__ __forceinline__ void put(const AttendArgs &a, const RowTile &t, int x, int row, int z, bool split) {
     float sum = l;
     sum += __shfl_xor(sum, 32);
     if (row >= t.count) return;
@@ -880,8 +935,8 @@ template <int DT, bool FULL> struct TileWave {
       for (int e = 0; e < 4; ++e) {
         const f32x4 v = {acc[o][4 * e], acc[o][4 * e + 1], acc[o][4 * e + 2], acc[o][4 * e + 3]};
         const int d = 32 * o + 8 * e + 4 * ((threadIdx.x & 63) >> 5);
-        if (split) put_part(a, ((int64_t)blockIdx.x * a.splits + z) * kTileRows + row, d, v, top, sum);
-        else put_row<uint16_t>(a, t, row, kvh, d, v, top, sum);
+        if (split) put_part(a, ((int64_t)x * a.splits + z) * kTileRows + row, d, v, top, sum);
+        else put_row<uint16_t>(a, t, row, x % a.pool.n_kv, d, v, top, sum);
       }
   }
 
@@ -1034,15 +1089,15 @@ template <int DT, bool FULL> struct TileWave {
   }
 };
 
-template <int DT, bool FULL, bool PHASED = false>
-__global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a) {
+// x: tile and cache head; z: split; k0 .. v1: kTileKeys rows each, in arrays of their own, so that reads of one
+// do not wait for loads into another.
+template <int DT, bool FULL, bool PHASED>
+__device__ __forceinline__ void attend_tile(const AttendArgs &a, int x, int z, uint8_t *k0, uint8_t *k1, uint8_t *v0, uint8_t *v1) {
   using Wave = TileWave<DT, FULL>;
   constexpr int kRow = Wave::kRow, kChunks = Wave::kChunks, kLoads = kTileKeys * kChunks / 256;
-  // (arrays of their own, so that reads of one do not wait for loads into another)
-  __shared__ __align__(16) uint8_t k0[kTileKeys * kRow], k1[kTileKeys * kRow], v0[kTileKeys * kRow], v1[kTileKeys * kRow];
 
-  const int kvh = blockIdx.x % a.pool.n_kv, z = blockIdx.y;
-  const RowTile t = find_tile<kTileRows, PHASED>(a, blockIdx.x / a.pool.n_kv);
+  const int kvh = x % a.pool.n_kv;
+  const RowTile t = find_tile<kTileRows, PHASED>(a, x / a.pool.n_kv);
   if (t.seq < 0) return;
   RowPlaces<kTileRows> places;
   if constexpr (PHASED) places.find(a, t);
@@ -1051,7 +1106,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
   else kb = key_blocks<kTileKeys>(a, t);
   const int parts = kb.n > a.per_split ? (kb.n + a.per_split - 1) / a.per_split : 1;
   if (z >= parts) {
-    if constexpr (PHASED) put_nothing<kTileRows>(a, t, z);
+    if constexpr (PHASED) put_nothing<kTileRows>(a, t, x, z);
     return;
   }
   const int b0 = z * a.per_split, b_end = kb.n < b0 + a.per_split ? kb.n : b0 + a.per_split;
@@ -1193,7 +1248,29 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
   };
   if (__syncthreads_or(run(Plain{}))) run(Odd{});
 
-  wave.put(a, t, kvh, row, z, parts > 1 || (PHASED && a.phase != kWhole));
+  wave.put(a, t, x, row, z, parts > 1 || PHASED);
+}
+
+template <int DT, bool FULL>
+__global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a) {
+  constexpr int kBytes = kTileKeys * TileWave<DT, FULL>::kRow;
+  __shared__ __align__(16) uint8_t k0[kBytes], k1[kBytes], v0[kBytes], v1[kBytes];
+  attend_tile<DT, FULL, false>(a, blockIdx.x, blockIdx.y, k0, k1, v0, v1);
+}
+// In phases, of tiles of 16 rows and of 128.
+template <int DT, bool FULL>
+__global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_phases_kernel(AttendArgs a, PhaseArgs p) {
+  constexpr int kBytes = kTileKeys * TileWave<DT, FULL>::kRow;
+  static_assert(kBytes >= RowsPart<uint16_t, DT>::kBytes, "");
+  __shared__ __align__(16) uint8_t k0[kBytes], k1[kBytes], v0[kBytes], v1[kBytes];
+  __shared__ float ml[4][16][2];
+  int x, z;
+  if (take_set(a, p, blockIdx.x, &x, &z) & 1) {
+    attend_tile<DT, FULL, true>(a, x, z, k0, k1, v0, v1);
+  } else {
+    uint8_t *const part[4] = {k0, k1, v0, v1};
+    attend_rows<uint16_t, DT, FULL, true>(a, x, z, part, ml);
+  }
 }
 
 // ------------------------------------------------------------------ join
@@ -1249,94 +1326,106 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   if (lane < lanes && d < a.dim) put_row<T>(a, t, r, blockIdx.x % a.pool.n_kv, d, o, top, l);
 }
 
-// The same where sequences share prefixes: a row's parts are those of its own tile (of R rows) and those
-// of its group's tile.  Every split of these has left a part, an empty one too, so that no block of
-// keys is counted here again.
+// The same where sequences share prefixes: a row's parts are those of its own tile (of R rows; set OWN) and
+// those of its group's tile.  Every split of these has left a part, an empty one too, so that no block of
+// keys is counted here again.  A workgroup takes `per` rows of a tile, W waves a row: what it looks up for
+// the tile is for all of them.
 template <typename T, int R, int W>
-__global__ __launch_bounds__(256) void attend_join_phases_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256) void attend_join_phases_kernel(AttendArgs a, PhaseArgs p, int per) {
   __shared__ float ls[W > 1 ? W : 1];
   __shared__ f32x4 os[W > 1 ? W : 1][64];
+  constexpr int kSet = R == 16 ? kOwnSmall : kOwnLarge;
+  const PhaseSet &own = p.set[kSet];
+  a.phase = kOwn, a.small = own.small, a.large = own.large;
   const int kvh = blockIdx.x % a.pool.n_kv;
   const RowTile t = find_tile<R, true>(a, blockIdx.x / a.pool.n_kv);
-  const int wave = threadIdx.x >> 6, r = blockIdx.y * (4 / W) + wave / W, w = wave % W, lane = threadIdx.x & 63;
-  if (t.seq < 0 || (W > 1 ? (int)blockIdx.y : r) >= t.count) return;  // (W > 1: a row a workgroup)
-  // where the row's parts are: of its own keys, and of the prefix
-  const float *part[2] = {a.part, nullptr}, *ml[2] = {a.part_ml, nullptr};
-  int64_t at[2] = {(int64_t)blockIdx.x * a.splits * R + r, 0};  // part z's row is at + z * rows
-  int splits[2] = {a.splits, 0}, rows[2] = {R, 0};
+  const int wave = threadIdx.x >> 6, w = wave % W, lane = threadIdx.x & 63;
+  const int end = (int)(blockIdx.y + 1) * per < t.count ? (int)(blockIdx.y + 1) * per : t.count;
+  if (t.seq < 0 || (int)blockIdx.y * per >= end) return;
+  // the group's rows: where this tile's first is among them, which launch took them, tiles before them
+  int in0 = -1, rows_g = 0, c = 0, tile0 = 0;
   const int g = group_of(a, t.seq);
   if (g >= 0) {
     const GroupView v = group_view(a, g);
-    const int in = (int)(t.start - v.start) * a.group + t.first + r, n = v.n * a.group;
-    const int c = n <= 16 ? !a.pre[0].small : a.pre[1].large;  // which launch took the group
-    const int tall = c ? kTileRows : 16;
-    if (in >= 0 && in < n) {
-      int tile = g;
-      if (a.max_tokens * a.group > tall) {
-        tile = in / tall;
-        for (int g0 = 0; g0 < g; g0 += 64) {
-          int m = 0;
-          if (g0 + lane < g) {
-            const int of = group_view(a, g0 + lane).n * a.group;
-            if (of <= 16 ? a.pre[c].small : a.pre[c].large) m = (of + tall - 1) / tall;
-          }
-#pragma unroll
-          for (int d = 32; d; d >>= 1) m += __shfl_xor(m, d);
-          tile += m;
+    rows_g = v.n * a.group;
+    in0 = (int)(t.start - v.start) * a.group + t.first;
+    c = rows_g <= 16 ? (p.set[kSharedSmall].small ? kSharedSmall : kSharedLarge)
+                     : (p.set[kSharedLarge].large ? kSharedLarge : kSharedSmall);
+    const int tall = c == kSharedLarge ? kTileRows : 16;
+    if (a.max_tokens * a.group > tall) {
+      for (int g0 = 0; g0 < g; g0 += 64) {
+        int m = 0;
+        if (g0 + lane < g) {
+          const int of = group_view(a, g0 + lane).n * a.group;
+          if (of <= 16 ? p.set[c].small : p.set[c].large) m = (of + tall - 1) / tall;
         }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) m += __shfl_xor(m, d);
+        tile0 += m;
       }
-      if (tile < a.pre[c].tiles) {  // (groups that overlap may have more tiles than a launch has)
-        part[1] = a.pre[c].part, ml[1] = a.pre[c].part_ml;
-        splits[1] = a.pre[c].splits, rows[1] = tall;
-        at[1] = ((int64_t)tile * a.pool.n_kv + kvh) * splits[1] * tall + in % tall;
-      }
+    } else {
+      tile0 = g;
     }
   }
-  float top = -INFINITY;
-  int used[2] = {0, 0};  // parts up to the last that holds anything
-#pragma unroll
-  for (int x = 0; x < 2; ++x)
-    for (int z0 = 0; z0 < splits[x]; z0 += 64) {
-      const int z = z0 + lane;
-      const float *p = ml[x] + (at[x] + (int64_t)(z < splits[x] ? z : 0) * rows[x]) * 2;
-      const float m = p[0], l = p[1];
-      if (z < splits[x]) top = fmaxf(top, m);
-      const uint64_t some = __ballot(z < splits[x] && l != 0.0f);
-      if (some) used[x] = z0 + 64 - __builtin_clzll(some);
-    }
-#pragma unroll
-  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  const float at0 = top == -INFINITY ? 0.0f : top;
-  const int lanes = a.dim <= 64 ? 16 : a.dim <= 128 ? 32 : 64, sub = lane / lanes, per = 64 / lanes;
+  const PhaseSet &pre = p.set[c];
+  const int tall = c == kSharedLarge ? kTileRows : 16;
+  const int lanes = a.dim <= 64 ? 16 : a.dim <= 128 ? 32 : 64, sub = lane / lanes, many = 64 / lanes;
   const int d = lane % lanes * 4, dd = d < a.dim ? d : 0;
-  float l = 0.0f;
-  f32x4 o = f32x4{0, 0, 0, 0};
-#pragma unroll
-  for (int x = 0; x < 2; ++x) {
-#pragma unroll 4
-    for (int z0 = w * per; z0 < used[x]; z0 += W * per) {
-      const int z = z0 + sub < used[x] ? z0 + sub : used[x] - 1;
-      const float *p = ml[x] + (at[x] + (int64_t)z * rows[x]) * 2;
-      const float lz = z0 + sub < used[x] ? p[1] : 0.0f, f = exp2_fast(p[0] - at0);
-      const f32x4 v = *reinterpret_cast<const f32x4 *>(part[x] + (at[x] + (int64_t)z * rows[x]) * a.dim + dd);
-      if (lz != 0.0f) l += lz * f, o += v * f;
+  for (int r = blockIdx.y * per + wave / W; r < end; r += 4 / W) {  // (W > 1: all waves are at one row)
+    // where the row's parts are: of its own keys, and of the prefix; part z's row is at + z * rows
+    const float *part[2] = {own.part, pre.part}, *ml[2] = {own.part_ml, pre.part_ml};
+    int64_t at[2] = {(int64_t)blockIdx.x * own.splits * R + r, 0};
+    int splits[2] = {own.splits, 0};
+    const int rows[2] = {R, tall}, in = in0 + r, tile = tile0 + in / tall;
+    if (in0 >= 0 && in < rows_g && tile < pre.tiles) {  // (groups that overlap may have more tiles than a launch has)
+      splits[1] = pre.splits;
+      at[1] = ((int64_t)tile * a.pool.n_kv + kvh) * splits[1] * tall + in % tall;
     }
-  }
-  for (int m = lanes; m < 64; m <<= 1) {
-    l += __shfl_xor(l, m);
+    float top = -INFINITY;
+    int used[2] = {0, 0};  // parts up to the last that holds anything
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], m);
-  }
-  if constexpr (W > 1) {
-    os[w][lane] = o;
-    if (lane == 0) ls[w] = l;
-    __syncthreads();
-    if (w) return;
-    o = f32x4{0, 0, 0, 0}, l = 0.0f;
+    for (int x = 0; x < 2; ++x)
+      for (int z0 = 0; z0 < splits[x]; z0 += 64) {
+        const int z = z0 + lane;
+        const float *q = ml[x] + (at[x] + (int64_t)(z < splits[x] ? z : 0) * rows[x]) * 2;
+        const float m = q[0], l = q[1];
+        if (z < splits[x]) top = fmaxf(top, m);
+        const uint64_t some = __ballot(z < splits[x] && l != 0.0f);
+        if (some) used[x] = z0 + 64 - __builtin_clzll(some);
+      }
 #pragma unroll
-    for (int i = 0; i < W; ++i) o += os[i][lane], l += ls[i];
+    for (int y = 32; y; y >>= 1) top = fmaxf(top, __shfl_xor(top, y));
+    const float at0 = top == -INFINITY ? 0.0f : top;
+    float l = 0.0f;
+    f32x4 o = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll 4
+      for (int z0 = w * many; z0 < used[x]; z0 += W * many) {
+        const int z = z0 + sub < used[x] ? z0 + sub : used[x] - 1;
+        const float *q = ml[x] + (at[x] + (int64_t)z * rows[x]) * 2;
+        const float lz = z0 + sub < used[x] ? q[1] : 0.0f, f = exp2_fast(q[0] - at0);
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(part[x] + (at[x] + (int64_t)z * rows[x]) * a.dim + dd);
+        if (lz != 0.0f) l += lz * f, o += v * f;
+      }
+    }
+    for (int m = lanes; m < 64; m <<= 1) {
+      l += __shfl_xor(l, m);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], m);
+    }
+    if constexpr (W > 1) {
+      __syncthreads();
+      os[w][lane] = o;
+      if (lane == 0) ls[w] = l;
+      __syncthreads();
+      if (w) continue;
+      o = f32x4{0, 0, 0, 0}, l = 0.0f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) o += os[i][lane], l += ls[i];
+    }
+    if (lane < lanes && d < a.dim) put_row<T>(a, t, r, kvh, d, o, top, l);
   }
-  if (lane < lanes && d < a.dim) put_row<T>(a, t, r, kvh, d, o, top, l);
 }
 
 }  // namespace sats

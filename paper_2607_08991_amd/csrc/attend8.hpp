@@ -4,7 +4,7 @@
 // Queries of float32 go in as three bf16 pieces (24 bits), weights for them too, so that float32
 // callers lose nothing but what the cache has lost.
 //
-// Pages have 16 tokens or more here, so that 16 keys have one address.  A kernel serves every phase.
+// Pages have 16 tokens or more here, so that 16 keys have one address.
 #pragma once
 
 #include "attend.hpp"
@@ -13,30 +13,31 @@ namespace sats {
 
 // ------------------------------------------------------------------ tiles of 16 rows
 
-template <typename T, int F, int DT, bool FULL>
-__global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_rows8_kernel(AttendArgs a) {
+template <typename T, int F, int DT, bool FULL, bool PHASED>
+__device__ __forceinline__ void attend_rows8(const AttendArgs &a, int x, int z, uint8_t *const (&lds)[4], float (&ml)[4][16][2]) {
   constexpr int kKeys = 32, kTiles = 2, kOut = DT / 16, kChunks = DT / 16, kSteps = DT / 64;
   constexpr int kLoads = kKeys * kChunks / 64, kPer = kLoads / kTiles, kPieces = sizeof(T) == 2 ? 1 : 3;
   constexpr bool kSkip = !FULL && DT <= 128;
-  constexpr int kPitch = DT * 2 + 32;
-  constexpr int kPart = kKeys * kPitch > 16 * DT * 4 ? kKeys * kPitch : 16 * DT * 4;
-  __shared__ __align__(16) uint8_t lds[4][kPart];
-  __shared__ float ml[4][16][2];
+  constexpr int kPitch = RowsPart<uint16_t, DT>::kPitch;  // (V is in LDS as of a bf16 cache)
 
-  const int kvh = blockIdx.x % a.pool.n_kv, z = blockIdx.y;
-  const RowTile t = find_tile<16, true>(a, blockIdx.x / a.pool.n_kv);
+  const int kvh = x % a.pool.n_kv;
+  const RowTile t = find_tile<16, PHASED>(a, x / a.pool.n_kv);
   if (t.seq < 0) return;
   RowPlaces<16> places;
-  places.find(a, t);
-  const KeyBlocks kb = key_blocks<kKeys>(a, t, places);
+  if constexpr (PHASED) places.find(a, t);
+  KeyBlocks kb;
+  if constexpr (PHASED) kb = key_blocks<kKeys>(a, t, places);
+  else kb = key_blocks<kKeys>(a, t);
   const int parts = kb.n > a.per_split ? (kb.n + a.per_split - 1) / a.per_split : 1;
   if (z >= parts) {
-    put_nothing<16>(a, t, z);
+    if constexpr (PHASED) put_nothing<16>(a, t, x, z);
     return;
   }
   const int b_end = kb.n < (z + 1) * a.per_split ? kb.n : (z + 1) * a.per_split;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, row = lane & 15, g = lane >> 4;
-  const int64_t place = places.of(row);
+  int64_t place;
+  if constexpr (PHASED) place = places.of(row);
+  else place = t.place0 + (t.first + (row < t.count ? row : t.count - 1)) / a.group;
   const bool several = kb.low != kb.high;
 
   // Q as the second operand: of this lane's row the dims 16 (g + 4 s) .. + 15, as a lane has a key's codes
@@ -79,16 +80,22 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_ro
   const char *kp = (const char *)a.k + head_bytes, *vp = (const char *)a.v + head_bytes;
   const char *ksp = (const char *)a.k_scale + head_rows, *vsp = (const char *)a.v_scale + head_rows;
 
-  u32x4 kr[kTiles][kSteps], vr[kLoads];
-  uint8_t ks[kTiles], vs[kLoads];
-  auto page_of = [&](int b) {  // of key lane % 32 of a block
-    return b < b_end ? key_page<true>(a, t, kb, block_key(kb, b, kKeys) + (lane & (kKeys - 1))) : -1;
+  // A block's codes and scales on their way, and which of its keys some row sees.
+  struct Held {
+    u32x4 k[kTiles][kSteps], v[kLoads];
+    uint8_t ks[kTiles], vs[kLoads];
+    uint32_t there;
   };
-  auto load = [&](int b, int page, uint32_t there) {
+  auto page_of = [&](int b) {  // of key lane % 32 of a block
+    return b < b_end ? key_page<PHASED>(a, t, kb, block_key(kb, b, kKeys) + (lane & (kKeys - 1))) : -1;
+  };
+  auto load = [&](Held &h, int b, int page) {
+    h.there = (uint32_t)__ballot(page >= 0);
+    if (b >= b_end) return;
     const int j0 = (int)(block_key(kb, b, kKeys) & (a.pool.page - 1));
 #pragma unroll
     for (int kt = 0; kt < kTiles; ++kt) {
-      const uint32_t here = there >> (16 * kt) & 0xffffu;
+      const uint32_t here = h.there >> (16 * kt) & 0xffffu;
       const int64_t p = here ? __builtin_amdgcn_readlane(page, 16 * kt + __builtin_ctz(here)) : 0;
       const int slot = (j0 + 16 * kt) & (a.pool.page - 1);
       const int64_t at = p * page_bytes + slot * a.dim, at_s = p * page_rows + slot;
@@ -98,16 +105,16 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_ro
       const uint32_t k_off = k_here ? row * a.dim + g * 16 : kNoRow;
 #pragma unroll
       for (int s = 0; s < kSteps; ++s)
-        kr[kt][s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                                  rk, FULL || (4 * s + g) * 16 < a.dim ? k_off + 64 * s : kNoRow, 0, 0));
-      ks[kt] = __builtin_amdgcn_raw_buffer_load_b8(rks, k_here ? row : kNoRow, 0, 0);
+        h.k[kt][s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                   rk, FULL || (4 * s + g) * 16 < a.dim ? k_off + 64 * s : kNoRow, 0, 0));
+      h.ks[kt] = __builtin_amdgcn_raw_buffer_load_b8(rks, k_here ? row : kNoRow, 0, 0);
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const int r = (i * 64 + lane) / kChunks, c = (i * 64 + lane) % kChunks;
         const bool v_here = here >> r & 1;
-        vr[kt * kPer + i] = __builtin_bit_cast(
+        h.v[kt * kPer + i] = __builtin_bit_cast(
             u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, v_here && (FULL || c * 16 < a.dim) ? r * a.dim + c * 16 : kNoRow, 0, 0));
-        vs[kt * kPer + i] = __builtin_amdgcn_raw_buffer_load_b8(rvs, v_here ? r : kNoRow, 0, 0);
+        h.vs[kt * kPer + i] = __builtin_amdgcn_raw_buffer_load_b8(rvs, v_here ? r : kNoRow, 0, 0);
       }
     }
   };
@@ -116,16 +123,12 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_ro
 #pragma unroll
   for (int i = 0; i < kOut; ++i) acc[i] = f32x4{0, 0, 0, 0};
   float m = -INFINITY, l = 0.0f;
-  uint8_t *mine = lds[w];
+  uint8_t *mine = w == 0 ? lds[0] : w == 1 ? lds[1] : w == 2 ? lds[2] : lds[3];
 
-  int b = z * a.per_split + w;
-  int page = page_of(b);
-  uint32_t there = (uint32_t)__ballot(page >= 0);
-  if (b < b_end) load(b, page, there);
-  int page_next = page_of(b + 4);
-  for (; b < b_end; b += 4) {
+  int page;  // of the block after the one whose codes are in the other registers
+  auto step = [&](Held &h, int b) {
     const int64_t j0 = block_key(kb, b, kKeys);
-    const uint32_t here = there;
+    const uint32_t here = h.there;
     const bool whole = here == ~0u && j0 + kKeys - 1 <= kb.low &&
                        (!a.window || kb.high - j0 < a.window || j0 + kKeys <= a.sinks);
     // scores: lane (row, keys 16 kt + 4 g + i)
@@ -133,40 +136,36 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_ro
 #pragma unroll
     for (int kt = 0; kt < kTiles; ++kt) {
       s[kt] = f32x4{0, 0, 0, 0};
-      const float f = scale_of(ks[kt]);
+      const float f = scale_of<F>(h.ks[kt]);
 #pragma unroll
       for (int st = 0; st < kSteps; ++st) {
         if (kSkip && st * 64 >= a.dim) break;
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-          const bf16x8_t k8 = __builtin_bit_cast(bf16x8_t, decode8<F>(kr[kt][st][2 * y], kr[kt][st][2 * y + 1], f));
+          const bf16x8_t k8 = __builtin_bit_cast(bf16x8_t, decode8<F>(h.k[kt][st][2 * y], h.k[kt][st][2 * y + 1], f));
 #pragma unroll
           for (int p = kPieces - 1; p >= 0; --p)
             s[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k8, __builtin_bit_cast(bf16x8_t, qv[p][st][y]), s[kt], 0, 0, 0);
         }
       }
     }
-    // V to LDS, and the next block's loads
+    // V to LDS, and the loads of the block after the next
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int r = (i * 64 + lane) / kChunks, c = (i * 64 + lane) % kChunks;  // (16 rows a tile: kPer loads)
-      const float f = scale_of(vs[i]);
+      const float f = scale_of<F>(h.vs[i]);
       uint8_t *to = mine + r * kPitch + c * 32;
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        const u32x4 v = decode8<F>(vr[i][2 * y], vr[i][2 * y + 1], f);
+        const u32x4 v = decode8<F>(h.v[i][2 * y], h.v[i][2 * y + 1], f);
         if (several && !whole) odd |= odd_value<uint16_t>(v);
         *reinterpret_cast<u32x4 *>(to + 16 * y) = v;
       }
     }
     odd = __any(odd);
-    page = page_next;
-    there = (uint32_t)__ballot(page >= 0);
-    if (b + 4 < b_end) {
-      load(b + 4, page, there);
-      page_next = page_of(b + 8);
-    }
+    load(h, b + 8, page);
+    page = page_of(b + 12);
 #pragma unroll
     for (int kt = 0; kt < kTiles; ++kt) s[kt] *= scale2;
     if (!whole) {
@@ -254,29 +253,57 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_ro
           }
       }
     }
+  };
+  // (two blocks of codes on their way: as many bytes as of a bf16 cache with one)
+  int b = z * a.per_split + w;
+  Held h0, h1;
+  load(h0, b, page_of(b));
+  load(h1, b + 4, page_of(b + 4));
+  page = page_of(b + 8);
+  for (; b < b_end; b += 8) {
+    step(h0, b);
+    if (b + 4 < b_end) step(h1, b + 4);
   }
-  finish_rows<T, DT>(a, t, kvh, z, parts > 1 || a.phase != kWhole, m, l, acc, &lds[0][0], ml);
+  finish_rows<T, DT>(a, t, x, z, parts > 1 || PHASED, m, l, acc, mine, lds, ml);
+}
+
+template <typename T, int F, int DT, bool FULL>
+__global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_rows8_kernel(AttendArgs a) {
+  __shared__ __align__(16) uint8_t lds[4][RowsPart<uint16_t, DT>::kBytes];
+  __shared__ float ml[4][16][2];
+  uint8_t *const part[4] = {lds[0], lds[1], lds[2], lds[3]};
+  attend_rows8<T, F, DT, FULL, false>(a, blockIdx.x, blockIdx.y, part, ml);
+}
+template <typename T, int F, int DT, bool FULL>
+__global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_rows8_phases_kernel(AttendArgs a, PhaseArgs p) {
+  __shared__ __align__(16) uint8_t lds[4][RowsPart<uint16_t, DT>::kBytes];
+  __shared__ float ml[4][16][2];
+  uint8_t *const part[4] = {lds[0], lds[1], lds[2], lds[3]};
+  int x, z;
+  take_set(a, p, blockIdx.x, &x, &z);
+  attend_rows8<T, F, DT, FULL, true>(a, x, z, part, ml);
 }
 
 // ------------------------------------------------------------------ tiles of 128 rows
 
-// As attend_tile_kernel, whose blocks come from memory straight into LDS: here a wave's codes of a block
+// As attend_tile, whose blocks come from memory straight into LDS: here a wave's codes of a block
 // are in registers for the length of a step, and become bf16 rows in LDS at the start of the next.
-template <int F, int DT, bool FULL>
-__global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile8_kernel(AttendArgs a) {
+template <int F, int DT, bool FULL, bool PHASED>
+__device__ __forceinline__ void attend_tile8(const AttendArgs &a, int x, int z, uint8_t *k0, uint8_t *k1, uint8_t *v0, uint8_t *v1) {
   using Wave = TileWave<DT, FULL>;
   constexpr int kRow = Wave::kRow, kCodes = DT / 16, kLoads = 16 * kCodes / 64;  // (a wave's 16 rows of a block)
-  __shared__ __align__(16) uint8_t k0[kTileKeys * kRow], k1[kTileKeys * kRow], v0[kTileKeys * kRow], v1[kTileKeys * kRow];
 
-  const int kvh = blockIdx.x % a.pool.n_kv, z = blockIdx.y;
-  const RowTile t = find_tile<kTileRows, true>(a, blockIdx.x / a.pool.n_kv);
+  const int kvh = x % a.pool.n_kv;
+  const RowTile t = find_tile<kTileRows, PHASED>(a, x / a.pool.n_kv);
   if (t.seq < 0) return;
   RowPlaces<kTileRows> places;
-  places.find(a, t);
-  const KeyBlocks kb = key_blocks<kTileKeys>(a, t, places);
+  if constexpr (PHASED) places.find(a, t);
+  KeyBlocks kb;
+  if constexpr (PHASED) kb = key_blocks<kTileKeys>(a, t, places);
+  else kb = key_blocks<kTileKeys>(a, t);
   const int parts = kb.n > a.per_split ? (kb.n + a.per_split - 1) / a.per_split : 1;
   if (z >= parts) {
-    put_nothing<kTileRows>(a, t, z);
+    if constexpr (PHASED) put_nothing<kTileRows>(a, t, x, z);
     return;
   }
   const int b0 = z * a.per_split, b_end = kb.n < b0 + a.per_split ? kb.n : b0 + a.per_split;
@@ -284,7 +311,8 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile8_kernel(Att
   const int row = 32 * w + col, r_in = row < t.count ? row : t.count - 1;  // (rows past the last repeat it)
 
   Wave wave;
-  wave.take_places(places, w, col);
+  if constexpr (PHASED) wave.take_places(places, w, col);
+  else wave.take_places(a, t, w, r_in);
   wave.take_rows(a, t, kvh, r_in);
   const int64_t head_rows = (int64_t)kvh << a.pool.shift, page_rows = (int64_t)a.pool.n_kv << a.pool.shift;
   const char *kp = (const char *)a.k + head_rows * a.dim, *vp = (const char *)a.v + head_rows * a.dim;
@@ -301,9 +329,9 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile8_kernel(Att
       held.page = p >= 0 && p < a.pool.n_pages ? p : -1;
     }
     const int p = __shfl(held.page, (int)(((j0 + lane) >> a.pool.shift) - held.first));
-    const bool inside = j0 + kTileKeys <= t.len && j0 >= kb.lo && j0 + kTileKeys - 1 <= kb.high &&
+    const bool inside = j0 + kTileKeys <= t.len && (!PHASED || j0 >= kb.lo) && j0 + kTileKeys - 1 <= kb.high &&
                         (!a.window || kb.low - j0 < a.window || j0 + kTileKeys <= a.sinks);
-    return inside || any_sees<true>(a, kb, t.len, j0 + lane) ? p : -1;
+    return inside || any_sees<PHASED>(a, kb, t.len, j0 + lane) ? p : -1;
   };
   // wave w's 16 rows of a block: load i holds rows i * (64 / kCodes) .., piece lane % kCodes
   struct Codes {
@@ -326,14 +354,19 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile8_kernel(Att
       to.s[i] = __builtin_amdgcn_raw_buffer_load_b8(rs, in ? r : kNoRow, 0, 0);
     }
   };
+  // (the places of a row's pieces are exchanged by bits of its number, and i and y are bits of their own: places
+  // differ from the first one in fixed bits, and in whole rows)
   auto put = [&](const Codes &from, uint8_t *to, auto place) {
+    int at = r0 * kRow + place(r0, 2 * c0) * 16;
+    asm volatile("" : "+v"(at));
+    to += 16 * w * kRow;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int r = 16 * w + i * (64 / kCodes) + r0;
-      const float f = scale_of(from.s[i]);
+      const int r = i * (64 / kCodes);
+      const float f = scale_of<F>(from.s[i]);
 #pragma unroll
       for (int y = 0; y < 2; ++y)
-        *reinterpret_cast<u32x4 *>(to + r * kRow + place(r, 2 * c0 + y) * 16) = decode8<F>(from.c[i][2 * y], from.c[i][2 * y + 1], f);
+        *reinterpret_cast<u32x4 *>(to + (at ^ (place(r, y) * 16)) + r * kRow) = decode8<F>(from.c[i][2 * y], from.c[i][2 * y + 1], f);
     }
   };
   auto put_k = [&](uint8_t *to) { put(kc, to, Wave::k_place); };
@@ -422,7 +455,27 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile8_kernel(Att
     return again;
   };
   if (__syncthreads_or(run(Plain{}))) run(Odd{});
-  wave.put(a, t, kvh, row, z, parts > 1 || a.phase != kWhole);
+  wave.put(a, t, x, row, z, parts > 1 || PHASED);
+}
+
+template <int F, int DT, bool FULL>
+__global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile8_kernel(AttendArgs a) {
+  constexpr int kBytes = kTileKeys * TileWave<DT, FULL>::kRow;
+  __shared__ __align__(16) uint8_t k0[kBytes], k1[kBytes], v0[kBytes], v1[kBytes];
+  attend_tile8<F, DT, FULL, false>(a, blockIdx.x, blockIdx.y, k0, k1, v0, v1);
+}
+template <int F, int DT, bool FULL>
+__global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend8_phases_kernel(AttendArgs a, PhaseArgs p) {
+  constexpr int kBytes = kTileKeys * TileWave<DT, FULL>::kRow;
+  __shared__ __align__(16) uint8_t k0[kBytes], k1[kBytes], v0[kBytes], v1[kBytes];
+  __shared__ float ml[4][16][2];
+  int x, z;
+  if (take_set(a, p, blockIdx.x, &x, &z) & 1) {
+    attend_tile8<F, DT, FULL, true>(a, x, z, k0, k1, v0, v1);
+  } else {
+    uint8_t *const part[4] = {k0, k1, v0, v1};
+    attend_rows8<uint16_t, F, DT, FULL, true>(a, x, z, part, ml);
+  }
 }
 
 }  // namespace sats

@@ -8,12 +8,16 @@
 namespace sats_host {
 
 typedef void (*AttendKernel)(sats::AttendArgs);
+typedef void (*PhasesKernel)(sats::AttendArgs, sats::PhaseArgs);
 
-// Kernels for heads of `dim`: in phases, of bf16 or float32 caches; of 8-bit caches, every phase.
-AttendKernel phase_rows_kernel(int elem_bytes, int dim);
-AttendKernel phase_tile_kernel(int dim);
-AttendKernel rows8_kernel(int form, int elem_bytes, int dim);
-AttendKernel tile8_kernel(int form, int dim);
+// Kernels for heads of `dim`: of 8-bit caches; of calls in phases (large: with tiles of 128 rows among them).
+AttendKernel e4m3_rows_kernel(int elem_bytes, int dim);
+AttendKernel e4m3_tile_kernel(int dim);
+AttendKernel int8_rows_kernel(int elem_bytes, int dim);
+AttendKernel int8_tile_kernel(int dim);
+PhasesKernel phases_kernel(int elem_bytes, int dim, bool large);
+PhasesKernel e4m3_phases_kernel(int elem_bytes, int dim, bool large);
+PhasesKernel int8_phases_kernel(int elem_bytes, int dim, bool large);
 
 // Attention of a batch, q and out of elem_bytes over a cache of this format: enqueued, or an error.
 int run_attention(sats::AttendArgs a, int form, int elem_bytes, hipStream_t stream);

@@ -21,8 +21,10 @@ enum : int { kPlain = 0, kE4m3 = 1, kInt8 = 2 };  // formats of a cache's rows (
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
-__device__ __forceinline__ float scale_of(uint32_t b) {
-  return __uint_as_float(b == 0 ? 0x00400000u : b == 255 ? 0x7fc00000u : b << 23);
+// The scale of byte b, as decode4 takes it: the conversion of E4M3 looks at the exponent alone, of
+// which 0 is 2^-127 and 255 NaN.
+template <int F> __device__ __forceinline__ float scale_of(uint32_t b) {
+  return __uint_as_float(F == kE4m3 ? b << 23 : b == 0 ? 0x00400000u : b == 255 ? 0x7fc00000u : b << 23);
 }
 
 // Four codes as bf16 numbers, two a word.
@@ -136,7 +138,7 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(ReadArgs a) {
         }
       } else {
         const uint2 c = *reinterpret_cast<const uint2 *>(src);
-        const u32x4 w = decode8<F>(c.x, c.y, scale_of((kv ? a.v_scale : a.k_scale)[row]));
+        const u32x4 w = decode8<F>(c.x, c.y, scale_of<F>((kv ? a.v_scale : a.k_scale)[row]));
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = unpack<uint16_t>(w, i);
       }

@@ -175,7 +175,7 @@ def attend8(*a, form=17, heads=32, window=0, **kw):
     return lib.sats_paged_attention(A(6), I(heads * kw.get("dim", 128)), ctypes.byref(c), I(0), ctypes.byref(b), I(heads), ctypes.c_float(0.1),
                                     I(window), I(0), P(1 << 50), P(0), P(0))
 def kinds():
-    return ["rows" if "rows" in n else "tile" if "tile" in n else "join" for n in launches(log())]
+    return ["join" if "join" in n else "rows" if "rows" in n else "tile" if "tile" in n else "both" for n in launches(log())]
 """
 
 
@@ -186,7 +186,8 @@ def run(tmp_path_factory):
 
 
 def test_which_kernels_shared_prefixes_take(run):
-    """The groups' tiles by the rows of a group, the sequences' by theirs, and a join for each kind of these."""
+    """One launch, of tiles of 16 rows or of these and those of 128, by the rows of the groups and of the sequences,
+    and a join for each kind of the sequences' tiles."""
     got = run("""
 out = []
 for a, kw in (((64, 64, 1, 34000, 1, 64, 32000, 2000), {}), ((4, 4, 1, 2200, 1, 4, 2000, 200), {}),
@@ -196,9 +197,9 @@ for a, kw in (((64, 64, 1, 34000, 1, 64, 32000, 2000), {}), ((4, 4, 1, 2200, 1, 
     assert shared(*a, **kw) == 0, lib.sats_last_error()
     out.append(kinds())
 print(json.dumps(out))""")
-    assert got[0] == ["tile", "rows", "join"] and got[1] == ["rows", "rows", "join"]
-    assert got[2] == ["rows", "tile", "rows", "tile", "join", "join"] == got[4]
-    assert got[3] == ["rows", "rows", "join"] == got[5]
+    assert got[0] == ["both", "join"] and got[1] == ["rows", "join"]
+    assert got[2] == ["both", "join", "join"] == got[4]
+    assert got[3] == ["rows", "join"] == got[5]
     assert got[6] == got[7] == got[8] == ["rows", "join"]
 
 
@@ -216,7 +217,7 @@ for dim in range(16, 257, 16):
                 out += [[dim, esz, n] for n in launches(log()) if "join" not in n]
 print(json.dumps(out))""")
     for dim, esz, name in got:
-        width, whole = re.search(r"attend_(?:rows|tile)8?_kernelI.*?Li(\d+)ELb([01])E", name.replace("Li1ELi", "Li").replace("Li2ELi", "Li")).groups()
+        width, whole = re.search(r"attend8?_(?:rows8?_|tile8?_)?(?:phases_)?kernelI.*?Li(\d+)ELb([01])E", name.replace("Li1ELi", "Li").replace("Li2ELi", "Li")).groups()
         assert int(width) >= dim and (whole == "0" or int(width) == dim), (dim, esz, name)
 
 
