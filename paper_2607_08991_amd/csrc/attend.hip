@@ -13,6 +13,8 @@ namespace {
 // of 4000 keys (16 parts) 12.2, 13.3, 13.3, 13.3; of 6000 12.6, 12.6, 14.5, 14.5; of 16000 (63) 22.5, 22.5,
 // 22.5, 34.3; 128 new tokens on 4000, whose tiles have 128 rows, 38.9, 35.4, 35.3, 35.3.
 constexpr int kJoinWave = 16;
+// In phases: up to this many rows.  us for four waves and one: 2048 rows of 33 parts 118.8, 124.1; 12000 of up to 20 116, 100.
+constexpr int kJoinRows = 4096;
 // Attention: workgroups that the chip holds at once (two a compute unit; of the kernels for
 // heads above 128 one, of the 16-row kernels for heads up to 96 three), which a launch that
 // splits its tiles aims at: a few more would wait for a second round.  8 sequences of 2000 to 6000
@@ -24,7 +26,6 @@ constexpr int kJoinWave = 16;
 // of 500 keys 10.1, 11.8, 14.8; of 2000 11.5, 12.5, 16.4; of 4000 10.7, 13.3, 16.7; of 8000 16.0, 14.2, 20.1.
 // For 2, 4, 8 blocks of 128: 64 new tokens on 500 18.8, 21.2, 26.6; on 2000 25.5, 23.6, 28.2; 256 on 1000
 // 34.5, 34.2, 31.5; 512 alone 31.8, 31.0, 32.6.
-constexpr int kJoinRows = 16;
 constexpr int kSlots = 512, kSlotsLong = 2048, kLongBlocks = 24, kRowsLeast = 8, kTileLeast = 4;
 
 
@@ -48,6 +49,10 @@ AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, in
   const int64_t wgs = std::max<int64_t>(1, p.tiles * a.pool.n_kv);
   int64_t slots = a.dim > 128 ? kSlots / 2 : kSlots;
   if (R == 16 && a.dim <= 96) slots = kSlots * 3 / 2;
+  // A group alone leaves half of the chip to its sequences' own keys where these are as many.  us for 512 and 256
+  // workgroups: 64 sequences on 32000 keys with 100 to 2000 of their own 118.8, 108.3; with one each 82.8, 83.1 and on
+  // 64000 128, 142; three groups of 500 to 9000 100, 124.
+  if (R != 16 && a.phase == sats::kShared && units == 1 && b.n_seqs * a.max_own >= p.tiles * range) slots /= 2;
   int64_t want = std::max<int64_t>(1, slots / wgs);
   if (R == 16) want = std::max(want, std::min<int64_t>(kSlotsLong / wgs, blocks / kLongBlocks));
   p.per_split = (int)std::max<int64_t>(least, (blocks + want - 1) / want);
@@ -125,12 +130,10 @@ AttendKernel join_kernel(int R, int esz, int form, bool four) {
   if (form) return four ? attend_join_kernel<float, 16, 4, 32> : attend_join_kernel<float, 16, 1, 32>;
   return four ? attend_join_kernel<float, 16, 4, 16> : attend_join_kernel<float, 16, 1, 16>;
 }
-typedef void (*JoinPhasesKernel)(sats::AttendArgs, sats::PhaseArgs, int);
-JoinPhasesKernel join_phases_kernel(int R, int esz, bool four) {
+PhasesKernel join_phases_kernel(int esz, bool four) {
   using namespace sats;
-  if (R != 16) return four ? attend_join_phases_kernel<uint16_t, kTileRows, 4> : attend_join_phases_kernel<uint16_t, kTileRows, 1>;
-  if (esz == 2) return four ? attend_join_phases_kernel<uint16_t, 16, 4> : attend_join_phases_kernel<uint16_t, 16, 1>;
-  return four ? attend_join_phases_kernel<float, 16, 4> : attend_join_phases_kernel<float, 16, 1>;
+  if (esz == 2) return four ? attend_join_phases_kernel<uint16_t, 4> : attend_join_phases_kernel<uint16_t, 1>;
+  return four ? attend_join_phases_kernel<float, 4> : attend_join_phases_kernel<float, 1>;
 }
 
 struct PrefixPlan {
@@ -144,19 +147,23 @@ PrefixPlan prefix_plan(sats::AttendArgs a, int form, int esz) {
   p.own = phase_plan(a, form, esz, a.batch.max_q, a.batch.n_seqs, a.max_own);
   return p;
 }
-// The parts of the four sets from mem on, and the bytes that they take.
-size_t place_sets(const sats::AttendArgs &a, const PrefixPlan &p, int esz, char *mem, sats::PhaseArgs *out) {
-  const AttendPlan *plans[4] = {&p.pre.small, &p.pre.large, &p.own.small, &p.own.large};
-  sats::AttendArgs x = a;
-  char *at = mem;
+// The four sets, their parts from mem on; the bytes that these take, or 0 where they are too many.
+size_t place_sets(const sats::AttendArgs &a, const PrefixPlan &plan, int esz, char *mem, sats::PhaseArgs *out) {
+  const AttendPlan *plans[4] = {&plan.pre.small, &plan.pre.large, &plan.own.small, &plan.own.large};
+  size_t rows = 0;
   for (int i = 0; i < 4; ++i) {
-    place_parts(x, *plans[i], i & 1 ? sats::kTileRows : 16, &at);
-    const bool there = plans[i]->tiles > 0;
-    out->set[i] = {x.part, x.part_ml, plans[i]->tiles, x.splits, x.per_split, there && (!(i & 1) || !plans[i - 1]->tiles),
-                   there && ((i & 1) || esz != 2)};
+    const AttendPlan &x = *plans[i];
+    const bool there = x.tiles > 0;
+    const size_t own = part_rows(x, i & 1 ? sats::kTileRows : 16, a.pool.n_kv);
+    if (rows + own > 0x7fffffff) return 0;
+    out->set[i] = {x.tiles, x.splits, x.per_split, there && (!(i & 1) || !plans[i - 1]->tiles), there && ((i & 1) || esz != 2),
+                   (int)rows, (int)own};
+    rows += own;
   }
-  out->chunk = kSlots / 2;
-  return (size_t)(at - mem);
+  out->part = reinterpret_cast<float *>(mem);
+  out->part_ml = out->part + rows * a.dim;
+  out->parts = reinterpret_cast<sats::RowParts *>(out->part_ml + rows * 2);
+  return rows * (a.dim + 2) * sizeof(float) + a.batch.n_tokens * a.n_q * sizeof(sats::RowParts);
 }
 
 // Workgroups of the launch of the four sets.
@@ -221,18 +228,11 @@ int run_prefix_attention(sats::AttendArgs a, int form, int esz, hipStream_t stre
                                                     : phases_kernel(esz, a.dim, large);
   kernel<<<(unsigned)phase_wgs(a, p), 256, 0, stream>>>(a, p);
   if ((rc = launched("attention kernel"))) return rc;
-  const int pre = std::max(plan.pre.small.splits, plan.pre.large.splits);
-  for (int i : {sats::kOwnSmall, sats::kOwnLarge}) {
-    const sats::PhaseSet &x = p.set[i];
-    if (!x.tiles) continue;
-    const int R = i == sats::kOwnSmall ? 16 : sats::kTileRows;
-    const bool four = pre + x.splits > kJoinWave;
-    const int64_t rows = std::min<int64_t>(R, a.batch.max_q * a.group);
-    const int per = kJoinRows;
-    join_phases_kernel(R, esz, four)<<<dim3((unsigned)(x.tiles * a.pool.n_kv), (unsigned)((rows + per - 1) / per)), 256, 0, stream>>>(a, p, per);
-    if ((rc = launched("attention join"))) return rc;
-  }
-  return rc;
+  const int parts = std::max(plan.pre.small.splits, plan.pre.large.splits) + std::max(plan.own.small.splits, plan.own.large.splits);
+  const int64_t rows = a.batch.n_tokens * a.n_q;
+  const bool four = parts > kJoinWave && rows <= kJoinRows;
+  join_phases_kernel(esz, four)<<<(unsigned)(four ? rows : (rows + 3) / 4), 256, 0, stream>>>(a, p);
+  return launched("attention join");
 }
 
 size_t attention_scratch(int64_t head_dim) {
@@ -245,7 +245,7 @@ int prefix_scratch(const sats::AttendArgs &a, int form, int esz, size_t *bytes) 
   if (rc || (rc = check_plan(a, p.own))) return rc;
   sats::PhaseArgs args;
   *bytes = place_sets(a, p, esz, nullptr, &args);
-  if (phase_wgs(a, args) > kMaxGrid) return fail(SATS_ERR_SHAPE, "too many rows for one call");
+  if (!*bytes || phase_wgs(a, args) > kMaxGrid || a.batch.n_tokens * a.n_q > kMaxGrid) return fail(SATS_ERR_SHAPE, "too many rows for one call");
   return SATS_OK;
 }
 

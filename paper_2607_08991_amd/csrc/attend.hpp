@@ -61,18 +61,21 @@ struct AttendArgs {
 };
 enum : int { kWhole = 0, kShared = 1, kOwn = 2 };  // phase: all keys, those of the groups, those of a sequence alone
 
-// A call in phases: its tiles, of 16 rows and of 128, of the groups and of the sequences (kSets).  One launch
-// takes them all: `chunk` workgroups of the groups' and of the sequences' by turns, while there are both, since
-// the former are bound by products and the latter by memory.
+// A call in phases: its tiles, of 16 rows and of 128, of the groups and of the sequences.  One launch takes them
+// all, the groups' first, which take longest.  (By turns, 64 to 256 workgroups of each, they take as long.)
 struct PhaseSet {
-  float *part, *part_ml;
   int64_t tiles;
   int splits, per_split, small, large;  // as in AttendArgs
+  int row0, rows;                       // its parts' rows among those of all sets
 };
 enum : int { kSharedSmall = 0, kSharedLarge = 1, kOwnSmall = 2, kOwnLarge = 3 };
+struct RowParts {  // where a row's first part is of its own keys, and of its prefix (-1: none)
+  int own, shared;
+};
 struct PhaseArgs {
   PhaseSet set[4];
-  int chunk;
+  float *part, *part_ml;  // of all sets
+  RowParts *parts;        // [n_tokens * n_q]
 };
 
 static __device__ u32x4 attend_zeros[64];  // a row of zeros
@@ -291,7 +294,12 @@ template <int R> struct RowPlaces {
     return v;
   }
 };
-// The smallest and largest of a number of each of N lanes (a power of two).
+// One number for all lanes, as what branches and addresses of a wave are made from.
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)v), hi = __builtin_amdgcn_readfirstlane((int)(v >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+// The smallest and largest of a number of each of N lanes (a power of two; other lanes have the same).
 template <int N> __device__ __forceinline__ void range_of(int64_t v, int64_t *low, int64_t *high) {
   int64_t lo = v, hi = v;
 #pragma unroll
@@ -299,7 +307,7 @@ template <int N> __device__ __forceinline__ void range_of(int64_t v, int64_t *lo
     const int64_t x = __shfl_xor(lo, d), y = __shfl_xor(hi, d);
     lo = x < lo ? x : lo, hi = y > hi ? y : hi;
   }
-  *low = lo, *high = hi;
+  *low = uniform(lo), *high = uniform(hi);
 }
 
 // The blocks of B keys that a tile's rows see.
@@ -412,28 +420,61 @@ template <int R> __device__ __forceinline__ void put_nothing(const AttendArgs &a
 }
 // The set of workgroup `block` of a call in phases, into a; its number there (tiles and heads first, then splits).
 __device__ __forceinline__ int take_set(AttendArgs &a, const PhaseArgs &p, int64_t block, int *x, int *z) {
-  const int64_t n_kv = a.pool.n_kv;
-  auto wgs = [&](int i) { return p.set[i].tiles * n_kv * p.set[i].splits; };
-  const int64_t shared = wgs(kSharedLarge) + wgs(kSharedSmall), own = wgs(kOwnLarge) + wgs(kOwnSmall), c = p.chunk;
-  const int64_t turns = (shared < own ? shared : own) / c, turn = block / c;  // whole chunks of both
-  int64_t at;
-  bool is_own;
-  if (turn < 2 * turns) {
-    is_own = turn & 1;
-    at = (turn >> 1) * c + block % c;
-  } else {
-    at = block - turns * c;
-    is_own = at >= shared;
-    if (is_own) at = block - shared;
+  int i = kSharedLarge;
+  int64_t heads = p.set[i].tiles * a.pool.n_kv;
+  for (int next : {kSharedSmall, kOwnLarge, kOwnSmall}) {
+    const int64_t wgs = heads * p.set[i].splits;
+    if (block < wgs) break;
+    block -= wgs;
+    i = next, heads = p.set[i].tiles * a.pool.n_kv;
   }
-  int i = is_own ? kOwnLarge : kSharedLarge;
-  if (at >= wgs(i)) at -= wgs(i), --i;
   const PhaseSet &s = p.set[i];
-  a.phase = is_own ? kOwn : kShared;
-  a.part = s.part, a.part_ml = s.part_ml, a.splits = s.splits, a.per_split = s.per_split, a.small = s.small, a.large = s.large;
-  const int64_t heads = s.tiles * n_kv;
-  *z = (int)(at / heads), *x = (int)(at % heads);
+  a.phase = i >= kOwnSmall ? kOwn : kShared;
+  a.part = p.part + (int64_t)s.row0 * a.dim, a.part_ml = p.part_ml + (int64_t)s.row0 * 2;
+  a.splits = s.splits, a.per_split = s.per_split, a.small = s.small, a.large = s.large;
+  *z = (int)(block / heads), *x = (int)(block % heads);
   return i;
+}
+// The parts of an own tile's rows, in p.parts (by the tile's first split; all lanes call it).
+template <int R>
+__device__ __forceinline__ void put_row_parts(const AttendArgs &a, const PhaseArgs &p, int x, int z) {
+  if (a.phase != kOwn || z) return;
+  const RowTile t = find_tile<R, true>(a, x / a.pool.n_kv);
+  if (t.seq < 0) return;
+  const int kvh = x % a.pool.n_kv, lane = threadIdx.x & 63;
+  // the group's rows: where this tile's first is among them, which launch took them, tiles before them
+  int in0 = -1, rows_g = 0, c = 0, tile0 = 0;
+  const int g = group_of(a, t.seq);
+  if (g >= 0) {
+    const GroupView v = group_view(a, g);
+    rows_g = v.n * a.group;
+    in0 = (int)(t.start - v.start) * a.group + t.first;
+    c = rows_g <= 16 ? (p.set[kSharedSmall].small ? kSharedSmall : kSharedLarge)
+                     : (p.set[kSharedLarge].large ? kSharedLarge : kSharedSmall);
+    const int tall = c == kSharedLarge ? 128 : 16;
+    if (a.max_tokens * a.group > tall) {
+      for (int g0 = 0; g0 < g; g0 += 64) {
+        int m = 0;
+        if (g0 + lane < g) {
+          const int of = group_view(a, g0 + lane).n * a.group;
+          if (of <= 16 ? p.set[c].small : p.set[c].large) m = (of + tall - 1) / tall;
+        }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) m += __shfl_xor(m, d);
+        tile0 += m;
+      }
+    } else {
+      tile0 = g;
+    }
+  }
+  const PhaseSet &pre = p.set[c], &own = p.set[R == 16 ? kOwnSmall : kOwnLarge];
+  const int tall = c == kSharedLarge ? 128 : 16, r = threadIdx.x, in = in0 + r, tile = tile0 + in / tall;
+  if (r >= t.count) return;
+  RowParts o = {own.row0 + (x * own.splits) * R + r, -1};
+  if (in0 >= 0 && in < rows_g && tile < pre.tiles)  // (groups that overlap may have more tiles than a launch has)
+    o.shared = pre.row0 + (tile * a.pool.n_kv + kvh) * pre.splits * tall + in % tall;
+  const int64_t tok = t.start + (t.first + r) / a.group;
+  p.parts[tok * a.n_q + kvh * a.group + (t.first + r) % a.group] = o;
 }
 
 template <typename T> __device__ __forceinline__ bool odd_value(const u32x4 &q) {  // an infinity or NaN among them
@@ -798,6 +839,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_ro
   int x, z;
   take_set(a, p, blockIdx.x, &x, &z);
   attend_rows<T, DT, FULL, true>(a, x, z, part, ml);
+  put_row_parts<16>(a, p, x, z);
 }
 
 // ------------------------------------------------------------------ tiles of 128 rows
@@ -1267,9 +1309,11 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_phases_kernel(At
   int x, z;
   if (take_set(a, p, blockIdx.x, &x, &z) & 1) {
     attend_tile<DT, FULL, true>(a, x, z, k0, k1, v0, v1);
+    put_row_parts<kTileRows>(a, p, x, z);
   } else {
     uint8_t *const part[4] = {k0, k1, v0, v1};
     attend_rows<uint16_t, DT, FULL, true>(a, x, z, part, ml);
+    put_row_parts<16>(a, p, x, z);
   }
 }
 
@@ -1326,106 +1370,76 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   if (lane < lanes && d < a.dim) put_row<T>(a, t, r, blockIdx.x % a.pool.n_kv, d, o, top, l);
 }
 
-// The same where sequences share prefixes: a row's parts are those of its own tile (of R rows; set OWN) and
-// those of its group's tile.  Every split of these has left a part, an empty one too, so that no block of
-// keys is counted here again.  A workgroup takes `per` rows of a tile, W waves a row: what it looks up for
-// the tile is for all of them.
-template <typename T, int R, int W>
-__global__ __launch_bounds__(256) void attend_join_phases_kernel(AttendArgs a, PhaseArgs p, int per) {
+// The same where sequences share prefixes: W waves a row, whose parts are where the launch before wrote that
+// they are (put_row_parts).  Every split has left a part, an empty one too.  What is read there is used only
+// within its set: a row that no tile was launched for holds anything.
+template <typename T, int W>
+__global__ __launch_bounds__(256) void attend_join_phases_kernel(AttendArgs a, PhaseArgs p) {
   __shared__ float ls[W > 1 ? W : 1];
   __shared__ f32x4 os[W > 1 ? W : 1][64];
-  constexpr int kSet = R == 16 ? kOwnSmall : kOwnLarge;
-  const PhaseSet &own = p.set[kSet];
-  a.phase = kOwn, a.small = own.small, a.large = own.large;
-  const int kvh = blockIdx.x % a.pool.n_kv;
-  const RowTile t = find_tile<R, true>(a, blockIdx.x / a.pool.n_kv);
   const int wave = threadIdx.x >> 6, w = wave % W, lane = threadIdx.x & 63;
-  const int end = (int)(blockIdx.y + 1) * per < t.count ? (int)(blockIdx.y + 1) * per : t.count;
-  if (t.seq < 0 || (int)blockIdx.y * per >= end) return;
-  // the group's rows: where this tile's first is among them, which launch took them, tiles before them
-  int in0 = -1, rows_g = 0, c = 0, tile0 = 0;
-  const int g = group_of(a, t.seq);
-  if (g >= 0) {
-    const GroupView v = group_view(a, g);
-    rows_g = v.n * a.group;
-    in0 = (int)(t.start - v.start) * a.group + t.first;
-    c = rows_g <= 16 ? (p.set[kSharedSmall].small ? kSharedSmall : kSharedLarge)
-                     : (p.set[kSharedLarge].large ? kSharedLarge : kSharedSmall);
-    const int tall = c == kSharedLarge ? kTileRows : 16;
-    if (a.max_tokens * a.group > tall) {
-      for (int g0 = 0; g0 < g; g0 += 64) {
-        int m = 0;
-        if (g0 + lane < g) {
-          const int of = group_view(a, g0 + lane).n * a.group;
-          if (of <= 16 ? p.set[c].small : p.set[c].large) m = (of + tall - 1) / tall;
-        }
-#pragma unroll
-        for (int d = 32; d; d >>= 1) m += __shfl_xor(m, d);
-        tile0 += m;
-      }
-    } else {
-      tile0 = g;
-    }
+  const int64_t row = (int64_t)blockIdx.x * (4 / W) + wave / W, tok = row / a.n_q;
+  bool live = tok < a.batch.n_tokens;
+  if (W == 1 && !live) return;
+  const RowParts at = p.parts[live ? row : 0];
+  // a row of some sequence?
+  bool in = false;
+  for (int s = lane; s < a.batch.n_seqs; s += 64) {
+    const SeqView v = seq_view(a.batch, a.pool, s);
+    in |= tok >= v.start && tok < v.start + v.n_new;
   }
-  const PhaseSet &pre = p.set[c];
-  const int tall = c == kSharedLarge ? kTileRows : 16;
-  const int lanes = a.dim <= 64 ? 16 : a.dim <= 128 ? 32 : 64, sub = lane / lanes, many = 64 / lanes;
+  live = live && __any(in);
+  const int set = at.own >= p.set[kOwnLarge].row0 ? kOwnLarge : kOwnSmall;
+  const int pre = at.shared >= p.set[kSharedLarge].row0 && p.set[kSharedLarge].tiles ? kSharedLarge : kSharedSmall;
+  int n[2], tall[2], first[2] = {at.own, at.shared};
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const PhaseSet &s = p.set[x ? pre : set];
+    tall[x] = (x ? pre : set) & 1 ? kTileRows : 16;
+    n[x] = s.splits;
+    if (!s.tiles || first[x] < s.row0 || first[x] - s.row0 > s.rows - 1 - (s.splits - 1) * tall[x]) n[x] = 0, first[x] = 0;
+  }
+  const int all = n[0] + n[1];
+  auto part_row = [&](int z) { return (int64_t)(z < n[0] ? first[0] + z * tall[0] : first[1] + (z - n[0]) * tall[1]); };
+  // the largest maximum; each lane has a part's of every 64
+  float top = -INFINITY;
+  for (int z = lane; z < all; z += 64) top = fmaxf(top, p.part_ml[part_row(z) * 2]);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float at0 = top == -INFINITY ? 0.0f : top;
+  const int lanes = a.dim <= 64 ? 16 : a.dim <= 128 ? 32 : 64, sub = lane / lanes, per = 64 / lanes;
   const int d = lane % lanes * 4, dd = d < a.dim ? d : 0;
-  for (int r = blockIdx.y * per + wave / W; r < end; r += 4 / W) {  // (W > 1: all waves are at one row)
-    // where the row's parts are: of its own keys, and of the prefix; part z's row is at + z * rows
-    const float *part[2] = {own.part, pre.part}, *ml[2] = {own.part_ml, pre.part_ml};
-    int64_t at[2] = {(int64_t)blockIdx.x * own.splits * R + r, 0};
-    int splits[2] = {own.splits, 0};
-    const int rows[2] = {R, tall}, in = in0 + r, tile = tile0 + in / tall;
-    if (in0 >= 0 && in < rows_g && tile < pre.tiles) {  // (groups that overlap may have more tiles than a launch has)
-      splits[1] = pre.splits;
-      at[1] = ((int64_t)tile * a.pool.n_kv + kvh) * splits[1] * tall + in % tall;
-    }
-    float top = -INFINITY;
-    int used[2] = {0, 0};  // parts up to the last that holds anything
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-      for (int z0 = 0; z0 < splits[x]; z0 += 64) {
-        const int z = z0 + lane;
-        const float *q = ml[x] + (at[x] + (int64_t)(z < splits[x] ? z : 0) * rows[x]) * 2;
-        const float m = q[0], l = q[1];
-        if (z < splits[x]) top = fmaxf(top, m);
-        const uint64_t some = __ballot(z < splits[x] && l != 0.0f);
-        if (some) used[x] = z0 + 64 - __builtin_clzll(some);
-      }
-#pragma unroll
-    for (int y = 32; y; y >>= 1) top = fmaxf(top, __shfl_xor(top, y));
-    const float at0 = top == -INFINITY ? 0.0f : top;
-    float l = 0.0f;
-    f32x4 o = f32x4{0, 0, 0, 0};
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-#pragma unroll 4
-      for (int z0 = w * many; z0 < used[x]; z0 += W * many) {
-        const int z = z0 + sub < used[x] ? z0 + sub : used[x] - 1;
-        const float *q = ml[x] + (at[x] + (int64_t)z * rows[x]) * 2;
-        const float lz = z0 + sub < used[x] ? q[1] : 0.0f, f = exp2_fast(q[0] - at0);
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(part[x] + (at[x] + (int64_t)z * rows[x]) * a.dim + dd);
-        if (lz != 0.0f) l += lz * f, o += v * f;
-      }
-    }
-    for (int m = lanes; m < 64; m <<= 1) {
-      l += __shfl_xor(l, m);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], m);
-    }
-    if constexpr (W > 1) {
-      __syncthreads();
-      os[w][lane] = o;
-      if (lane == 0) ls[w] = l;
-      __syncthreads();
-      if (w) continue;
-      o = f32x4{0, 0, 0, 0}, l = 0.0f;
-#pragma unroll
-      for (int i = 0; i < W; ++i) o += os[i][lane], l += ls[i];
-    }
-    if (lane < lanes && d < a.dim) put_row<T>(a, t, r, kvh, d, o, top, l);
+  float l = 0.0f;
+  f32x4 o = f32x4{0, 0, 0, 0};
+#pragma unroll 8
+  for (int z0 = w * per; z0 < all; z0 += W * per) {
+    const int z = z0 + sub;
+    const int64_t r = part_row(z < all ? z : z0);
+    const float *ml = p.part_ml + r * 2;
+    const float lz = z < all ? ml[1] : 0.0f, f = exp2_fast(ml[0] - at0);
+    // (an empty part holds no sums)
+    const f32x4 v = *reinterpret_cast<const f32x4 *>(p.part + r * a.dim + dd);
+    if (lz != 0.0f) l += lz * f, o += v * f;
   }
+  for (int m = lanes; m < 64; m <<= 1) {
+    l += __shfl_xor(l, m);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], m);
+  }
+  if constexpr (W > 1) {
+    os[w][lane] = o;
+    if (lane == 0) ls[w] = l;
+    __syncthreads();
+    if (w) return;
+    o = f32x4{0, 0, 0, 0}, l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) o += os[i][lane], l += ls[i];
+  }
+  if (!live || !n[0] || lane >= lanes || d >= a.dim) return;
+  RowTile t;  // (the row as one of a tile of its own)
+  t.start = tok, t.first = 0;
+  const int h = (int)(row - tok * a.n_q);
+  put_row<T>(a, t, h % a.group, h / a.group, d, o, top, l);
 }
 
 }  // namespace sats

@@ -90,8 +90,7 @@ __device__ __forceinline__ void attend_rows8(const AttendArgs &a, int x, int z, 
     return b < b_end ? key_page<PHASED>(a, t, kb, block_key(kb, b, kKeys) + (lane & (kKeys - 1))) : -1;
   };
   auto load = [&](Held &h, int b, int page) {
-    h.there = (uint32_t)__ballot(page >= 0);
-    if (b >= b_end) return;
+    h.there = (uint32_t)__ballot(page >= 0);  // (of a block past the last: none, and every load below reads zeros)
     const int j0 = (int)(block_key(kb, b, kKeys) & (a.pool.page - 1));
 #pragma unroll
     for (int kt = 0; kt < kTiles; ++kt) {
@@ -150,22 +149,23 @@ __device__ __forceinline__ void attend_rows8(const AttendArgs &a, int x, int z, 
       }
     }
     // V to LDS, and the loads of the block after the next
-    bool odd = false;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int r = (i * 64 + lane) / kChunks, c = (i * 64 + lane) % kChunks;  // (16 rows a tile: kPer loads)
       const float f = scale_of<F>(h.vs[i]);
       uint8_t *to = mine + r * kPitch + c * 32;
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const u32x4 v = decode8<F>(h.v[i][2 * y], h.v[i][2 * y + 1], f);
-        if (several && !whole) odd |= odd_value<uint16_t>(v);
-        *reinterpret_cast<u32x4 *>(to + 16 * y) = v;
-      }
+      for (int y = 0; y < 2; ++y) *reinterpret_cast<u32x4 *>(to + 16 * y) = decode8<F>(h.v[i][2 * y], h.v[i][2 * y + 1], f);
     }
-    odd = __any(odd);
+    const int after = page_of(b + 12);
     load(h, b + 8, page);
-    page = page_of(b + 12);
+    page = after;
+    bool odd = false;  // the block's values hold infinities or NaN, and rows disagree on a key
+    if (several && !whole) {
+      for (int i = lane; i < kKeys * DT / 8; i += 64)
+        odd |= odd_value<uint16_t>(*reinterpret_cast<const u32x4 *>(mine + i / (DT / 8) * kPitch + i % (DT / 8) * 16));
+      odd = __any(odd);
+    }
 #pragma unroll
     for (int kt = 0; kt < kTiles; ++kt) s[kt] *= scale2;
     if (!whole) {
@@ -257,12 +257,16 @@ __device__ __forceinline__ void attend_rows8(const AttendArgs &a, int x, int z, 
   // (two blocks of codes on their way: as many bytes as of a bf16 cache with one)
   int b = z * a.per_split + w;
   Held h0, h1;
-  load(h0, b, page_of(b));
-  load(h1, b + 4, page_of(b + 4));
+  const int p0 = page_of(b), p1 = page_of(b + 4);
   page = page_of(b + 8);
-  for (; b < b_end; b += 8) {
+  load(h0, b, p0);
+  load(h1, b + 4, p1);
+  // (no load is under a condition, so that a wait for one block's leaves the next one's on their way)
+  while (b < b_end) {
     step(h0, b);
-    if (b + 4 < b_end) step(h1, b + 4);
+    if ((b += 4) >= b_end) break;
+    step(h1, b);
+    b += 4;
   }
   finish_rows<T, DT>(a, t, x, z, parts > 1 || PHASED, m, l, acc, mine, lds, ml);
 }
@@ -282,6 +286,7 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_ro
   int x, z;
   take_set(a, p, blockIdx.x, &x, &z);
   attend_rows8<T, F, DT, FULL, true>(a, x, z, part, ml);
+  put_row_parts<16>(a, p, x, z);
 }
 
 // ------------------------------------------------------------------ tiles of 128 rows
@@ -472,9 +477,11 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend8_phases_kernel(A
   int x, z;
   if (take_set(a, p, blockIdx.x, &x, &z) & 1) {
     attend_tile8<F, DT, FULL, true>(a, x, z, k0, k1, v0, v1);
+    put_row_parts<kTileRows>(a, p, x, z);
   } else {
     uint8_t *const part[4] = {k0, k1, v0, v1};
     attend_rows8<uint16_t, F, DT, FULL, true>(a, x, z, part, ml);
+    put_row_parts<16>(a, p, x, z);
   }
 }
 

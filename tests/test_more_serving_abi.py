@@ -187,7 +187,7 @@ def run(tmp_path_factory):
 
 def test_which_kernels_shared_prefixes_take(run):
     """One launch, of tiles of 16 rows or of these and those of 128, by the rows of the groups and of the sequences,
-    and a join for each kind of the sequences' tiles."""
+    and a join."""
     got = run("""
 out = []
 for a, kw in (((64, 64, 1, 34000, 1, 64, 32000, 2000), {}), ((4, 4, 1, 2200, 1, 4, 2000, 200), {}),
@@ -198,7 +198,7 @@ for a, kw in (((64, 64, 1, 34000, 1, 64, 32000, 2000), {}), ((4, 4, 1, 2200, 1, 
     out.append(kinds())
 print(json.dumps(out))""")
     assert got[0] == ["both", "join"] and got[1] == ["rows", "join"]
-    assert got[2] == ["both", "join", "join"] == got[4]
+    assert got[2] == ["both", "join"] == got[4]
     assert got[3] == ["rows", "join"] == got[5]
     assert got[6] == got[7] == got[8] == ["rows", "join"]
 
