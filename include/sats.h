@@ -419,7 +419,7 @@ typedef struct {
 
 /*
  * A cache of 8 bits: every call that takes a cache takes &c8.kv, whose elem_bytes says
- * the format.  k and v hold codes, a byte each, and the scale arrays (of any alignment) a byte b for
+ * the format.  k and v hold codes, a byte each, and the scale arrays (4-byte aligned) a byte b for
  * each row of head_dim codes (a token's head):
  *   k_scale, v_scale   [n_layers][n_pages][n_kv_heads][page_size]
  * Code c stands for c 2^(b - 127), and for NaN where b is 255.  Codes are E4M3 numbers (4 bits

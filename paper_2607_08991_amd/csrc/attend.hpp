@@ -376,12 +376,16 @@ __device__ __forceinline__ bool any_sees(const AttendArgs &a, const KeyBlocks &k
   return j < len && (!PHASED || j >= k.lo) && j <= k.high && (!a.window || k.low - j < a.window || j < a.sinks);
 }
 
-// Page of key j where some row sees it, else -1.
+// The table's entry for key j where some row sees it, else -1.  (Whether it is a page is looked at where it is
+// used, a step later: a comparison here would wait for it, and for every load before it.)
 template <bool PHASED = false>
-__device__ __forceinline__ int key_page(const AttendArgs &a, const RowTile &t, const KeyBlocks &k, int64_t j) {
-  if (!any_sees<PHASED>(a, k, t.len, j)) return -1;
-  const int p = a.batch.table[t.seq * a.batch.max_pages + (j >> a.pool.shift)];
-  return p >= 0 && p < a.pool.n_pages ? p : -1;
+__device__ __forceinline__ int key_entry(const AttendArgs &a, const RowTile &t, const KeyBlocks &k, int64_t j) {
+  int p = -1;
+  if (any_sees<PHASED>(a, k, t.len, j)) p = a.batch.table[t.seq * a.batch.max_pages + (j >> a.pool.shift)];
+  return p;
+}
+__device__ __forceinline__ int page_or_none(const AttendArgs &a, int entry) {
+  return entry >= 0 && entry < a.pool.n_pages ? entry : -1;
 }
 
 // Four elements of a row's result, from dim d on: o and l relative to the maximum m.
@@ -617,8 +621,8 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, int x, int z, u
   const int row_bytes = a.dim * (int)sizeof(T);
 
   u32x4 kr[kLoads], vr[kLoads];
-  auto page_of = [&](int b) {  // of key lane % kKeys of a block
-    return b < b_end ? key_page<PHASED>(a, t, kb, block_key(kb, b, kKeys) + (lane & (kKeys - 1))) : -1;
+  auto entry_of = [&](int b) {  // of key lane % kKeys of a block
+    return b < b_end ? key_entry<PHASED>(a, t, kb, block_key(kb, b, kKeys) + (lane & (kKeys - 1))) : -1;
   };
   auto load = [&](int b, int page, uint32_t there) {
     const int j0 = (int)(block_key(kb, b, kKeys) & (a.pool.page - 1));  // (blocks and pages are powers of two)
@@ -671,10 +675,10 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, int x, int z, u
   uint8_t *mine = w == 0 ? lds[0] : w == 1 ? lds[1] : w == 2 ? lds[2] : lds[3];
 
   int b = z * a.per_split + w;
-  int page = page_of(b);
+  int page = page_or_none(a, entry_of(b));
   uint32_t there = (uint32_t)__ballot(page >= 0);
   if (b < b_end) load(b, page, there);
-  int page_next = page_of(b + 4);
+  int entry_next = entry_of(b + 4);
   for (; b < b_end; b += 4) {
     const int64_t j0 = block_key(kb, b, kKeys);
     const uint32_t here = there & (uint32_t)((1ull << kKeys) - 1);
@@ -713,11 +717,11 @@ __device__ __forceinline__ void attend_rows(const AttendArgs &a, int x, int z, u
       const int at = i * 64 + lane, r = at / kChunks;
       *reinterpret_cast<u32x4 *>(mine + r * kPitch + at % kChunks * 16) = vr[i];
     }
-    page = page_next;
+    page = page_or_none(a, entry_next);
     there = (uint32_t)__ballot(page >= 0);
     if (b + 4 < b_end) {
       load(b + 4, page, there);
-      page_next = page_of(b + 8);
+      entry_next = entry_of(b + 8);
     }
 #pragma unroll
     for (int kt = 0; kt < kTiles; ++kt) s[kt] *= scale2;

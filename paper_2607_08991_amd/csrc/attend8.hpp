@@ -11,14 +11,43 @@
 
 namespace sats {
 
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2_t lds_i32x2;
+
 // ------------------------------------------------------------------ tiles of 16 rows
 
+// As attend_rows, with two blocks of a wave on their way: K's codes in registers, V's straight into LDS (as
+// codes: its transposing reads give a lane eight keys of a dim, which it converts then).  V's scales belong to the keys,
+// so they go into the weights.
+//
+// Rows of V lie in LDS as in the cache, their 16-byte pieces exchanged so that the eight rows of a read
+// (keys 4 g .. and 16 + 4 g ..) are in different banks.
+template <int DT> struct Rows8 {
+  static constexpr int kKeys = 32, kChunks = DT / 16, kBytes = kKeys * DT;  // of a wave's buffer
+  __device__ __forceinline__ static int piece(int r, int c) {
+    return c ^ (DT > 64 ? (r & 3) | (r >> 2 & 4) : r >> 4 & 1);
+  }
+};
+// Waits until at most N loads are on their way, or for LDS.
+template <int N> __device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0xf70);
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  asm volatile("" ::: "memory");
+}
+
+// x: tile and cache head; z: split.  v0, v1: a buffer for each wave; lds: 16 x DT floats for each wave, over the same.
 template <typename T, int F, int DT, bool FULL, bool PHASED>
-__device__ __forceinline__ void attend_rows8(const AttendArgs &a, int x, int z, uint8_t *const (&lds)[4], float (&ml)[4][16][2]) {
-  constexpr int kKeys = 32, kTiles = 2, kOut = DT / 16, kChunks = DT / 16, kSteps = DT / 64;
+__device__ __forceinline__ void attend_rows8(const AttendArgs &a, int x, int z, uint8_t *v0, uint8_t *v1, uint8_t *const (&lds)[4],
+                                             float (&ml)[4][16][2]) {
+  using R8 = Rows8<DT>;
+  constexpr int kKeys = R8::kKeys, kTiles = 2, kOut = DT / 16, kChunks = R8::kChunks, kSteps = DT / 64;
   constexpr int kLoads = kKeys * kChunks / 64, kPer = kLoads / kTiles, kPieces = sizeof(T) == 2 ? 1 : 3;
   constexpr bool kSkip = !FULL && DT <= 128;
-  constexpr int kPitch = RowsPart<uint16_t, DT>::kPitch;  // (V is in LDS as of a bf16 cache)
 
   const int kvh = x % a.pool.n_kv;
   const RowTile t = find_tile<16, PHASED>(a, x / a.pool.n_kv);
@@ -34,7 +63,7 @@ __device__ __forceinline__ void attend_rows8(const AttendArgs &a, int x, int z, 
     return;
   }
   const int b_end = kb.n < (z + 1) * a.per_split ? kb.n : (z + 1) * a.per_split;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, row = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, g = lane >> 4;
   int64_t place;
   if constexpr (PHASED) place = places.of(row);
   else place = t.place0 + (t.first + (row < t.count ? row : t.count - 1)) / a.group;
@@ -80,40 +109,59 @@ __device__ __forceinline__ void attend_rows8(const AttendArgs &a, int x, int z, 
   const char *kp = (const char *)a.k + head_bytes, *vp = (const char *)a.v + head_bytes;
   const char *ksp = (const char *)a.k_scale + head_rows, *vsp = (const char *)a.v_scale + head_rows;
 
-  // A block's codes and scales on their way, and which of its keys some row sees.
+  // A block on its way: K's codes and scales (of key 16 kt + row), V's scales (of keys 16 kt + 4 g ..), which of its keys
+  // some row sees.
   struct Held {
-    u32x4 k[kTiles][kSteps], v[kLoads];
-    uint8_t ks[kTiles], vs[kLoads];
+    u32x4 k[kTiles][kSteps];
+    uint32_t vs[kTiles];
+    uint8_t ks[kTiles];
     uint32_t there;
+    int page;  // of key lane % 32
   };
-  auto page_of = [&](int b) {  // of key lane % 32 of a block
-    return b < b_end ? key_page<PHASED>(a, t, kb, block_key(kb, b, kKeys) + (lane & (kKeys - 1))) : -1;
+  constexpr int kHeldLoads = kTiles * (kSteps + 2);
+  auto entry_of = [&](int b) {
+    return b < b_end ? key_entry<PHASED>(a, t, kb, block_key(kb, b, kKeys) + (lane & (kKeys - 1))) : -1;
   };
-  auto load = [&](Held &h, int b, int page) {
-    h.there = (uint32_t)__ballot(page >= 0);  // (of a block past the last: none, and every load below reads zeros)
-    const int j0 = (int)(block_key(kb, b, kKeys) & (a.pool.page - 1));
+  // the pages and first slot of 16 keys of a block
+  auto page_at = [&](const Held &h, int kt) {
+    const uint32_t here = h.there >> (16 * kt) & 0xffffu;
+    return here ? (int64_t)__builtin_amdgcn_readlane(h.page, 16 * kt + __builtin_ctz(here)) : 0;
+  };
+  auto slot_at = [&](int b, int kt) {
+    return ((int)(block_key(kb, b, kKeys) & (a.pool.page - 1)) + 16 * kt) & (a.pool.page - 1);
+  };
+  // (Of a block past the last no key is there: every load reads zeros.  No load is under a condition, so that the
+  // waits count them.)
+  auto load = [&](Held &h, int b, int entry) {
+    h.page = page_or_none(a, entry);
+    h.there = (uint32_t)__ballot(h.page >= 0);
 #pragma unroll
     for (int kt = 0; kt < kTiles; ++kt) {
       const uint32_t here = h.there >> (16 * kt) & 0xffffu;
-      const int64_t p = here ? __builtin_amdgcn_readlane(page, 16 * kt + __builtin_ctz(here)) : 0;
-      const int slot = (j0 + 16 * kt) & (a.pool.page - 1);
-      const int64_t at = p * page_bytes + slot * a.dim, at_s = p * page_rows + slot;
-      const __amdgpu_buffer_rsrc_t rk = rows_rsrc(kp + at), rv = rows_rsrc(vp + at);
-      const __amdgpu_buffer_rsrc_t rks = rows_rsrc(ksp + at_s), rvs = rows_rsrc(vsp + at_s);
+      const int64_t p = page_at(h, kt);
+      const int slot = slot_at(b, kt);
+      const __amdgpu_buffer_rsrc_t rk = rows_rsrc(kp + p * page_bytes + slot * a.dim);
+      const __amdgpu_buffer_rsrc_t rks = rows_rsrc(ksp + p * page_rows + slot), rvs = rows_rsrc(vsp + p * page_rows + slot);
       const bool k_here = here >> row & 1;
       const uint32_t k_off = k_here ? row * a.dim + g * 16 : kNoRow;
+      h.ks[kt] = __builtin_amdgcn_raw_buffer_load_b8(rks, k_here ? row : kNoRow, 0, 0);
+      h.vs[kt] = __builtin_amdgcn_raw_buffer_load_b32(rvs, here ? 4 * g : kNoRow, 0, 0);
 #pragma unroll
       for (int s = 0; s < kSteps; ++s)
         h.k[kt][s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
                                                    rk, FULL || (4 * s + g) * 16 < a.dim ? k_off + 64 * s : kNoRow, 0, 0));
-      h.ks[kt] = __builtin_amdgcn_raw_buffer_load_b8(rks, k_here ? row : kNoRow, 0, 0);
+    }
+  };
+  auto load_v = [&](const Held &h, int b, uint8_t *to) {
+#pragma unroll
+    for (int kt = 0; kt < kTiles; ++kt) {
+      const uint32_t here = h.there >> (16 * kt) & 0xffffu;
+      const char *from = vp + page_at(h, kt) * page_bytes + slot_at(b, kt) * a.dim;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const int r = (i * 64 + lane) / kChunks, c = (i * 64 + lane) % kChunks;
-        const bool v_here = here >> r & 1;
-        h.v[kt * kPer + i] = __builtin_bit_cast(
-            u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, v_here && (FULL || c * 16 < a.dim) ? r * a.dim + c * 16 : kNoRow, 0, 0));
-        h.vs[kt * kPer + i] = __builtin_amdgcn_raw_buffer_load_b8(rvs, v_here ? r : kNoRow, 0, 0);
+        const int r = (i * 64 + lane) / kChunks, c = R8::piece(16 * kt + r, lane % kChunks);
+        load_to_lds<0>(from, (here >> r & 1) && (FULL || c * 16 < a.dim) ? (uint32_t)(r * a.dim + c * 16) : kNoRow,
+                       to + (kt * kPer + i) * 1024);
       }
     }
   };
@@ -122,10 +170,9 @@ __device__ __forceinline__ void attend_rows8(const AttendArgs &a, int x, int z, 
 #pragma unroll
   for (int i = 0; i < kOut; ++i) acc[i] = f32x4{0, 0, 0, 0};
   float m = -INFINITY, l = 0.0f;
-  uint8_t *mine = w == 0 ? lds[0] : w == 1 ? lds[1] : w == 2 ? lds[2] : lds[3];
 
-  int page;  // of the block after the one whose codes are in the other registers
-  auto step = [&](Held &h, int b) {
+  int entry;  // the table's, of the block after the next
+  auto step = [&](Held &h, int b, uint8_t *mine) {
     const int64_t j0 = block_key(kb, b, kKeys);
     const uint32_t here = h.there;
     const bool whole = here == ~0u && j0 + kKeys - 1 <= kb.low &&
@@ -148,34 +195,29 @@ __device__ __forceinline__ void attend_rows8(const AttendArgs &a, int x, int z, 
         }
       }
     }
-    // V to LDS, and the loads of the block after the next
+    uint32_t vs[kTiles];
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int r = (i * 64 + lane) / kChunks, c = (i * 64 + lane) % kChunks;  // (16 rows a tile: kPer loads)
-      const float f = scale_of<F>(h.vs[i]);
-      uint8_t *to = mine + r * kPitch + c * 32;
-#pragma unroll
-      for (int y = 0; y < 2; ++y) *reinterpret_cast<u32x4 *>(to + 16 * y) = decode8<F>(h.v[i][2 * y], h.v[i][2 * y + 1], f);
-    }
-    const int after = page_of(b + 12);
-    load(h, b + 8, page);
-    page = after;
-    bool odd = false;  // the block's values hold infinities or NaN, and rows disagree on a key
-    if (several && !whole) {
-      for (int i = lane; i < kKeys * DT / 8; i += 64)
-        odd |= odd_value<uint16_t>(*reinterpret_cast<const u32x4 *>(mine + i / (DT / 8) * kPitch + i % (DT / 8) * 16));
-      odd = __any(odd);
-    }
+    for (int kt = 0; kt < kTiles; ++kt) vs[kt] = h.vs[kt];
+    asm volatile("" ::: "memory");
+    const int after = entry_of(b + 12);
+    load(h, b + 8, entry);
+    entry = after;
+    asm volatile("" ::: "memory");
 #pragma unroll
     for (int kt = 0; kt < kTiles; ++kt) s[kt] *= scale2;
+    uint32_t seen = ~0u;  // which of its eight keys this lane's row sees: bit 4 kt + i
     if (!whole) {
       const Sight sight = sight_of(a, place, j0);
-      const uint32_t mine = here >> (4 * g);
+      const uint32_t mask = here >> (4 * g);
+      seen = 0;
 #pragma unroll
       for (int kt = 0; kt < kTiles; ++kt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          s[kt][i] = ((mine >> (16 * kt + i) & 1) != 0) & sight.sees(16 * kt + 4 * g + i) ? s[kt][i] : -INFINITY;
+        for (int i = 0; i < 4; ++i) {
+          const bool sees = ((mask >> (16 * kt + i) & 1) != 0) & sight.sees(16 * kt + 4 * g + i);
+          s[kt][i] = sees ? s[kt][i] : -INFINITY;
+          seen |= (uint32_t)sees << (4 * kt + i);
+        }
     }
     float top = -INFINITY;
 #pragma unroll
@@ -193,13 +235,32 @@ __device__ __forceinline__ void attend_rows8(const AttendArgs &a, int x, int z, 
       for (int i = 0; i < 4; ++i) {
         s[kt][i] = exp2_fast(s[kt][i] - at0);
         sum += s[kt][i];
+        // the weight of the key's codes (255, NaN, goes in as infinity: its codes are zeros)
+        const uint32_t byte = vs[kt] >> (8 * i) & 0xffu;
+        s[kt][i] *= __uint_as_float(byte ? byte << 23 : 0x00400000u);
       }
+    if (!whole) {
+#pragma unroll
+      for (int kt = 0; kt < kTiles; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[kt][i] = seen >> (4 * kt + i) & 1 ? s[kt][i] : 0.0f;
+    }
     l = l * f + sum;
 #pragma unroll
     for (int i = 0; i < kOut; ++i) acc[i] *= f;
+    // V of this block is there: what was issued since is the next one's and half of the one after
+    wait_loads<kLoads + 2 * kHeldLoads>();
+    bool odd = false;  // codes that are NaN, in a block in which rows disagree on a key
+    if (F == kE4m3 && several && !whole) {
+      for (int i = lane; i < R8::kBytes / 4; i += 64) {
+        const uint32_t c = reinterpret_cast<const uint32_t *>(mine)[i];
+        odd |= ((c & 0x7f7f7f7fu) + 0x01010101u & 0x80808080u) != 0;
+      }
+      odd = __any(odd);
+    }
     auto product = [&](auto kind) {
       constexpr bool kOdd = decltype(kind)::kOdd;
-      // a weight in two pieces of 8 bits (the second as attend_rows_kernel has it), for float32 in three
+      // a weight in two pieces of 8 bits (the second as attend_rows has it), for float32 in three
       constexpr int kWeights = kPieces == 1 ? 2 : 3;
       bf16x8_t p[kWeights];
 #pragma unroll
@@ -213,18 +274,21 @@ __device__ __forceinline__ void attend_rows8(const AttendArgs &a, int x, int z, 
         }
         p[kWeights - 1][e] = (__bf16)x;
       }
+      // contraction slot (g, e): key 4 g + e of tile 0, then of tile 1
+      const int j = row >> 1, r = (j < 4 ? 0 : 12) + 4 * g + j;
+      int at = r * DT + R8::piece(r, 0) * 16 + (row & 1) * 8;
 #pragma unroll
       for (int o = 0; o < kOut; ++o) {
         if (kSkip && 16 * o >= a.dim) break;
-        i16x4_t v2[2];
+        i32x2_t c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(mine + (at ^ (16 * o))));
+        if (kOdd) {
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-          const int r = 16 * kt + 4 * g + (row >> 2);
-          v2[kt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(mine + r * kPitch + 32 * o + (row & 3) * 8));
-          if (kOdd) v2[kt] = sane(v2[kt]);
+          for (int y = 0; y < 2; ++y) {
+            const uint32_t nan = ((uint32_t)c[y] & 0x7f7f7f7fu) + 0x01010101u & 0x80808080u;
+            c[y] &= ~((nan >> 7) * 0xffu);
+          }
         }
-        bf16x8_t v8;
-        __builtin_memcpy(&v8, v2, 16);
+        const bf16x8_t v8 = __builtin_bit_cast(bf16x8_t, decode8<F>((uint32_t)c[0], (uint32_t)c[1], 1.0f));
 #pragma unroll
         for (int i = kWeights - 1; i >= 0; --i) acc[o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, p[i], acc[o], 0, 0, 0);
       }
@@ -236,56 +300,58 @@ __device__ __forceinline__ void attend_rows8(const AttendArgs &a, int x, int z, 
       const Sight sight = sight_of(a, place, j0);
 #pragma unroll 1
       for (int k = 0; k < kKeys; ++k) {
-        const bool seen = ((here >> k & 1) != 0) & sight.sees(k);
-        float p = 0.0f;
-#pragma unroll
-        for (int kt = 0; kt < kTiles; ++kt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if ((k >> 4) == kt && (k & 3) == i) p = s[kt][i];
-        p = __shfl(p, row + 16 * ((k >> 2) & 3));
+        if (!(((here >> k & 1) != 0) & sight.sees(k))) continue;
 #pragma unroll
         for (int o = 0; o < kOut; ++o)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint16_t v = reinterpret_cast<const uint16_t *>(mine + k * kPitch)[16 * o + 4 * g + e];
-            if (seen && odd_bits(v)) acc[o][e] += p * bf16_to_f32(v);
-          }
+          for (int e = 0; e < 4; ++e)
+            if ((mine[k * DT + R8::piece(k, o) * 16 + 4 * g + e] & 0x7f) == 0x7f) acc[o][e] = __uint_as_float(0x7fc00000u);
       }
     }
+    wait_lds();  // (its buffer is the one of the block after the next)
+    load_v(h, b + 8, mine);
+    asm volatile("" ::: "memory");
   };
-  // (two blocks of codes on their way: as many bytes as of a bf16 cache with one)
   int b = z * a.per_split + w;
+  uint8_t *const mine0 = v0 + w * R8::kBytes, *const mine1 = v1 + w * R8::kBytes;
   Held h0, h1;
-  const int p0 = page_of(b), p1 = page_of(b + 4);
-  page = page_of(b + 8);
+  const int p0 = entry_of(b), p1 = entry_of(b + 4);
+  entry = entry_of(b + 8);
+  asm volatile("" ::: "memory");
   load(h0, b, p0);
+  asm volatile("" ::: "memory");
+  load_v(h0, b, mine0);
+  asm volatile("" ::: "memory");
   load(h1, b + 4, p1);
-  // (no load is under a condition, so that a wait for one block's leaves the next one's on their way)
+  asm volatile("" ::: "memory");
+  load_v(h1, b + 4, mine1);
+  asm volatile("" ::: "memory");
   while (b < b_end) {
-    step(h0, b);
+    step(h0, b, mine0);
     if ((b += 4) >= b_end) break;
-    step(h1, b);
+    step(h1, b, mine1);
     b += 4;
   }
+  wait_loads<0>();  // (before others write their sums where these loads go)
+  uint8_t *mine = w == 0 ? lds[0] : w == 1 ? lds[1] : w == 2 ? lds[2] : lds[3];
   finish_rows<T, DT>(a, t, x, z, parts > 1 || PHASED, m, l, acc, mine, lds, ml);
 }
 
 template <typename T, int F, int DT, bool FULL>
 __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_rows8_kernel(AttendArgs a) {
-  __shared__ __align__(16) uint8_t lds[4][RowsPart<uint16_t, DT>::kBytes];
+  __shared__ __align__(16) uint8_t v0[4 * Rows8<DT>::kBytes], v1[4 * Rows8<DT>::kBytes];
   __shared__ float ml[4][16][2];
-  uint8_t *const part[4] = {lds[0], lds[1], lds[2], lds[3]};
-  attend_rows8<T, F, DT, FULL, false>(a, blockIdx.x, blockIdx.y, part, ml);
+  uint8_t *const part[4] = {v0, v0 + 64 * DT, v1, v1 + 64 * DT};
+  attend_rows8<T, F, DT, FULL, false>(a, blockIdx.x, blockIdx.y, v0, v1, part, ml);
 }
 template <typename T, int F, int DT, bool FULL>
 __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_rows8_phases_kernel(AttendArgs a, PhaseArgs p) {
-  __shared__ __align__(16) uint8_t lds[4][RowsPart<uint16_t, DT>::kBytes];
+  __shared__ __align__(16) uint8_t v0[4 * Rows8<DT>::kBytes], v1[4 * Rows8<DT>::kBytes];
   __shared__ float ml[4][16][2];
-  uint8_t *const part[4] = {lds[0], lds[1], lds[2], lds[3]};
+  uint8_t *const part[4] = {v0, v0 + 64 * DT, v1, v1 + 64 * DT};
   int x, z;
   take_set(a, p, blockIdx.x, &x, &z);
-  attend_rows8<T, F, DT, FULL, true>(a, x, z, part, ml);
+  attend_rows8<T, F, DT, FULL, true>(a, x, z, v0, v1, part, ml);
   put_row_parts<16>(a, p, x, z);
 }
 
@@ -479,8 +545,9 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend8_phases_kernel(A
     attend_tile8<F, DT, FULL, true>(a, x, z, k0, k1, v0, v1);
     put_row_parts<kTileRows>(a, p, x, z);
   } else {
-    uint8_t *const part[4] = {k0, k1, v0, v1};
-    attend_rows8<uint16_t, F, DT, FULL, true>(a, x, z, part, ml);
+    static_assert(kBytes == 4 * Rows8<DT>::kBytes, "");
+    uint8_t *const part[4] = {k0, k0 + 64 * DT, k1, k1 + 64 * DT};
+    attend_rows8<uint16_t, F, DT, FULL, true>(a, x, z, k0, k1, part, ml);
     put_row_parts<16>(a, p, x, z);
   }
 }

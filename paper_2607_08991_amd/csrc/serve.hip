@@ -68,6 +68,8 @@ int check_cache(const sats_kv_cache *c, bool data) {
   if (!c8 && c->elem_bytes != 2 && c->elem_bytes != 4)
     return fail(SATS_ERR_ARG, "elem_bytes must be 2, 4, SATS_KV_E4M3 or SATS_KV_INT8");
   if (c8 && data && (!c8->k_scale || !c8->v_scale)) return fail(SATS_ERR_NULL, "the cache's k_scale and v_scale must be non-null");
+  if (c8 && data && (reinterpret_cast<uintptr_t>(c8->k_scale) % 4 || reinterpret_cast<uintptr_t>(c8->v_scale) % 4))
+    return fail(SATS_ERR_ARG, "the cache's k_scale and v_scale must be 4-byte aligned");
   if (c8 && c8->q_elem_bytes != 2 && c8->q_elem_bytes != 4) return fail(SATS_ERR_ARG, "q_elem_bytes must be 2 or 4");
   if (c->n_layers < 1 || c->n_pages < 1 || c->n_kv_heads < 1 || c->n_layers > 4096 || c->n_pages > kMaxCount ||
       c->n_kv_heads > 1024)

@@ -29,7 +29,7 @@ def attend8(form=_lib.SATS_KV_E4M3, **kw):
 @pytest.mark.parametrize("want,kw", [
     (NULL, dict(k=None)), (NULL, dict(k_scale=None)), (NULL, dict(v_scale=None)), (ARG, dict(q_elem_bytes=1)),
     (ARG, dict(q_elem_bytes=0)), (ARG, dict(k=P + 8)), (SHAPE, dict(page_size=8)), (SHAPE, dict(head_dim=72)), (SHAPE, dict(head_dim=8)),
-    (SHAPE, dict(head_dim=272)), (OK, dict()), (OK, dict(k_scale=2 * P + 1)), (OK, dict(q_elem_bytes=4)), (OK, dict(page_size=4096)),
+    (SHAPE, dict(head_dim=272)), (OK, dict()), (ARG, dict(k_scale=2 * P + 2)), (ARG, dict(v_scale=3 * P + 1)), (OK, dict(k_scale=2 * P + 4)), (OK, dict(q_elem_bytes=4)), (OK, dict(page_size=4096)),
     # 10 pages of 2 x 16 rows in 2 layers: 640 bytes of scales
     (ARG, dict(n_tokens=1, max_q_len=0, out=2 * P + 624)), (ARG, dict(n_tokens=1, max_q_len=0, out=3 * P - 496)),
     (OK, dict(n_tokens=1, max_q_len=0, out=2 * P + 640)), (OK, dict(n_tokens=1, max_q_len=0, out=3 * P - 512)),
