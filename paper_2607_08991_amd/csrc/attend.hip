@@ -26,6 +26,9 @@ constexpr int kJoinRows = 4096;
 // of 500 keys 10.1, 11.8, 14.8; of 2000 11.5, 12.5, 16.4; of 4000 10.7, 13.3, 16.7; of 8000 16.0, 14.2, 20.1.
 // For 2, 4, 8 blocks of 128: 64 new tokens on 500 18.8, 21.2, 26.6; on 2000 25.5, 23.6, 28.2; 256 on 1000
 // 34.5, 34.2, 31.5; 512 alone 31.8, 31.0, 32.6.
+// Of 8 bits: 4, 8, 16 blocks, a sequence of 4000 keys 12.3, 14.7, 17.2.  Tiles of 20 blocks (six sequences, a window of 512)
+// 20.7 as they are and 25.6 in two, where the join takes 5.
+constexpr int kRowsLeast8 = 4, kRowsAlone8 = 24;
 constexpr int kSlots = 512, kSlotsLong = 2048, kLongBlocks = 24, kRowsLeast = 8, kTileLeast = 4;
 
 
@@ -36,7 +39,8 @@ struct AttendPlan {
   int splits, per_split;
 };
 // Tiles of `units` sequences or groups with up to max_q tokens each, which see `range` keys at most.
-AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, int64_t max_q, int64_t units, int64_t range) {
+// (least: blocks of a split; alone: blocks up to which a tile is not split where that would cost a join.)
+AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, int alone, int64_t max_q, int64_t units, int64_t range) {
   const sats::BatchView &b = a.batch;
   const int64_t per_unit = (max_q * a.group + R - 1) / R;
   AttendPlan p;
@@ -55,6 +59,7 @@ AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, in
   if (R != 16 && a.phase == sats::kShared && units == 1 && b.n_seqs * a.max_own >= p.tiles * range) slots /= 2;
   int64_t want = std::max<int64_t>(1, slots / wgs);
   if (R == 16) want = std::max(want, std::min<int64_t>(kSlotsLong / wgs, blocks / kLongBlocks));
+  if (a.phase == sats::kWhole && blocks <= alone) want = 1;
   p.per_split = (int)std::max<int64_t>(least, (blocks + want - 1) / want);
   p.splits = (int)((blocks + p.per_split - 1) / p.per_split);
   return p;
@@ -70,8 +75,8 @@ PhasePlan phase_plan(const sats::AttendArgs &a, int form, int esz, int64_t max_q
   PhasePlan p;
   const bool any_large = esz == 2 && max_q * a.group > 16;
   if (!any_large || units > 1)
-    p.small = attend_plan(a, 16, form || esz == 2 ? 32 : 16, kRowsLeast, any_large ? 16 / a.group : max_q, units, range);
-  if (any_large) p.large = attend_plan(a, sats::kTileRows, sats::kTileKeys, kTileLeast, max_q, units, range);
+    p.small = attend_plan(a, 16, form || esz == 2 ? 32 : 16, form ? kRowsLeast8 : kRowsLeast, form ? kRowsAlone8 : 0, any_large ? 16 / a.group : max_q, units, range);
+  if (any_large) p.large = attend_plan(a, sats::kTileRows, sats::kTileKeys, kTileLeast, 0, max_q, units, range);
   return p;
 }
 int check_plan(const sats::AttendArgs &a, const PhasePlan &p) {
