@@ -428,7 +428,7 @@ typedef struct {
  * within the codes, each value to the nearest code, ties to even (at most, one that does not
  * read as an infinity); a row that holds an infinity or NaN as zeros under 255.  Values are
  * attended to, and read, as bf16 holds them, which is exactly (below 2^-126: cut off or rounded to its
- * step).
+ * step); what a value adds to a result may be left out where it is below 2^-117.
  * page_size is at least 16 and head_dim a multiple of 16.  q_elem_bytes (2 or 4) is the
  * type of what is appended and of the queries and results of an attention over the cache.
  */
@@ -443,8 +443,8 @@ typedef struct {
  * Groups of a batch's sequences that share a prefix (sats_prefix_attention): the sequences seq_start[g] ..
  * seq_start[g + 1] - 1 (which follow each other in the batch) have their first len[g] tokens
  * in common (as far as each has them), as after sats_cache_fork.  seq_start [n_groups + 1] and len [n_groups]
- * are device data; sequences outside of every group, and groups of one or with no
- * prefix, are fine.  max_tokens (new tokens of a group), max_len (of a prefix) and max_own (of
+ * are device data (n_groups <= 65535); sequences outside of every group, and groups of one or
+ * with no prefix, are fine.  max_tokens (new tokens of a group), max_len (of a prefix) and max_own (of
  * any sequence's tokens behind its prefix, the new ones included) are upper bounds on the host:
  * what is beyond them is cut off.
  */

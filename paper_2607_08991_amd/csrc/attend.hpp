@@ -1388,9 +1388,16 @@ __global__ __launch_bounds__(256) void attend_join_phases_kernel(AttendArgs a, P
   const RowParts at = p.parts[live ? row : 0];
   // a row of some sequence?
   bool in = false;
-  for (int s = lane; s < a.batch.n_seqs; s += 64) {
+  auto within = [&](int s) {
     const SeqView v = seq_view(a.batch, a.pool, s);
-    in |= tok >= v.start && tok < v.start + v.n_new;
+    return tok >= v.start && tok < v.start + v.n_new;
+  };
+  if (a.batch.n_seqs <= 256) {  // (at once, or one after another's half)
+    for (int s = lane; s < a.batch.n_seqs; s += 64) in |= within(s);
+  } else {
+    int s;
+    token_place(a.batch, tok, &s);
+    in = within(s);
   }
   live = live && __any(in);
   const int set = at.own >= p.set[kOwnLarge].row0 ? kOwnLarge : kOwnSmall;

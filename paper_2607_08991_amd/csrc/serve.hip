@@ -383,9 +383,9 @@ int attend_args(const void *q, int64_t q_stride, const sats_kv_cache *cache, int
 
 int check_prefix(const sats_kv_prefix *p) {
   if (!p) return fail(SATS_ERR_NULL, "prefix must be non-null");
-  if (p->n_groups < 0 || p->max_tokens < 0 || p->max_len < 0 || p->max_own < 0 || p->n_groups > kMaxCount || p->max_tokens > kMaxCount ||
+  if (p->n_groups < 0 || p->max_tokens < 0 || p->max_len < 0 || p->max_own < 0 || p->n_groups > 65535 || p->max_tokens > kMaxCount ||
       p->max_len >= (int64_t)1 << 31 || p->max_own >= (int64_t)1 << 31)
-    return fail(SATS_ERR_SHAPE, "a prefix's sizes must be >= 0, at most 2^30 (lengths below 2^31)");
+    return fail(SATS_ERR_SHAPE, "a prefix's sizes must be >= 0, at most 2^30 (groups 65535, lengths below 2^31)");
   if (p->n_groups > 0 && (!p->seq_start || !p->len)) return fail(SATS_ERR_NULL, "the prefix's seq_start and len must be non-null");
   return SATS_OK;
 }

@@ -84,6 +84,7 @@ SHAPES = [  # q_len, kv_len, groups, heads, kv_heads, dim, page, window, sinks
     ([1, 1, 1], [500, 600, 700], [], 4, 2, 64, 16, 0, 0),
     ([1] * 6, [4000, 4100, 4200, 4300, 4400, 4500], [(0, 6, 3990)], 32, 8, 128, 16, 0, 0),
     ([200, 200], [700, 600], [(0, 2, 400)], 2, 1, 96, 64, 0, 0),
+    ([1] * 300, [60 + i % 40 for i in range(300)], [(0, 150, 48), (151, 300, 33)], 4, 2, 64, 16, 0, 0),
 ]
 
 

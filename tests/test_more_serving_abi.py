@@ -97,7 +97,7 @@ def prefix(**kw):
 @pytest.mark.parametrize("want,kw", [
     (NULL, dict(seq_start=None)), (NULL, dict(len=None)), (OK, dict(n_groups=0, seq_start=None, len=None)),
     (SHAPE, dict(n_groups=-1)), (SHAPE, dict(max_tokens=-1)), (SHAPE, dict(max_len=-1)), (SHAPE, dict(max_own=-1)),
-    (SHAPE, dict(max_len=1 << 31)), (SHAPE, dict(max_own=1 << 31)), (SHAPE, dict(n_groups=(1 << 30) + 1)),
+    (SHAPE, dict(max_len=1 << 31)), (SHAPE, dict(max_own=1 << 31)), (SHAPE, dict(n_groups=1 << 16)), (OK, dict(n_groups=65535)),
     (SHAPE, dict(max_tokens=(1 << 30) + 1)), (OK, dict())])
 def test_prefixes_refuse(want, kw):
     lib = sats.load()
