@@ -506,8 +506,9 @@ int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *c
 /*
  * The same attention for a batch whose sequences share prefixes: the keys of a
  * prefix are read once for all rows of its group (from the pages of the first of its
- * sequences that is as long; shorter ones see of it what they have), the others from each sequence's own.  Results agree with sats_paged_attention's
- * within rounding.  Scratch memory as said at sats_reserve_prefix.
+ * sequences that is as long, or as long as any; shorter ones see of it what they have), the others
+ * from each sequence's own.  Results agree with sats_paged_attention's within rounding.  Scratch
+ * memory as said at sats_reserve_prefix.
  */
 int sats_prefix_attention(const void *q, int64_t q_stride, const sats_kv_cache *cache, int64_t layer,
                           const sats_kv_batch *batch, const sats_kv_prefix *prefix, int64_t n_q_heads, float scale,

@@ -31,7 +31,6 @@ constexpr int kJoinRows = 4096;
 constexpr int kRowsLeast8 = 4, kRowsAlone8 = 24;
 constexpr int kSlots = 512, kSlotsLong = 2048, kLongBlocks = 24, kRowsLeast = 8, kTileLeast = 4;
 
-
 // The split of a launch: row tiles of R rows, their number at most, and over how many
 // workgroups a tile's blocks of `keys` keys go.
 struct AttendPlan {

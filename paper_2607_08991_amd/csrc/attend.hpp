@@ -513,7 +513,7 @@ struct Odd { static constexpr bool kOdd = true; };
 // one is worked on.
 //
 // Bound by the cache's bytes: 64 sequences of 500 to 8000 keys (8 heads of 128, four rows each,
-// bf16, 711 MB) take 151 us with the join, 4.7 TB/s (counters: 712 MB fetched, no bank
+// bf16, 711 MB) take 146 us with the join, 4.9 TB/s (counters: 712 MB fetched, no bank
 // conflicts); one sequence of 32768 keys (134 MB) 29.7 us in this kernel, 4.5 TB/s, and 8.3 in
 // the join.  Of other widths the same sequences reach, in TB/s, 4.2 (64), 3.8 (80), 3.3 (96, which
 // spills registers at three waves a SIMD), 3.0 (136) to 4.3 (256: one workgroup a compute unit);
@@ -834,7 +834,9 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
   uint8_t *const part[4] = {lds[0], lds[1], lds[2], lds[3]};
   attend_rows<T, DT, FULL, false>(a, blockIdx.x, blockIdx.y, part, ml);
 }
-// The same in phases, of tiles of 16 rows only.
+// The same in phases, of tiles of 16 rows only (decode over short groups, float32).  Four sequences of 32 heads of
+// 128 on 8 that share 2000 keys, with up to 300 of their own (bf16, 9.8 MB): 11.9 us, and the join 5.0; the chain of a
+// workgroup's numbers, table, keys and end, as without groups, bounds it.
 template <typename T, int DT, bool FULL>
 __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_rows_phases_kernel(AttendArgs a, PhaseArgs p) {
   __shared__ __align__(16) uint8_t lds[4][RowsPart<T, DT>::kBytes];
@@ -1303,7 +1305,13 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
   __shared__ __align__(16) uint8_t k0[kBytes], k1[kBytes], v0[kBytes], v1[kBytes];
   attend_tile<DT, FULL, false>(a, blockIdx.x, blockIdx.y, k0, k1, v0, v1);
 }
-// In phases, of tiles of 16 rows and of 128.
+// In phases, of tiles of 16 rows and of 128.  The rows of all sequences of a group share a tile, so that the
+// prefix is read once for 128 of them: 64 sequences of 32 heads of 128 on 8 with 32000 keys in common and 100 to 2000 of
+// their own (bf16) read 299 MB instead of 8.7 GB, 97.7 us with the join (traced 9.8), where attention sequence after sequence takes
+// 1456.  Both phases are in one launch, since the prefix's tiles are bound by products and the sequences' own by
+// memory.  A workgroup's registers and LDS are those of the larger tile for both, so two of them a compute unit are all
+// the loads that decode has in flight here; that, and parts of unlike lengths (about 5 us of each before its first
+// product), is what is left above the 62 us of the bytes.
 template <int DT, bool FULL>
 __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_phases_kernel(AttendArgs a, PhaseArgs p) {
   constexpr int kBytes = kTileKeys * TileWave<DT, FULL>::kRow;
@@ -1377,6 +1385,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 // The same where sequences share prefixes: W waves a row, whose parts are where the launch before wrote that
 // they are (put_row_parts).  Every split has left a part, an empty one too.  What is read there is used only
 // within its set: a row that no tile was launched for holds anything.
+// Latency: three dependent loads, and the parts' bytes: 5.0 us for 128 rows of up to 11 parts, 9.8 for 2048 of up to 36,
+// 13.4 for 12000 of up to 20 (of which a wave a row where rows are many: kJoinRows).
 template <typename T, int W>
 __global__ __launch_bounds__(256) void attend_join_phases_kernel(AttendArgs a, PhaseArgs p) {
   __shared__ float ls[W > 1 ? W : 1];

@@ -20,6 +20,13 @@ typedef __attribute__((address_space(3))) i32x2_t lds_i32x2;
 // codes: its transposing reads give a lane eight keys of a dim, which it converts then).  V's scales belong to the keys,
 // so they go into the weights.
 //
+// Bound by the cache's bytes and by their conversion (two numbers an instruction for E4M3, five instructions for two of
+// INT8): 64 sequences of 500 to 8000 keys (8 heads of 128, four rows each, 359 MB of E4M3) take 95.5 us with the join, 3.75
+// TB/s, where a bf16 cache takes 146 us for 711 MB; INT8 99.6.  Two blocks ahead because one of 8 bits is half the bytes: with one, and
+// three workgroups a compute unit, 139.  Heads of 64, 80, 96, 256 (half as many of the last): 61, 100, 103, 156.
+// One sequence of 32768 keys: 21.9 us and 8.3 in the join (67.6 MB, 14 us).  float32 over the same 64
+// sequences (INT8): 107 us, three products for one with queries and three for two with values.
+//
 // Rows of V lie in LDS as in the cache, their 16-byte pieces exchanged so that the eight rows of a read
 // (keys 4 g .. and 16 + 4 g ..) are in different banks.
 template <int DT> struct Rows8 {
@@ -359,6 +366,11 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_ro
 
 // As attend_tile, whose blocks come from memory straight into LDS: here a wave's codes of a block
 // are in registers for the length of a step, and become bf16 rows in LDS at the start of the next.
+//
+// Bound by instruction issue: a step converts 2 x 8 pieces a wave and stores them, which a bf16 cache leaves to
+// its loads.  2048 tokens on 4096 (32 heads of 128 on 8, 172 Gflop): E4M3 241 us (713 TFLOP/s), INT8 313 to 343, bf16
+// 200.  The places of a row's pieces in LDS differ in fixed bits, so that a step has one address for its stores (276 us
+// with an address for each).  Heads of 64 and 256 (half and twice as many dims): 284 and 400 of E4M3, 355 and 561 of INT8.
 template <int F, int DT, bool FULL, bool PHASED>
 __device__ __forceinline__ void attend_tile8(const AttendArgs &a, int x, int z, uint8_t *k0, uint8_t *k1, uint8_t *v0, uint8_t *v1) {
   using Wave = TileWave<DT, FULL>;

@@ -10,7 +10,9 @@
 //
 // Bound by memory where there are tokens: 4096 of 32 + 8 + 8 heads of 128 with norms (bf16,
 // 102.8 MB in and out) take 23.2 us, 4.4 TB/s, where a large copy reaches 4.9.  One token is
-// the launch: 3.8 us of kernel in 11.2 us of a call from Python.
+// the launch: 3.8 us of kernel in 11.2 us of a call from Python.  Into a cache of 8 bits the row's largest magnitude
+// is one more maximum over its lanes, and its codes are stored by four: the same tokens (INT8, 94.5 MB) take 25.4 us, 3.7
+// TB/s, where the maximum waits for the norm and the rotation, and a row of 128 codes is stored by 8 lanes in words of four.
 #pragma once
 
 #include "elem.hpp"
