@@ -84,6 +84,10 @@ SHAPES = [  # q_len, kv_len, groups, heads, kv_heads, dim, page, window, sinks
     ([1, 1, 1], [500, 600, 700], [], 4, 2, 64, 16, 0, 0),
     ([1] * 6, [4000, 4100, 4200, 4300, 4400, 4500], [(0, 6, 3990)], 32, 8, 128, 16, 0, 0),
     ([200, 200], [700, 600], [(0, 2, 400)], 2, 1, 96, 64, 0, 0),
+    ([1] * 3, [500, 520, 700], [(0, 2, 490)], 24, 1, 128, 16, 0, 0),  # more heads on a cache head than a small tile's rows
+    ([1, 3, 0, 2], [300, 310, 0, 305], [(0, 4, 290)], 64, 1, 64, 16, 0, 0),
+    ([1] * 5, [40, 200, 210, 220, 50], [(0, 2, 32), (2, 4, 199)], 34, 2, 48, 16, 60, 3),
+    ([1, 1], [900, 880], [(0, 2, 870)], 40, 2, 256, 16, 0, 0),
     ([1] * 300, [60 + i % 40 for i in range(300)], [(0, 150, 48), (151, 300, 33)], 4, 2, 64, 16, 0, 0),
 ]
 
