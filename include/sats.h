@@ -507,8 +507,10 @@ int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *c
  * The same attention for a batch whose sequences share prefixes: the keys of a
  * prefix are read once for all rows of its group (from the pages of the first of its
  * sequences that is as long, or as long as any; shorter ones see of it what they have), the others
- * from each sequence's own.  Results agree with sats_paged_attention's within rounding.  Scratch
- * memory as said at sats_reserve_prefix.
+ * from each sequence's own.  With window > 0 a sequence may have given back the pages that its new
+ * tokens do not see: each page of the prefix is then the longest sequence's that has one in its place.  A
+ * sequence has to have the pages of the prefix that its new tokens see.  Results agree with
+ * sats_paged_attention's within rounding.  Scratch memory as said at sats_reserve_prefix.
  */
 int sats_prefix_attention(const void *q, int64_t q_stride, const sats_kv_cache *cache, int64_t layer,
                           const sats_kv_batch *batch, const sats_kv_prefix *prefix, int64_t n_q_heads, float scale,

@@ -170,11 +170,30 @@ size_t place_sets(const sats::AttendArgs &a, const PrefixPlan &plan, int esz, ch
   return rows * (a.dim + 2) * sizeof(float) + a.batch.n_tokens * a.n_q * sizeof(sats::RowParts);
 }
 
+// Under a window the groups' rows of the table come behind the sets, at mem: their width, and the bytes that they take.
+int64_t group_width(const sats::AttendArgs &a) {
+  const int64_t top = std::min({a.max_len, a.batch.max_kv, a.batch.max_pages << a.pool.shift});
+  return (top + a.pool.page - 1) >> a.pool.shift;
+}
+// (A wave reads 64 entries at a time, of the last row past its end too.)
+size_t group_bytes(const sats::AttendArgs &a) { return ((size_t)a.n_groups * group_width(a) + 64) * sizeof(int32_t); }
+
 // Workgroups of the launch of the four sets.
 int64_t phase_wgs(const sats::AttendArgs &a, const sats::PhaseArgs &p) {
   double n = 0;
   for (const sats::PhaseSet &s : p.set) n += (double)s.tiles * a.pool.n_kv * s.splits;
   return (int64_t)std::min(n, 1e18);
+}
+
+// The bytes of the sets.
+int prefix_sets(const sats::AttendArgs &a, int form, int esz, size_t *bytes) {
+  const PrefixPlan p = prefix_plan(a, form, esz);
+  int rc = check_plan(a, p.pre);
+  if (rc || (rc = check_plan(a, p.own))) return rc;
+  sats::PhaseArgs args;
+  *bytes = place_sets(a, p, esz, nullptr, &args);
+  if (!*bytes || phase_wgs(a, args) > kMaxGrid || a.batch.n_tokens * a.n_q > kMaxGrid) return fail(SATS_ERR_SHAPE, "too many rows for one call");
+  return SATS_OK;
 }
 
 }  // namespace
@@ -214,16 +233,24 @@ int run_attention(sats::AttendArgs a, int form, int esz, hipStream_t stream) {
   return rc;
 }
 
-// The groups' tiles and the sequences' tiles, and the joins of the latter's rows with both.
+// (Under a window the groups' pages,) the groups' tiles and the sequences' tiles, and the joins of the latter's rows
+// with both.
 int run_prefix_attention(sats::AttendArgs a, int form, int esz, hipStream_t stream) {
   if (a.n_groups == 0 || a.max_len == 0 || a.max_tokens == 0) return run_attention(a, form, esz, stream);
-  size_t bytes = 0;
-  int rc = prefix_scratch(a, form, esz, &bytes);
+  size_t sets = 0;
+  int rc = prefix_sets(a, form, esz, &sets);
   if (rc) return rc;
   const PrefixPlan plan = prefix_plan(a, form, esz);
   char *mem = nullptr;
   Turn turn;
-  if ((rc = serve_workspace(stream, bytes, &mem, &turn))) return rc;
+  const int64_t width = a.window ? group_width(a) : 0, width_wgs = (width + 31) / 32;
+  if (width_wgs > kMaxGrid) return fail(SATS_ERR_SHAPE, "too many pages for one call");
+  if ((rc = serve_workspace(stream, sets + (width ? group_bytes(a) : 0), &mem, &turn))) return rc;
+  if (width) {
+    a.group_rows = reinterpret_cast<int32_t *>(mem + sets), a.group_width = width;
+    sats::attend_group_pages_kernel<<<dim3((unsigned)width_wgs, (unsigned)a.n_groups), 256, 0, stream>>>(a);
+    if ((rc = launched("attend_group_pages_kernel"))) return rc;
+  }
   sats::PhaseArgs p;
   place_sets(a, plan, esz, mem, &p);
   const bool large = p.set[sats::kSharedLarge].tiles || p.set[sats::kOwnLarge].tiles;
@@ -244,13 +271,9 @@ size_t attention_scratch(int64_t head_dim) {
   return (size_t)std::max(kSlotsLong * 16, kSlots * sats::kTileRows) * (head_dim + 2) * sizeof(float);
 }
 int prefix_scratch(const sats::AttendArgs &a, int form, int esz, size_t *bytes) {
-  const PrefixPlan p = prefix_plan(a, form, esz);
-  int rc = check_plan(a, p.pre);
-  if (rc || (rc = check_plan(a, p.own))) return rc;
-  sats::PhaseArgs args;
-  *bytes = place_sets(a, p, esz, nullptr, &args);
-  if (!*bytes || phase_wgs(a, args) > kMaxGrid || a.batch.n_tokens * a.n_q > kMaxGrid) return fail(SATS_ERR_SHAPE, "too many rows for one call");
-  return SATS_OK;
+  const int rc = prefix_sets(a, form, esz, bytes);
+  *bytes += group_bytes(a);
+  return rc;
 }
 
 }  // namespace sats_host

@@ -58,6 +58,8 @@ struct AttendArgs {
   int phase, n_groups;
   const int32_t *seq_start, *shared;
   int64_t max_tokens, max_len, max_own;  // of a group's new tokens, of a prefix, of a sequence's other keys
+  int32_t *group_rows;  // or null: [n_groups][group_width] pages of the prefixes (attend_group_pages_kernel)
+  int64_t group_width;
 };
 enum : int { kWhole = 0, kShared = 1, kOwn = 2 };  // phase: all keys, those of the groups, those of a sequence alone
 
@@ -89,13 +91,13 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 // A tile of rows: rows first .. first + count - 1 of (token, group) pairs of a sequence.
 struct RowTile {
-  int seq;          // -1: none
+  int seq;          // -1: none (of a group: its first)
   int first, count;
   int64_t start, place0, len;  // sequence's first token; place of its first new token; length
-  // (in phases) the first key that counts; the group's sequences, whose tokens the tile's rows are (seq: the one
-  // whose pages are read)
+  // (in phases) the first key that counts; the group's sequences, whose tokens the tile's rows are
   int64_t lo;
   int seq0, seq_end;
+  const int32_t *pages;  // (in phases) their row of a table
 };
 
 __device__ __forceinline__ bool takes(const AttendArgs &a, int rows) { return rows <= 16 ? a.small : a.large; }
@@ -148,6 +150,32 @@ __device__ __forceinline__ int group_leader(const AttendArgs &a, const GroupView
     if (long_enough) return __builtin_amdgcn_readfirstlane(base + __builtin_ctzll(long_enough));
   }
   return v.s0;
+}
+// Under a window sequences give back the pages behind it, each its own: the rows of the table that are read for the
+// groups then, where a place has the page of the longest sequence that has one there (so it has all keys that any of them
+// has there).  32 places a workgroup, by 8 threads each: 64 sequences on 32000 shared keys under a window of 2048 take
+// 184 us with it, 181 from one sequence's pages.  (The kernels that attend looking for a page that is not there
+// themselves cost every call 1 to 14 %, by the registers that it takes.)
+inline __global__ __launch_bounds__(256) void attend_group_pages_kernel(AttendArgs a) {
+  __shared__ int64_t best[8][32];
+  const GroupView v = group_view(a, blockIdx.y);
+  const int at = threadIdx.x & 31, slice = threadIdx.x >> 5;
+  const int64_t place = (int64_t)blockIdx.x * 32 + at, key = place << a.pool.shift;
+  const bool in = key < v.len;
+  int64_t most = -1;  // a length, then the page
+  if (in) {
+#pragma unroll 4
+    for (int s = v.s0 + slice; s < v.s1; s += 8) {
+      const int64_t kv = a.batch.kv_len[s], p = a.batch.table[s * a.batch.max_pages + place];
+      if (p >= 0 && p < a.pool.n_pages && kv > key && (kv << 32 | p) > most) most = kv << 32 | p;
+    }
+  }
+  best[slice][at] = most;
+  __syncthreads();
+  if (slice || !in) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) most = best[i][at] > most ? best[i][at] : most;
+  a.group_rows[blockIdx.y * a.group_width + place] = most < 0 ? -1 : (int)most;
 }
 // The place of token `tok` in the one of sequences s0 .. s1 - 1 that it is of (-1: of none).  (All lanes call it.)
 __device__ __forceinline__ int64_t group_place(const AttendArgs &a, int s0, int s1, int64_t tok) {
@@ -204,7 +232,8 @@ template <int R> __device__ __forceinline__ RowTile find_group_tile(const Attend
   idx = __builtin_amdgcn_readfirstlane(idx);
   const GroupView v = group_view(a, g);
   if (!v.n || !takes(a, v.n * a.group)) return o;
-  o.seq = group_leader(a, v), o.seq0 = v.s0, o.seq_end = v.s1;
+  o.seq = v.s0, o.seq0 = v.s0, o.seq_end = v.s1;
+  o.pages = a.group_rows ? a.group_rows + g * a.group_width : a.batch.table + group_leader(a, v) * a.batch.max_pages;
   o.first = idx * R;
   const int rows = v.n * a.group - o.first;
   o.count = rows < R ? rows : R;
@@ -266,6 +295,7 @@ __device__ __forceinline__ RowTile find_tile(const AttendArgs &a, int t) {
   o.place0 = (int64_t)a.batch.kv_len[o.seq] - (a.batch.q_start[o.seq + 1] - v.start);
   o.len = v.len;
   if (PHASED && a.phase == kOwn) {
+    o.pages = a.batch.table + o.seq * a.batch.max_pages;
     const int g = group_of(a, o.seq);
     if (g >= 0) o.lo = group_view(a, g).len;
     if (o.len - o.lo > a.max_own) o.len = o.lo + a.max_own;
@@ -381,7 +411,7 @@ __device__ __forceinline__ bool any_sees(const AttendArgs &a, const KeyBlocks &k
 template <bool PHASED = false>
 __device__ __forceinline__ int key_entry(const AttendArgs &a, const RowTile &t, const KeyBlocks &k, int64_t j) {
   int p = -1;
-  if (any_sees<PHASED>(a, k, t.len, j)) p = a.batch.table[t.seq * a.batch.max_pages + (j >> a.pool.shift)];
+  if (any_sees<PHASED>(a, k, t.len, j)) p = (PHASED ? t.pages : a.batch.table + t.seq * a.batch.max_pages)[j >> a.pool.shift];
   return p;
 }
 __device__ __forceinline__ int page_or_none(const AttendArgs &a, int entry) {
@@ -1170,7 +1200,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &a, int x, int z, u
   const int64_t page_bytes = ((int64_t)a.pool.n_kv << a.pool.shift) * a.dim * 2;
   const char *kp = (const char *)a.k + head_bytes, *vp = (const char *)a.v + head_bytes;
   const int row_bytes = a.dim * 2;
-  const int32_t *table = a.batch.table + t.seq * a.batch.max_pages;
+  const int32_t *table = PHASED ? t.pages : a.batch.table + t.seq * a.batch.max_pages;
 
   HeldPages held;
   // page of key `lane` of a block where some row of the tile sees it, else -1

@@ -400,7 +400,7 @@ __device__ __forceinline__ void attend_tile8(const AttendArgs &a, int x, int z, 
   const int64_t head_rows = (int64_t)kvh << a.pool.shift, page_rows = (int64_t)a.pool.n_kv << a.pool.shift;
   const char *kp = (const char *)a.k + head_rows * a.dim, *vp = (const char *)a.v + head_rows * a.dim;
   const char *ksp = (const char *)a.k_scale + head_rows, *vsp = (const char *)a.v_scale + head_rows;
-  const int32_t *table = a.batch.table + t.seq * a.batch.max_pages;
+  const int32_t *table = PHASED ? t.pages : a.batch.table + t.seq * a.batch.max_pages;
 
   HeldPages held;
   auto page_of = [&](int b) {
