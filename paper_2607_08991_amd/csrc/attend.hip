@@ -36,6 +36,7 @@ constexpr int kSlots = 512, kSlotsLong = 2048, kLongBlocks = 24, kRowsLeast = 8,
 struct AttendPlan {
   int64_t tiles;
   int splits, per_split;
+  int most;  // splits, at most, of a call that differs in its window alone (fewer blocks can be more splits: 33 in 7, 32 in 8)
 };
 // Tiles of `units` sequences or groups with up to max_q tokens each, which see `range` keys at most.
 // (least: blocks of a split; alone: blocks up to which a tile is not split where that would cost a join.)
@@ -58,6 +59,7 @@ AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, in
   if (R != 16 && a.phase == sats::kShared && units == 1 && b.n_seqs * a.max_own >= p.tiles * range) slots /= 2;
   int64_t want = std::max<int64_t>(1, slots / wgs);
   if (R == 16) want = std::max(want, std::min<int64_t>(kSlotsLong / wgs, blocks / kLongBlocks));
+  p.most = (int)std::min<int64_t>(want, (blocks + least - 1) / least);  // (for blocks of no window; both grow with them)
   if (a.phase == sats::kWhole && blocks <= alone) want = 1;
   p.per_split = (int)std::max<int64_t>(least, (blocks + want - 1) / want);
   p.splits = (int)((blocks + p.per_split - 1) / p.per_split);
@@ -185,9 +187,8 @@ int64_t phase_wgs(const sats::AttendArgs &a, const sats::PhaseArgs &p) {
   return (int64_t)std::min(n, 1e18);
 }
 
-// The bytes of the sets.
-int prefix_sets(const sats::AttendArgs &a, int form, int esz, size_t *bytes) {
-  const PrefixPlan p = prefix_plan(a, form, esz);
+// The bytes of the sets of a plan.
+int prefix_sets(const sats::AttendArgs &a, const PrefixPlan &p, int esz, size_t *bytes) {
   int rc = check_plan(a, p.pre);
   if (rc || (rc = check_plan(a, p.own))) return rc;
   sats::PhaseArgs args;
@@ -237,10 +238,10 @@ int run_attention(sats::AttendArgs a, int form, int esz, hipStream_t stream) {
 // with both.
 int run_prefix_attention(sats::AttendArgs a, int form, int esz, hipStream_t stream) {
   if (a.n_groups == 0 || a.max_len == 0 || a.max_tokens == 0) return run_attention(a, form, esz, stream);
-  size_t sets = 0;
-  int rc = prefix_sets(a, form, esz, &sets);
-  if (rc) return rc;
   const PrefixPlan plan = prefix_plan(a, form, esz);
+  size_t sets = 0;
+  int rc = prefix_sets(a, plan, esz, &sets);
+  if (rc) return rc;
   char *mem = nullptr;
   Turn turn;
   const int64_t width = a.window ? group_width(a) : 0, width_wgs = (width + 31) / 32;
@@ -271,7 +272,9 @@ size_t attention_scratch(int64_t head_dim) {
   return (size_t)std::max(kSlotsLong * 16, kSlots * sats::kTileRows) * (head_dim + 2) * sizeof(float);
 }
 int prefix_scratch(const sats::AttendArgs &a, int form, int esz, size_t *bytes) {
-  const int rc = prefix_sets(a, form, esz, bytes);
+  PrefixPlan plan = prefix_plan(a, form, esz);
+  for (AttendPlan *x : {&plan.pre.small, &plan.pre.large, &plan.own.small, &plan.own.large}) x->splits = x->most;
+  const int rc = prefix_sets(a, plan, esz, bytes);
   *bytes += group_bytes(a);
   return rc;
 }

@@ -1,0 +1,50 @@
+"""What attention over shared prefixes asks of its scratch memory and its launches, without a GPU: sats_reserve_prefix
+is enough for every window, and the limits are those of the launches."""
+import pytest
+
+from test_more_serving_abi import MORE_PRE, run  # noqa: F401
+from test_serving_abi import SHAPE
+
+# [shape, options]: sequences, tokens, new tokens, keys, groups, tokens of a group, shared keys, own keys
+WINDOWED = """
+def windows(a, kw, sizes):
+    '''Codes of a reserve and of captured calls under windows, and what these do besides launching.'''
+    fake.fake_capture(0)
+    rcs = [reserve_prefix(*a, **kw)]
+    log()
+    fake.fake_capture(1)
+    rcs += [shared(*a, window=w, **kw) for w in sizes]
+    bad = [l for l in log() if l[0] != "launch"]
+    fake.fake_capture(0)
+    lib.sats_release()
+    log()
+    return [rcs, bad]
+"""
+
+
+@pytest.mark.parametrize("form", [dict(), dict(esz=4), dict(form=17), dict(form=18), dict(form=17, esz=4)], ids=str)
+@pytest.mark.parametrize("shape,kw,window", [
+    ((4, 256, 64, 6000, 1, 256, 4000, 2048), dict(heads=32, kv=8), 1800),
+    ((4, 4, 1, 36096, 1, 4, 32000, 4096), dict(heads=32, kv=4), 3984),
+    ((8, 128, 16, 8096, 3, 64, 4000, 4096), dict(heads=8, kv=2), 3700),
+], ids=str)
+def test_a_reserve_is_enough_under_a_window(run, shape, kw, window, form):  # noqa: F811
+    rcs, bad = run(WINDOWED + f"print(json.dumps(windows({shape}, {dict(kw, **form)}, [0, {window}, 1, 500, 1000000])))")
+    assert set(rcs) == {0} and bad == []
+
+
+def test_a_reserve_is_enough_under_any_window(run):  # noqa: F811
+    """Windows of every length in blocks, and in between, over shapes, heads, widths and forms."""
+    got = run(WINDOWED + """
+sizes = [0, 1, 7] + list(range(32, 4200, 32)) + [5000, 9000, 33000, 1 << 40]
+out = []
+for seqs, q in ((1, 1), (4, 1), (5, 3), (8, 16), (64, 1), (4, 64), (3, 300)):
+    for groups, pre, own in ((1, 32000, 4096), (1, 4000, 2048), (3, 1500, 3000), (2, 70, 700)):
+        if groups > seqs: continue
+        for h, k, dim in ((32, 8, 128), (32, 4, 128), (8, 2, 64), (16, 16, 96), (64, 1, 256)):
+            for kw in ({}, dict(form=17), dict(form=18, esz=4)):
+                a = (seqs, seqs * q, q, pre + own, groups, -(-seqs // groups) * q, pre, own)
+                rcs, bad = windows(a, dict(heads=h, kv=k, dim=dim, **kw), sizes)
+                if set(rcs) != {0} or bad: out.append([a, h, k, dim, kw, sum(r != 0 for r in rcs)])
+print(json.dumps(out))""")
+    assert got == []
