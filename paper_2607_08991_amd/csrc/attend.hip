@@ -187,13 +187,19 @@ int64_t phase_wgs(const sats::AttendArgs &a, const sats::PhaseArgs &p) {
   return (int64_t)std::min(n, 1e18);
 }
 
+// Workgroups of their join, by four waves a row or by one (more than kJoinRows rows).
+int64_t join_wgs(const sats::AttendArgs &a, bool four) {
+  const int64_t rows = a.batch.n_tokens * a.n_q;
+  return four ? rows : (rows + 3) / 4;
+}
+
 // The bytes of the sets of a plan.
 int prefix_sets(const sats::AttendArgs &a, const PrefixPlan &p, int esz, size_t *bytes) {
   int rc = check_plan(a, p.pre);
   if (rc || (rc = check_plan(a, p.own))) return rc;
   sats::PhaseArgs args;
   *bytes = place_sets(a, p, esz, nullptr, &args);
-  if (!*bytes || phase_wgs(a, args) > kMaxGrid || a.batch.n_tokens * a.n_q > kMaxGrid) return fail(SATS_ERR_SHAPE, "too many rows for one call");
+  if (!*bytes || phase_wgs(a, args) > kMaxGrid || join_wgs(a, false) > kMaxGrid) return fail(SATS_ERR_SHAPE, "too many rows for one call");
   return SATS_OK;
 }
 
@@ -261,9 +267,8 @@ int run_prefix_attention(sats::AttendArgs a, int form, int esz, hipStream_t stre
   kernel<<<(unsigned)phase_wgs(a, p), 256, 0, stream>>>(a, p);
   if ((rc = launched("attention kernel"))) return rc;
   const int parts = std::max(plan.pre.small.splits, plan.pre.large.splits) + std::max(plan.own.small.splits, plan.own.large.splits);
-  const int64_t rows = a.batch.n_tokens * a.n_q;
-  const bool four = parts > kJoinWave && rows <= kJoinRows;
-  join_phases_kernel(esz, four)<<<(unsigned)(four ? rows : (rows + 3) / 4), 256, 0, stream>>>(a, p);
+  const bool four = parts > kJoinWave && a.batch.n_tokens * a.n_q <= kJoinRows;
+  join_phases_kernel(esz, four)<<<(unsigned)join_wgs(a, four), 256, 0, stream>>>(a, p);
   return launched("attention join");
 }
 

@@ -48,3 +48,19 @@ for seqs, q in ((1, 1), (4, 1), (5, 3), (8, 16), (64, 1), (4, 64), (3, 300)):
                 if set(rcs) != {0} or bad: out.append([a, h, k, dim, kw, sum(r != 0 for r in rcs)])
 print(json.dumps(out))""")
     assert got == []
+
+
+def test_rows_up_to_what_a_launch_takes(run):  # noqa: F811
+    """The join takes four rows a workgroup where rows are many: 4 (2^24 - 1) of them are within its grid, one more is not."""
+    got = run("""
+out = []
+for tokens, heads, k, dim in ((131071, 128, 8, 128), (131072, 128, 8, 128), ((1 << 26) - 4, 1, 1, 16), ((1 << 26) - 3, 1, 1, 16),
+                              (1 << 14, 4096, 1024, 16)):
+    q = -(-tokens // 128)
+    a = (128, tokens, q, 4096, 2, 64 * q, 2048, 2048)
+    out.append([reserve_prefix(*a, heads=heads, kv=k, dim=dim), shared(*a, heads=heads, kv=k, dim=dim)])
+    out[-1] += [l[2] for l in log() if l[0] == "launch" and "join" in l[1]]
+    lib.sats_release()
+    log()
+print(json.dumps(out))""")
+    assert got == [[0, 0, "4194272x1"], [0, 0, "4194304x1"], [0, 0, f"{2 ** 24 - 1}x1"], [SHAPE] * 2, [SHAPE] * 2]
