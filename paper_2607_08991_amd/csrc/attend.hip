@@ -153,7 +153,8 @@ PrefixPlan prefix_plan(sats::AttendArgs a, int form, int esz) {
   p.own = phase_plan(a, form, esz, a.batch.max_q, a.batch.n_seqs, a.max_own);
   return p;
 }
-// The four sets, their parts from mem on; the bytes that these take, or 0 where they are too many.
+constexpr size_t kTooMany = ~(size_t)0;
+// The four sets, their parts from mem on; the bytes that these take, or kTooMany.
 size_t place_sets(const sats::AttendArgs &a, const PrefixPlan &plan, int esz, char *mem, sats::PhaseArgs *out) {
   const AttendPlan *plans[4] = {&plan.pre.small, &plan.pre.large, &plan.own.small, &plan.own.large};
   size_t rows = 0;
@@ -161,7 +162,7 @@ size_t place_sets(const sats::AttendArgs &a, const PrefixPlan &plan, int esz, ch
     const AttendPlan &x = *plans[i];
     const bool there = x.tiles > 0;
     const size_t own = part_rows(x, i & 1 ? sats::kTileRows : 16, a.pool.n_kv);
-    if (rows + own > 0x7fffffff) return 0;
+    if (rows + own > 0x7fffffff) return kTooMany;
     out->set[i] = {x.tiles, x.splits, x.per_split, there && (!(i & 1) || !plans[i - 1]->tiles), there && ((i & 1) || esz != 2),
                    (int)rows, (int)own};
     rows += own;
@@ -199,7 +200,7 @@ int prefix_sets(const sats::AttendArgs &a, const PrefixPlan &p, int esz, size_t 
   if (rc || (rc = check_plan(a, p.own))) return rc;
   sats::PhaseArgs args;
   *bytes = place_sets(a, p, esz, nullptr, &args);
-  if (!*bytes || phase_wgs(a, args) > kMaxGrid || join_wgs(a, false) > kMaxGrid) return fail(SATS_ERR_SHAPE, "too many rows for one call");
+  if (*bytes == kTooMany || phase_wgs(a, args) > kMaxGrid || join_wgs(a, false) > kMaxGrid) return fail(SATS_ERR_SHAPE, "too many rows for one call");
   return SATS_OK;
 }
 

@@ -64,3 +64,16 @@ for tokens, heads, k, dim in ((131071, 128, 8, 128), (131072, 128, 8, 128), ((1 
     log()
 print(json.dumps(out))""")
     assert got == [[0, 0, "4194272x1"], [0, 0, "4194304x1"], [0, 0, f"{2 ** 24 - 1}x1"], [SHAPE] * 2, [SHAPE] * 2]
+
+
+@pytest.mark.parametrize("shape", [(4, 0, 0, 400, 1, 0, 200, 200), (4, 0, 1, 400, 1, 4, 200, 200), (0, 0, 0, 0, 0, 0, 0, 0),
+                                   (4, 4, 0, 400, 1, 4, 200, 200), (4, 4, 1, 0, 1, 4, 0, 0), (4, 4, 1, 400, 0, 0, 0, 0)], ids=str)
+def test_a_reserve_for_nothing_is_none(run, shape):  # noqa: F811
+    """Sizes that leave no row or no key to compute: the call does nothing, or attends without groups."""
+    rcs = run(f"""
+rcs = [reserve_prefix(*{shape})]
+fake.fake_capture(1)
+log()
+rcs += [shared(*{shape})]
+print(json.dumps([rcs, [l for l in log() if l[0] != "launch"]]))""")
+    assert rcs == [[0, 0], []]
