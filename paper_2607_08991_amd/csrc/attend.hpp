@@ -1117,10 +1117,14 @@ template <int DT, bool FULL> struct TileWave {
   // to bf16 for the instruction, l is the sum of the float32 weights: the error of a result is 0.0023
   // of the norm where its own rounding makes 0.0016.  A second product with the rest of each weight,
   // as the tiles of 16 rows have, brings it down to that, and 2048 tokens on 4096 from 199 us to 262.
-  template <bool SANE, bool NEXT>
+  // REST: with that second product.  In phases tiles have it, since the rows of a group can be single tokens', which have those
+  // bits where each sequence is attended to by itself.  us without and with it: 64 tokens on 32000 shared keys 99.6, 103 (E4M3
+  // 106, 114); groups with chunks 75, 89 (E4M3 88, 97); 64 chunks of 16 on 8000 shared keys 255, 313.  Only for groups that have
+  // single tokens, chosen in the kernel: 120, 96 and 294, by the registers that both ways of it take.
+  template <bool SANE, bool NEXT, bool REST>
   __device__ __forceinline__ void product(const f32x16_t (&s)[2], const uint8_t *vt, const f32x16_t (&sn)[2], float *top) {
     constexpr int kSlots = 4 * kOut, kAhead = 4;
-    bf16x8_t ring[kAhead], p;
+    bf16x8_t ring[kAhead], p, rest;
     float t = sn[0][0];
     const int vx = v_base();
 #pragma unroll
@@ -1130,9 +1134,16 @@ template <int DT, bool FULL> struct TileWave {
       const int st = i / kOut, o = i % kOut;
       if (o == 0) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[st >> 1][8 * (st & 1) + e];
+        for (int e = 0; e < 8; ++e) {
+          const float x = s[st >> 1][8 * (st & 1) + e], top = REST ? __uint_as_float(__float_as_uint(x) & 0xffff0000u) : x;
+          p[e] = (__bf16)top;
+          if (REST) rest[e] = (__bf16)fmaf(x, 1.0f + 0x1p-20f, -top);
+        }
       }
-      if (FULL || 32 * o < dim) acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % kAhead], p, acc[o], 0, 0, 0);
+      if (FULL || 32 * o < dim) {
+        acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % kAhead], p, acc[o], 0, 0, 0);
+        if (REST) acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % kAhead], rest, acc[o], 0, 0, 0);
+      }
       if (i + kAhead < kSlots) ring[i % kAhead] = v_piece<SANE>(vt, vx, (i + kAhead) / kOut, (i + kAhead) % kOut);
 #pragma unroll
       for (int e = i * 32 / kSlots; NEXT && e < (i + 1) * 32 / kSlots; ++e) t = fmaxf(t, sn[e >> 4][e & 15]);
@@ -1290,10 +1301,10 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &a, int x, int z, u
       some = !wave.whole(a, there_next, j1);
       if (some) wave.mask(a, there_next, j1, sn);
       if (kOdd && odd) {
-        wave.template product<true, true>(s, vt, sn, &top);
+        wave.template product<true, true, PHASED>(s, vt, sn, &top);
         wave.add_odd(a, here, block_key(kb, b, kTileKeys), s, vt);
       } else {
-        wave.template product<false, true>(s, vt, sn, &top);
+        wave.template product<false, true, PHASED>(s, vt, sn, &top);
         again |= odd;
       }
       wave.rescale(top);
@@ -1304,10 +1315,10 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &a, int x, int z, u
       const bool odd = some && Wave::odd_block(vt);
       wave.template weights<false>(s, vt, s);
       if (kOdd && odd) {
-        wave.template product<true, false>(s, vt, s, &top);
+        wave.template product<true, false, PHASED>(s, vt, s, &top);
         wave.add_odd(a, here, block_key(kb, b, kTileKeys), s, vt);
       } else {
-        wave.template product<false, false>(s, vt, s, &top);
+        wave.template product<false, false, PHASED>(s, vt, s, &top);
         again |= odd;
       }
     };

@@ -503,10 +503,10 @@ __device__ __forceinline__ void attend_tile8(const AttendArgs &a, int x, int z, 
       some = !wave.whole(a, there_next, j1);
       if (some) wave.mask(a, there_next, j1, sn);
       if (kOdd && odd) {
-        wave.template product<true, true>(s, vt, sn, &top);
+        wave.template product<true, true, PHASED>(s, vt, sn, &top);
         wave.add_odd(a, here, block_key(kb, b, kTileKeys), s, vt);
       } else {
-        wave.template product<false, true>(s, vt, sn, &top);
+        wave.template product<false, true, PHASED>(s, vt, sn, &top);
         again |= odd;
       }
       wave.rescale(top);
@@ -517,10 +517,10 @@ __device__ __forceinline__ void attend_tile8(const AttendArgs &a, int x, int z, 
       const bool odd = some && Wave::odd_block(vt);
       wave.template weights<false>(s, vt, s);
       if (kOdd && odd) {
-        wave.template product<true, false>(s, vt, s, &top);
+        wave.template product<true, false, PHASED>(s, vt, s, &top);
         wave.add_odd(a, here, block_key(kb, b, kTileKeys), s, vt);
       } else {
-        wave.template product<false, false>(s, vt, s, &top);
+        wave.template product<false, false, PHASED>(s, vt, s, &top);
         again |= odd;
       }
     };
