@@ -16,9 +16,11 @@ constexpr int kJoinWave = 16;
 // In phases: up to this many rows.  us for four waves and one: 2048 rows of 33 parts 118.8, 124.1; 12000 of up to 20 116, 100.
 constexpr int kJoinRows = 4096;
 // Attention: workgroups that the chip holds at once (two a compute unit; of the kernels for
-// heads above 128 one, of the 16-row kernels for heads up to 96 three), which a launch that
+// heads above 128 one, of the 16-row kernels for heads up to 96 three: up to 64 over 8 bits and in
+// phases, and never beside tiles of 128 rows in one launch), which a launch that
 // splits its tiles aims at: a few more would wait for a second round.  8 sequences of 2000 to 6000
-// keys: 512 workgroups 30.8 us, 768 38.1.
+// keys: 512 workgroups 30.8 us, 768 38.1; heads of 96 over E4M3 29.0, 36.5, and one of 32000 27.7, 35.4 (but 20 of
+// 500 to 3000, of unlike lengths, 31.8, 29.0); 16 sequences on 4000 shared keys, heads of 64, 23.3, 26.9.
 // Tiles of 16 rows whose parts stay at kLongBlocks blocks or more are split over up to
 // kSlotsLong workgroups, since sequences of different lengths then share the chip more
 // evenly (64 sequences of 500 to 8000 keys 156 -> 150 us).
@@ -40,7 +42,8 @@ struct AttendPlan {
 };
 // Tiles of `units` sequences or groups with up to max_q tokens each, which see `range` keys at most.
 // (least: blocks of a split; alone: blocks up to which a tile is not split where that would cost a join.)
-AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, int alone, int64_t max_q, int64_t units, int64_t range) {
+// (three: head dims up to which a compute unit holds three of the 16-row kernel's workgroups.)
+AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, int alone, int three, int64_t max_q, int64_t units, int64_t range) {
   const sats::BatchView &b = a.batch;
   const int64_t per_unit = (max_q * a.group + R - 1) / R;
   AttendPlan p;
@@ -52,7 +55,7 @@ AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, in
   const int64_t blocks = std::max<int64_t>(1, (range + keys - 1) / keys + 1);
   const int64_t wgs = std::max<int64_t>(1, p.tiles * a.pool.n_kv);
   int64_t slots = a.dim > 128 ? kSlots / 2 : kSlots;
-  if (R == 16 && a.dim <= 96) slots = kSlots * 3 / 2;
+  if (R == 16 && a.dim <= three) slots = kSlots * 3 / 2;
   // A group alone leaves half of the chip to its sequences' own keys where these are as many.  us for 512 and 256
   // workgroups: 64 sequences on 32000 keys with 100 to 2000 of their own 118.8, 108.3; with one each 82.8, 83.1 and on
   // 64000 128, 142; three groups of 500 to 9000 100, 124.
@@ -75,9 +78,11 @@ struct PhasePlan {
 PhasePlan phase_plan(const sats::AttendArgs &a, int form, int esz, int64_t max_q, int64_t units, int64_t range) {
   PhasePlan p;
   const bool any_large = esz == 2 && max_q * a.group > 16;
+  const bool beside = a.phase != sats::kWhole && esz == 2 && std::max(a.batch.max_q, a.max_tokens) * a.group > 16;
+  const int three = beside ? 0 : form || a.phase != sats::kWhole ? 64 : 96;
   if (!any_large || units > 1)
-    p.small = attend_plan(a, 16, form || esz == 2 ? 32 : 16, form ? kRowsLeast8 : kRowsLeast, form ? kRowsAlone8 : 0, any_large ? 16 / a.group : max_q, units, range);
-  if (any_large) p.large = attend_plan(a, sats::kTileRows, sats::kTileKeys, kTileLeast, 0, max_q, units, range);
+    p.small = attend_plan(a, 16, form || esz == 2 ? 32 : 16, form ? kRowsLeast8 : kRowsLeast, form ? kRowsAlone8 : 0, three, any_large ? 16 / a.group : max_q, units, range);
+  if (any_large) p.large = attend_plan(a, sats::kTileRows, sats::kTileKeys, kTileLeast, 0, three, max_q, units, range);
   return p;
 }
 int check_plan(const sats::AttendArgs &a, const PhasePlan &p) {
