@@ -614,10 +614,10 @@ int sats_adjust_logits(const void *logits, int elem_bytes, int64_t stride, const
                        int out_elem_bytes, int64_t out_stride, int64_t n, int64_t vocab, hipStream_t stream);
 
 /*
- * Allocate the scratch memory of (current device, stream) for sats_prefix_attention calls with these
- * sizes (of cache, batch and prefix; their pointers may be NULL): the batch's rows, n_q_heads a
- * token, in each of the parts that a launch splits their keys into, head_dim + 2 floats each, and a page table row
- * a group.  It is enough under any window.  Else as
+ * Allocate the scratch memory of (current device, stream) for sats_prefix_attention calls over such a cache, of
+ * batches and prefixes up to these sizes (their pointers may be NULL) and any window: the batch's rows, n_q_heads a
+ * token, in each of the parts that a launch splits their keys into, head_dim + 2 floats each (where
+ * rows have many keys 196608 of them and more), and a page table row a group.  Else as
  * sats_reserve_serving, which covers the other calls; a stream's scratch memory is one for all.
  */
 int sats_reserve_prefix(const sats_kv_cache *cache, const sats_kv_batch *batch, const sats_kv_prefix *prefix, int64_t n_q_heads,

@@ -730,7 +730,7 @@ def sats_adjust_logits(logits, rules, out, stream=None):
 
 
 def sats_reserve_prefix(cache, batch, prefix, n_q_heads, stream=None):
-    """Scratch memory of sats_prefix_attention calls of these sizes, ahead of stream capture."""
+    """Scratch memory of sats_prefix_attention calls up to these sizes, ahead of stream capture."""
     _call("sats_reserve_prefix", cache.ref, batch.ref, prefix.ref, n_q_heads, _stream(stream))
 
 

@@ -38,7 +38,7 @@ constexpr int kSlots = 512, kSlotsLong = 2048, kLongBlocks = 24, kRowsLeast = 8,
 struct AttendPlan {
   int64_t tiles;
   int splits, per_split;
-  int most;  // splits, at most, of a call that differs in its window alone (fewer blocks can be more splits: 33 in 7, 32 in 8)
+  int64_t most;  // workgroups, at most, of any call up to these sizes (fewer blocks can be more splits: 33 in 7, 32 in 8)
 };
 // Tiles of `units` sequences or groups with up to max_q tokens each, which see `range` keys at most.
 // (least: blocks of a split; alone: blocks up to which a tile is not split where that would cost a join.)
@@ -62,7 +62,7 @@ AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, in
   if (R != 16 && a.phase == sats::kShared && units == 1 && b.n_seqs * a.max_own >= p.tiles * range) slots /= 2;
   int64_t want = std::max<int64_t>(1, slots / wgs);
   if (R == 16) want = std::max(want, std::min<int64_t>(kSlotsLong / wgs, blocks / kLongBlocks));
-  p.most = (int)std::min<int64_t>(want, (blocks + least - 1) / least);  // (for blocks of no window; both grow with them)
+  p.most = std::max(wgs, std::min<int64_t>(R == 16 ? kSlotsLong : kSlots, wgs * ((blocks + least - 1) / least)));
   if (a.phase == sats::kWhole && blocks <= alone) want = 1;
   p.per_split = (int)std::max<int64_t>(least, (blocks + want - 1) / want);
   p.splits = (int)((blocks + p.per_split - 1) / p.per_split);
@@ -158,6 +158,10 @@ PrefixPlan prefix_plan(sats::AttendArgs a, int form, int esz) {
   p.own = phase_plan(a, form, esz, a.batch.max_q, a.batch.n_seqs, a.max_own);
   return p;
 }
+// The bytes of so many parts' rows, and of where each row's parts are.
+size_t set_bytes(const sats::AttendArgs &a, size_t rows) {
+  return rows * (a.dim + 2) * sizeof(float) + a.batch.n_tokens * a.n_q * sizeof(sats::RowParts);
+}
 constexpr size_t kTooMany = ~(size_t)0;
 // The four sets, their parts from mem on; the bytes that these take, or kTooMany.
 size_t place_sets(const sats::AttendArgs &a, const PrefixPlan &plan, int esz, char *mem, sats::PhaseArgs *out) {
@@ -175,7 +179,7 @@ size_t place_sets(const sats::AttendArgs &a, const PrefixPlan &plan, int esz, ch
   out->part = reinterpret_cast<float *>(mem);
   out->part_ml = out->part + rows * a.dim;
   out->parts = reinterpret_cast<sats::RowParts *>(out->part_ml + rows * 2);
-  return rows * (a.dim + 2) * sizeof(float) + a.batch.n_tokens * a.n_q * sizeof(sats::RowParts);
+  return set_bytes(a, rows);
 }
 
 // Under a window the groups' rows of the table come behind the sets, at mem: their width, and the bytes that they take.
@@ -283,11 +287,18 @@ size_t attention_scratch(int64_t head_dim) {
   return (size_t)std::max(kSlotsLong * 16, kSlots * sats::kTileRows) * (head_dim + 2) * sizeof(float);
 }
 int prefix_scratch(const sats::AttendArgs &a, int form, int esz, size_t *bytes) {
-  PrefixPlan plan = prefix_plan(a, form, esz);
-  for (AttendPlan *x : {&plan.pre.small, &plan.pre.large, &plan.own.small, &plan.own.large}) x->splits = x->most;
-  const int rc = prefix_sets(a, plan, esz, bytes);
-  *bytes += group_bytes(a);
-  return rc;
+  const PrefixPlan plan = prefix_plan(a, form, esz);
+  int rc = prefix_sets(a, plan, esz, bytes);
+  if (rc) return rc;
+  // a smaller batch can need more: it is split further, and of so few tokens that its tiles have 16 rows
+  sats::AttendArgs few = a;
+  few.batch.max_q = std::min<int64_t>(a.batch.max_q, 16 / a.group), few.max_tokens = std::min<int64_t>(a.max_tokens, 16 / a.group);
+  const PrefixPlan small = prefix_plan(few, form, esz);
+  size_t rows = 0;
+  for (const PhasePlan PrefixPlan::*set : {&PrefixPlan::pre, &PrefixPlan::own})
+    rows += std::max((plan.*set).small.most, (small.*set).small.most) * 16 + (plan.*set).large.most * sats::kTileRows;
+  *bytes = std::max(*bytes, set_bytes(a, rows)) + group_bytes(a);
+  return SATS_OK;
 }
 
 }  // namespace sats_host

@@ -24,8 +24,8 @@ int run_attention(sats::AttendArgs a, int form, int elem_bytes, hipStream_t stre
 // The same with a's groups of sequences that share prefixes.
 int run_prefix_attention(sats::AttendArgs a, int form, int elem_bytes, hipStream_t stream);
 
-// Scratch memory of any run_attention with heads of head_dim, and of these run_prefix_attention (a has no window)
-// under any window.
+// Scratch memory of any run_attention with heads of head_dim, and of any run_prefix_attention up to these sizes
+// (a has no window: of any).
 size_t attention_scratch(int64_t head_dim);
 int prefix_scratch(const sats::AttendArgs &a, int form, int elem_bytes, size_t *bytes);
 

@@ -77,3 +77,31 @@ log()
 rcs += [shared(*{shape})]
 print(json.dumps([rcs, [l for l in log() if l[0] != "launch"]]))""")
     assert rcs == [[0, 0], []]
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(esz=4), dict(form=17), dict(form=18, esz=4), dict(heads=8, kv=2, dim=64), dict(heads=64, kv=1, dim=256),
+                                dict(heads=40, kv=2, dim=96)], ids=str)
+def test_a_reserve_covers_smaller_batches(run, kw):  # noqa: F811
+    """One reserve, and captured calls of every batch within its sizes: as a server captures a graph for 1, 2, 4 .. sequences."""
+    got = run(WINDOWED + f"""
+kw = {kw}
+out = []
+for seqs, q, groups, pre, own in ((64, 1, 4, 32000, 2000), (64, 16, 3, 8000, 3000), (5, 300, 1, 4000, 4000), (1, 700, 1, 600, 9000)):
+    fake.fake_capture(0)
+    out += [reserve_prefix(seqs, seqs * q, q, pre + own, groups, seqs * q, pre, own, **kw)]
+    fake.fake_capture(1)
+    log()
+    for n in {{seqs, 40, 33, 17, 16, 9, 8, 5, 4, 3, 2, 1}}:
+        for m in {{q, 100, 17, 16, 5, 4, 2, 1}}:
+            for g in {{groups, 2, 1}}:
+                for p, o in ((pre, own), (pre // 2, own // 3), (pre // 9, own), (pre, 40), (200, 100), (33, 1)):
+                    if n > seqs or m > q or g > groups: continue
+                    for w in (0, 700):
+                        rc = shared(n, n * m, m, p + o, g, -(-n // g) * m, p, o, window=w, **kw)
+                        if rc: out.append([seqs, q, n, m, g, p, o, w])
+    out += [l for l in log() if l[0] != "launch"]
+    fake.fake_capture(0)
+    lib.sats_release()
+    log()
+print(json.dumps(out))""")
+    assert got == [0] * 4
