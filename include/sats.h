@@ -428,7 +428,8 @@ typedef struct {
  * within the codes, each value to the nearest code, ties to even (at most, one that does not
  * read as an infinity); a row that holds an infinity or NaN as zeros under 255.  Values are
  * attended to, and read, as bf16 holds them, which is exactly (below 2^-126: cut off or rounded to its
- * step); what a value adds to a result may be left out where it is below 2^-117.
+ * step; codes of other origin must not stand for more than the largest bf16 number); what a value
+ * adds to a result may be left out where it is below 2^-117.
  * page_size is at least 16 and head_dim a multiple of 16.  q_elem_bytes (2 or 4) is the
  * type of what is appended and of the queries and results of an attention over the cache.
  */
@@ -505,8 +506,9 @@ int sats_paged_attention(const void *q, int64_t q_stride, const sats_kv_cache *c
 
 /*
  * The same attention for a batch whose sequences share prefixes: the keys of a
- * prefix are read once for all rows of its group (from the pages of the first of its
- * sequences that is as long, or as long as any; shorter ones see of it what they have), the others
+ * prefix are read once for each tile of its group's rows (of a cache head 128 rows, 16 of float32, whose
+ * sequence does not matter), from the pages of the first of its
+ * sequences that is as long, or as long as any (shorter ones see of it what they have), the others
  * from each sequence's own.  With window > 0 a sequence may have given back the pages that its new
  * tokens do not see: each page of the prefix is then the longest sequence's that has one in its place.  A
  * sequence has to have the pages of the prefix that its new tokens see.  Results agree with

@@ -641,7 +641,7 @@ def sats_paged_attention(q, cache, layer, batch, out, scale, window=0, n_sinks=0
 
 
 def sats_prefix_attention(q, cache, layer, batch, prefix, out, scale, window=0, n_sinks=0, lse=None, stream=None):
-    """sats_paged_attention for a batch whose sequences share prefixes (KVPrefix), read once for each group."""
+    """sats_paged_attention for a batch whose sequences share prefixes (KVPrefix), read once for 128 rows of a group (float32: 16)."""
     qp, qs, hq = _attend(q, cache, batch, out, lse)
     _call("sats_prefix_attention", qp, qs, cache.ref, layer, batch.ref, prefix.ref, hq, scale, window, n_sinks, _ptr(out),
           _f32(lse, None, "lse"), _cur_stream(stream))

@@ -865,8 +865,10 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 96 ? 2 : 3) void attend_ro
   attend_rows<T, DT, FULL, false>(a, blockIdx.x, blockIdx.y, part, ml);
 }
 // The same in phases, of tiles of 16 rows only (decode over short groups, float32).  Four sequences of 32 heads of
-// 128 on 8 that share 2000 keys, with up to 300 of their own (bf16, 9.8 MB): 11.9 us, and the join 5.0; the chain of a
-// workgroup's numbers, table, keys and end, as without groups, bounds it.
+// 128 on 8 that share 2000 keys, with up to 300 of their own (bf16, 9.8 MB): 12.3 us, and the join 5.0; the chain of a
+// workgroup's numbers, table, keys and end, as without groups, bounds it.  Float32 groups of any size are tiles of 16 rows
+// here, each of which reads the prefix: 64 sequences on 32000 shared keys (256 rows a cache head, 16 tiles) 540 us, where bf16
+// takes 103 and the float32 products' rate would be 222.
 template <typename T, int DT, bool FULL>
 __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_rows_phases_kernel(AttendArgs a, PhaseArgs p) {
   __shared__ __align__(16) uint8_t lds[4][RowsPart<T, DT>::kBytes];
@@ -1348,11 +1350,12 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_tile_kernel(Atte
 }
 // In phases, of tiles of 16 rows and of 128.  The rows of all sequences of a group share a tile, so that the
 // prefix is read once for 128 of them: 64 sequences of 32 heads of 128 on 8 with 32000 keys in common and 100 to 2000 of
-// their own (bf16) read 299 MB instead of 8.7 GB, 97.7 us with the join (traced 9.8), where attention sequence after sequence takes
-// 1456.  Both phases are in one launch, since the prefix's tiles are bound by products and the sequences' own by
+// their own (bf16) have 299 MB to read instead of 8.7 GB (the 256 rows of a cache head are two tiles), 103 us with the join (traced
+// 9.9), where attention sequence after sequence takes 1460.  Both phases are in one launch, since the prefix's tiles are bound by products and the sequences' own by
 // memory.  A workgroup's registers and LDS are those of the larger tile for both, so two of them a compute unit are all
 // the loads that decode has in flight here; that, and parts of unlike lengths (about 5 us of each before its first
-// product), is what is left above the 62 us of the bytes.
+// product), is what is left above the 62 us of the bytes.  The compiler spills 78 of a wave's registers at 128 dims, 120 at
+// 256 (attend_tile_kernel 52 and 115).
 template <int DT, bool FULL>
 __global__ __launch_bounds__(256, DT > 128 ? 1 : 2) void attend_phases_kernel(AttendArgs a, PhaseArgs p) {
   constexpr int kBytes = kTileKeys * TileWave<DT, FULL>::kRow;
@@ -1424,9 +1427,9 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 }
 
 // The same where sequences share prefixes: W waves a row, whose parts are where the launch before wrote that
-// they are (put_row_parts).  Every split has left a part, an empty one too.  What is read there is used only
+// they are (put_row_parts).  Every split has left a part, an empty one too, whose sums are loaded as well.  What is read there is used only
 // within its set: a row that no tile was launched for holds anything.
-// Latency: three dependent loads, and the parts' bytes: 5.0 us for 128 rows of up to 11 parts, 9.8 for 2048 of up to 36,
+// Latency: three dependent loads, and the parts' bytes: 5.0 us for 128 rows of up to 11 parts, 9.9 for 2048 of up to 36,
 // 13.4 for 12000 of up to 20 (of which a wave a row where rows are many: kJoinRows).
 template <typename T, int W>
 __global__ __launch_bounds__(256) void attend_join_phases_kernel(AttendArgs a, PhaseArgs p) {

@@ -368,9 +368,12 @@ __global__ __launch_bounds__(256, DT > 128 ? 1 : DT > 64 ? 2 : 3) void attend_ro
 // are in registers for the length of a step, and become bf16 rows in LDS at the start of the next.
 //
 // Bound by instruction issue: a step converts 2 x 8 pieces a wave and stores them, which a bf16 cache leaves to
-// its loads.  2048 tokens on 4096 (32 heads of 128 on 8, 172 Gflop): E4M3 241 us (713 TFLOP/s), INT8 313 to 343, bf16
-// 200.  The places of a row's pieces in LDS differ in fixed bits, so that a step has one address for its stores (276 us
-// with an address for each).  Heads of 64 and 256 (half and twice as many dims): 284 and 400 of E4M3, 355 and 561 of INT8.
+// its loads, and INT8 takes more instructions for it (2750 for two blocks, E4M3 2240).  2048 tokens on 4096 (32 heads of 128 on
+// 8, 172 Gflop): E4M3 241 us (713 TFLOP/s), INT8 313 to 343, bf16 200.  K's and V's codes, their scales and pages live through a step
+// in a kernel that has no registers left: the compiler spills 90 (E4M3, 128 dims) and 273 (INT8), 253 and 543 at 256 dims,
+// where attend_tile_kernel spills 52 and 115; in phases 136 and 289, 171 and 521.  At 128 dims 8 and 19 of the accesses are
+// in the loop of two blocks, the others around it and in the loop for infinities and NaN (73 and 185).  The places of a row's pieces in LDS differ in fixed bits, so that a step has one address for its stores (276 us
+// with an address for each).  Heads of 64 and 256 (half and twice as many dims): 282 and 398 of E4M3, 354 and 560 of INT8.
 template <int F, int DT, bool FULL, bool PHASED>
 __device__ __forceinline__ void attend_tile8(const AttendArgs &a, int x, int z, uint8_t *k0, uint8_t *k1, uint8_t *v0, uint8_t *v1) {
   using Wave = TileWave<DT, FULL>;
