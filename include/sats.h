@@ -590,8 +590,8 @@ int sats_sample(const void *logits, int elem_bytes, int64_t stride, int64_t n, i
  *   l <- l + the sum of the id's biases, in their order
  *   l <- -infinity                                       ids without a bit in the row's mask
  * each rounded once to the type of out (elem_bytes and out_elem_bytes: 2 or 4; strides in elements).
- * out may be logits itself (same stride and type): logits that no rule changes are then not touched;
- * other overlap is rejected.  All arrays are on the device; max_history, n_bias or n_masks 0: no such rule:
+ * out may be logits itself (same stride and type): eight neighbours that no rule changes are then not
+ * touched; other overlap is rejected.  All arrays are on the device; max_history, n_bias or n_masks 0: no such rule:
  *   history        [n_seqs][history_stride] ids so far, the prompt first: of row i the first history_len[s] of row
  *                  s = seqs[i] (seqs NULL: i), at most max_history; from prompt_len[s] on (NULL: 0) they are
  *                  the answer

@@ -62,7 +62,8 @@ AttendPlan attend_plan(const sats::AttendArgs &a, int R, int keys, int least, in
   if (R != 16 && a.phase == sats::kShared && units == 1 && b.n_seqs * a.max_own >= p.tiles * range) slots /= 2;
   int64_t want = std::max<int64_t>(1, slots / wgs);
   if (R == 16) want = std::max(want, std::min<int64_t>(kSlotsLong / wgs, blocks / kLongBlocks));
-  p.most = std::max(wgs, std::min<int64_t>(R == 16 ? kSlotsLong : kSlots, wgs * ((blocks + least - 1) / least)));
+  const int64_t limit = R == 16 ? kSlotsLong : kSlots;
+  p.most = wgs >= limit ? wgs : std::min(limit, wgs * ((blocks + least - 1) / least));
   if (a.phase == sats::kWhole && blocks <= alone) want = 1;
   p.per_split = (int)std::max<int64_t>(least, (blocks + want - 1) / want);
   p.splits = (int)((blocks + p.per_split - 1) / p.per_split);

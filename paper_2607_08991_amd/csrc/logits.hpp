@@ -41,7 +41,7 @@ struct LogitArgs {
   const uint32_t *masks;
   const int32_t *mask_of;
   int64_t n_masks, mask_stride;
-  int in_place;  // out is logits: what no rule changes is neither read nor written
+  int in_place;  // out is logits: a step (of V) that no rule changes is neither read nor written
 };
 
 // Adds this thread's bias (live: it has one, of id `at` of the chunk) to those of the chunk: in rounds, in
